@@ -357,6 +357,152 @@ typedef struct spz_kernel_stat {
  * into out and their count into *n_out; waits for the context's work first. */
 int spz_profile_read(spz_ctx* ctx, spz_kernel_stat* out, int32_t max, int32_t* n_out);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators of a recurrent residual block. The policy of a task that one observation does
+ * not describe acts on a history: sequences of the shared pool's transitions when the
+ * update process trains it (Section 3.2), one step a call for the N samplers (Section
+ * 3.1.1). One block of such a network is
+ *     u = norm(x);  f, v, z = products of u;  h = scan(f, v);
+ *     x' = x + scale * dropout(gate(z) * norm(h));  u' = norm(x')  (the next block's)
+ * Conventions of all of them
+ *   - No context. Pointers are DEVICE pointers of the current HIP device, owned by the
+ *     caller; work is enqueued on `hip_stream` (a hipStream_t of that device; NULL = the
+ *     null stream) without waiting. Nothing is allocated, copied to the host or kept, so
+ *     calls may be captured into a HIP graph and may run on any streams and threads at
+ *     once, each with its own workspace. The workspace's contents before and after a call
+ *     do not matter; it is 16-byte aligned and at least as large as the *_workspace call
+ *     of the same arguments says (0: may be NULL).
+ *   - `prec` is the type of the named arrays (SPZ_PREC_FP32, SPZ_PREC_BF16). Statistics,
+ *     states and sums are float32 and every output is rounded once. Parameter vectors,
+ *     their gradients and states are float32.
+ *   - Strides are in elements; the last dimension is contiguous. Rows may be any distance
+ *     apart (inputs: 0 repeats a row); an output's rows must not overlap each other, nor
+ *     any other array of the call unless said otherwise. Any alignment of the element
+ *     type is taken; 16-byte aligned rows are faster.
+ *   - Every extent may be 0 and is below 2^31; a call without elements checks its
+ *     arguments and writes what remains (zero sums, the state).
+ *   - Results depend on the arguments alone: sums are taken in a fixed order.
+ *   - Errors: SPZ_EINVAL (NULL where an array is needed, an extent, stride, selector or
+ *     rate out of range, a pointer not aligned to its type), SPZ_ESIZE (workspace too
+ *     small), SPZ_EHIP (launch).
+ */
+
+/* Gated linear recurrence over `steps` of each of `batch` sequences, `width` channels:
+ *     a_t = 1 / (1 + exp(-f_t)),   h_t = a_t k_t h_{t-1} + (1 - a_t) v_t,   y_t = h_t
+ * with h_{-1} = h0 and k_t = 0 where reset[t] != 0 (step t starts an episode: nothing of
+ * the state before it, finite or not, passes), else 1. Sequence b has lengths[b] steps
+ * (clamped to [0, steps]): behind them nothing is read, y is 0 and the state stays, so
+ * hT = h of the last step (h0 of an empty sequence). The state is float32 throughout.
+ * steps = 1 is the samplers' form; hT may be h0 (the state is updated in place).
+ *
+ * Backward, from dy and dhT (the gradient to hT): with c = dhT behind the last step,
+ *     g_t = dy_t + c,  dv_t = g_t (1 - a_t),  df_t = g_t a_t (1 - a_t) (k_t h_{t-1} - v_t),
+ *     c = k_t a_t g_t;   dh0 = c in front of the first step
+ * df, dv are 0 behind a sequence's length. It needs `saved` of the forward call with the same
+ * f, v, h0, reset and lengths: the states it recomputes h from. */
+typedef struct spz_scan_args {
+  int64_t batch, steps, width;
+  const void *f, *v;                       /* [batch, steps, width]                              */
+  int64_t f_batch, f_step, v_batch, v_step;
+  const uint8_t* reset;                    /* [batch, steps] or NULL (no episode starts)         */
+  int64_t reset_batch, reset_step;
+  const int32_t* lengths;                  /* [batch] or NULL (all of them `steps`)              */
+  const float* h0;                         /* [batch, width] contiguous, or NULL (zeros)         */
+  void* y;                                 /* forward: [batch, steps, width]                     */
+  int64_t y_batch, y_step;
+  float* hT;                               /* forward: [batch, width] contiguous, or NULL        */
+  float* saved;                            /* spz_scan_saved floats: written by the forward call
+                                              (NULL: not wanted), read by the backward one       */
+  const void* dy;                          /* backward: [batch, steps, width] or NULL (zeros)    */
+  int64_t dy_batch, dy_step;
+  const float* dhT;                        /* backward: [batch, width] contiguous, or NULL       */
+  void *df, *dv;                           /* backward: [batch, steps, width]                    */
+  int64_t df_batch, df_step, dv_batch, dv_step;
+  float* dh0;                              /* backward: [batch, width] contiguous, or NULL       */
+  int32_t prec;                            /* of f, v, y, dy, df, dv                             */
+} spz_scan_args;
+
+/* Floats of `saved` (negative code on error). Only batch, steps, width and prec are read. */
+int64_t spz_scan_saved(const spz_scan_args* args);
+/* Bytes of the workspace (negative code on error). Only batch, steps, width and prec are read. */
+int64_t spz_scan_workspace(const spz_scan_args* args, int32_t backward);
+int spz_scan_forward(const spz_scan_args* args, void* workspace, int64_t workspace_bytes, void* hip_stream);
+int spz_scan_backward(const spz_scan_args* args, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* Norms before and after a block, its gate, dropout and residual scale, row by row:
+ *     n  = post(h) * w_post + b_post;   o = dropout(gate(z) * n)
+ *     x' = x + scale * o;               u = pre(x') * w_pre + b_pre
+ * post, pre: none (identity, without w and b), RMS: t / sqrt(mean(t^2) + eps), or layer:
+ * (t - mean(t)) / sqrt(mean((t - mean(t))^2) + eps). gate: 1 (z unused), sigmoid(z) or
+ * z sigmoid(z). dropout: spz_dropout's, of element row * width + column (drop_p = 0: none).
+ * h NULL: no block in front, x' = x, and x_out is not written (may be NULL): the first
+ * block's pre norm. Vectors of `width` floats; NULL stands for ones (w_post, w_pre, scale)
+ * or zeros (b_post, b_pre). u is taken from x' before x' is rounded. Rows r with
+ * valid[r] == 0 are not read: their outputs are zero and they give no gradient.
+ *
+ * Backward, from dx_out and du (NULL: zeros): dx, dh, dz (rounded to prec) and the sums
+ * over the rows dw_post, db_post, dscale, dw_pre, db_pre (float32, written; NULL: not
+ * wanted). dx, dh, dz may be NULL too. */
+#define SPZ_NORM_NONE 0
+#define SPZ_NORM_RMS 1
+#define SPZ_NORM_LAYER 2
+#define SPZ_GATE_NONE 0
+#define SPZ_GATE_SIGMOID 1
+#define SPZ_GATE_SILU 2
+typedef struct spz_block_norm_args {
+  int64_t rows, width;
+  const void *x, *h, *z;                   /* [rows, width]                                      */
+  int64_t x_row, h_row, z_row;
+  const float *w_post, *b_post, *scale, *w_pre, *b_pre;
+  const uint8_t* valid;                    /* [rows] or NULL (all of them)                       */
+  void *x_out, *u;                         /* forward: [rows, width]; u NULL where pre is none   */
+  int64_t x_out_row, u_row;
+  const void *dx_out, *du;                 /* backward: [rows, width]                            */
+  int64_t dx_out_row, du_row;
+  void *dx, *dh, *dz;                      /* backward: [rows, width]                            */
+  int64_t dx_row, dh_row, dz_row;
+  float *dw_post, *db_post, *dscale, *dw_pre, *db_pre;
+  uint64_t seed;                           /* dropout's, as in spz_dropout                       */
+  uint32_t step, tensor;
+  float drop_p, eps;                       /* eps > 0                                            */
+  int32_t post, pre, gate;
+  int32_t prec;                            /* of x, h, z, x_out, u and their gradients           */
+} spz_block_norm_args;
+
+/* Bytes of the backward call's workspace (negative code on error). */
+int64_t spz_block_norm_workspace(const spz_block_norm_args* args);
+int spz_block_norm_forward(const spz_block_norm_args* args, void* hip_stream);
+int spz_block_norm_backward(const spz_block_norm_args* args, void* workspace, int64_t workspace_bytes,
+                            void* hip_stream);
+
+/* Dropout whose mask is never stored: y = x * 65536 / (65536 - d) on kept elements, else 0,
+ * d = p rounded to 65536ths. Element i = row * width + column is kept when 16-bit word i & 7
+ * of Philox4x32-10 (key seed; counter (i >> 3 low 32 bits, step, 5 + 256 (i >> 35), tensor);
+ * low half of each 32-bit word first) is at least d. The same call on the gradient is the
+ * backward pass. p in [0, 1]. y may be x (with the same row stride). */
+int spz_dropout(int32_t prec, int64_t rows, int64_t width, const void* x, int64_t x_row, void* y, int64_t y_row,
+                float p, uint64_t seed, uint32_t step, uint32_t tensor, void* hip_stream);
+
+/* 8-bit integers with a scale for each row: scale[r] = max_c |x[r, c]| / 127 (float32),
+ * q[r, c] = x[r, c] / scale[r] rounded to the nearest integer, ties to even, within +-127; 0
+ * and 0 for a row of zeros. A row with an infinity or NaN gets a NaN scale and zeros. */
+int spz_quant_rows(int32_t prec, int64_t rows, int64_t width, const void* x, int64_t x_row, int8_t* q, int64_t q_row,
+                   float* scale, void* hip_stream);
+
+/* Weights q [outer, inner] in the order in which the product reads them, made once per set of
+ * weights: spz_quant_image_bytes (negative code on error) bytes, 16-byte aligned. */
+int64_t spz_quant_image_bytes(int64_t outer, int64_t inner);
+int spz_quant_pack(int64_t outer, int64_t inner, const int8_t* q, int64_t q_row, void* image, void* hip_stream);
+
+/* y[m, n] = s[m] w_scale[n] sum_k q[m, k] w[n, k] + bias[n], with q and s of spz_quant_rows
+ * of x (taken within the call) and the sum exact in 32-bit integers (inner <= 131072).
+ * x [rows, inner] and y [rows, outer] in `prec`; bias NULL: zeros. For the samplers' few rows
+ * (Section 3.1.1) as for whole batches. */
+int64_t spz_quant_linear_workspace(int32_t prec, int64_t rows, int64_t outer, int64_t inner);
+int spz_quant_linear(int32_t prec, int64_t rows, int64_t outer, int64_t inner, const void* x, int64_t x_row,
+                     const void* image, const float* w_scale, const float* bias, void* y, int64_t y_row,
+                     void* workspace, int64_t workspace_bytes, void* hip_stream);
+
 /* Message of the last failure: of ctx, or of the calling thread when ctx is
  * NULL. Never NULL; empty when there was none. Valid until the next call. */
 const char* spz_last_error(const spz_ctx* ctx);

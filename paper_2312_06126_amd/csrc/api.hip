@@ -36,6 +36,7 @@
 #include <new>
 
 #include "../../include/spz_testing.h"
+#include "ops.h"
 #include "rows.h"
 
 using namespace spz;
@@ -244,6 +245,20 @@ int set_err(spz_ctx* c, int code, const std::string& msg) {
 int fail_hip(spz_ctx* c, hipError_t e, const char* what) {
   return set_err(c, SPZ_EHIP, std::string(what) + ": " + hipGetErrorString(e));
 }
+
+}  // namespace
+
+// Error of a call without a context (ops.h): the thread's message. Never throws.
+int spz::op_error(int code, const char* call, const char* what) noexcept {
+  try {
+    tl_err = std::string(call) + ": " + what;
+  } catch (...) {
+    tl_err.clear();
+  }
+  return code;
+}
+
+namespace {
 
 #define CK(x)                                          \
   do {                                                 \

@@ -1,0 +1,793 @@
+// Norms before and after a block with its gate, dropout and residual scale in one pass over the
+// rows (spz_block_norm_*), and dropout by itself (spz_dropout).
+//
+//   n = post(h) w_post + b_post,  o = drop(gate(z) n),  x' = x + scale o,  u = pre(x') w_pre + b_pre
+//
+// Bound by HBM: forward 3 arrays read and 2 written, backward 5 read and 3 written, for about 30
+// and 90 instructions an element. A row stays in the registers of TPR threads (16 lanes, a wave, or
+// a workgroup, by its width) from its loads to its stores, so the statistics of both norms and their
+// gradients are sums over registers and nothing is read twice; variances are of the centred values.
+// The backward pass recomputes the forward one from x, h and z (cheaper than reading x' and the
+// statistics back). Its groups walk the rows with a stride and keep the column sums of the vector
+// gradients in registers; a workgroup adds its groups in LDS, then norm_sums adds the workgroups
+// in order: no atomics, the same bits on every run. Rows wider than the registers hold take
+// norm_wide, which reads them again for each statistic.
+#include "ops.h"
+
+namespace spz {
+namespace {
+
+constexpr int NORM_THREADS = 256;
+constexpr int NORM_VECTORS = 5;          // dw_post, db_post, dscale, dw_pre, db_pre
+constexpr int64_t NORM_MAX_BLOCKS = 512; // of the backward pass: two workgroups a compute unit
+
+struct Drop { uint32_t d; float gain; bool on; };
+
+struct NormArgs {
+  spz_block_norm_args a;
+  Drop drop;
+  float* part;        // backward: [blocks, NORM_VECTORS, width]
+};
+
+// ----------------------------------------------------------------------------- sums over a row
+template <int CTRL> __device__ inline float dpp_add(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+}
+// Over 16 lanes (every lane gets it): neighbours, pairs, the halves mirrored, the row mirrored.
+__device__ inline float sum16(float x) {
+  x = dpp_add<0xB1>(x);
+  x = dpp_add<0x4E>(x);
+  x = dpp_add<0x141>(x);
+  return dpp_add<0x140>(x);
+}
+__device__ inline float sum64(float x) {
+  x = sum16(x);
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+// Sums over the TPR threads of a row. More than a wave: through LDS, two buffers in turn so that one
+// barrier a sum is enough (a wave that writes a buffer again has passed the other one's barrier).
+template <int TPR> struct RowSum {
+  __device__ float operator()(float x) { return TPR == 16 ? sum16(x) : sum64(x); }
+};
+template <int TPR> struct WideSum {
+  float (*buf)[TPR / 64];
+  int slot = 0;
+  __device__ float operator()(float x) {
+    x = sum64(x);
+    if (threadIdx.x % 64 == 0) buf[slot][threadIdx.x / 64] = x;
+    __syncthreads();
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < TPR / 64; ++i) s += buf[slot][i];
+    slot ^= 1;
+    return s;
+  }
+};
+
+// ----------------------------------------------------------------------------- a row in registers
+// Thread `lane` of TPR holds K chunks of VW elements. VEC: chunk j is the VW columns from
+// (j TPR + lane) VW on, one 16-byte access; else its elements are TPR columns apart, so that
+// the threads of a row still read neighbours.
+template <typename T, bool VEC, int TPR, int K> struct RowMap {
+  static constexpr int VW = OP_VEC<T>, N = K * VW;
+  int lane;
+  int64_t D;
+  __device__ int64_t col(int j, int i) const {
+    return VEC ? ((int64_t)j * TPR + lane) * VW + i : ((int64_t)j * VW + i) * TPR + lane;
+  }
+  __device__ void load(const T* p, float (&x)[N]) const {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      if constexpr (VEC) {
+        float t[VW];
+        u32x4 w = {0, 0, 0, 0};
+        if (col(j, 0) < D) w = *reinterpret_cast<const u32x4*>(p + col(j, 0));
+        unpack(w, t);
+#pragma unroll
+        for (int i = 0; i < VW; ++i) x[j * VW + i] = t[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < VW; ++i) x[j * VW + i] = col(j, i) < D ? to_f<T>(p[col(j, i)]) : 0.0f;
+      }
+    }
+  }
+  __device__ void store(T* p, const float (&x)[N]) const {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      if constexpr (VEC) {
+        float t[VW];
+#pragma unroll
+        for (int i = 0; i < VW; ++i) t[i] = x[j * VW + i];
+        if (col(j, 0) < D) *reinterpret_cast<u32x4*>(p + col(j, 0)) = pack(t);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VW; ++i)
+          if (col(j, i) < D) p[col(j, i)] = from_f<T>(x[j * VW + i]);
+      }
+    }
+  }
+  // A parameter vector; NULL: `other`. Columns past the width: 0.
+  __device__ void vec(const float* p, float other, float (&x)[N]) const {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      if constexpr (VEC) {
+#pragma unroll
+        for (int i = 0; i < VW; i += 4) {
+          f32x4 w = {other, other, other, other};
+          if (p && col(j, 0) < D) w = *reinterpret_cast<const f32x4*>(p + col(j, i));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[j * VW + i + k] = w[k];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < VW; ++i) x[j * VW + i] = p && col(j, i) < D ? p[col(j, i)] : other;
+      }
+    }
+  }
+  // Dropout's factor of each element of the row.
+  __device__ void factor(const spz_block_norm_args& a, const Drop& d, int64_t row, float (&x)[N]) const {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      if constexpr (VEC) {
+        const uint64_t e = (uint64_t)row * D + col(j, 0);
+        const U4 w = drop_words(e >> 3, a.seed, a.step, a.tensor);
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+          const uint32_t h = VW == 8 ? drop_half(w, i) : ((e & 4) ? drop_half(w, 4 + (i & 3)) : drop_half(w, i & 3));
+          x[j * VW + i] = h >= d.d ? d.gain : 0.0f;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+          const uint64_t e = (uint64_t)row * D + col(j, i);
+          const U4 w = drop_words(e >> 3, a.seed, a.step, a.tensor);
+          const uint32_t v = (e & 4) ? ((e & 2) ? w.w : w.z) : ((e & 2) ? w.y : w.x);
+          x[j * VW + i] = ((e & 1) ? v >> 16 : v & 0xFFFFu) >= d.d ? d.gain : 0.0f;
+        }
+      }
+    }
+  }
+  // Normalised in place; returns the factor 1 / sqrt(var + eps) (1 where the norm is none).
+  template <typename SUM> __device__ float norm(int kind, float eps, float inv_d, SUM& sum, float (&x)[N]) const {
+    if (kind == SPZ_NORM_NONE) return 1.0f;
+    if (kind == SPZ_NORM_LAYER) {
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) s += x[i];
+      const float mean = sum(s) * inv_d;
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int i = 0; i < VW; ++i) x[j * VW + i] = col(j, i) < D ? x[j * VW + i] - mean : 0.0f;
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s = fmaf(x[i], x[i], s);
+    const float r = 1.0f / sqrtf(fmaf(sum(s), inv_d, eps));
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] *= r;
+    return r;
+  }
+  // dn (gradient to the normalised n, times its weight) -> gradient to the norm's input.
+  template <typename SUM>
+  __device__ void norm_back(int kind, float r, float inv_d, SUM& sum, const float (&n)[N], float (&dn)[N]) const {
+    if (kind == SPZ_NORM_NONE) return;
+    float s = 0.0f, q = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      s = fmaf(dn[i], n[i], s);
+      q += dn[i];
+    }
+    s = sum(s) * inv_d;
+    q = kind == SPZ_NORM_LAYER ? sum(q) * inv_d : 0.0f;
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+#pragma unroll
+      for (int i = 0; i < VW; ++i) {
+        const int e = j * VW + i;
+        dn[e] = col(j, i) < D ? r * (dn[e] - fmaf(n[e], s, q)) : 0.0f;
+      }
+  }
+};
+
+// gate(z) and its slope.
+__device__ inline void gate_value(int kind, float z, float& g, float& slope) {
+  if (kind == SPZ_GATE_NONE) {
+    g = 1.0f;
+    slope = 0.0f;
+    return;
+  }
+  float s, t;
+  sigmoid2(z, s, t);
+  // z = -inf closes the gate: z sigmoid(z) -> 0 there, not -inf * 0.
+  g = kind == SPZ_GATE_SIGMOID ? s : (s == 0.0f ? 0.0f : z * s);
+  slope = kind == SPZ_GATE_SIGMOID ? s * t : (s == 0.0f || t == 0.0f ? s : s * fmaf(z, t, 1.0f));
+}
+
+template <typename T, bool VEC, int TPR, int K>
+__global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void norm_forward(NormArgs g) {
+  using M = RowMap<T, VEC, TPR, K>;
+  constexpr int N = M::N, GROUPS = TPR >= NORM_THREADS ? 1 : NORM_THREADS / TPR;
+  const spz_block_norm_args& a = g.a;
+  const M m{(int)(threadIdx.x % TPR), a.width};
+  const int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / TPR;
+  if (row >= a.rows) return;
+  T* xo = a.h ? static_cast<T*>(a.x_out) + row * a.x_out_row : nullptr;
+  T* u = a.pre != SPZ_NORM_NONE ? static_cast<T*>(a.u) + row * a.u_row : nullptr;
+  float x[N], h[N], z[N], w[N];
+  if (a.valid && !a.valid[row]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = 0.0f;
+    if (xo) m.store(xo, x);
+    if (u) m.store(u, x);
+    return;
+  }
+  const float inv_d = 1.0f / (float)a.width;
+  __shared__ float buf[2][TPR > 64 ? TPR / 64 : 1];
+  typename std::conditional<(TPR > 64), WideSum<(TPR > 64 ? TPR : 128)>, RowSum<TPR>>::type sum{};
+  if constexpr (TPR > 64) sum.buf = buf;
+  m.load(static_cast<const T*>(a.x) + row * a.x_row, x);
+  if (a.h) {
+    m.load(static_cast<const T*>(a.h) + row * a.h_row, h);
+    if (a.gate != SPZ_GATE_NONE) m.load(static_cast<const T*>(a.z) + row * a.z_row, z);
+    m.norm(a.post, a.eps, inv_d, sum, h);
+    if (a.post != SPZ_NORM_NONE) {
+      if (a.w_post) {
+        m.vec(a.w_post, 1.0f, w);
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[i] *= w[i];
+      }
+      if (a.b_post) {
+        m.vec(a.b_post, 0.0f, w);
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[i] += w[i];
+      }
+    }
+    if (a.gate != SPZ_GATE_NONE) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        float gt, slope;
+        gate_value(a.gate, z[i], gt, slope);
+        h[i] *= gt;
+      }
+    }
+    if (g.drop.on) {
+      m.factor(a, g.drop, row, w);
+#pragma unroll
+      for (int i = 0; i < N; ++i) h[i] = w[i] == 0.0f ? 0.0f : h[i] * w[i];
+    }
+    m.vec(a.scale, 1.0f, w);
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+#pragma unroll
+      for (int i = 0; i < M::VW; ++i) {
+        const int e = j * M::VW + i;
+        x[e] = m.col(j, i) < a.width ? fmaf(w[e], h[e], x[e]) : 0.0f;
+      }
+    m.store(xo, x);
+  }
+  if (!u) return;
+  m.norm(a.pre, a.eps, inv_d, sum, x);
+  if (a.w_pre) {
+    m.vec(a.w_pre, 1.0f, w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] *= w[i];
+  }
+  if (a.b_pre) {
+    m.vec(a.b_pre, 0.0f, w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += w[i];
+  }
+  m.store(u, x);
+}
+
+template <typename T, bool VEC, int TPR, int K>
+__global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void norm_backward(NormArgs g) {
+  using M = RowMap<T, VEC, TPR, K>;
+  constexpr int N = M::N, GROUPS = TPR >= NORM_THREADS ? 1 : NORM_THREADS / TPR;
+  const spz_block_norm_args& a = g.a;
+  const M m{(int)(threadIdx.x % TPR), a.width};
+  const float inv_d = 1.0f / (float)a.width;
+  __shared__ float buf[2][TPR > 64 ? TPR / 64 : 1];
+  typename std::conditional<(TPR > 64), WideSum<(TPR > 64 ? TPR : 128)>, RowSum<TPR>>::type sum{};
+  if constexpr (TPR > 64) sum.buf = buf;
+  float acc[NORM_VECTORS][N];
+#pragma unroll
+  for (int k = 0; k < NORM_VECTORS; ++k)
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[k][i] = 0.0f;
+
+  for (int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * GROUPS) {
+    float x[N], h[N], z[N], w[N], d[N], du[N];
+    if (a.valid && !a.valid[row]) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = 0.0f;
+      if (a.dx) m.store(static_cast<T*>(a.dx) + row * a.dx_row, x);
+      if (a.h && a.dh) m.store(static_cast<T*>(a.dh) + row * a.dh_row, x);
+      if (a.h && a.gate != SPZ_GATE_NONE && a.dz) m.store(static_cast<T*>(a.dz) + row * a.dz_row, x);
+      continue;
+    }
+    m.load(static_cast<const T*>(a.x) + row * a.x_row, x);
+    if (a.h) m.load(static_cast<const T*>(a.h) + row * a.h_row, h);
+    if (a.h && a.gate != SPZ_GATE_NONE) m.load(static_cast<const T*>(a.z) + row * a.z_row, z);
+    if (a.dx_out) m.load(static_cast<const T*>(a.dx_out) + row * a.dx_out_row, d);
+    else
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] = 0.0f;
+    const bool has_du = a.du && a.pre != SPZ_NORM_NONE;
+    if (has_du) m.load(static_cast<const T*>(a.du) + row * a.du_row, du);
+
+    // Forward: n in h, t = n w + b, gate and its slope (in z), dropout's factor, o, x' in x.
+    float t[N], gt[N], f[N], rh = 1.0f;
+    if (a.h) {
+      rh = m.norm(a.post, a.eps, inv_d, sum, h);
+#pragma unroll
+      for (int i = 0; i < N; ++i) t[i] = h[i];
+      if (a.post != SPZ_NORM_NONE) {
+        m.vec(a.w_post, 1.0f, w);
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] *= w[i];
+        if (a.b_post) {
+          m.vec(a.b_post, 0.0f, w);
+#pragma unroll
+          for (int i = 0; i < N; ++i) t[i] += w[i];
+        }
+      }
+      if (a.gate != SPZ_GATE_NONE) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          float slope;
+          gate_value(a.gate, z[i], gt[i], slope);
+          z[i] = slope;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) { gt[i] = 1.0f; z[i] = 0.0f; }
+      }
+      if (g.drop.on) m.factor(a, g.drop, row, f);
+      else
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = 1.0f;
+      m.vec(a.scale, 1.0f, w);
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int i = 0; i < M::VW; ++i) {
+          const int e = j * M::VW + i;
+          const float o = f[e] == 0.0f ? 0.0f : gt[e] * t[e] * f[e];
+          x[e] = m.col(j, i) < a.width ? fmaf(w[e], o, x[e]) : 0.0f;
+        }
+    }
+    // Through the pre norm: d becomes the gradient to x'.
+    if (has_du) {
+      const float rx = m.norm(a.pre, a.eps, inv_d, sum, x);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        acc[3][i] = fmaf(du[i], x[i], acc[3][i]);
+        acc[4][i] += du[i];
+      }
+      m.vec(a.w_pre, 1.0f, w);
+#pragma unroll
+      for (int i = 0; i < N; ++i) du[i] *= w[i];
+      m.norm_back(a.pre, rx, inv_d, sum, x, du);
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] += du[i];
+    }
+    if (a.dx) m.store(static_cast<T*>(a.dx) + row * a.dx_row, d);
+    if (!a.h) continue;
+    m.vec(a.scale, 1.0f, w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float gd = f[i] == 0.0f ? 0.0f : d[i] * f[i];   // through dropout
+      acc[2][i] = fmaf(gd, gt[i] * t[i], acc[2][i]);
+      d[i] = gd * w[i];                                     // gradient to gate(z) n
+      z[i] *= d[i] * t[i];
+      d[i] *= gt[i];                                        // gradient to n w + b
+      acc[0][i] = fmaf(d[i], h[i], acc[0][i]);
+      acc[1][i] += d[i];
+    }
+    if (a.gate != SPZ_GATE_NONE && a.dz) m.store(static_cast<T*>(a.dz) + row * a.dz_row, z);
+    if (!a.dh) continue;
+    if (a.post != SPZ_NORM_NONE) {
+      m.vec(a.w_post, 1.0f, w);
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] *= w[i];
+      m.norm_back(a.post, rh, inv_d, sum, h, d);
+    }
+    m.store(static_cast<T*>(a.dh) + row * a.dh_row, d);
+  }
+
+  // Column sums of the workgroup's groups, in their order.
+  if constexpr (GROUPS == 1) {
+#pragma unroll
+    for (int k = 0; k < NORM_VECTORS; ++k)
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int i = 0; i < M::VW; ++i)
+          if (m.col(j, i) < a.width)
+            g.part[((int64_t)blockIdx.x * NORM_VECTORS + k) * a.width + m.col(j, i)] = acc[k][j * M::VW + i];
+  } else {
+    __shared__ float sums[GROUPS][TPR * N];
+    for (int k = 0; k < NORM_VECTORS; ++k) {
+      __syncthreads();
+#pragma unroll
+      for (int kk = 0; kk < NORM_VECTORS; ++kk)
+        if (kk == k)
+#pragma unroll
+          for (int i = 0; i < N; ++i) sums[threadIdx.x / TPR][i * TPR + m.lane] = acc[kk][i];
+      __syncthreads();
+      for (int e = threadIdx.x; e < TPR * N; e += NORM_THREADS) {
+        const M me{e % TPR, a.width};
+        const int64_t c = me.col(e / TPR / M::VW, e / TPR % M::VW);
+        if (c >= a.width) continue;
+        float s = 0.0f;
+#pragma unroll
+        for (int r = 0; r < GROUPS; ++r) s += sums[r][e];
+        g.part[((int64_t)blockIdx.x * NORM_VECTORS + k) * a.width + c] = s;
+      }
+    }
+  }
+}
+
+// out[k][c] = sum over the workgroups b of part[b][k][c]: 8 threads a column take every 8th each.
+struct SumArgs { float* out[NORM_VECTORS]; };
+constexpr int SUM_COLS = 32, SUM_GROUPS = 8;
+__global__ __launch_bounds__(SUM_COLS * SUM_GROUPS) void norm_sums(const float* part, SumArgs o, int64_t width, int blocks) {
+  __shared__ float s[SUM_GROUPS][SUM_COLS];
+  const int c = threadIdx.x % SUM_COLS, gr = threadIdx.x / SUM_COLS, k = blockIdx.x % NORM_VECTORS;
+  float* out = o.out[k];
+  if (!out) return;
+  const int64_t col = (int64_t)(blockIdx.x / NORM_VECTORS) * SUM_COLS + c;
+  float x = 0.0f;
+  if (col < width)
+    for (int b = gr; b < blocks; b += SUM_GROUPS) x += part[((int64_t)b * NORM_VECTORS + k) * width + col];
+  s[gr][c] = x;
+  __syncthreads();
+  if (gr || col >= width) return;
+#pragma unroll
+  for (int i = 1; i < SUM_GROUPS; ++i) x += s[i][c];
+  out[col] = x;
+}
+
+// ----------------------------------------------------------------------------- rows of any width
+// One workgroup a row, which reads it once for every statistic (from L2 after the first time).
+constexpr int WIDE_THREADS = 1024;
+template <typename T, bool BACK> __global__ __launch_bounds__(WIDE_THREADS) void norm_wide(NormArgs g) {
+  const spz_block_norm_args& a = g.a;
+  __shared__ float buf[2][WIDE_THREADS / 64];
+  WideSum<WIDE_THREADS> sum{buf};
+  const int64_t D = a.width;
+  const float inv_d = 1.0f / (float)D;
+  float* part = BACK ? g.part + (int64_t)blockIdx.x * NORM_VECTORS * D : nullptr;
+  if (BACK)
+    for (int64_t c = threadIdx.x; c < D; c += WIDE_THREADS)
+      for (int k = 0; k < NORM_VECTORS; ++k) part[k * D + c] = 0.0f;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const bool on = !a.valid || a.valid[row];
+    const bool has_du = BACK && a.du && a.pre != SPZ_NORM_NONE;
+    const auto at = [&](const void* p, int64_t stride, int64_t c) { return to_f<T>(static_cast<const T*>(p)[row * stride + c]); };
+    const auto put = [&](void* p, int64_t stride, int64_t c, float v) {
+      if (p) static_cast<T*>(p)[row * stride + c] = from_f<T>(v);
+    };
+    const auto w = [&](const float* p, float other, int64_t c) { return p ? p[c] : other; };
+    if (!on) {
+      for (int64_t c = threadIdx.x; c < D; c += WIDE_THREADS) {
+        if (BACK) {
+          put(a.dx, a.dx_row, c, 0.0f);
+          if (a.h) put(a.dh, a.dh_row, c, 0.0f);
+          if (a.h && a.gate != SPZ_GATE_NONE) put(a.dz, a.dz_row, c, 0.0f);
+        } else {
+          if (a.h) put(a.x_out, a.x_out_row, c, 0.0f);
+          if (a.pre != SPZ_NORM_NONE) put(a.u, a.u_row, c, 0.0f);
+        }
+      }
+      continue;
+    }
+    float mh = 0.0f, rh = 1.0f, mx = 0.0f, rx = 1.0f;
+    struct El { float n, t, gt, slope, f, x; };
+    const auto value = [&](int64_t c) {   // the element's forward values up to x'
+      El e{0.0f, 0.0f, 1.0f, 0.0f, 1.0f, at(a.x, a.x_row, c)};
+      if (!a.h) return e;
+      e.n = (at(a.h, a.h_row, c) - mh) * rh;
+      e.t = a.post != SPZ_NORM_NONE ? fmaf(e.n, w(a.w_post, 1.0f, c), w(a.b_post, 0.0f, c)) : e.n;
+      if (a.gate != SPZ_GATE_NONE) gate_value(a.gate, at(a.z, a.z_row, c), e.gt, e.slope);
+      if (g.drop.on) {
+        const uint64_t i = (uint64_t)row * D + c;
+        const U4 v = drop_words(i >> 3, a.seed, a.step, a.tensor);
+        const uint32_t q = (i & 4) ? ((i & 2) ? v.w : v.z) : ((i & 2) ? v.y : v.x);
+        e.f = ((i & 1) ? q >> 16 : q & 0xFFFFu) >= g.drop.d ? g.drop.gain : 0.0f;
+      }
+      if (e.f != 0.0f) e.x = fmaf(w(a.scale, 1.0f, c), e.gt * e.t * e.f, e.x);
+      return e;
+    };
+    const auto total = [&](auto&& term) {
+      float s = 0.0f;
+      for (int64_t c = threadIdx.x; c < D; c += WIDE_THREADS) s += term(c);
+      return sum(s);
+    };
+    if (a.h && a.post != SPZ_NORM_NONE) {
+      if (a.post == SPZ_NORM_LAYER) mh = total([&](int64_t c) { return at(a.h, a.h_row, c); }) * inv_d;
+      rh = 1.0f / sqrtf(total([&](int64_t c) { const float v = at(a.h, a.h_row, c) - mh; return v * v; }) * inv_d + a.eps);
+    }
+    if (BACK ? has_du : a.pre != SPZ_NORM_NONE) {
+      if (a.pre == SPZ_NORM_LAYER) mx = total([&](int64_t c) { return value(c).x; }) * inv_d;
+      rx = 1.0f / sqrtf(total([&](int64_t c) { const float v = value(c).x - mx; return v * v; }) * inv_d + a.eps);
+    }
+    if (!BACK) {
+      for (int64_t c = threadIdx.x; c < D; c += WIDE_THREADS) {
+        const El e = value(c);
+        if (a.h) put(a.x_out, a.x_out_row, c, e.x);
+        if (a.pre != SPZ_NORM_NONE) put(a.u, a.u_row, c, fmaf((e.x - mx) * rx, w(a.w_pre, 1.0f, c), w(a.b_pre, 0.0f, c)));
+      }
+      continue;
+    }
+    float s1 = 0.0f, s2 = 0.0f, q1 = 0.0f, q2 = 0.0f;
+    if (has_du) {
+      s1 = total([&](int64_t c) { return at(a.du, a.du_row, c) * w(a.w_pre, 1.0f, c) * ((value(c).x - mx) * rx); }) * inv_d;
+      if (a.pre == SPZ_NORM_LAYER) s2 = total([&](int64_t c) { return at(a.du, a.du_row, c) * w(a.w_pre, 1.0f, c); }) * inv_d;
+    }
+    const auto grad = [&](int64_t c, const El& e) {   // to x'
+      float d = a.dx_out ? at(a.dx_out, a.dx_out_row, c) : 0.0f;
+      if (has_du) d += rx * (at(a.du, a.du_row, c) * w(a.w_pre, 1.0f, c) - fmaf((e.x - mx) * rx, s1, s2));
+      return d;
+    };
+    const auto grad_t = [&](int64_t c, const El& e) {   // to n w_post + b_post
+      return e.f == 0.0f ? 0.0f : grad(c, e) * e.f * w(a.scale, 1.0f, c) * e.gt;
+    };
+    if (a.h && a.dh && a.post != SPZ_NORM_NONE) {
+      q1 = total([&](int64_t c) { const El e = value(c); return grad_t(c, e) * w(a.w_post, 1.0f, c) * e.n; }) * inv_d;
+      if (a.post == SPZ_NORM_LAYER)
+        q2 = total([&](int64_t c) { const El e = value(c); return grad_t(c, e) * w(a.w_post, 1.0f, c); }) * inv_d;
+    }
+    for (int64_t c = threadIdx.x; c < D; c += WIDE_THREADS) {
+      const El e = value(c);
+      const float d = grad(c, e), dt = grad_t(c, e);
+      put(a.dx, a.dx_row, c, d);
+      if (has_du) {
+        const float u = at(a.du, a.du_row, c);
+        part[3 * D + c] += u * ((e.x - mx) * rx);
+        part[4 * D + c] += u;
+      }
+      if (!a.h) continue;
+      const float gd = e.f == 0.0f ? 0.0f : d * e.f;
+      part[0 * D + c] += dt * e.n;
+      part[1 * D + c] += dt;
+      part[2 * D + c] += gd * (e.gt * e.t);
+      if (a.gate != SPZ_GATE_NONE) put(a.dz, a.dz_row, c, gd * w(a.scale, 1.0f, c) * e.t * e.slope);
+      if (a.dh)
+        put(a.dh, a.dh_row, c, a.post != SPZ_NORM_NONE ? rh * (dt * w(a.w_post, 1.0f, c) - fmaf(e.n, q1, q2)) : dt);
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------- dropout
+// Eight elements a thread: one Philox block. FLAT: rows follow each other without a gap and the
+// arrays are 16-byte aligned, so that they are one row of eights with a ragged end.
+template <typename T, bool FLAT>
+__global__ __launch_bounds__(256) void dropout(const T* x, int64_t x_row, T* y, int64_t y_row, int64_t width, int64_t n,
+                                               Drop d, uint64_t seed, uint32_t step, uint32_t tensor) {
+  constexpr int VW = OP_VEC<T>;
+  const int64_t blk = (int64_t)blockIdx.x * 256 + threadIdx.x, i0 = blk * 8;
+  if (i0 >= n) return;
+  if (FLAT && i0 + 8 <= n) {
+    float v[8 / VW][VW];
+#pragma unroll
+    for (int j = 0; j < 8 / VW; ++j) unpack(*reinterpret_cast<const u32x4*>(x + i0 + j * VW), v[j]);
+    const U4 w = drop_words((uint64_t)blk, seed, step, tensor);
+#pragma unroll
+    for (int j = 0; j < 8 / VW; ++j) {
+#pragma unroll
+      for (int i = 0; i < VW; ++i) v[j][i] = drop_half(w, j * VW + i) >= d.d ? v[j][i] * d.gain : 0.0f;
+      *reinterpret_cast<u32x4*>(y + i0 + j * VW) = pack(v[j]);
+    }
+    return;
+  }
+  const U4 w = drop_words((uint64_t)blk, seed, step, tensor);
+  int64_t r = i0 / width, c = i0 - r * width;
+  float v[8];
+  int64_t to[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    to[i] = -1;
+    if (i0 + i < n) {
+      v[i] = drop_half(w, i) >= d.d ? to_f<T>(x[r * x_row + c]) * d.gain : 0.0f;
+      to[i] = r * y_row + c;
+    }
+    if (++c == width) { c = 0; ++r; }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (to[i] >= 0) y[to[i]] = from_f<T>(v[i]);
+}
+
+// ----------------------------------------------------------------------------- launches
+template <typename T, bool VEC, int TPR, int K> void norm_launch(const NormArgs& g, bool back, int64_t blocks, hipStream_t s) {
+  constexpr int threads = TPR > NORM_THREADS ? TPR : NORM_THREADS, groups = threads / TPR;
+  if (back) norm_backward<T, VEC, TPR, K><<<dim3((unsigned)blocks), threads, 0, s>>>(g);
+  else norm_forward<T, VEC, TPR, K><<<dim3((unsigned)op_div_up(g.a.rows, groups)), threads, 0, s>>>(g);
+}
+
+// Threads a row: the fewest of 16, 64, 256, 1024 that hold it in at most 32 elements each (16 lanes
+// and 1024 threads: 16); 0: norm_wide.
+int norm_tpr(int64_t width, int vw) {
+  const int64_t chunks = op_div_up(width, vw), k = 32 / vw;
+  return chunks <= 16 * (k / 2) ? 16 : chunks <= 64 * k ? 64 : chunks <= 256 * k ? 256 : chunks <= 1024 * (k / 2) ? 1024 : 0;
+}
+int64_t norm_blocks(const spz_block_norm_args& a) {   // of the backward pass
+  const int tpr = norm_tpr(a.width, 16 / op_size(a.prec));
+  const int64_t rows = tpr == 0 || tpr >= NORM_THREADS ? 1 : NORM_THREADS / tpr;
+  const int64_t n = op_div_up(a.rows, rows);
+  return n < NORM_MAX_BLOCKS ? n : NORM_MAX_BLOCKS;
+}
+
+template <typename T, bool VEC> void norm_dispatch(const NormArgs& g, bool back, int64_t blocks, hipStream_t s) {
+  constexpr int VW = OP_VEC<T>, KM = 32 / VW;
+  const int tpr = norm_tpr(g.a.width, VW);
+  const int64_t k = tpr ? op_div_up(op_div_up(g.a.width, VW), tpr) : 0;
+  if (tpr == 16) {
+    if (k <= KM / 4) norm_launch<T, VEC, 16, KM / 4>(g, back, blocks, s);
+    else norm_launch<T, VEC, 16, KM / 2>(g, back, blocks, s);
+  } else if (tpr == 64) {
+    if (k <= KM / 2) norm_launch<T, VEC, 64, KM / 2>(g, back, blocks, s);
+    else norm_launch<T, VEC, 64, KM>(g, back, blocks, s);
+  } else if (tpr == 256) {
+    if (k <= KM / 2) norm_launch<T, VEC, 256, KM / 2>(g, back, blocks, s);
+    else norm_launch<T, VEC, 256, KM>(g, back, blocks, s);
+  } else if (tpr == 1024) {
+    norm_launch<T, VEC, 1024, KM / 2>(g, back, blocks, s);
+  } else if (back) {
+    norm_wide<T, true><<<dim3((unsigned)blocks), WIDE_THREADS, 0, s>>>(g);
+  } else {
+    norm_wide<T, false><<<dim3((unsigned)(g.a.rows < 65536 ? g.a.rows : 65536)), WIDE_THREADS, 0, s>>>(g);
+  }
+}
+
+const char* norm_check(const spz_block_norm_args* p) {
+  if (!p) return "NULL arguments";
+  const spz_block_norm_args& a = *p;
+  if (!op_prec_ok(a.prec)) return "unknown precision";
+  if (!op_extent_ok(a.rows) || !op_extent_ok(a.width)) return "extent out of range";
+  if (a.width && a.rows > ((int64_t)1 << 44) / a.width) return "extents out of range";
+  if (a.post < SPZ_NORM_NONE || a.post > SPZ_NORM_LAYER || a.pre < SPZ_NORM_NONE || a.pre > SPZ_NORM_LAYER)
+    return "unknown norm";
+  if (a.gate < SPZ_GATE_NONE || a.gate > SPZ_GATE_SILU) return "unknown gate";
+  if (!(a.eps > 0.0f) || !(a.eps < 3.0e38f)) return "eps out of range";
+  if (!(a.drop_p >= 0.0f && a.drop_p <= 1.0f)) return "drop_p outside [0, 1]";
+  return nullptr;
+}
+
+const char* norm_check_arrays(const spz_block_norm_args& a, bool back) {
+  const bool some = a.rows > 0 && a.width > 0, z = a.h && a.gate != SPZ_GATE_NONE, pre = a.pre != SPZ_NORM_NONE;
+  const size_t e = op_size(a.prec);
+  if (some && !a.x) return "NULL x";
+  if (some && !a.h && !pre) return "neither a block nor a pre norm";
+  if (some && z && !a.z) return "NULL z";
+  if (some && !back && ((a.h && !a.x_out) || (pre && !a.u))) return "NULL output";
+  for (const void* p : {a.x, a.h, a.z, a.dx_out, a.du, (const void*)a.x_out, (const void*)a.u, (const void*)a.dx,
+                        (const void*)a.dh, (const void*)a.dz})
+    if (!op_aligned(p, e)) return "array not aligned to its type";
+  for (const float* p : {a.w_post, a.b_post, a.scale, a.w_pre, a.b_pre, (const float*)a.dw_post, (const float*)a.db_post,
+                         (const float*)a.dscale, (const float*)a.dw_pre, (const float*)a.db_pre})
+    if (!op_aligned(p, 4)) return "vector not aligned to 4 bytes";
+  if (!op_in_stride_ok(a.x_row) || (a.h && !op_in_stride_ok(a.h_row)) || (z && !op_in_stride_ok(a.z_row)))
+    return "input stride out of range";
+  if (!back) {
+    if (a.h && !op_out_stride_ok(a.rows, a.width, a.x_out_row)) return "rows of x_out overlap";
+    if (pre && !op_out_stride_ok(a.rows, a.width, a.u_row)) return "rows of u overlap";
+    return nullptr;
+  }
+  if ((a.dx_out && !op_in_stride_ok(a.dx_out_row)) || (a.du && pre && !op_in_stride_ok(a.du_row))) return "input stride out of range";
+  if (a.dx && !op_out_stride_ok(a.rows, a.width, a.dx_row)) return "rows of dx overlap";
+  if (a.h && a.dh && !op_out_stride_ok(a.rows, a.width, a.dh_row)) return "rows of dh overlap";
+  if (z && a.dz && !op_out_stride_ok(a.rows, a.width, a.dz_row)) return "rows of dz overlap";
+  return nullptr;
+}
+
+// 16-byte accesses everywhere: every array that the call touches is aligned for them.
+bool norm_vec(const spz_block_norm_args& a, bool back) {
+  const int e = op_size(a.prec);
+  if (a.width % (16 / e)) return false;
+  const auto ok = [&](const void* p, int64_t s) { return !p || op_vec_ok(p, s, e); };
+  for (const float* p : {a.w_post, a.b_post, a.scale, a.w_pre, a.b_pre})
+    if (!op_aligned(p, 16)) return false;
+  const bool z = a.h && a.gate != SPZ_GATE_NONE, pre = a.pre != SPZ_NORM_NONE;
+  if (!ok(a.x, a.x_row) || !ok(a.h, a.h_row) || (z && !ok(a.z, a.z_row))) return false;
+  if (!back) return (!a.h || ok(a.x_out, a.x_out_row)) && (!pre || ok(a.u, a.u_row));
+  return ok(a.dx_out, a.dx_out_row) && (!pre || ok(a.du, a.du_row)) && ok(a.dx, a.dx_row) &&
+         (!a.h || ok(a.dh, a.dh_row)) && (!z || ok(a.dz, a.dz_row));
+}
+
+int norm_run(const char* call, const spz_block_norm_args* args, bool back, void* ws, int64_t ws_bytes, void* stream) {
+  const char* bad = norm_check(args);
+  if (!bad) bad = norm_check_arrays(*args, back);
+  if (bad) return op_error(SPZ_EINVAL, call, bad);
+  NormArgs g{};
+  g.a = *args;
+  const spz_block_norm_args& a = g.a;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int64_t blocks = back ? norm_blocks(a) : 0;
+  if (back) {
+    const int64_t need = spz_block_norm_workspace(args);
+    if (need > 0 && (!ws || ws_bytes < need)) return op_error(SPZ_ESIZE, call, "workspace too small");
+    if (need > 0 && !op_aligned(ws, 16)) return op_error(SPZ_EINVAL, call, "workspace not aligned to 16 bytes");
+    g.part = static_cast<float*>(ws);
+  }
+  if (a.width == 0) return SPZ_OK;
+  g.drop.d = drop_threshold(a.drop_p);
+  g.drop.gain = drop_gain(g.drop.d);
+  g.drop.on = g.drop.d > 0;
+  const bool vec = norm_vec(a, back);
+  if (a.rows > 0) {
+    if (a.prec == SPZ_PREC_BF16) {
+      if (vec) norm_dispatch<bf16_t, true>(g, back, blocks, s);
+      else norm_dispatch<bf16_t, false>(g, back, blocks, s);
+    } else {
+      if (vec) norm_dispatch<float, true>(g, back, blocks, s);
+      else norm_dispatch<float, false>(g, back, blocks, s);
+    }
+  }
+  if (back) {
+    const SumArgs o{{a.dw_post, a.db_post, a.dscale, a.dw_pre, a.db_pre}};
+    if (a.dw_post || a.db_post || a.dscale || a.dw_pre || a.db_pre)
+      norm_sums<<<dim3((unsigned)(op_div_up(a.width, SUM_COLS) * NORM_VECTORS)), SUM_COLS * SUM_GROUPS, 0, s>>>(
+          g.part, o, a.width, (int)blocks);
+  }
+  return op_launched(call);
+}
+
+}  // namespace
+}  // namespace spz
+
+using namespace spz;
+
+extern "C" {
+
+int64_t spz_block_norm_workspace(const spz_block_norm_args* args) {
+  const char* bad = norm_check(args);
+  if (bad) return op_error(SPZ_EINVAL, "spz_block_norm_workspace", bad);
+  return norm_blocks(*args) * NORM_VECTORS * args->width * 4;
+}
+
+int spz_block_norm_forward(const spz_block_norm_args* args, void* hip_stream) {
+  return norm_run("spz_block_norm_forward", args, false, nullptr, 0, hip_stream);
+}
+
+int spz_block_norm_backward(const spz_block_norm_args* args, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  return norm_run("spz_block_norm_backward", args, true, workspace, workspace_bytes, hip_stream);
+}
+
+int spz_dropout(int32_t prec, int64_t rows, int64_t width, const void* x, int64_t x_row, void* y, int64_t y_row,
+                float p, uint64_t seed, uint32_t step, uint32_t tensor, void* hip_stream) {
+  const char* call = "spz_dropout";
+  if (!op_prec_ok(prec)) return op_error(SPZ_EINVAL, call, "unknown precision");
+  if (!op_extent_ok(rows) || !op_extent_ok(width)) return op_error(SPZ_EINVAL, call, "extent out of range");
+  if (width && rows > ((int64_t)1 << 41) / width) return op_error(SPZ_EINVAL, call, "extents out of range");
+  if (!(p >= 0.0f && p <= 1.0f)) return op_error(SPZ_EINVAL, call, "p outside [0, 1]");
+  const int64_t n = rows * width;
+  if (n > 0 && (!x || !y)) return op_error(SPZ_EINVAL, call, "NULL array");
+  const int e = op_size(prec);
+  if (!op_aligned(x, e) || !op_aligned(y, e)) return op_error(SPZ_EINVAL, call, "array not aligned to its type");
+  if (!op_in_stride_ok(x_row) || !op_out_stride_ok(rows, width, y_row))
+    return op_error(SPZ_EINVAL, call, "stride out of range");
+  if (n == 0) return SPZ_OK;
+  const Drop d{drop_threshold(p), drop_gain(drop_threshold(p)), true};
+  const bool flat = (rows == 1 || (x_row == width && y_row == width)) && op_aligned(x, 16) && op_aligned(y, 16);
+  const dim3 grid((unsigned)op_div_up(op_div_up(n, 8), 256));
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const auto go = [&](auto kernel, auto tag) {
+    using T = decltype(tag);
+    kernel<<<grid, 256, 0, s>>>(static_cast<const T*>(x), x_row, static_cast<T*>(y), y_row, width, n, d, seed, step, tensor);
+  };
+  if (prec == SPZ_PREC_BF16) {
+    if (flat) go(dropout<bf16_t, true>, bf16_t{});
+    else go(dropout<bf16_t, false>, bf16_t{});
+  } else {
+    if (flat) go(dropout<float, true>, float{});
+    else go(dropout<float, false>, float{});
+  }
+  return op_launched(call);
+}
+
+}  // extern "C"

@@ -1,0 +1,110 @@
+// Shared by the operators of the recurrent block (scan.hip, block_norm.hip, quant.hip):
+// argument checks, vector accesses and the arithmetic they have in common.
+#pragma once
+
+#include "internal.h"
+
+namespace spz {
+
+// Sets the calling thread's error message ("call: what") and returns `code`.
+int op_error(int code, const char* call, const char* what) noexcept;
+
+// ----------------------------------------------------------------------------- checks
+constexpr int64_t OP_MAX_EXTENT = (int64_t)1 << 31;   // extents are below this
+constexpr int64_t OP_MAX_STRIDE = (int64_t)1 << 42;   // keeps every byte offset within 62 bits
+
+inline bool op_prec_ok(int32_t prec) { return prec == SPZ_PREC_FP32 || prec == SPZ_PREC_BF16; }
+inline int op_size(int32_t prec) { return prec == SPZ_PREC_BF16 ? 2 : 4; }
+inline bool op_extent_ok(int64_t n) { return n >= 0 && n < OP_MAX_EXTENT; }
+__host__ __device__ inline bool op_aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline bool op_in_stride_ok(int64_t s) { return s >= 0 && s < OP_MAX_STRIDE; }
+// Rows of `width` elements at stride s do not overlap (one row: any stride).
+inline bool op_out_stride_ok(int64_t rows, int64_t width, int64_t s) {
+  return op_in_stride_ok(s) && (rows <= 1 || s >= width);
+}
+// Elements of a [n0, n1, width] output do not overlap, for either order of the outer two.
+inline bool op_out_strides_ok(int64_t n0, int64_t n1, int64_t width, int64_t s0, int64_t s1) {
+  if (n0 == 0 || n1 == 0 || width == 0) return op_in_stride_ok(s0) && op_in_stride_ok(s1);
+  if (!op_out_stride_ok(n0, width, s0) || !op_out_stride_ok(n1, width, s1)) return false;
+  if (n0 <= 1 || n1 <= 1) return true;
+  // The inner dimension's span fits between two elements of the outer one.
+  return s0 >= s1 ? s0 >= (n1 - 1) * s1 + width : s1 >= (n0 - 1) * s0 + width;
+}
+// 16-byte vectors of this array's rows: base and row distance (elements of e bytes).
+inline bool op_vec_ok(const void* p, int64_t stride, int e) { return op_aligned(p, 16) && stride * e % 16 == 0; }
+
+inline int64_t op_div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+inline int op_launched(const char* call) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SPZ_OK : op_error(SPZ_EHIP, call, hipGetErrorString(e));
+}
+
+// ----------------------------------------------------------------------------- vectors
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Elements of one 16-byte access.
+template <typename T> constexpr int OP_VEC = 16 / (int)sizeof(T);
+
+__device__ inline void unpack(const u32x4& w, float (&x)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u = w[i];   // a bit_cast of w[i] itself would take the vector's first element
+    x[i] = __builtin_bit_cast(float, u);
+  }
+}
+__device__ inline void unpack(const u32x4& w, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+    x[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xFFFF0000u);
+  }
+}
+__device__ inline u32x4 pack(const float (&x)[4]) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, x[i]);
+  return w;
+}
+__device__ inline u32x4 pack(const float (&x)[8]) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+  return w;
+}
+
+// ----------------------------------------------------------------------------- arithmetic
+// a = 1 / (1 + exp(-x)) and b = 1 - a = 1 / (1 + exp(x)), each to float32's relative precision
+// (1 - a by subtraction would lose b where a is near 1): with e = exp(-|x|) in (0, 1] the two are
+// 1 / (1 + e) and e / (1 + e). The hardware's exponential and reciprocal (1 ulp) serve.
+__device__ inline void sigmoid2(float x, float& a, float& b) {
+  // exp(-|x|) = 2^t (1 + r ln 2) with t + r = -|x| log2(e) in two parts, so that the rounding of t
+  // costs no precision at large |x|.
+  const float m = -fabsf(x);
+  const float t = m * 1.44269504f;
+  const float r = fmaf(m, 1.92596299e-8f, fmaf(m, 1.44269504f, -t));
+  const float p = __builtin_amdgcn_exp2f(t);
+  const float e = t > -127.0f ? fmaf(p, r * 0.693147181f, p) : p;   // also keeps x = +-inf from 0 * NaN
+  const float q = __builtin_amdgcn_rcpf(1.0f + e);
+  const float eq = e * q;
+  a = x < 0.0f ? eq : q;
+  b = x < 0.0f ? q : eq;
+}
+
+// Dropout's 16-bit words of elements 8 blk .. 8 blk + 7 (two to a word, low half first).
+constexpr uint32_t P_DROP = 5;
+__device__ inline U4 drop_words(uint64_t blk, uint64_t seed, uint32_t step, uint32_t tensor) {
+  return philox(U4{(uint32_t)blk, step, P_DROP + ((uint32_t)(blk >> 32) << 8), tensor}, (uint32_t)seed,
+                (uint32_t)(seed >> 32));
+}
+__device__ inline uint32_t drop_half(const U4& w, int i) {
+  const uint32_t v = i < 4 ? (i < 2 ? w.x : w.y) : (i < 6 ? w.z : w.w);
+  return (i & 1) ? v >> 16 : v & 0xFFFFu;
+}
+// p as 65536ths, rounded to nearest, ties to even (p in [0, 1]).
+inline uint32_t drop_threshold(float p) { return (uint32_t)__builtin_nearbyint((double)p * 65536.0); }
+inline float drop_gain(uint32_t d) { return d < 65536u ? (float)(65536.0 / (65536.0 - d)) : 0.0f; }
+
+}  // namespace spz

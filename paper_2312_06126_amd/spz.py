@@ -32,7 +32,13 @@ EXPORTS = ["spz_hparams_default", "spz_create", "spz_destroy", "spz_buffer_push"
            "spz_update", "spz_synchronize", "spz_step", "spz_set_step", "spz_param_count",
            "spz_read_params", "spz_write_params", "spz_read_losses", "spz_debug_read", "spz_last_error",
            "spz_profile_enable", "spz_profile_only", "spz_profile_stride", "spz_profile_read", "spz_set_batch", "spz_batch", "spz_autotune_batch",
-           "spz_save", "spz_load", "spz_act", "spz_buffer_push_async", "spz_act_noalloc"]
+           "spz_save", "spz_load", "spz_act", "spz_buffer_push_async", "spz_act_noalloc",
+           "spz_scan_saved", "spz_scan_workspace", "spz_scan_forward", "spz_scan_backward",
+           "spz_block_norm_workspace", "spz_block_norm_forward", "spz_block_norm_backward", "spz_dropout",
+           "spz_quant_rows", "spz_quant_image_bytes", "spz_quant_pack", "spz_quant_linear_workspace",
+           "spz_quant_linear"]
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+GATES = {"none": 0, "sigmoid": 1, "silu": 2}
 
 
 class SpzError(RuntimeError):
@@ -57,6 +63,28 @@ class KernelStat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("M", ctypes.c_int32), ("N", ctypes.c_int32),
                 ("K", ctypes.c_int32), ("bf16", ctypes.c_int32), ("launches", ctypes.c_int64),
                 ("total_ms", ctypes.c_double), ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
+
+
+def _fields(**groups):
+    """ctypes fields, a type's names after each other: I64="a b" etc., in the given order."""
+    types = {"I64": ctypes.c_int64, "P": ctypes.c_void_p, "I32": ctypes.c_int32, "U64": ctypes.c_uint64,
+             "U32": ctypes.c_uint32, "F32": ctypes.c_float}
+    return [(n, types[k.split("_")[0]]) for k, names in groups.items() for n in names.split()]
+
+
+class ScanArgs(ctypes.Structure):
+    _fields_ = _fields(I64="batch steps width", P="f v", I64_1="f_batch f_step v_batch v_step", P_1="reset",
+                       I64_2="reset_batch reset_step", P_2="lengths h0 y", I64_3="y_batch y_step", P_3="hT saved dy",
+                       I64_4="dy_batch dy_step", P_4="dhT df dv", I64_5="df_batch df_step dv_batch dv_step",
+                       P_5="dh0", I32="prec")
+
+
+class BlockNormArgs(ctypes.Structure):
+    _fields_ = _fields(I64="rows width", P="x h z", I64_1="x_row h_row z_row",
+                       P_1="w_post b_post scale w_pre b_pre valid x_out u", I64_2="x_out_row u_row", P_2="dx_out du",
+                       I64_3="dx_out_row du_row", P_3="dx dh dz", I64_4="dx_row dh_row dz_row",
+                       P_4="dw_post db_post dscale dw_pre db_pre", U64="seed", U32="step tensor", F32="drop_p eps",
+                       I32="post pre gate prec")
 
 
 _lib = None
@@ -105,6 +133,23 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "spz_profile_read": (ctypes.c_int, [P, ctypes.POINTER(KernelStat), ctypes.c_int32,
                                             ctypes.POINTER(ctypes.c_int32)]),
     }
+    I32, I64, U32, U64, F = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float
+    sa, na = ctypes.POINTER(ScanArgs), ctypes.POINTER(BlockNormArgs)
+    sig.update({
+        "spz_scan_saved": (I64, [sa]),
+        "spz_scan_workspace": (I64, [sa, I32]),
+        "spz_scan_forward": (ctypes.c_int, [sa, P, I64, P]),
+        "spz_scan_backward": (ctypes.c_int, [sa, P, I64, P]),
+        "spz_block_norm_workspace": (I64, [na]),
+        "spz_block_norm_forward": (ctypes.c_int, [na, P]),
+        "spz_block_norm_backward": (ctypes.c_int, [na, P, I64, P]),
+        "spz_dropout": (ctypes.c_int, [I32, I64, I64, P, I64, P, I64, F, U64, U32, U32, P]),
+        "spz_quant_rows": (ctypes.c_int, [I32, I64, I64, P, I64, P, I64, P, P]),
+        "spz_quant_image_bytes": (I64, [I64, I64]),
+        "spz_quant_pack": (ctypes.c_int, [I64, I64, P, I64, P, P]),
+        "spz_quant_linear_workspace": (I64, [I32, I64, I64, I64]),
+        "spz_quant_linear": (ctypes.c_int, [I32, I64, I64, I64, P, I64, P, P, P, P, I64, P, I64, P]),
+    })
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
         f.restype = res
