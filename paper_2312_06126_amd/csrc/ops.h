@@ -76,21 +76,14 @@ __device__ inline u32x4 pack(const float (&x)[8]) {
 }
 
 // ----------------------------------------------------------------------------- arithmetic
-// a = 1 / (1 + exp(-x)) and b = 1 - a = 1 / (1 + exp(x)), each to float32's relative precision
-// (1 - a by subtraction would lose b where a is near 1): with e = exp(-|x|) in (0, 1] the two are
-// 1 / (1 + e) and e / (1 + e). The hardware's exponential and reciprocal (1 ulp) serve.
+// a = 1 / (1 + exp(-x)) and b = 1 - a = exp(-x) / (1 + exp(-x)), each to float32's relative precision:
+// 1 - a by subtraction only where a < 1/2, which is also where exp(-x) may overflow. The
+// hardware's exponential and reciprocal (1 ulp) serve; the exponential's argument is rounded, which
+// costs b some |x| / 2 ulp where it is small.
 __device__ inline void sigmoid2(float x, float& a, float& b) {
-  // exp(-|x|) = 2^t (1 + r ln 2) with t + r = -|x| log2(e) in two parts, so that the rounding of t
-  // costs no precision at large |x|.
-  const float m = -fabsf(x);
-  const float t = m * 1.44269504f;
-  const float r = fmaf(m, 1.92596299e-8f, fmaf(m, 1.44269504f, -t));
-  const float p = __builtin_amdgcn_exp2f(t);
-  const float e = t > -127.0f ? fmaf(p, r * 0.693147181f, p) : p;   // also keeps x = +-inf from 0 * NaN
-  const float q = __builtin_amdgcn_rcpf(1.0f + e);
-  const float eq = e * q;
-  a = x < 0.0f ? eq : q;
-  b = x < 0.0f ? q : eq;
+  const float e = __builtin_amdgcn_exp2f(x * -1.44269504f);
+  a = __builtin_amdgcn_rcpf(1.0f + e);
+  b = x < 0.0f ? 1.0f - a : e * a;
 }
 
 // Dropout's 16-bit words of elements 8 blk .. 8 blk + 7 (two to a word, low half first).

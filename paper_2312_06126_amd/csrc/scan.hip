@@ -11,68 +11,91 @@
 // few threads time is cut into pieces: each piece's map is taken first (scan_piece), the maps
 // are joined into the state in front of every piece (scan_join), then every piece is walked
 // (scan_forward, scan_backward). The second reading of f and v comes mostly from the 256 MB
-// last-level cache. An episode start inside a piece makes its map independent of the state: such a
+// last-level cache. Maps are kept in 64 bits: a state that a map gives is a sum of terms that may
+// cancel, and then has to be as near as the one that steps in a row give. An episode start inside a piece makes its map independent of the state: such a
 // map is marked by A = -1 (A is a product of sigmoids, else >= 0), so that a state that is not
 // finite does not pass it as 0 * inf.
 //
 // Backward the same with time reversed: c -> P c + Q is the gradient handed from step to step.
 // h_{t-1} is not stored by the forward pass: `saved` holds the state in front of every SEG-th step
-// (3% of the bytes moved), from which a thread recomputes SEG steps in registers.
+// (6% of the bytes moved in bf16), from which a thread recomputes SEG steps in registers.
+#include <type_traits>
+
 #include "ops.h"
 
 namespace spz {
 namespace {
 
 constexpr int SCAN_THREADS = 256;
-constexpr int SCAN_V = 4;                    // channels a thread, where rows are aligned for it
-template <typename T> constexpr int SEG = 32 / (int)sizeof(T);   // bf16 16, float32 8 (registers)
-constexpr int JOIN_CH = 16, JOIN_GROUPS = 16;
+constexpr int SCAN_V = 4, SCAN_V_BACK = 2;   // channels a thread, where rows are aligned for them
+                                             // (backward: more values a step, in 256 registers)
+constexpr int SEG = 8;                        // steps in registers at once, and between saved states
+constexpr int JOIN_CH = 8, JOIN_GROUPS = 128;
 
 struct ScanArgs {
   spz_scan_args a;
   int64_t chunks;       // of V channels
   int64_t pieces, len;  // time pieces and their steps (a multiple of SEG)
-  float *map_a, *map_h; // [pieces, batch, width]: maps; map_h then the carries
+  double *map_a, *map_h; // [pieces, batch, width]: maps; map_h then the states between the pieces
 };
 
-// V elements at p, as floats.
-template <typename T, int V> __device__ inline void load_v(const T* p, float (&x)[V]) {
+// V elements of an array as they are stored, and as floats.
+template <typename T, int V> struct Raw;
+template <> struct Raw<float, 4> { u32x4 w; };
+template <> struct Raw<bf16_t, 4> { u32x2 w; };
+template <> struct Raw<float, 2> { u32x2 w; };
+template <> struct Raw<bf16_t, 2> { uint32_t w; };
+template <typename T> struct Raw<T, 1> { T w; };
+template <typename T, int V> __device__ inline void load_raw(const T* p, Raw<T, V>& r) {
+  r.w = *reinterpret_cast<const decltype(r.w)*>(p);
+}
+template <typename T, int V> __device__ inline void floats(const Raw<T, V>& r, float (&x)[V]) {
   if constexpr (V == 1) {
-    x[0] = to_f<T>(*p);
-  } else if constexpr (sizeof(T) == 4) {
-    unpack(*reinterpret_cast<const u32x4*>(p), x);
+    x[0] = to_f<T>(r.w);
   } else {
-    const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+    uint32_t w[V * sizeof(T) / 4];
+    __builtin_memcpy(w, &r.w, sizeof(w));
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      x[2 * i] = __builtin_bit_cast(float, w[i] << 16);
-      x[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xFFFF0000u);
+    for (int i = 0; i < V; ++i) {
+      if (sizeof(T) == 4) x[i] = __builtin_bit_cast(float, w[i % (V * sizeof(T) / 4)]);
+      else x[i] = __builtin_bit_cast(float, (i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     }
   }
 }
 template <typename T, int V> __device__ inline void store_v(T* p, const float (&x)[V]) {
   if constexpr (V == 1) {
     *p = from_f<T>(x[0]);
-  } else if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<u32x4*>(p) = pack(x);
   } else {
-    *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    Raw<T, V> r;
+    uint32_t w[V * sizeof(T) / 4];
+#pragma unroll
+    for (int i = 0; i < (int)(V * sizeof(T) / 4); ++i) {
+      if (sizeof(T) == 4) w[i] = __builtin_bit_cast(uint32_t, x[i]);
+      else w[i] = pack_bf16x2(x[(2 * i) % V], x[(2 * i + 1) % V]);
+    }
+    __builtin_memcpy(&r.w, w, sizeof(w));
+    *reinterpret_cast<decltype(r.w)*>(p) = r.w;
   }
 }
 // V floats of a [.., width] state array: its rows are aligned only where width is.
 template <int V> __device__ inline void load_s(const float* p, bool vec, float (&x)[V]) {
-  if (V == 4 && vec) {
-    const f32x4 w = *reinterpret_cast<const f32x4*>(p);
+  typedef float vf __attribute__((ext_vector_type(V)));
+  if (V > 1 && vec) {
+    const vf w = *reinterpret_cast<const vf*>(p);
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = w[i & 3];
+    for (int i = 0; i < V; ++i) x[i] = w[i];
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = p[i];
   }
 }
 template <int V> __device__ inline void store_s(float* p, bool vec, const float (&x)[V]) {
-  if (V == 4 && vec) {
-    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1 % V], x[2 % V], x[3 % V]};
+  typedef float vf __attribute__((ext_vector_type(V)));
+  if (V > 1 && vec) {
+    vf w;
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = x[i];
+    *reinterpret_cast<vf*>(p) = w;
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) p[i] = x[i];
@@ -94,95 +117,188 @@ __device__ inline int64_t scan_length(const spz_scan_args& a, int64_t b) {
   const int64_t n = a.lengths[b];
   return n < 0 ? 0 : (n < a.steps ? n : a.steps);
 }
-__device__ inline bool cut_at(const spz_scan_args& a, int64_t b, int64_t t) {
-  return a.reset && a.reset[b * a.reset_batch + t * a.reset_step] != 0;
+// The same number, of which the compiler cannot know that it grows by a constant from segment to
+// segment: else it keeps a pointer of its own for every access of a segment in registers (80 of them).
+__device__ inline int64_t opaque(int64_t x) {
+  asm("" : "+v"(x));
+  return x;
+}
+
+// SEG steps of N arrays of a thread's channels and of the episode starts, as loaded: the next
+// segment's loads are issued before the present one is worked on, so that each thread keeps
+// N SEG accesses in flight. Steps past the last one (`last`, which exists) load that one again.
+template <typename T, int V, int N> struct Segment {
+  Raw<T, V> x[N][SEG];
+  uint32_t cut;   // bit j: step j starts an episode
+  __device__ void load(const spz_scan_args& a, int64_t b, const T* const (&p)[N], const int64_t (&step)[N], int64_t ts,
+                       int64_t last) {
+    ts = opaque(ts);
+    const int n = (int)(last - ts);
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (p[k]) {
+        const T* q = p[k] + ts * step[k];
+        if (n >= SEG - 1) {
+#pragma unroll
+          for (int j = 0; j < SEG; ++j) load_raw<T, V>(q + j * step[k], x[k][j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < SEG; ++j) load_raw<T, V>(q + (j < n ? j : n) * step[k], x[k][j]);
+        }
+      }
+    cut = 0;
+    if (!a.reset) return;
+    const uint8_t* r = a.reset + b * a.reset_batch + ts * a.reset_step;
+    if (a.reset_step == 1 && n >= SEG - 1) {
+      uint64_t w;
+      __builtin_memcpy(&w, r, SEG);
+      // Bit 8 j + 7 of the sum: byte j is not 0.
+      w = ((w & 0x7F7F7F7F7F7F7F7Full) + 0x7F7F7F7F7F7F7F7Full) | w;
+#pragma unroll
+      for (int j = 0; j < SEG; ++j) cut |= (uint32_t)(w >> (8 * j + 7) & 1) << j;
+    } else {
+#pragma unroll
+      for (int j = 0; j < SEG; ++j) cut |= (uint32_t)(r[(j < n ? j : n) * a.reset_step] != 0) << j;
+    }
+  }
+};
+
+// step(j, k) over the `cnt` steps of a segment, from the last one where BACK, k: step j starts an
+// episode. Whole segments without a start, nearly all of them, run without a branch or select.
+template <bool BACK, typename F> __device__ inline void walk(int cnt, uint32_t cut, F&& step) {
+  if (cnt == SEG && cut == 0) {
+#pragma unroll
+    for (int j = 0; j < SEG; ++j) step(BACK ? SEG - 1 - j : j, false);
+  } else {
+#pragma unroll
+    for (int jj = 0; jj < SEG; ++jj) {
+      const int j = BACK ? SEG - 1 - jj : jj;
+      if (j < cnt) step(j, (cut >> j & 1) != 0);
+    }
+  }
 }
 
 // The affine map of each piece: BACK = false (f, v), true (f, dy; from the piece's end).
-template <typename T, int V, bool BACK> __global__ __launch_bounds__(SCAN_THREADS) void scan_piece(ScanArgs g) {
+template <typename T, int V, bool BACK> __global__ __launch_bounds__(SCAN_THREADS, 2) void scan_piece(ScanArgs g) {
   ScanPos q;
   if (!scan_pos<V>(g, q)) return;
   const spz_scan_args& a = g.a;
   const int64_t t0 = q.p * g.len, end = t0 + g.len, n = scan_length(a, q.b), t1 = n < end ? n : end;
-  float A[V], H[V];
+  double A[V], H[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) { A[i] = 1.0f; H[i] = 0.0f; }
+  for (int i = 0; i < V; ++i) { A[i] = 1.0; H[i] = 0.0; }
   const T* f = static_cast<const T*>(a.f) + q.b * a.f_batch + q.c;
-  const T* v = static_cast<const T*>(BACK ? a.dy : a.v) + q.b * (BACK ? a.dy_batch : a.v_batch) + q.c;
-  const int64_t v_step = BACK ? a.dy_step : a.v_step;
-  bool cut = false;
-  for (int64_t s = t0; s < t1; ++s) {
-    const int64_t t = BACK ? t1 - 1 - (s - t0) : s;
-    float x[V], w[V];
-    load_v<T, V>(f + t * a.f_step, x);
-    if (BACK && !a.dy) {
+  const T* w = static_cast<const T*>(BACK ? a.dy : a.v);
+  if (w) w += q.b * (BACK ? a.dy_batch : a.v_batch) + q.c;
+  const T* const p[2] = {f, w};
+  const int64_t step[2] = {a.f_step, BACK ? a.dy_step : a.v_step};
+  uint32_t cut = 0;
+  if (t1 > t0) {
+    const int64_t segs = (t1 - t0 + SEG - 1) / SEG;
+    Segment<T, V, 2> now, next;
+    now.load(a, q.b, p, step, t0 + (BACK ? segs - 1 : 0) * SEG, t1 - 1);
+    for (int64_t s = 0; s < segs; ++s) {
+      const int64_t ts = t0 + (BACK ? segs - 1 - s : s) * SEG;
+      if (s + 1 < segs) next.load(a, q.b, p, step, BACK ? ts - SEG : ts + SEG, t1 - 1);
+      const int cnt = (int)(t1 - ts < SEG ? t1 - ts : SEG);
+      cut |= now.cut & ((1u << cnt) - 1);
+      walk<BACK>(cnt, now.cut, [&](int j, bool k) {
+        float x[V], y[V];
+        floats<T, V>(now.x[0][j], x);
+        if (w) floats<T, V>(now.x[1][j], y);
 #pragma unroll
-      for (int i = 0; i < V; ++i) w[i] = 0.0f;
-    } else {
-      load_v<T, V>(v + t * v_step, w);
-    }
-    const bool k = cut_at(a, q.b, t);
-    cut |= k;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      float al, be;
-      sigmoid2(x[i], al, be);
-      if (BACK) {
-        H[i] = k ? 0.0f : al * (H[i] + w[i]);
-      } else {
-        H[i] = fmaf(be, w[i], k ? 0.0f : al * H[i]);
-      }
-      A[i] *= al;
+        for (int i = 0; i < V; ++i) {
+          float al, be;
+          sigmoid2(x[i], al, be);
+          if (BACK) H[i] = k ? 0.0 : (double)al * (w ? H[i] + (double)y[i] : H[i]);
+          else H[i] = k ? (double)(be * y[i]) : fma((double)al, H[i], (double)(be * y[i]));
+          A[i] *= (double)al;
+        }
+      });
+      now = next;
     }
   }
   if (cut) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) A[i] = -1.0f;
+    for (int i = 0; i < V; ++i) A[i] = -1.0;
   }
   const int64_t o = (q.p * a.batch + q.b) * a.width + q.c;
-  const bool vec = a.width % 4 == 0;
-  store_s<V>(g.map_a + o, vec, A);
-  store_s<V>(g.map_h + o, vec, H);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    g.map_a[o + i] = A[i];
+    g.map_h[o + i] = H[i];
+  }
 }
 
+// (A, H) after (A1, H1): the map that applies (A1, H1) first.
+__device__ inline void join_maps(double A1, double H1, double& A, double& H) {
+  const bool cut = A == -1.0;
+  H = cut ? H : fma(A, H1, H);
+  A = cut || A1 == -1.0 ? -1.0 : A * A1;
+}
+__device__ inline double apply_map(double A, double H, double h) { return A == -1.0 ? H : fma(A, h, H); }
+
 // map_h[p] <- the state in front of piece p (backward: behind it), from the maps and the first
-// state (`first`, NULL: zeros). 16 channels a workgroup; 16 groups of threads each join a range of
-// pieces, then walk it from the ranges' joint maps.
-__global__ __launch_bounds__(JOIN_CH * JOIN_GROUPS) void scan_join(const float* map_a, float* map_h, const float* first,
+// state (`first`, NULL: zeros). 8 channels a workgroup; 128 groups of threads each join a range of
+// pieces, the ranges' maps are joined by doubling, then each range is walked from its first state.
+__global__ __launch_bounds__(JOIN_CH * JOIN_GROUPS) void scan_join(const double* map_a, double* map_h, const float* first,
                                                                    int64_t channels, int64_t pieces, bool back) {
-  __shared__ float sa[JOIN_GROUPS][JOIN_CH], sh[JOIN_GROUPS][JOIN_CH];
+  __shared__ double sa[JOIN_GROUPS][JOIN_CH], sh[JOIN_GROUPS][JOIN_CH];
   const int c = threadIdx.x % JOIN_CH, gr = threadIdx.x / JOIN_CH;
   const int64_t ch = (int64_t)blockIdx.x * JOIN_CH + c;
   const bool on = ch < channels;
   const int64_t per = (pieces + JOIN_GROUPS - 1) / JOIN_GROUPS;
-  const int64_t p0 = gr * per < pieces ? gr * per : pieces, p1 = p0 + per < pieces ? p0 + per : pieces;
-  float A = 1.0f, H = 0.0f;
-  for (int64_t p = p0; on && p < p1; ++p) {
-    const int64_t o = (back ? pieces - 1 - p : p) * channels + ch;
-    const float ma = map_a[o], mh = map_h[o];
-    if (ma == -1.0f) {
-      A = -1.0f;
-      H = mh;
-    } else {
-      A = A == -1.0f ? -1.0f : A * ma;
-      H = fmaf(ma, H, mh);
+  const int64_t p0 = gr * per < pieces ? gr * per : pieces, p1 = on ? (p0 + per < pieces ? p0 + per : pieces) : p0;
+  const auto at = [&](int64_t p) { return (back ? pieces - 1 - p : p) * channels + ch; };
+  constexpr int U = 8;   // maps loaded at once
+  double A = 1.0, H = 0.0;
+  for (int64_t p = p0; p < p1; p += U) {
+    double ma[U], mh[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int64_t o = at(p + j < p1 ? p + j : p1 - 1);
+      ma[j] = map_a[o];
+      mh[j] = map_h[o];
     }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      if (p + j >= p1) continue;
+      join_maps(A, H, ma[j], mh[j]);
+      A = ma[j];
+      H = mh[j];
+    }
+  }
+  for (int d = 1; d < JOIN_GROUPS; d *= 2) {
+    sa[gr][c] = A;
+    sh[gr][c] = H;
+    __syncthreads();
+    if (gr >= d) join_maps(sa[gr - d][c], sh[gr - d][c], A, H);
+    __syncthreads();
   }
   sa[gr][c] = A;
   sh[gr][c] = H;
   __syncthreads();
   if (!on) return;
-  float h = first ? first[ch] : 0.0f;
-  for (int j = 0; j < gr; ++j) h = sa[j][c] == -1.0f ? sh[j][c] : fmaf(sa[j][c], h, sh[j][c]);
-  for (int64_t p = p0; p < p1; ++p) {
-    const int64_t o = (back ? pieces - 1 - p : p) * channels + ch;
-    const float ma = map_a[o], mh = map_h[o];
-    map_h[o] = h;
-    h = ma == -1.0f ? mh : fmaf(ma, h, mh);
+  double h = first ? first[ch] : 0.0;
+  if (gr) h = apply_map(sa[gr - 1][c], sh[gr - 1][c], h);
+  for (int64_t p = p0; p < p1; p += U) {
+    double ma[U], mh[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int64_t o = at(p + j < p1 ? p + j : p1 - 1);
+      ma[j] = map_a[o];
+      mh[j] = map_h[o];
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      if (p + j >= p1) continue;
+      map_h[at(p + j)] = h;
+      h = apply_map(ma[j], mh[j], h);
+    }
   }
 }
 
-template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS) void scan_forward(ScanArgs g) {
+template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS, 2) void scan_forward(ScanArgs g) {
   ScanPos q;
   if (!scan_pos<V>(g, q)) return;
   const spz_scan_args& a = g.a;
@@ -190,32 +306,44 @@ template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS) void sca
   const int64_t t0 = q.p * g.len, end = t0 + g.len, n = scan_length(a, q.b);
   const int64_t t2 = end < a.steps ? end : a.steps, t1 = n < t2 ? n : t2;
   const int64_t st = q.b * a.width + q.c;
-  const T* f = static_cast<const T*>(a.f) + q.b * a.f_batch + q.c;
-  const T* v = static_cast<const T*>(a.v) + q.b * a.v_batch + q.c;
+  const T* const p[2] = {static_cast<const T*>(a.f) + q.b * a.f_batch + q.c, static_cast<const T*>(a.v) + q.b * a.v_batch + q.c};
+  const int64_t step[2] = {a.f_step, a.v_step};
   T* y = static_cast<T*>(a.y) + q.b * a.y_batch + q.c;
-  const int64_t segs = (a.steps + SEG<T> - 1) / SEG<T>;
+  const int64_t saves = (a.steps + SEG - 1) / SEG;
+  const bool vs = vec && op_aligned16(a.saved);
   float h[V];
   if (g.pieces > 1) {
-    load_s<V>(g.map_h + q.p * a.batch * a.width + st, vec, h);
+    const double* m = g.map_h + q.p * a.batch * a.width + st;
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] = (float)m[i];
   } else if (a.h0) {
     load_s<V>(a.h0 + st, vec && op_aligned16(a.h0), h);
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) h[i] = 0.0f;
   }
-  for (int64_t t = t0; t < t1; ++t) {
-    if (a.saved && t % SEG<T> == 0) store_s<V>(a.saved + ((q.b * segs + t / SEG<T>) * a.width + q.c), vec && op_aligned16(a.saved), h);
-    float x[V], w[V];
-    load_v<T, V>(f + t * a.f_step, x);
-    load_v<T, V>(v + t * a.v_step, w);
-    const bool k = cut_at(a, q.b, t);
+  if (t1 > t0) {
+    Segment<T, V, 2> now, next;
+    now.load(a, q.b, p, step, t0, t1 - 1);
+    for (int64_t ts = t0; ts < t1; ts += SEG) {
+      if (ts + SEG < t1) next.load(a, q.b, p, step, ts + SEG, t1 - 1);
+      if (a.saved) store_s<V>(a.saved + (q.b * saves + ts / SEG) * a.width + q.c, vs, h);
+      const int cnt = (int)(t1 - ts < SEG ? t1 - ts : SEG);
+      T* const out = y + opaque(ts) * a.y_step;
+      walk<false>(cnt, now.cut, [&](int j, bool k) {
+        float x[V], w[V];
+        floats<T, V>(now.x[0][j], x);
+        floats<T, V>(now.x[1][j], w);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      float al, be;
-      sigmoid2(x[i], al, be);
-      h[i] = fmaf(be, w[i], k ? 0.0f : al * h[i]);
+        for (int i = 0; i < V; ++i) {
+          float al, be;
+          sigmoid2(x[i], al, be);
+          h[i] = fmaf(be, w[i], k ? 0.0f : al * h[i]);
+        }
+        store_v<T, V>(out + j * a.y_step, h);
+      });
+      now = next;
     }
-    store_v<T, V>(y + t * a.y_step, h);
   }
   float zero[V];
 #pragma unroll
@@ -224,7 +352,7 @@ template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS) void sca
   if (a.hT && q.p == g.pieces - 1) store_s<V>(a.hT + st, vec && op_aligned16(a.hT), h);
 }
 
-template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS) void scan_backward(ScanArgs g) {
+template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS, 2) void scan_backward(ScanArgs g) {
   ScanPos q;
   if (!scan_pos<V>(g, q)) return;
   const spz_scan_args& a = g.a;
@@ -232,12 +360,13 @@ template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS) void sca
   const int64_t t0 = q.p * g.len, end = t0 + g.len, n = scan_length(a, q.b);
   const int64_t t2 = end < a.steps ? end : a.steps, t1 = n < t2 ? n : t2;
   const int64_t st = q.b * a.width + q.c;
-  const T* f = static_cast<const T*>(a.f) + q.b * a.f_batch + q.c;
-  const T* v = static_cast<const T*>(a.v) + q.b * a.v_batch + q.c;
-  const T* dy = a.dy ? static_cast<const T*>(a.dy) + q.b * a.dy_batch + q.c : nullptr;
+  const T* const p[3] = {static_cast<const T*>(a.f) + q.b * a.f_batch + q.c, static_cast<const T*>(a.v) + q.b * a.v_batch + q.c,
+                         a.dy ? static_cast<const T*>(a.dy) + q.b * a.dy_batch + q.c : nullptr};
+  const int64_t step[3] = {a.f_step, a.v_step, a.dy_step};
   T* df = static_cast<T*>(a.df) + q.b * a.df_batch + q.c;
   T* dv = static_cast<T*>(a.dv) + q.b * a.dv_batch + q.c;
-  const int64_t segs = (a.steps + SEG<T> - 1) / SEG<T>;
+  const float* saved = a.saved + q.b * ((a.steps + SEG - 1) / SEG) * a.width + q.c;
+  const bool vs = vec && op_aligned16(a.saved);
   float zero[V], c[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) zero[i] = 0.0f;
@@ -246,71 +375,299 @@ template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS) void sca
     store_v<T, V>(dv + t * a.dv_step, zero);
   }
   if (g.pieces > 1) {
-    load_s<V>(g.map_h + q.p * a.batch * a.width + st, vec, c);
+    const double* m = g.map_h + q.p * a.batch * a.width + st;
+#pragma unroll
+    for (int i = 0; i < V; ++i) c[i] = (float)m[i];
   } else if (a.dhT) {
     load_s<V>(a.dhT + st, vec && op_aligned16(a.dhT), c);
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) c[i] = 0.0f;
   }
-  for (int64_t ts = t1 > t0 ? t0 + (t1 - 1 - t0) / SEG<T> * SEG<T> : t0 - 1; ts >= t0; ts -= SEG<T>) {
-    const int cnt = (int)(t1 - ts < SEG<T> ? t1 - ts : SEG<T>);
-    // Forward through the segment: before[i] = k_t h_{t-1}.
-    float before[SEG<T>][V], h[V];
-    load_s<V>(a.saved + ((q.b * segs + ts / SEG<T>) * a.width + q.c), vec && op_aligned16(a.saved), h);
-#pragma unroll
-    for (int j = 0; j < SEG<T>; ++j) {
-      if (j >= cnt) continue;
-      const int64_t t = ts + j;
-      float x[V], w[V];
-      load_v<T, V>(f + t * a.f_step, x);
-      load_v<T, V>(v + t * a.v_step, w);
-      const bool k = cut_at(a, q.b, t);
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float al, be;
-        sigmoid2(x[i], al, be);
-        before[j][i] = k ? 0.0f : h[i];
-        h[i] = fmaf(be, w[i], al * before[j][i]);
+  if (t1 > t0) {
+    Segment<T, V, 3> now, next;
+    float h[V], h_next[V];
+    int64_t ts = t0 + (t1 - 1 - t0) / SEG * SEG;
+    now.load(a, q.b, p, step, ts, t1 - 1);
+    load_s<V>(saved + ts / SEG * a.width, vs, h);
+    for (; ts >= t0; ts -= SEG) {
+      if (ts > t0) {
+        next.load(a, q.b, p, step, ts - SEG, t1 - 1);
+        load_s<V>(saved + (ts / SEG - 1) * a.width, vs, h_next);
       }
-    }
+      const int cnt = (int)(t1 - ts < SEG ? t1 - ts : SEG);
+      // Forward through the segment: the sigmoids, and k_t h_{t-1} - v_t times a_t.
+      float al[SEG][V], be[SEG][V], gap[SEG][V];
+      walk<false>(cnt, now.cut, [&](int j, bool k) {
+        float x[V], w[V];
+        floats<T, V>(now.x[0][j], x);
+        floats<T, V>(now.x[1][j], w);
 #pragma unroll
-    for (int j = SEG<T> - 1; j >= 0; --j) {
-      if (j >= cnt) continue;
-      const int64_t t = ts + j;
-      float x[V], w[V], d[V], of[V], ov[V];
-      load_v<T, V>(f + t * a.f_step, x);
-      load_v<T, V>(v + t * a.v_step, w);
-      if (dy) load_v<T, V>(dy + t * a.dy_step, d);
-      const bool k = cut_at(a, q.b, t);
+        for (int i = 0; i < V; ++i) {
+          sigmoid2(x[i], al[j][i], be[j][i]);
+          const float before = k ? 0.0f : h[i];
+          gap[j][i] = al[j][i] * (before - w[i]);
+          h[i] = fmaf(be[j][i], w[i], al[j][i] * before);
+        }
+      });
+      T* const out_f = df + opaque(ts) * a.df_step;
+      T* const out_v = dv + opaque(ts) * a.dv_step;
+      walk<true>(cnt, now.cut, [&](int j, bool k) {
+        float d[V], of[V], ov[V];
+        if (p[2]) floats<T, V>(now.x[2][j], d);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float al, be;
-        sigmoid2(x[i], al, be);
-        const float gr = dy ? d[i] + c[i] : c[i];
-        ov[i] = gr * be;
-        of[i] = ov[i] * al * (before[j][i] - w[i]);
-        c[i] = k ? 0.0f : al * gr;
-      }
-      store_v<T, V>(df + t * a.df_step, of);
-      store_v<T, V>(dv + t * a.dv_step, ov);
+        for (int i = 0; i < V; ++i) {
+          const float gr = p[2] ? d[i] + c[i] : c[i];
+          ov[i] = gr * be[j][i];
+          of[i] = ov[i] * gap[j][i];
+          c[i] = k ? 0.0f : al[j][i] * gr;
+        }
+        store_v<T, V>(out_f + j * a.df_step, of);
+        store_v<T, V>(out_v + j * a.dv_step, ov);
+      });
+      now = next;
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[i] = h_next[i];
     }
   }
   if (a.dh0 && q.p == 0) store_s<V>(a.dh0 + st, vec && op_aligned16(a.dh0), c);
 }
 
-// Time pieces: one where the channels alone give SCAN_FILL threads (eight waves a compute unit),
-// else enough for as many, of at least SCAN_MIN_LEN steps each.
-constexpr int64_t SCAN_FILL = 131072, SCAN_MIN_LEN = 32;
-struct ScanPlan { int64_t pieces, len; };
+// ----------------------------------------------------------------------------- tiles of time
+// One workgroup a sequence and CL chunks of channels: its TILE_WAVES waves of 64 / CL time lanes
+// each take SEG steps at once (CL = 16: 256 steps), join their maps within the workgroup, and go on
+// to the next steps from the joint state, with its loads in flight. Everything is read once, in one
+// launch. Order position (wave, time lane) runs with time, backward against it.
+constexpr int TILE_THREADS = 256, TILE_WAVES = TILE_THREADS / 64;
+
+template <int V, int CL, bool BACK> struct Tile {
+  static constexpr int TL = 64 / CL, LANES = TILE_WAVES * TL;
+  double (*maps)[TILE_WAVES][CL][2 * V];   // [2]: the waves' maps, two buffers in turn
+  int wave, tl, cl, slot = 0;
+  // From each thread's map: the state in front of its steps; carry becomes the one behind the tile.
+  __device__ void join(double (&A)[V], double (&H)[V], double (&carry)[V], float (&h)[V]) {
+    double eA[V], eH[V];
+#pragma unroll
+    for (int d = 1; d < TL; d *= 2)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const double A1 = __shfl_up(A[i], d * CL), H1 = __shfl_up(H[i], d * CL);
+        if (tl >= d) join_maps(A1, H1, A[i], H[i]);
+      }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      eA[i] = TL > 1 ? __shfl_up(A[i], CL) : 1.0;
+      eH[i] = TL > 1 ? __shfl_up(H[i], CL) : 0.0;
+      if (tl == 0) { eA[i] = 1.0; eH[i] = 0.0; }
+    }
+    double* mine = maps[slot][wave][cl];
+    if (tl == TL - 1)
+#pragma unroll
+      for (int i = 0; i < V; ++i) { mine[i] = A[i]; mine[V + i] = H[i]; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < TILE_WAVES; ++w) {
+      const double* m = maps[slot][w][cl];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (w == wave) h[i] = (float)apply_map(eA[i], eH[i], carry[i]);
+        carry[i] = apply_map(m[i], m[V + i], carry[i]);
+      }
+    }
+    slot ^= 1;   // a wave that writes this buffer again has passed the other one's barrier
+  }
+};
+
+template <typename T, int V, int CL> __global__ __launch_bounds__(TILE_THREADS, 2) void scan_tile_forward(ScanArgs g) {
+  const spz_scan_args& a = g.a;
+  using Ti = Tile<V, CL, false>;
+  __shared__ double maps[2][TILE_WAVES][CL][2 * V];
+  Ti tile{maps, (int)threadIdx.x / 64, (int)threadIdx.x % 64 / CL, (int)threadIdx.x % CL};
+  const int64_t groups = (g.chunks + CL - 1) / CL, b = blockIdx.x / groups;
+  const int64_t chunk = blockIdx.x % groups * CL + tile.cl, c = chunk * V;
+  const bool on = chunk < g.chunks, vec = a.width % 4 == 0;
+  const int64_t n = scan_length(a, b), saves = (a.steps + SEG - 1) / SEG, st = b * a.width + c;
+  const T* const p[2] = {static_cast<const T*>(a.f) + b * a.f_batch + c, static_cast<const T*>(a.v) + b * a.v_batch + c};
+  const int64_t step[2] = {a.f_step, a.v_step};
+  T* y = static_cast<T*>(a.y) + b * a.y_batch + c;
+  const bool vs = vec && op_aligned16(a.saved);
+  double carry[V];
+  float h[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) h[i] = 0.0f;
+  if (on && a.h0) load_s<V>(a.h0 + st, vec && op_aligned16(a.h0), h);
+#pragma unroll
+  for (int i = 0; i < V; ++i) carry[i] = h[i];
+  Segment<T, V, 2> now, next;
+  int64_t ts = (int64_t)(tile.wave * Ti::TL + tile.tl) * SEG;
+  if (on && ts < n) now.load(a, b, p, step, ts, n - 1);
+  for (int64_t t0 = 0; t0 < n; t0 += Ti::LANES * SEG, ts += Ti::LANES * SEG) {
+    const int64_t ahead = ts + Ti::LANES * SEG;
+    if (on && ahead < n) next.load(a, b, p, step, ahead, n - 1);
+    const int cnt = !on || ts >= n ? 0 : (int)(n - ts < SEG ? n - ts : SEG);
+    float al[SEG][V], bw[SEG][V];
+    double A[V], H[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) { A[i] = 1.0; H[i] = 0.0; }
+    if (cnt) {
+      walk<false>(cnt, now.cut, [&](int j, bool k) {
+        float x[V], w[V];
+        floats<T, V>(now.x[0][j], x);
+        floats<T, V>(now.x[1][j], w);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          float be;
+          sigmoid2(x[i], al[j][i], be);
+          bw[j][i] = be * w[i];
+          H[i] = k ? (double)bw[j][i] : fma((double)al[j][i], H[i], (double)bw[j][i]);
+          A[i] *= (double)al[j][i];
+        }
+      });
+      if (now.cut & ((1u << cnt) - 1)) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) A[i] = -1.0;
+      }
+    }
+    tile.join(A, H, carry, h);
+    if (cnt) {
+      if (a.saved) store_s<V>(a.saved + (b * saves + ts / SEG) * a.width + c, vs, h);
+      T* const out = y + opaque(ts) * a.y_step;
+      walk<false>(cnt, now.cut, [&](int j, bool k) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[i] = k ? bw[j][i] : fmaf(al[j][i], h[i], bw[j][i]);
+        store_v<T, V>(out + j * a.y_step, h);
+      });
+      // The last state comes from its own steps, not from the joint maps, whose sums may cancel.
+      if (a.hT && ts + SEG >= n) store_s<V>(a.hT + st, vec && op_aligned16(a.hT), h);
+    }
+    now = next;
+  }
+  if (!on) return;
+  float zero[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) zero[i] = 0.0f;
+  for (int64_t t = n + tile.wave * Ti::TL + tile.tl; t < a.steps; t += Ti::LANES) store_v<T, V>(y + t * a.y_step, zero);
+  if (a.hT && n == 0 && threadIdx.x < CL) store_s<V>(a.hT + st, vec && op_aligned16(a.hT), h);
+}
+
+template <typename T, int V, int CL> __global__ __launch_bounds__(TILE_THREADS, 2) void scan_tile_backward(ScanArgs g) {
+  const spz_scan_args& a = g.a;
+  using Ti = Tile<V, CL, true>;
+  __shared__ double maps[2][TILE_WAVES][CL][2 * V];
+  Ti tile{maps, (int)threadIdx.x / 64, (int)threadIdx.x % 64 / CL, (int)threadIdx.x % CL};
+  const int64_t groups = (g.chunks + CL - 1) / CL, b = blockIdx.x / groups;
+  const int64_t chunk = blockIdx.x % groups * CL + tile.cl, c0 = chunk * V;
+  const bool on = chunk < g.chunks, vec = a.width % 4 == 0;
+  const int64_t n = scan_length(a, b), st = b * a.width + c0;
+  const T* const p[3] = {static_cast<const T*>(a.f) + b * a.f_batch + c0, static_cast<const T*>(a.v) + b * a.v_batch + c0,
+                         a.dy ? static_cast<const T*>(a.dy) + b * a.dy_batch + c0 : nullptr};
+  const int64_t step[3] = {a.f_step, a.v_step, a.dy_step};
+  T* df = static_cast<T*>(a.df) + b * a.df_batch + c0;
+  T* dv = static_cast<T*>(a.dv) + b * a.dv_batch + c0;
+  const float* saved = a.saved + b * ((a.steps + SEG - 1) / SEG) * a.width + c0;
+  const bool vs = vec && op_aligned16(a.saved);
+  double carry[V];
+  float c[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) c[i] = 0.0f;
+  if (on && a.dhT) load_s<V>(a.dhT + st, vec && op_aligned16(a.dhT), c);
+#pragma unroll
+  for (int i = 0; i < V; ++i) carry[i] = c[i];
+  Segment<T, V, 3> now, next;
+  float h[V], h_next[V];
+  const int64_t tiles = (n + Ti::LANES * SEG - 1) / (Ti::LANES * SEG);
+  int64_t ts = (tiles * Ti::LANES - 1 - (tile.wave * Ti::TL + tile.tl)) * SEG;
+  if (on && tiles && ts < n) {
+    now.load(a, b, p, step, ts, n - 1);
+    load_s<V>(saved + ts / SEG * a.width, vs, h);
+  }
+  for (int64_t k = 0; k < tiles; ++k, ts -= Ti::LANES * SEG) {
+    if (on && k + 1 < tiles) {   // the tiles in front of the last one are whole
+      next.load(a, b, p, step, ts - Ti::LANES * SEG, n - 1);
+      load_s<V>(saved + (ts / SEG - Ti::LANES) * a.width, vs, h_next);
+    }
+    const int cnt = !on || ts >= n ? 0 : (int)(n - ts < SEG ? n - ts : SEG);
+    float al[SEG][V], be[SEG][V], gap[SEG][V];
+    double P[V], Q[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) { P[i] = 1.0; Q[i] = 0.0; }
+    if (cnt) {
+      walk<false>(cnt, now.cut, [&](int j, bool cut) {
+        float x[V], w[V];
+        floats<T, V>(now.x[0][j], x);
+        floats<T, V>(now.x[1][j], w);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          sigmoid2(x[i], al[j][i], be[j][i]);
+          const float before = cut ? 0.0f : h[i];
+          gap[j][i] = al[j][i] * (before - w[i]);
+          h[i] = fmaf(be[j][i], w[i], al[j][i] * before);
+          P[i] *= (double)al[j][i];
+        }
+      });
+      walk<true>(cnt, now.cut, [&](int j, bool cut) {
+        float d[V];
+        if (p[2]) floats<T, V>(now.x[2][j], d);
+#pragma unroll
+        for (int i = 0; i < V; ++i) Q[i] = cut ? 0.0 : (double)al[j][i] * (p[2] ? Q[i] + (double)d[i] : Q[i]);
+      });
+      if (now.cut & ((1u << cnt) - 1)) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) P[i] = -1.0;
+      }
+    }
+    tile.join(P, Q, carry, c);
+    if (cnt) {
+      T* const out_f = df + opaque(ts) * a.df_step;
+      T* const out_v = dv + opaque(ts) * a.dv_step;
+      walk<true>(cnt, now.cut, [&](int j, bool cut) {
+        float d[V], of[V], ov[V];
+        if (p[2]) floats<T, V>(now.x[2][j], d);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float gr = p[2] ? d[i] + c[i] : c[i];
+          ov[i] = gr * be[j][i];
+          of[i] = ov[i] * gap[j][i];
+          c[i] = cut ? 0.0f : al[j][i] * gr;
+        }
+        store_v<T, V>(out_f + j * a.df_step, of);
+        store_v<T, V>(out_v + j * a.dv_step, ov);
+      });
+      if (a.dh0 && ts == 0) store_s<V>(a.dh0 + st, vec && op_aligned16(a.dh0), c);   // as hT forward
+    }
+    now = next;
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] = h_next[i];
+  }
+  if (!on) return;
+  float zero[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) zero[i] = 0.0f;
+  for (int64_t t = n + tile.wave * Ti::TL + tile.tl; t < a.steps; t += Ti::LANES) {
+    store_v<T, V>(df + t * a.df_step, zero);
+    store_v<T, V>(dv + t * a.dv_step, zero);
+  }
+  if (a.dh0 && n == 0 && threadIdx.x < CL) store_s<V>(a.dh0 + st, vec && op_aligned16(a.dh0), c);
+}
+
+// How a call is spread over the threads, by its sizes alone:
+//   serial: a thread walks the whole sequence: sequences of at most SCAN_SHORT steps, or channels
+//     enough for SCAN_FILL threads (eight waves a compute unit);
+//   tiles: a workgroup walks it in tiles of time: SCAN_TILES workgroups or more, or so few tiles that
+//     one launch is shorter than the three of
+//   pieces: time cut into pieces, for SCAN_FILL threads but of at least SCAN_MIN_LEN steps each.
+constexpr int64_t SCAN_SHORT = 16, SCAN_FILL = 131072, SCAN_MIN_LEN = 32, SCAN_TILES = 128, SCAN_FEW_STEPS = 1024;
+enum ScanWay { SCAN_SERIAL, SCAN_TILED, SCAN_PIECES };
+struct ScanPlan { ScanWay way; int64_t pieces, len; };
 ScanPlan scan_plan(const spz_scan_args& a) {
   const int64_t threads = a.batch * op_div_up(a.width, SCAN_V);
-  int64_t pieces = threads > 0 ? op_div_up(SCAN_FILL, threads) : 1;
+  if (a.steps <= SCAN_SHORT || threads * 2 > SCAN_FILL) return {SCAN_SERIAL, 1, a.steps};
+  if (a.steps <= SCAN_FEW_STEPS || a.batch * op_div_up(a.width, 32) >= SCAN_TILES) return {SCAN_TILED, 1, a.steps};
+  int64_t pieces = op_div_up(SCAN_FILL, threads);
   const int64_t most = a.steps / SCAN_MIN_LEN;
-  if (threads * 2 > SCAN_FILL || most < 2) return {1, a.steps};
   if (pieces > most) pieces = most;
-  const int64_t len = op_div_up(op_div_up(a.steps, pieces), 16) * 16;
-  return {op_div_up(a.steps, len), len};
+  const int64_t len = op_div_up(op_div_up(a.steps, pieces), SEG) * SEG;
+  return {SCAN_PIECES, op_div_up(a.steps, len), len};
 }
 
 const char* scan_check(const spz_scan_args* a) {
@@ -344,23 +701,40 @@ const char* scan_check_arrays(const spz_scan_args& a, bool back, int64_t ws_byte
   return nullptr;
 }
 
-template <typename T, int V> void scan_launch(const ScanArgs& g, bool back, hipStream_t s) {
-  const int64_t threads = g.chunks * g.a.batch * g.pieces;
-  const dim3 grid((unsigned)op_div_up(threads, SCAN_THREADS));
-  if (g.pieces > 1) {
-    const int64_t channels = g.a.batch * g.a.width;
-    if (back) scan_piece<T, V, true><<<grid, SCAN_THREADS, 0, s>>>(g);
-    else scan_piece<T, V, false><<<grid, SCAN_THREADS, 0, s>>>(g);
-    scan_join<<<dim3((unsigned)op_div_up(channels, JOIN_CH)), JOIN_CH * JOIN_GROUPS, 0, s>>>(
-        g.map_a, g.map_h, back ? g.a.dhT : g.a.h0, channels, g.pieces, back);
+template <typename T, int V, bool BACK> void scan_launch(const ScanArgs& g, ScanWay way, hipStream_t s) {
+  if (way == SCAN_TILED) {
+    const auto tiles = [&](auto lanes) {
+      constexpr int CL = decltype(lanes)::value;
+      const dim3 grid((unsigned)(g.a.batch * op_div_up(g.chunks, CL)));
+      if constexpr (BACK) scan_tile_backward<T, V, CL><<<grid, TILE_THREADS, 0, s>>>(g);
+      else scan_tile_forward<T, V, CL><<<grid, TILE_THREADS, 0, s>>>(g);
+    };
+    // 32 channels a workgroup; with 8 or fewer, the lanes that they leave are better used in time.
+    if (g.chunks <= 8 / V) tiles(std::integral_constant<int, 8 / V>{});
+    else tiles(std::integral_constant<int, 32 / V>{});
+    return;
   }
-  if (back) scan_backward<T, V><<<grid, SCAN_THREADS, 0, s>>>(g);
+  const dim3 grid((unsigned)op_div_up(g.chunks * g.a.batch * g.pieces, SCAN_THREADS));
+  if (way == SCAN_PIECES) {
+    const int64_t channels = g.a.batch * g.a.width;
+    scan_piece<T, V, BACK><<<grid, SCAN_THREADS, 0, s>>>(g);
+    scan_join<<<dim3((unsigned)op_div_up(channels, JOIN_CH)), JOIN_CH * JOIN_GROUPS, 0, s>>>(
+        g.map_a, g.map_h, BACK ? g.a.dhT : g.a.h0, channels, g.pieces, BACK);
+  }
+  if constexpr (BACK) scan_backward<T, V><<<grid, SCAN_THREADS, 0, s>>>(g);
   else scan_forward<T, V><<<grid, SCAN_THREADS, 0, s>>>(g);
+}
+
+template <typename T> void scan_dispatch(const ScanArgs& g, ScanWay way, bool back, bool vectors, hipStream_t s) {
+  if (back && vectors) scan_launch<T, SCAN_V_BACK, true>(g, way, s);
+  else if (back) scan_launch<T, 1, true>(g, way, s);
+  else if (vectors) scan_launch<T, SCAN_V, false>(g, way, s);
+  else scan_launch<T, 1, false>(g, way, s);
 }
 
 int64_t scan_workspace(const spz_scan_args& a) {
   const ScanPlan p = scan_plan(a);
-  return p.pieces > 1 ? 2 * p.pieces * a.batch * a.width * 4 + 16 : 0;
+  return p.way == SCAN_PIECES ? 2 * p.pieces * a.batch * a.width * 8 : 0;
 }
 
 int scan_run(const char* call, const spz_scan_args* args, bool back, void* ws, int64_t ws_bytes, void* stream) {
@@ -376,31 +750,25 @@ int scan_run(const char* call, const spz_scan_args* args, bool back, void* ws, i
   ScanArgs g{};
   g.a = a;
   g.pieces = plan.pieces;
-  g.len = plan.pieces > 1 ? plan.len : a.steps;
-  if (plan.pieces > 1) {
-    const int64_t n = plan.pieces * a.batch * a.width;
-    g.map_a = static_cast<float*>(ws);
-    g.map_h = g.map_a + op_div_up(n, 4) * 4;
+  g.len = plan.len;
+  if (plan.way == SCAN_PIECES) {
+    g.map_a = static_cast<double*>(ws);
+    g.map_h = g.map_a + plan.pieces * a.batch * a.width;
   }
-  // Vectors of SCAN_V channels need every touched row aligned for them.
-  const int e = op_size(a.prec);
+  // Vectors of channels need every touched row aligned for them.
+  const int e = op_size(a.prec), v = back ? SCAN_V_BACK : SCAN_V;
   const auto vec = [&](const void* p, int64_t s0, int64_t s1) {
-    return !p || (op_aligned(p, SCAN_V * e) && s0 % SCAN_V == 0 && s1 % SCAN_V == 0);
+    return !p || (op_aligned(p, v * e) && s0 % v == 0 && s1 % v == 0);
   };
-  const bool v4 = a.width % SCAN_V == 0 && vec(a.f, a.f_batch, a.f_step) && vec(a.v, a.v_batch, a.v_step) &&
+  const bool vectors = a.width % v == 0 && vec(a.f, a.f_batch, a.f_step) && vec(a.v, a.v_batch, a.v_step) &&
                   (back ? vec(a.dy, a.dy_batch, a.dy_step) && vec(a.df, a.df_batch, a.df_step) && vec(a.dv, a.dv_batch, a.dv_step)
                         : vec(a.y, a.y_batch, a.y_step));
-  g.chunks = v4 ? a.width / SCAN_V : a.width;
+  g.chunks = vectors ? a.width / v : a.width;
   if (op_div_up(g.chunks * a.batch * g.pieces, SCAN_THREADS) >= OP_MAX_EXTENT)
     return op_error(SPZ_EINVAL, call, "extents out of range");
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (a.prec == SPZ_PREC_BF16) {
-    if (v4) scan_launch<bf16_t, SCAN_V>(g, back, s);
-    else scan_launch<bf16_t, 1>(g, back, s);
-  } else {
-    if (v4) scan_launch<float, SCAN_V>(g, back, s);
-    else scan_launch<float, 1>(g, back, s);
-  }
+  if (a.prec == SPZ_PREC_BF16) scan_dispatch<bf16_t>(g, plan.way, back, vectors, s);
+  else scan_dispatch<float>(g, plan.way, back, vectors, s);
   return op_launched(call);
 }
 
@@ -414,8 +782,7 @@ extern "C" {
 int64_t spz_scan_saved(const spz_scan_args* args) {
   const char* bad = scan_check(args);
   if (bad) return op_error(SPZ_EINVAL, "spz_scan_saved", bad);
-  const int64_t seg = args->prec == SPZ_PREC_BF16 ? SEG<bf16_t> : SEG<float>;
-  return args->batch * op_div_up(args->steps, seg) * args->width;
+  return args->batch * op_div_up(args->steps, SEG) * args->width;
 }
 
 int64_t spz_scan_workspace(const spz_scan_args* args, int32_t backward) {

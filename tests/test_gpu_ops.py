@@ -78,7 +78,8 @@ def scan_check(t, reset, lengths, prec, layout=lambda x: x, **kw):
 
 
 SCANS = [(1, 1, 1), (3, 1, 5), (16, 1, 256), (2, 7, 3), (5, 16, 8), (2, 17, 12), (3, 50, 64), (2, 64, 200), (1, 63, 4), (1, 64, 4),
-         (1, 65, 4), (2, 129, 7), (1, 1000, 1), (1, 1000, 36), (7, 333, 20), (1, 4099, 8), (130, 40, 513), (70, 33, 1024)]
+         (1, 65, 4), (2, 129, 7), (1, 1000, 1), (1, 1000, 36), (7, 333, 20), (1, 4099, 8), (130, 40, 513), (70, 33, 1024), (2, 1500, 40),
+         (1, 3001, 7), (4, 1024, 72), (3, 520, 257), (2, 2100, 4096), (600, 18, 900)]
 
 
 @pytest.mark.parametrize("prec", PRECS)
@@ -91,7 +92,7 @@ def test_scan(shape, prec):
 
 
 @pytest.mark.parametrize("prec", PRECS)
-@pytest.mark.parametrize("shape", [(3, 50, 64), (1, 700, 40), (4, 130, 9)], ids=str)
+@pytest.mark.parametrize("shape", [(3, 50, 64), (1, 700, 40), (4, 130, 9), (1, 1300, 24), (600, 17, 904)], ids=str)
 def test_scan_layouts(shape, prec):
     """Time-major arrays, parts of one projection, rows at odd distances and unaligned starts give the
     results of contiguous ones."""
