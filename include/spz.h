@@ -442,7 +442,7 @@ int spz_scan_backward(const spz_scan_args* args, void* workspace, int64_t worksp
  *
  * Backward, from dx_out and du (NULL: zeros): dx, dh, dz (rounded to prec) and the sums
  * over the rows dw_post, db_post, dscale, dw_pre, db_pre (float32, written; NULL: not
- * wanted). dx, dh, dz may be NULL too. */
+ * wanted; zeros for the vectors of a norm that is none). dx, dh, dz may be NULL too. */
 #define SPZ_NORM_NONE 0
 #define SPZ_NORM_RMS 1
 #define SPZ_NORM_LAYER 2
@@ -464,7 +464,7 @@ typedef struct spz_block_norm_args {
   float *dw_post, *db_post, *dscale, *dw_pre, *db_pre;
   uint64_t seed;                           /* dropout's, as in spz_dropout                       */
   uint32_t step, tensor;
-  float drop_p, eps;                       /* eps > 0                                            */
+  float drop_p, eps;                       /* eps: a normal number > 0                             */
   int32_t post, pre, gate;
   int32_t prec;                            /* of x, h, z, x_out, u and their gradients           */
 } spz_block_norm_args;

@@ -4,14 +4,17 @@
 //   n = post(h) w_post + b_post,  o = drop(gate(z) n),  x' = x + scale o,  u = pre(x') w_pre + b_pre
 //
 // Bound by HBM: forward 3 arrays read and 2 written, backward 5 read and 3 written, for about 30
-// and 90 instructions an element. A row stays in the registers of TPR threads (16 lanes, a wave, or
-// a workgroup, by its width) from its loads to its stores, so the statistics of both norms and their
+// and 90 instructions an element. A row stays in the registers of TPR threads (16 lanes to a
+// workgroup, by its width) from its loads to its stores, so the statistics of both norms and their
 // gradients are sums over registers and nothing is read twice; variances are of the centred values.
 // The backward pass recomputes the forward one from x, h and z (cheaper than reading x' and the
-// statistics back). Its groups walk the rows with a stride and keep the column sums of the vector
-// gradients in registers; a workgroup adds its groups in LDS, then norm_sums adds the workgroups
-// in order: no atomics, the same bits on every run. Rows wider than the registers hold take
-// norm_wide, which reads them again for each statistic.
+// statistics back). Its rows are walked with a stride, the next row's loads in flight; parameter
+// vectors and the column sums of their gradients stay in registers, which is why a thread has only
+// eight elements of a row there. A workgroup adds its rows in LDS, norm_sums the workgroups in order: no
+// atomics, the same bits on every run. Rows wider than the registers hold take norm_wide, which
+// reads them again for each statistic.
+#include <type_traits>
+
 #include "ops.h"
 
 namespace spz {
@@ -19,7 +22,8 @@ namespace {
 
 constexpr int NORM_THREADS = 256;
 constexpr int NORM_VECTORS = 5;          // dw_post, db_post, dscale, dw_pre, db_pre
-constexpr int64_t NORM_MAX_BLOCKS = 512; // of the backward pass: two workgroups a compute unit
+constexpr int64_t NORM_MAX_WAVES = 2048; // of the backward pass: eight a compute unit
+constexpr int NORM_CHUNK = 8;            // adjacent elements of a thread: one Philox block
 
 struct Drop { uint32_t d; float gain; bool on; };
 
@@ -27,6 +31,7 @@ struct NormArgs {
   spz_block_norm_args a;
   Drop drop;
   float* part;        // backward: [blocks, NORM_VECTORS, width]
+  bool wants[NORM_VECTORS];
 };
 
 // ----------------------------------------------------------------------------- sums over a row
@@ -40,15 +45,22 @@ __device__ inline float sum16(float x) {
   x = dpp_add<0x141>(x);
   return dpp_add<0x140>(x);
 }
-__device__ inline float sum64(float x) {
+__device__ inline float sum32(float x) {
   x = sum16(x);
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a = r[0], b = r[1];
+  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+__device__ inline float sum64(float x) {
+  x = sum32(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a = r[0], b = r[1];
+  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
 }
 // Sums over the TPR threads of a row. More than a wave: through LDS, two buffers in turn so that one
 // barrier a sum is enough (a wave that writes a buffer again has passed the other one's barrier).
 template <int TPR> struct RowSum {
-  __device__ float operator()(float x) { return TPR == 16 ? sum16(x) : sum64(x); }
+  __device__ float operator()(float x) { return TPR == 16 ? sum16(x) : TPR == 32 ? sum32(x) : sum64(x); }
 };
 template <int TPR> struct WideSum {
   float (*buf)[TPR / 64];
@@ -66,48 +78,89 @@ template <int TPR> struct WideSum {
 };
 
 // ----------------------------------------------------------------------------- a row in registers
-// Thread `lane` of TPR holds K chunks of VW elements. VEC: chunk j is the VW columns from
-// (j TPR + lane) VW on, one 16-byte access; else its elements are TPR columns apart, so that
+// Thread `lane` of TPR holds K chunks of NORM_CHUNK elements. VEC: chunk j is the columns from
+// (j TPR + lane) NORM_CHUNK on, in 16-byte accesses; else its elements are TPR columns apart, so that
 // the threads of a row still read neighbours.
 template <typename T, bool VEC, int TPR, int K> struct RowMap {
-  static constexpr int VW = OP_VEC<T>, N = K * VW;
-  int lane;
-  int64_t D;
-  __device__ int64_t col(int j, int i) const {
-    return VEC ? ((int64_t)j * TPR + lane) * VW + i : ((int64_t)j * VW + i) * TPR + lane;
+  static constexpr int VW = NORM_CHUNK, N = K * VW;
+  static constexpr int MASK = TPR * K + 2;   // bytes of a row's dropout mask: its Philox blocks
+  uint32_t lane, D;
+  __device__ uint32_t col(int j, int i) const { return VEC ? (j * TPR + lane) * VW + i : (j * VW + i) * TPR + lane; }
+  // Element i of chunk j exists (VEC: whole chunks do; the width is a multiple of theirs).
+  __device__ bool in(int j, int i) const { return col(j, VEC ? 0 : i) < D; }
+  // Element c of a row. The row's address is the same for a whole wave (where it is one): with a 32-bit
+  // byte offset beside it no thread needs 64-bit arithmetic or registers for its addresses.
+  template <typename E> static __device__ E* at(E* row, uint32_t c) {
+    return reinterpret_cast<E*>(reinterpret_cast<char*>(const_cast<typename std::remove_const<E>::type*>(row)) + c * (uint32_t)sizeof(E));
   }
-  __device__ void load(const T* p, float (&x)[N]) const {
+  // The thread's part of a row as it is stored. Elements past the width are set to zero once (clear)
+  // and never loaded, so that they add nothing to a sum.
+  struct Raw {
+    static constexpr int WORDS = N * (int)sizeof(T) / 16;
+    typename std::conditional<VEC, u32x4[WORDS], T[N]>::type w;
+    __device__ void clear() {
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      if constexpr (VEC) {
-        float t[VW];
-        u32x4 w = {0, 0, 0, 0};
-        if (col(j, 0) < D) w = *reinterpret_cast<const u32x4*>(p + col(j, 0));
-        unpack(w, t);
-#pragma unroll
-        for (int i = 0; i < VW; ++i) x[j * VW + i] = t[i];
-      } else {
-#pragma unroll
-        for (int i = 0; i < VW; ++i) x[j * VW + i] = col(j, i) < D ? to_f<T>(p[col(j, i)]) : 0.0f;
-      }
+      for (int i = 0; i < (VEC ? WORDS : N); ++i) w[i] = decltype(+w[0]){};
     }
-  }
-  __device__ void store(T* p, const float (&x)[N]) const {
+  };
+  __device__ void load(const T* p, Raw& r) const {
+    if constexpr (VEC) {
+      constexpr int E = OP_VEC<T>, P = VW / E;
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      if constexpr (VEC) {
-        float t[VW];
+      for (int j = 0; j < K; ++j)
 #pragma unroll
-        for (int i = 0; i < VW; ++i) t[i] = x[j * VW + i];
-        if (col(j, 0) < D) *reinterpret_cast<u32x4*>(p + col(j, 0)) = pack(t);
-      } else {
+        for (int k = 0; k < P; ++k)
+          if (in(j, 0)) r.w[j * P + k] = *reinterpret_cast<const u32x4*>(at(p, col(j, k * E)));
+    } else {
+#pragma unroll
+      for (int j = 0; j < K; ++j)
 #pragma unroll
         for (int i = 0; i < VW; ++i)
-          if (col(j, i) < D) p[col(j, i)] = from_f<T>(x[j * VW + i]);
-      }
+          if (in(j, i)) r.w[j * VW + i] = *at(p, col(j, i));
     }
   }
-  // A parameter vector; NULL: `other`. Columns past the width: 0.
+  __device__ void floats(const Raw& r, float (&x)[N]) const {
+    if constexpr (VEC) {
+      constexpr int E = OP_VEC<T>;
+#pragma unroll
+      for (int k = 0; k < N / E; ++k) {
+        float t[E];
+        unpack(r.w[k], t);
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[k * E + i] = t[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = to_f<T>(r.w[i]);
+    }
+  }
+  __device__ void load(const T* p, float (&x)[N]) const {
+    Raw r;
+    r.clear();
+    load(p, r);
+    floats(r, x);
+  }
+  __device__ void store(T* p, const float (&x)[N]) const {
+    if constexpr (VEC) {
+      constexpr int E = OP_VEC<T>, P = VW / E;
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          float t[E];
+#pragma unroll
+          for (int i = 0; i < E; ++i) t[i] = x[j * VW + k * E + i];
+          if (in(j, 0)) *reinterpret_cast<u32x4*>(at(p, col(j, k * E))) = pack(t);
+        }
+    } else {
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int i = 0; i < VW; ++i)
+          if (in(j, i)) *at(p, col(j, i)) = from_f<T>(x[j * VW + i]);
+    }
+  }
+  // A parameter vector; NULL: `other`, also past the width.
   __device__ void vec(const float* p, float other, float (&x)[N]) const {
 #pragma unroll
     for (int j = 0; j < K; ++j) {
@@ -115,36 +168,56 @@ template <typename T, bool VEC, int TPR, int K> struct RowMap {
 #pragma unroll
         for (int i = 0; i < VW; i += 4) {
           f32x4 w = {other, other, other, other};
-          if (p && col(j, 0) < D) w = *reinterpret_cast<const f32x4*>(p + col(j, i));
+          if (p && in(j, 0)) w = *reinterpret_cast<const f32x4*>(at(p, col(j, i)));
 #pragma unroll
           for (int k = 0; k < 4; ++k) x[j * VW + i + k] = w[k];
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < VW; ++i) x[j * VW + i] = p && col(j, i) < D ? p[col(j, i)] : other;
+        for (int i = 0; i < VW; ++i) x[j * VW + i] = p && in(j, i) ? *at(p, col(j, i)) : other;
       }
     }
   }
-  // Dropout's factor of each element of the row.
-  __device__ void factor(const spz_block_norm_args& a, const Drop& d, int64_t row, float (&x)[N]) const {
+  // Dropout of the thread's elements. VEC: a chunk is one Philox block, whose words are kept. Else the
+  // row's threads take a block each and hand its bits over through LDS (`mask`, MASK bytes, a buffer
+  // that no thread of the row reads any more; one barrier where the row is more than a wave).
+  struct Kept {
+    U4 w[VEC ? K : 1];
+    uint32_t bits;   // bit j VW + i
+    uint32_t d;
+    __device__ float pass(int e, float x) const {
+      const bool keep = VEC ? drop_half(w[e / VW], e % VW) >= d : (bits >> e & 1) != 0;
+      return keep ? x : 0.0f;
+    }
+  };
+  __device__ void kept(const spz_block_norm_args& a, uint32_t d, int64_t row, uint8_t* mask, Kept& q) const {
+    const uint64_t e0 = (uint64_t)row * D;
+    q.d = d;
+    q.bits = 0;
+    if constexpr (VEC) {
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      if constexpr (VEC) {
-        const uint64_t e = (uint64_t)row * D + col(j, 0);
-        const U4 w = drop_words(e >> 3, a.seed, a.step, a.tensor);
+      for (int j = 0; j < K; ++j) q.w[j] = drop_words((e0 + col(j, 0)) >> 3, a.seed, a.step, a.tensor);
+    } else {
+      const uint64_t b0 = e0 >> 3, b1 = (e0 + D - 1) >> 3;
+      for (uint32_t k = lane; k <= (uint32_t)(b1 - b0); k += TPR) {
+        const U4 w = drop_words(b0 + k, a.seed, a.step, a.tensor);
+        uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
-          const uint32_t h = VW == 8 ? drop_half(w, i) : ((e & 4) ? drop_half(w, 4 + (i & 3)) : drop_half(w, i & 3));
-          x[j * VW + i] = h >= d.d ? d.gain : 0.0f;
-        }
+        for (int i = 0; i < 8; ++i) m |= (uint32_t)(drop_half(w, i) >= d) << i;
+        mask[k] = (uint8_t)m;
+      }
+      if (TPR > 64) {
+        __syncthreads();
       } else {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      }
+      const uint32_t first = (uint32_t)(e0 & 7);
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
-          const uint64_t e = (uint64_t)row * D + col(j, i);
-          const U4 w = drop_words(e >> 3, a.seed, a.step, a.tensor);
-          const uint32_t v = (e & 4) ? ((e & 2) ? w.w : w.z) : ((e & 2) ? w.y : w.x);
-          x[j * VW + i] = ((e & 1) ? v >> 16 : v & 0xFFFFu) >= d.d ? d.gain : 0.0f;
-        }
+      for (int e = 0; e < N; ++e) {
+        const uint32_t c = first + (in(e / VW, e % VW) ? col(e / VW, e % VW) : D - 1);
+        q.bits |= (uint32_t)(mask[c >> 3] >> (c & 7) & 1) << e;
       }
     }
   }
@@ -159,12 +232,12 @@ template <typename T, bool VEC, int TPR, int K> struct RowMap {
 #pragma unroll
       for (int j = 0; j < K; ++j)
 #pragma unroll
-        for (int i = 0; i < VW; ++i) x[j * VW + i] = col(j, i) < D ? x[j * VW + i] - mean : 0.0f;
+        for (int i = 0; i < VW; ++i) x[j * VW + i] = in(j, i) ? x[j * VW + i] - mean : 0.0f;
     }
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) s = fmaf(x[i], x[i], s);
-    const float r = 1.0f / sqrtf(fmaf(sum(s), inv_d, eps));
+    const float r = __builtin_amdgcn_rsqf(fmaf(sum(s), inv_d, eps));
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] *= r;
     return r;
@@ -180,38 +253,77 @@ template <typename T, bool VEC, int TPR, int K> struct RowMap {
       q += dn[i];
     }
     s = sum(s) * inv_d;
-    q = kind == SPZ_NORM_LAYER ? sum(q) * inv_d : 0.0f;
+    if (kind == SPZ_NORM_LAYER) {
+      q = sum(q) * inv_d;
 #pragma unroll
-    for (int j = 0; j < K; ++j)
+      for (int j = 0; j < K; ++j)
 #pragma unroll
-      for (int i = 0; i < VW; ++i) {
-        const int e = j * VW + i;
-        dn[e] = col(j, i) < D ? r * (dn[e] - fmaf(n[e], s, q)) : 0.0f;
-      }
+        for (int i = 0; i < VW; ++i) dn[j * VW + i] -= in(j, i) ? q : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) dn[i] = r * fmaf(-n[i], s, dn[i]);
   }
 };
 
-// gate(z) and its slope.
-__device__ inline void gate_value(int kind, float z, float& g, float& slope) {
-  if (kind == SPZ_GATE_NONE) {
-    g = 1.0f;
-    slope = 0.0f;
-    return;
-  }
+// gate(z) and its slope, of kind SIGMOID or SILU.
+template <int KIND> __device__ inline void gate_of(float z, float& g, float& slope) {
   float s, t;
   sigmoid2(z, s, t);
-  // z = -inf closes the gate: z sigmoid(z) -> 0 there, not -inf * 0.
-  g = kind == SPZ_GATE_SIGMOID ? s : (s == 0.0f ? 0.0f : z * s);
-  slope = kind == SPZ_GATE_SIGMOID ? s * t : (s == 0.0f || t == 0.0f ? s : s * fmaf(z, t, 1.0f));
+  if (KIND == SPZ_GATE_SIGMOID) {
+    g = s;
+    slope = s * t;
+  } else {
+    // z = +-inf: z sigmoid(z) and z (1 - sigmoid(z)) are 0 where the sigmoid is, not inf * 0.
+    g = s == 0.0f ? 0.0f : z * s;
+    slope = t == 0.0f ? s : fmaf(g, t, s);
+  }
+}
+__device__ inline void gate_value(int kind, float z, float& g, float& slope) {
+  if (kind == SPZ_GATE_SIGMOID) {
+    gate_of<SPZ_GATE_SIGMOID>(z, g, slope);
+  } else if (kind == SPZ_GATE_SILU) {
+    gate_of<SPZ_GATE_SILU>(z, g, slope);
+  } else {
+    g = 1.0f;
+    slope = 0.0f;
+  }
+}
+// Of a row's elements: the choice is made once.
+template <int N> __device__ inline void gate_row(int kind, const float (&z)[N], float (&g)[N], float (&slope)[N]) {
+  if (kind == SPZ_GATE_SIGMOID) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) gate_of<SPZ_GATE_SIGMOID>(z[i], g[i], slope[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) gate_of<SPZ_GATE_SILU>(z[i], g[i], slope[i]);
+  }
 }
 
+// The first row of a thread: uniform over its wave where the row fills one.
+template <int TPR> __device__ inline int64_t first_row() {
+  constexpr int GROUPS = TPR > 64 ? 1 : NORM_THREADS / TPR;
+  if constexpr (GROUPS == 1) return blockIdx.x;
+  const int sub = threadIdx.x / TPR;
+  return (int64_t)blockIdx.x * GROUPS + (TPR == 64 ? __builtin_amdgcn_readfirstlane(sub) : sub);
+}
+
+// Workgroups: rows of more than a wave have one to themselves (its barriers are the row's).
+template <int TPR> constexpr int norm_threads = TPR > 64 ? TPR : NORM_THREADS;
+
+// The threads' sums over a row, and its place in LDS.
+#define NORM_ROW_SUM()                                                                                  \
+  __shared__ float buf[2][TPR > 64 ? TPR / 64 : 1];                                                     \
+  typename std::conditional<(TPR > 64), WideSum<(TPR > 64 ? TPR : 128)>, RowSum<TPR>>::type sum{};      \
+  if constexpr (TPR > 64) sum.buf = buf;                                                                \
+  __shared__ uint8_t masks[2][VEC ? 1 : GROUPS][VEC ? 1 : M::MASK]
+
 template <typename T, bool VEC, int TPR, int K>
-__global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void norm_forward(NormArgs g) {
+__global__ __launch_bounds__(norm_threads<TPR>) void norm_forward(NormArgs g) {
   using M = RowMap<T, VEC, TPR, K>;
-  constexpr int N = M::N, GROUPS = TPR >= NORM_THREADS ? 1 : NORM_THREADS / TPR;
+  constexpr int N = M::N, GROUPS = norm_threads<TPR> / TPR;
   const spz_block_norm_args& a = g.a;
-  const M m{(int)(threadIdx.x % TPR), a.width};
-  const int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / TPR;
+  const M m{threadIdx.x % TPR, (uint32_t)a.width};
+  const int64_t row = first_row<TPR>();
   if (row >= a.rows) return;
   T* xo = a.h ? static_cast<T*>(a.x_out) + row * a.x_out_row : nullptr;
   T* u = a.pre != SPZ_NORM_NONE ? static_cast<T*>(a.u) + row * a.u_row : nullptr;
@@ -224,13 +336,13 @@ __global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void norm_
     return;
   }
   const float inv_d = 1.0f / (float)a.width;
-  __shared__ float buf[2][TPR > 64 ? TPR / 64 : 1];
-  typename std::conditional<(TPR > 64), WideSum<(TPR > 64 ? TPR : 128)>, RowSum<TPR>>::type sum{};
-  if constexpr (TPR > 64) sum.buf = buf;
+  NORM_ROW_SUM();
   m.load(static_cast<const T*>(a.x) + row * a.x_row, x);
   if (a.h) {
     m.load(static_cast<const T*>(a.h) + row * a.h_row, h);
     if (a.gate != SPZ_GATE_NONE) m.load(static_cast<const T*>(a.z) + row * a.z_row, z);
+    typename M::Kept kept;
+    if (g.drop.on) m.kept(a, g.drop.d, row, masks[0][VEC ? 0 : threadIdx.x / TPR], kept);
     m.norm(a.post, a.eps, inv_d, sum, h);
     if (a.post != SPZ_NORM_NONE) {
       if (a.w_post) {
@@ -245,26 +357,19 @@ __global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void norm_
       }
     }
     if (a.gate != SPZ_GATE_NONE) {
+      float slope[N];
+      gate_row(a.gate, z, w, slope);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float gt, slope;
-        gate_value(a.gate, z[i], gt, slope);
-        h[i] *= gt;
-      }
+      for (int i = 0; i < N; ++i) h[i] *= w[i];
     }
     if (g.drop.on) {
-      m.factor(a, g.drop, row, w);
 #pragma unroll
-      for (int i = 0; i < N; ++i) h[i] = w[i] == 0.0f ? 0.0f : h[i] * w[i];
+      for (int i = 0; i < N; ++i) h[i] = kept.pass(i, h[i] * g.drop.gain);
     }
     m.vec(a.scale, 1.0f, w);
+    // Past the width h is 0: the loads, the normalised values, and b_post as vec() fills it.
 #pragma unroll
-    for (int j = 0; j < K; ++j)
-#pragma unroll
-      for (int i = 0; i < M::VW; ++i) {
-        const int e = j * M::VW + i;
-        x[e] = m.col(j, i) < a.width ? fmaf(w[e], h[e], x[e]) : 0.0f;
-      }
+    for (int i = 0; i < N; ++i) x[i] = fmaf(w[i], h[i], x[i]);
     m.store(xo, x);
   }
   if (!u) return;
@@ -283,157 +388,174 @@ __global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void norm_
 }
 
 template <typename T, bool VEC, int TPR, int K>
-__global__ __launch_bounds__(TPR > NORM_THREADS ? TPR : NORM_THREADS) void norm_backward(NormArgs g) {
+__global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g) {
   using M = RowMap<T, VEC, TPR, K>;
-  constexpr int N = M::N, GROUPS = TPR >= NORM_THREADS ? 1 : NORM_THREADS / TPR;
+  constexpr int N = M::N, GROUPS = norm_threads<TPR> / TPR;
   const spz_block_norm_args& a = g.a;
-  const M m{(int)(threadIdx.x % TPR), a.width};
+  const M m{threadIdx.x % TPR, (uint32_t)a.width};
   const float inv_d = 1.0f / (float)a.width;
-  __shared__ float buf[2][TPR > 64 ? TPR / 64 : 1];
-  typename std::conditional<(TPR > 64), WideSum<(TPR > 64 ? TPR : 128)>, RowSum<TPR>>::type sum{};
-  if constexpr (TPR > 64) sum.buf = buf;
-  float acc[NORM_VECTORS][N];
+  NORM_ROW_SUM();
+  int slot = 0;
+  const bool gated = a.h && a.gate != SPZ_GATE_NONE, has_du = a.du && a.pre != SPZ_NORM_NONE;
+  float acc[NORM_VECTORS][N], wq[N], bq[N], sc[N], wp[N];
 #pragma unroll
   for (int k = 0; k < NORM_VECTORS; ++k)
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[k][i] = 0.0f;
+  const bool post = a.post != SPZ_NORM_NONE;
+  m.vec(post ? a.w_post : nullptr, 1.0f, wq);
+  m.vec(post ? a.b_post : nullptr, 0.0f, bq);
+  m.vec(a.scale, 1.0f, sc);
+  m.vec(a.w_pre, 1.0f, wp);
 
-  for (int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * GROUPS) {
-    float x[N], h[N], z[N], w[N], d[N], du[N];
-    if (a.valid && !a.valid[row]) {
+  struct Rows { typename M::Raw x, h, z, d, du; bool on; };
+  const auto load = [&](int64_t row, Rows& r) {
+    r.on = !a.valid || a.valid[row];
+    if (!r.on) return;
+    m.load(static_cast<const T*>(a.x) + row * a.x_row, r.x);
+    if (a.h) m.load(static_cast<const T*>(a.h) + row * a.h_row, r.h);
+    if (gated) m.load(static_cast<const T*>(a.z) + row * a.z_row, r.z);
+    if (a.dx_out) m.load(static_cast<const T*>(a.dx_out) + row * a.dx_out_row, r.d);
+    if (has_du) m.load(static_cast<const T*>(a.du) + row * a.du_row, r.du);
+  };
+  const auto take = [&](int64_t row, const Rows& now) {
+    float x[N];
+    if (!now.on) {
 #pragma unroll
       for (int i = 0; i < N; ++i) x[i] = 0.0f;
       if (a.dx) m.store(static_cast<T*>(a.dx) + row * a.dx_row, x);
       if (a.h && a.dh) m.store(static_cast<T*>(a.dh) + row * a.dh_row, x);
-      if (a.h && a.gate != SPZ_GATE_NONE && a.dz) m.store(static_cast<T*>(a.dz) + row * a.dz_row, x);
-      continue;
+      if (gated && a.dz) m.store(static_cast<T*>(a.dz) + row * a.dz_row, x);
+      return;
     }
-    m.load(static_cast<const T*>(a.x) + row * a.x_row, x);
-    if (a.h) m.load(static_cast<const T*>(a.h) + row * a.h_row, h);
-    if (a.h && a.gate != SPZ_GATE_NONE) m.load(static_cast<const T*>(a.z) + row * a.z_row, z);
-    if (a.dx_out) m.load(static_cast<const T*>(a.dx_out) + row * a.dx_out_row, d);
+    // Forward: n in h, gate and its slope, x' in x. Past the width all of them are 0 (but the gate).
+    float h[N], gt[N], slope[N], rh = 1.0f;
+    typename M::Kept kept;
+    m.floats(now.x, x);
+    if (a.h) {
+      if (g.drop.on) {
+        m.kept(a, g.drop.d, row, masks[slot][VEC ? 0 : threadIdx.x / TPR], kept);
+        slot ^= 1;
+      }
+      m.floats(now.h, h);
+      rh = m.norm(a.post, a.eps, inv_d, sum, h);
+      if (gated) {
+        float z[N];
+        m.floats(now.z, z);
+        gate_row(a.gate, z, gt, slope);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) { gt[i] = 1.0f; slope[i] = 0.0f; }
+      }
+      if (g.drop.on) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = fmaf(sc[i], kept.pass(i, gt[i] * fmaf(h[i], wq[i], bq[i]) * g.drop.gain), x[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = fmaf(sc[i], gt[i] * fmaf(h[i], wq[i], bq[i]), x[i]);
+      }
+    }
+    // Through the pre norm: d becomes the gradient to x'.
+    float d[N];
+    if (a.dx_out) m.floats(now.d, d);
     else
 #pragma unroll
       for (int i = 0; i < N; ++i) d[i] = 0.0f;
-    const bool has_du = a.du && a.pre != SPZ_NORM_NONE;
-    if (has_du) m.load(static_cast<const T*>(a.du) + row * a.du_row, du);
-
-    // Forward: n in h, t = n w + b, gate and its slope (in z), dropout's factor, o, x' in x.
-    float t[N], gt[N], f[N], rh = 1.0f;
-    if (a.h) {
-      rh = m.norm(a.post, a.eps, inv_d, sum, h);
-#pragma unroll
-      for (int i = 0; i < N; ++i) t[i] = h[i];
-      if (a.post != SPZ_NORM_NONE) {
-        m.vec(a.w_post, 1.0f, w);
-#pragma unroll
-        for (int i = 0; i < N; ++i) t[i] *= w[i];
-        if (a.b_post) {
-          m.vec(a.b_post, 0.0f, w);
-#pragma unroll
-          for (int i = 0; i < N; ++i) t[i] += w[i];
-        }
-      }
-      if (a.gate != SPZ_GATE_NONE) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          float slope;
-          gate_value(a.gate, z[i], gt[i], slope);
-          z[i] = slope;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) { gt[i] = 1.0f; z[i] = 0.0f; }
-      }
-      if (g.drop.on) m.factor(a, g.drop, row, f);
-      else
-#pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = 1.0f;
-      m.vec(a.scale, 1.0f, w);
-#pragma unroll
-      for (int j = 0; j < K; ++j)
-#pragma unroll
-        for (int i = 0; i < M::VW; ++i) {
-          const int e = j * M::VW + i;
-          const float o = f[e] == 0.0f ? 0.0f : gt[e] * t[e] * f[e];
-          x[e] = m.col(j, i) < a.width ? fmaf(w[e], o, x[e]) : 0.0f;
-        }
-    }
-    // Through the pre norm: d becomes the gradient to x'.
     if (has_du) {
+      float du[N];
+      m.floats(now.du, du);
       const float rx = m.norm(a.pre, a.eps, inv_d, sum, x);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         acc[3][i] = fmaf(du[i], x[i], acc[3][i]);
         acc[4][i] += du[i];
+        du[i] *= wp[i];
       }
-      m.vec(a.w_pre, 1.0f, w);
-#pragma unroll
-      for (int i = 0; i < N; ++i) du[i] *= w[i];
       m.norm_back(a.pre, rx, inv_d, sum, x, du);
 #pragma unroll
       for (int i = 0; i < N; ++i) d[i] += du[i];
     }
     if (a.dx) m.store(static_cast<T*>(a.dx) + row * a.dx_row, d);
-    if (!a.h) continue;
-    m.vec(a.scale, 1.0f, w);
+    if (!a.h) return;
+    if (g.drop.on) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] = kept.pass(i, d[i] * g.drop.gain);
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float gd = f[i] == 0.0f ? 0.0f : d[i] * f[i];   // through dropout
-      acc[2][i] = fmaf(gd, gt[i] * t[i], acc[2][i]);
-      d[i] = gd * w[i];                                     // gradient to gate(z) n
-      z[i] *= d[i] * t[i];
-      d[i] *= gt[i];                                        // gradient to n w + b
-      acc[0][i] = fmaf(d[i], h[i], acc[0][i]);
-      acc[1][i] += d[i];
+      const float t = fmaf(h[i], wq[i], bq[i]);
+      acc[2][i] = fmaf(d[i], gt[i] * t, acc[2][i]);
+      d[i] *= sc[i];          // gradient to gate(z) n
+      slope[i] *= d[i] * t;   // to z
+      d[i] *= gt[i];          // to n w + b
     }
-    if (a.gate != SPZ_GATE_NONE && a.dz) m.store(static_cast<T*>(a.dz) + row * a.dz_row, z);
-    if (!a.dh) continue;
-    if (a.post != SPZ_NORM_NONE) {
-      m.vec(a.w_post, 1.0f, w);
+    if (gated && a.dz) m.store(static_cast<T*>(a.dz) + row * a.dz_row, slope);
+    if (post) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) d[i] *= w[i];
-      m.norm_back(a.post, rh, inv_d, sum, h, d);
+      for (int i = 0; i < N; ++i) {
+        acc[0][i] = fmaf(d[i], h[i], acc[0][i]);
+        acc[1][i] += d[i];
+        d[i] *= wq[i];
+      }
     }
+    if (!a.dh) return;
+    m.norm_back(a.post, rh, inv_d, sum, h, d);
     m.store(static_cast<T*>(a.dh) + row * a.dh_row, d);
+  };
+  // Two rows in turn, so that none is copied: the other one's loads are in flight.
+  const int64_t stride = (int64_t)gridDim.x * GROUPS;
+  Rows r0, r1;
+  for (Rows* r : {&r0, &r1})
+    for (typename M::Raw* w : {&r->x, &r->h, &r->z, &r->d, &r->du}) w->clear();
+  int64_t row = first_row<TPR>();
+  if (row < a.rows) load(row, r0);
+  while (row < a.rows) {
+    if (row + stride < a.rows) load(row + stride, r1);
+    take(row, r0);
+    row += stride;
+    if (row >= a.rows) break;
+    if (row + stride < a.rows) load(row + stride, r0);
+    take(row, r1);
+    row += stride;
   }
 
-  // Column sums of the workgroup's groups, in their order.
+  // Column sums of the workgroup's rows, in their order.
+  float* part = g.part + (int64_t)blockIdx.x * NORM_VECTORS * a.width;
   if constexpr (GROUPS == 1) {
 #pragma unroll
-    for (int k = 0; k < NORM_VECTORS; ++k)
+    for (int k = 0; k < NORM_VECTORS; ++k) {
+      if (!g.wants[k]) continue;
 #pragma unroll
       for (int j = 0; j < K; ++j)
 #pragma unroll
         for (int i = 0; i < M::VW; ++i)
-          if (m.col(j, i) < a.width)
-            g.part[((int64_t)blockIdx.x * NORM_VECTORS + k) * a.width + m.col(j, i)] = acc[k][j * M::VW + i];
+          if (m.in(j, i)) part[k * a.width + m.col(j, i)] = acc[k][j * M::VW + i];
+    }
   } else {
     __shared__ float sums[GROUPS][TPR * N];
+#pragma unroll
     for (int k = 0; k < NORM_VECTORS; ++k) {
+      if (!g.wants[k]) continue;
       __syncthreads();
 #pragma unroll
-      for (int kk = 0; kk < NORM_VECTORS; ++kk)
-        if (kk == k)
-#pragma unroll
-          for (int i = 0; i < N; ++i) sums[threadIdx.x / TPR][i * TPR + m.lane] = acc[kk][i];
+      for (int i = 0; i < N; ++i) sums[threadIdx.x / TPR][i * TPR + m.lane] = acc[k][i];
       __syncthreads();
-      for (int e = threadIdx.x; e < TPR * N; e += NORM_THREADS) {
-        const M me{e % TPR, a.width};
-        const int64_t c = me.col(e / TPR / M::VW, e / TPR % M::VW);
-        if (c >= a.width) continue;
+      for (int e = threadIdx.x; e < TPR * N; e += norm_threads<TPR>) {
+        const M me{(uint32_t)e % TPR, m.D};
+        const uint32_t c = me.col(e / TPR / M::VW, e / TPR % M::VW);
+        if (c >= m.D) continue;
         float s = 0.0f;
 #pragma unroll
         for (int r = 0; r < GROUPS; ++r) s += sums[r][e];
-        g.part[((int64_t)blockIdx.x * NORM_VECTORS + k) * a.width + c] = s;
+        part[k * a.width + c] = s;
       }
     }
   }
 }
 
-// out[k][c] = sum over the workgroups b of part[b][k][c]: 8 threads a column take every 8th each.
+// out[k][c] = sum over the workgroups b of part[b][k][c]: 32 threads a column take every 32nd each.
 struct SumArgs { float* out[NORM_VECTORS]; };
-constexpr int SUM_COLS = 32, SUM_GROUPS = 8;
+constexpr int SUM_COLS = 32, SUM_GROUPS = 32;
 __global__ __launch_bounds__(SUM_COLS * SUM_GROUPS) void norm_sums(const float* part, SumArgs o, int64_t width, int blocks) {
   __shared__ float s[SUM_GROUPS][SUM_COLS];
   const int c = threadIdx.x % SUM_COLS, gr = threadIdx.x / SUM_COLS, k = blockIdx.x % NORM_VECTORS;
@@ -441,8 +563,20 @@ __global__ __launch_bounds__(SUM_COLS * SUM_GROUPS) void norm_sums(const float* 
   if (!out) return;
   const int64_t col = (int64_t)(blockIdx.x / NORM_VECTORS) * SUM_COLS + c;
   float x = 0.0f;
-  if (col < width)
-    for (int b = gr; b < blocks; b += SUM_GROUPS) x += part[((int64_t)b * NORM_VECTORS + k) * width + col];
+  if (col < width) {
+    const float* p = part + k * width + col;
+    constexpr int U = 8;
+    for (int b = gr; b < blocks; b += U * SUM_GROUPS) {
+      float v[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int q = b + j * SUM_GROUPS;
+        v[j] = q < blocks ? p[(int64_t)q * NORM_VECTORS * width] : 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) x += v[j];
+    }
+  }
   s[gr][c] = x;
   __syncthreads();
   if (gr || col >= width) return;
@@ -552,8 +686,10 @@ template <typename T, bool BACK> __global__ __launch_bounds__(WIDE_THREADS) void
       }
       if (!a.h) continue;
       const float gd = e.f == 0.0f ? 0.0f : d * e.f;
-      part[0 * D + c] += dt * e.n;
-      part[1 * D + c] += dt;
+      if (a.post != SPZ_NORM_NONE) {
+        part[0 * D + c] += dt * e.n;
+        part[1 * D + c] += dt;
+      }
       part[2 * D + c] += gd * (e.gt * e.t);
       if (a.gate != SPZ_GATE_NONE) put(a.dz, a.dz_row, c, gd * w(a.scale, 1.0f, c) * e.t * e.slope);
       if (a.dh)
@@ -603,45 +739,57 @@ __global__ __launch_bounds__(256) void dropout(const T* x, int64_t x_row, T* y, 
 }
 
 // ----------------------------------------------------------------------------- launches
-template <typename T, bool VEC, int TPR, int K> void norm_launch(const NormArgs& g, bool back, int64_t blocks, hipStream_t s) {
-  constexpr int threads = TPR > NORM_THREADS ? TPR : NORM_THREADS, groups = threads / TPR;
-  if (back) norm_backward<T, VEC, TPR, K><<<dim3((unsigned)blocks), threads, 0, s>>>(g);
-  else norm_forward<T, VEC, TPR, K><<<dim3((unsigned)op_div_up(g.a.rows, groups)), threads, 0, s>>>(g);
-}
-
-// Threads a row: the fewest of 16, 64, 256, 1024 that hold it in at most 32 elements each (16 lanes
-// and 1024 threads: 16); 0: norm_wide.
-int norm_tpr(int64_t width, int vw) {
-  const int64_t chunks = op_div_up(width, vw), k = 32 / vw;
-  return chunks <= 16 * (k / 2) ? 16 : chunks <= 64 * k ? 64 : chunks <= 256 * k ? 256 : chunks <= 1024 * (k / 2) ? 1024 : 0;
+// How a row is held: TPR threads with K chunks each (0: norm_wide). Forward up to four chunks,
+// so that rows of up to 2048 stay within a wave, without barriers; backward one (two above 4096: 256 registers
+// do not hold more).
+struct NormWay { int tpr, k; };
+NormWay norm_way(int64_t width, bool back) {
+  const int64_t c = op_div_up(width, NORM_CHUNK);
+  if (c <= 16) return {16, 1};
+  if (c <= 32) return {32, 1};
+  if (c <= 64) return {64, 1};
+  if (back) return c <= 128 ? NormWay{128, 1} : c <= 256 ? NormWay{256, 1} : c <= 512 ? NormWay{512, 1} : c <= 1024 ? NormWay{512, 2} : NormWay{0, 0};
+  return c <= 128 ? NormWay{64, 2} : c <= 256 ? NormWay{64, 4} : c <= 512 ? NormWay{256, 2} : c <= 1024 ? NormWay{256, 4} : c <= 2048 ? NormWay{1024, 2} : NormWay{0, 0};
 }
 int64_t norm_blocks(const spz_block_norm_args& a) {   // of the backward pass
-  const int tpr = norm_tpr(a.width, 16 / op_size(a.prec));
-  const int64_t rows = tpr == 0 || tpr >= NORM_THREADS ? 1 : NORM_THREADS / tpr;
-  const int64_t n = op_div_up(a.rows, rows);
-  return n < NORM_MAX_BLOCKS ? n : NORM_MAX_BLOCKS;
+  const int tpr = norm_way(a.width, true).tpr;
+  const int64_t threads = tpr == 0 ? WIDE_THREADS : tpr > 64 ? tpr : NORM_THREADS;
+  const int64_t n = op_div_up(a.rows, tpr == 0 || tpr > 64 ? 1 : threads / tpr), most = NORM_MAX_WAVES * 64 / threads;
+  return n < most ? n : most;
 }
 
 template <typename T, bool VEC> void norm_dispatch(const NormArgs& g, bool back, int64_t blocks, hipStream_t s) {
-  constexpr int VW = OP_VEC<T>, KM = 32 / VW;
-  const int tpr = norm_tpr(g.a.width, VW);
-  const int64_t k = tpr ? op_div_up(op_div_up(g.a.width, VW), tpr) : 0;
-  if (tpr == 16) {
-    if (k <= KM / 4) norm_launch<T, VEC, 16, KM / 4>(g, back, blocks, s);
-    else norm_launch<T, VEC, 16, KM / 2>(g, back, blocks, s);
-  } else if (tpr == 64) {
-    if (k <= KM / 2) norm_launch<T, VEC, 64, KM / 2>(g, back, blocks, s);
-    else norm_launch<T, VEC, 64, KM>(g, back, blocks, s);
-  } else if (tpr == 256) {
-    if (k <= KM / 2) norm_launch<T, VEC, 256, KM / 2>(g, back, blocks, s);
-    else norm_launch<T, VEC, 256, KM>(g, back, blocks, s);
-  } else if (tpr == 1024) {
-    norm_launch<T, VEC, 1024, KM / 2>(g, back, blocks, s);
-  } else if (back) {
-    norm_wide<T, true><<<dim3((unsigned)blocks), WIDE_THREADS, 0, s>>>(g);
-  } else {
-    norm_wide<T, false><<<dim3((unsigned)(g.a.rows < 65536 ? g.a.rows : 65536)), WIDE_THREADS, 0, s>>>(g);
-  }
+  const NormWay way = norm_way(g.a.width, back);
+  const auto go = [&](auto tpr, auto k) {
+    constexpr int TPR = decltype(tpr)::value, K = decltype(k)::value;
+    if constexpr (K == 1 || TPR == 512) {
+      if (back) {
+        norm_backward<T, VEC, TPR, K><<<dim3((unsigned)blocks), norm_threads<TPR>, 0, s>>>(g);
+        return;
+      }
+    }
+    if constexpr ((K > 1 && TPR != 512) || TPR <= 64)
+      norm_forward<T, VEC, TPR, K><<<dim3((unsigned)op_div_up(g.a.rows, norm_threads<TPR> / TPR)), norm_threads<TPR>, 0, s>>>(g);
+  };
+  using std::integral_constant;
+  const auto is = [&](int tpr, int k) { return way.tpr == tpr && way.k == k; };
+  const integral_constant<int, 1> k1{};
+  const integral_constant<int, 2> k2{};
+  const integral_constant<int, 4> k4{};
+  if (is(16, 1)) go(integral_constant<int, 16>{}, k1);
+  else if (is(32, 1)) go(integral_constant<int, 32>{}, k1);
+  else if (is(64, 1)) go(integral_constant<int, 64>{}, k1);
+  else if (is(64, 2)) go(integral_constant<int, 64>{}, k2);
+  else if (is(64, 4)) go(integral_constant<int, 64>{}, k4);
+  else if (is(128, 1)) go(integral_constant<int, 128>{}, k1);
+  else if (is(256, 1)) go(integral_constant<int, 256>{}, k1);
+  else if (is(256, 2)) go(integral_constant<int, 256>{}, k2);
+  else if (is(256, 4)) go(integral_constant<int, 256>{}, k4);
+  else if (is(512, 1)) go(integral_constant<int, 512>{}, k1);
+  else if (is(512, 2)) go(integral_constant<int, 512>{}, k2);
+  else if (is(1024, 2)) go(integral_constant<int, 1024>{}, k2);
+  else if (back) norm_wide<T, true><<<dim3((unsigned)blocks), WIDE_THREADS, 0, s>>>(g);
+  else norm_wide<T, false><<<dim3((unsigned)(g.a.rows < 65536 ? g.a.rows : 65536)), WIDE_THREADS, 0, s>>>(g);
 }
 
 const char* norm_check(const spz_block_norm_args* p) {
@@ -653,7 +801,7 @@ const char* norm_check(const spz_block_norm_args* p) {
   if (a.post < SPZ_NORM_NONE || a.post > SPZ_NORM_LAYER || a.pre < SPZ_NORM_NONE || a.pre > SPZ_NORM_LAYER)
     return "unknown norm";
   if (a.gate < SPZ_GATE_NONE || a.gate > SPZ_GATE_SILU) return "unknown gate";
-  if (!(a.eps > 0.0f) || !(a.eps < 3.0e38f)) return "eps out of range";
+  if (!(a.eps >= 1.2e-38f) || !(a.eps < 3.0e38f)) return "eps out of range";
   if (!(a.drop_p >= 0.0f && a.drop_p <= 1.0f)) return "drop_p outside [0, 1]";
   return nullptr;
 }
@@ -688,7 +836,7 @@ const char* norm_check_arrays(const spz_block_norm_args& a, bool back) {
 // 16-byte accesses everywhere: every array that the call touches is aligned for them.
 bool norm_vec(const spz_block_norm_args& a, bool back) {
   const int e = op_size(a.prec);
-  if (a.width % (16 / e)) return false;
+  if (a.width % NORM_CHUNK) return false;
   const auto ok = [&](const void* p, int64_t s) { return !p || op_vec_ok(p, s, e); };
   for (const float* p : {a.w_post, a.b_post, a.scale, a.w_pre, a.b_pre})
     if (!op_aligned(p, 16)) return false;
@@ -719,6 +867,8 @@ int norm_run(const char* call, const spz_block_norm_args* args, bool back, void*
   g.drop.gain = drop_gain(g.drop.d);
   g.drop.on = g.drop.d > 0;
   const bool vec = norm_vec(a, back);
+  const SumArgs o{{a.dw_post, a.db_post, a.dscale, a.dw_pre, a.db_pre}};
+  for (int k = 0; k < NORM_VECTORS; ++k) g.wants[k] = o.out[k] != nullptr;
   if (a.rows > 0) {
     if (a.prec == SPZ_PREC_BF16) {
       if (vec) norm_dispatch<bf16_t, true>(g, back, blocks, s);
@@ -729,7 +879,6 @@ int norm_run(const char* call, const spz_block_norm_args* args, bool back, void*
     }
   }
   if (back) {
-    const SumArgs o{{a.dw_post, a.db_post, a.dscale, a.dw_pre, a.db_pre}};
     if (a.dw_post || a.db_post || a.dscale || a.dw_pre || a.db_pre)
       norm_sums<<<dim3((unsigned)(op_div_up(a.width, SUM_COLS) * NORM_VECTORS)), SUM_COLS * SUM_GROUPS, 0, s>>>(
           g.part, o, a.width, (int)blocks);
