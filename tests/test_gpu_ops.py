@@ -433,7 +433,9 @@ def quant_check(x, wq, sw, bias, prec, weights, **kw):
 
 
 QUANTS = [(1, 1, 1), (1, 32, 32), (16, 256, 64), (3, 31, 33), (33, 33, 31), (16, 1024, 1024), (100, 393, 400), (300, 64, 34), (257, 1000, 130),
-          (64, 1030, 70), (129, 2500, 300), (5, 4096, 96), (513, 96, 1), (2049, 40, 260), (1000, 768, 512), (4100, 512, 264)]
+          (64, 1030, 70), (129, 2500, 300), (5, 4096, 96), (513, 96, 1), (2049, 40, 260), (1000, 768, 512), (4100, 512, 264),
+          (33000, 64, 136), (32700, 48, 72), (32768, 1024, 600), (17000, 2048, 200), (16500, 100, 540), (8300, 33, 33),
+          (8200, 2080, 80), (1100, 4096, 2100), (70, 4128, 40), (300, 6000, 200)]
 
 
 @pytest.mark.parametrize("prec", PRECS)

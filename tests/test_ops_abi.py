@@ -142,7 +142,7 @@ def test_dropout_refusals(lib, kw):
     (dict(bias=PTR + 2), -1), (dict(x_row=-1), -1), (dict(y_row=31), -1), (dict(ws=None), -4), (dict(n=0), -4)])
 def test_quant_refusals(lib, kw, code):
     # A shape whose rows go through the workspace.
-    d = dict(prec=0, rows=512, outer=32, inner=4096, x=PTR, x_row=4096, image=PTR, w_scale=PTR, bias=None, y=PTR, y_row=32, ws=PTR,
+    d = dict(prec=0, rows=512, outer=32, inner=8192, x=PTR, x_row=8192, image=PTR, w_scale=PTR, bias=None, y=PTR, y_row=32, ws=PTR,
              n=1 << 40, stream=None)
     d.update(kw)
     assert lib.spz_quant_linear(*d.values()) == code
