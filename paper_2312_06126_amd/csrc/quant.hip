@@ -12,6 +12,7 @@
 // compute unit: large calls are bound by reading x and writing y, small ones by latency. Longer
 // rows go through the workspace (quant_rows, quant_product).
 #include <atomic>
+#include <type_traits>
 
 #include "ops.h"
 
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(256) void quant_product(const int8_t* x, const int8
 // ----------------------------------------------------------------------------- rows in LDS
 constexpr int64_t QUANT_LDS_INNER = 4096;
 constexpr int QUANT_THREADS = 512, QUANT_WAVES = QUANT_THREADS / 64;
-constexpr int QUANT_SCRATCH = QUANT_WAVES * 4096;   // bytes of LDS beside the rows
+constexpr int QUANT_SCRATCH = 2560;   // bytes of LDS a wave beside the rows
 
 struct QuantArgs {
   const void* x; int64_t x_row;
@@ -119,25 +120,40 @@ struct QuantArgs {
   int64_t rows, outer;
   int inner, steps;         // steps of 32 inputs
   int row_tiles, parts, units;  // quant_wide: units of 64 channels, shared out over `parts` workgroups
-  bool y_vec, w_vec;        // 16-byte stores of y; 16-byte loads of w_scale and bias
+  bool y_vec;               // 16-byte stores of y
 };
 
-// Sixteen elements over s, rounded to integers, as bytes. The quotient that counts is the correctly
-// rounded x / s; x times the reciprocal differs from it by less than NEAR, so only where some
-// element lies that near to a half is the division done (8% of the waves' sixteens).
+// Sixteen elements over s, rounded to integers, as bytes. r is 1 / s correctly rounded; then, with q = x r
+// (within an ulp of the quotient) and its exact remainder x - q s, q + remainder * r is the correctly
+// rounded quotient (Markstein, 1990) in three operations. Ties are common where x is bfloat16
+// (127 x / max |x| is a ratio of small integers), so an estimate would not do. Where s is so tiny that
+// the remainder could underflow, x and s are first multiplied by 2^64, and quotients are held to 127
+// (a subnormal s is a coarse one).
 constexpr float QUANT_MAGIC = 12582912.0f;   // 1.5 * 2^23: the sum's low byte is the rounded integer
-__device__ inline u32x4 quantise16(const float (&x)[16], float s, float r) {
-  constexpr float NEAR = 4e-5f;   // 127 (3 * 2^-24) + 2^-18 < 3e-5
-  float t[16], far = 0.0f;
+constexpr float QUANT_TINY = 1e-30f, QUANT_LIFT = 18446744073709551616.0f;
+struct RowScale { float s, r; bool tiny; };
+__device__ inline RowScale row_factors(float s) {
+  const bool tiny = s < QUANT_TINY;
+  const float t = tiny ? s * QUANT_LIFT : s;
+  return RowScale{t, 1.0f / t, tiny};
+}
+__device__ inline u32x4 quantise16(float (&x)[16], const RowScale& f) {
+  float t[16];
+  if (f.tiny) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] *= QUANT_LIFT;
+  }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    t[i] = fmaf(x[i], r, QUANT_MAGIC);
-    far = fmaxf(far, fabsf(fmaf(x[i], r, QUANT_MAGIC - t[i])));
+    const float q = x[i] * f.r;
+    t[i] = fmaf(fmaf(-q, f.s, x[i]), f.r, q);
   }
-  if (!(far < 0.5f - NEAR) || s < 1e-30f) {
+  if (f.tiny) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t[i] = (float)quantised(x[i], s) + QUANT_MAGIC;
+    for (int i = 0; i < 16; ++i) t[i] = fminf(fmaxf(t[i], -127.0f), 127.0f);
   }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) t[i] += QUANT_MAGIC;
   u32x4 w;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -149,24 +165,36 @@ __device__ inline u32x4 quantise16(const float (&x)[16], float s, float r) {
   return w;
 }
 
-// Rows row0 .. row0 + RT - 1 of x into LDS: units of 16 inputs, unit k of row r at k RT + (r ^ (k & 7)), so
-// that 32 rows of a unit are contiguous for the products and eight units of a row fall on different
-// banks here. A wave has 4 / NU rows in flight, NU units (of inputs up to 1024 NU) a lane. What lies
-// past a row's inputs within its last step meets zero weights, what lies past the rows is not stored.
-template <typename T, bool VEC, int RT, int NU>
-__device__ inline void quantise_rows(const QuantArgs& g, int64_t row0, u32x4* a, float* scale) {
-  constexpr int RU = 4 / NU, PER = RT / QUANT_WAVES;
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  for (int j0 = 0; j0 < PER; j0 += RU) {
-    if (row0 + wave * PER + j0 >= g.rows) break;
-    uint32_t m[RU];
-    if constexpr (VEC) {
-      constexpr int E = OP_VEC<T>, W = 16 / E;
-      u32x4 raw[RU][NU][W];
+// The larger of m and the magnitudes in w, as bits (bfloat16: of each half by itself).
+template <typename T> __device__ inline uint32_t largest(const u32x4& w, uint32_t m) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-      for (int j = 0; j < RU; ++j) {
-        const int64_t row = row0 + wave * PER + j0 + j;
-        const T* p = static_cast<const T*>(g.x) + (row < g.rows ? row : g.rows - 1) * g.x_row;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t v = w[i];
+    if constexpr (sizeof(T) == 2) {
+      m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, v & 0x7FFF7FFFu), __builtin_bit_cast(u16x2, m)));
+    } else {
+      m = (v & 0x7FFFFFFFu) > m ? v & 0x7FFFFFFFu : m;
+    }
+  }
+  return m;
+}
+
+// R rows of x as a wave loads them, NU units of 16 inputs a lane (up to 1024 NU inputs), and their way
+// into LDS: unit k of the workgroup's row r at k RT + (r ^ (k & 7)), so that 32 rows of a unit are contiguous
+// for the products and eight units of a row fall on different banks here. What lies past a row's
+// inputs within its last step meets zero weights; what lies past the rows is not stored.
+template <typename T, bool VEC, int R, int NU> struct RowChunk {
+  static constexpr int E = OP_VEC<T>, W = 16 / E;
+  typename std::conditional<VEC, u32x4[R][NU][W], float[R][NU * 16]>::type raw;
+
+  __device__ void load(const QuantArgs& g, int64_t row0) {
+    const int lane = threadIdx.x % 64;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const int64_t row = row0 + j < g.rows ? row0 + j : g.rows - 1;
+      const T* p = static_cast<const T*>(g.x) + row * g.x_row;
+      if constexpr (VEC) {
 #pragma unroll
         for (int u = 0; u < NU; ++u)
 #pragma unroll
@@ -175,230 +203,313 @@ __device__ inline void quantise_rows(const QuantArgs& g, int64_t row0, u32x4* a,
             const uint32_t c = (u * 64 + lane) * 16;
             if (c < (uint32_t)g.inner) raw[j][u][k] = *reinterpret_cast<const u32x4*>(p + c + k * E);
           }
-      }
-#pragma unroll
-      for (int j = 0; j < RU; ++j) {
-        m[j] = 0;
-#pragma unroll
-        for (int u = 0; u < NU; ++u)
-#pragma unroll
-          for (int k = 0; k < W; ++k) {
-            float v[E];
-            unpack(raw[j][u][k], v);
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-              const uint32_t b = __builtin_bit_cast(uint32_t, v[i]) & 0x7FFFFFFFu;
-              m[j] = b > m[j] ? b : m[j];
-            }
-          }
-        m[j] = wave_max(m[j]);
-      }
-#pragma unroll
-      for (int j = 0; j < RU; ++j) {
-        const int r = wave * PER + j0 + j;
-        bool zero;
-        const float s = row_scale(m[j], zero), inv = __builtin_amdgcn_rcpf(s);
-        if (lane == 0) scale[r] = s;
-#pragma unroll
-        for (int u = 0; u < NU; ++u) {
-          const int k = u * 64 + lane;
-          if (k >= 2 * g.steps) continue;
-          float v[16];
-#pragma unroll
-          for (int q = 0; q < W; ++q) {
-            float t[E];
-            unpack(raw[j][u][q], t);
-#pragma unroll
-            for (int i = 0; i < E; ++i) v[q * E + i] = t[i];
-          }
-          a[k * RT + (r ^ (k & 7))] = zero ? u32x4{0, 0, 0, 0} : quantise16(v, s, inv);
-        }
-      }
-    } else {
-      float v[RU][NU * 16];
-#pragma unroll
-      for (int j = 0; j < RU; ++j) {
-        const int64_t row = row0 + wave * PER + j0 + j;
-        const T* p = static_cast<const T*>(g.x) + (row < g.rows ? row : g.rows - 1) * g.x_row;
-        m[j] = 0;
+      } else {
 #pragma unroll
         for (int i = 0; i < NU * 16; ++i) {
           const int c = i * 64 + lane;
-          v[j][i] = c < g.inner ? to_f<T>(p[c]) : 0.0f;
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < RU; ++j) {
-        const int r = wave * PER + j0 + j;
-#pragma unroll
-        for (int i = 0; i < NU * 16; ++i) {
-          const uint32_t b = __builtin_bit_cast(uint32_t, v[j][i]) & 0x7FFFFFFFu;
-          m[j] = b > m[j] ? b : m[j];
-        }
-        bool zero;
-        const float s = row_scale(wave_max(m[j]), zero), inv = __builtin_amdgcn_rcpf(s);
-        if (lane == 0) scale[r] = s;
-#pragma unroll
-        for (int h = 0; h < NU; ++h) {
-          float t[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) t[i] = v[j][h * 16 + i];
-          const u32x4 w = zero ? u32x4{0, 0, 0, 0} : quantise16(t, s, inv);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int c = (h * 16 + i) * 64 + lane, k = c / 16;
-            if (c < g.inner)
-              reinterpret_cast<uint8_t*>(a + (k * RT + (r ^ (k & 7))))[c % 16] = (uint8_t)(w[i / 4] >> (i % 4 * 8));
-          }
+          raw[j][i] = c < g.inner ? to_f<T>(p[c]) : 0.0f;
         }
       }
     }
   }
-}
 
-// y of RBW blocks of 32 rows by 64 channels a wave: lane l holds row l % 32 and, of each 32 channels, those
-// of which bit 2 is l / 32; they go through 4 KB of LDS a wave to leave as whole 128-byte pieces of rows.
-template <typename T, int RBW>
-__device__ inline void quant_store(const QuantArgs& g, const i32x16 (&acc)[RBW][2], const float (&xs)[RBW], int64_t row0, int64_t n0,
-                                   uint8_t* scratch) {
-  const int lane = threadIdx.x % 64, l = lane % 32, h = lane / 32;
-  constexpr int CB = 128 / (32 * (int)sizeof(T));   // channel blocks of 32 in a 128-byte piece
+  // The rows' scales and their integers, 16 bytes a unit of the lane (the inputs as load() took them).
+  __device__ void quantise(float (&scale)[R], u32x4 (&q)[R][NU]) const {
+    uint32_t m[R];
 #pragma unroll
-  for (int cb = 0; cb < 2; cb += CB) {
-    float sw[CB][4][4], bn[CB][4][4];
+    for (int j = 0; j < R; ++j) {
+      m[j] = 0;
+      if constexpr (VEC) {
 #pragma unroll
-    for (int c = 0; c < CB; ++c)
+        for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t n = n0 + (cb + c) * 32 + q * 8 + h * 4;
-        if (g.w_vec && n + 4 <= g.outer) {
-          const f32x4 w = *reinterpret_cast<const f32x4*>(g.w_scale + n);
-          f32x4 b = {0.0f, 0.0f, 0.0f, 0.0f};
-          if (g.bias) b = *reinterpret_cast<const f32x4*>(g.bias + n);
+          for (int k = 0; k < W; ++k) m[j] = largest<T>(raw[j][u][k], m[j]);
+        if (sizeof(T) == 2) m[j] = (m[j] << 16) > (m[j] & 0xFFFF0000u) ? m[j] << 16 : m[j] & 0xFFFF0000u;
+      } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) { sw[c][q][i] = w[i]; bn[c][q][i] = b[i]; }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int64_t e = n + i < g.outer ? n + i : g.outer - 1;
-            sw[c][q][i] = g.w_scale[e];
-            bn[c][q][i] = g.bias ? g.bias[e] : 0.0f;
-          }
+        for (int i = 0; i < NU * 16; ++i) {
+          const uint32_t b = __builtin_bit_cast(uint32_t, raw[j][i]) & 0x7FFFFFFFu;
+          m[j] = b > m[j] ? b : m[j];
         }
       }
+      m[j] = __builtin_amdgcn_readfirstlane(wave_max(m[j]));
+    }
 #pragma unroll
-    for (int rb = 0; rb < RBW; ++rb) {
+    for (int j = 0; j < R; ++j) {
+      bool zero;
+      scale[j] = row_scale(m[j], zero);
+      const RowScale f = row_factors(scale[j]);
 #pragma unroll
-      for (int c = 0; c < CB; ++c)
+      for (int u = 0; u < NU; ++u) {
+        float v[16];
+        if constexpr (VEC) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float v[4];
+          for (int k = 0; k < W; ++k) {
+            float t[E];
+            unpack(raw[j][u][k], t);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = fmaf((float)acc[rb][cb + c][q * 4 + i], xs[rb] * sw[c][q][i], bn[c][q][i]);
-          if constexpr (sizeof(T) == 2) {
-            const int unit = (c * 4 + q) ^ (l & 7);
-            *reinterpret_cast<u32x2*>(scratch + l * 128 + unit * 16 + h * 8) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-          } else {
-            const int unit = (2 * q + h) ^ (l & 7);
-            *reinterpret_cast<u32x4*>(scratch + l * 128 + unit * 16) = pack(v);
+            for (int i = 0; i < E; ++i) v[k * E + i] = t[i];
           }
-        }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      constexpr int E = OP_VEC<T>, COLS = 8 * E;
-      const int64_t base = n0 + cb * 32;
-      if (g.y_vec) {
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = i * 8 + lane / 8, unit = lane % 8;
-          const u32x4 w = *reinterpret_cast<const u32x4*>(scratch + r * 128 + ((unit ^ (r & 7)) * 16));
-          const int64_t row = row0 + rb * 32 + r, n = base + unit * E;
-          if (row < g.rows && n < g.outer) *reinterpret_cast<u32x4*>(static_cast<T*>(g.y) + row * g.y_row + n) = w;
+          for (int i = 0; i < 16; ++i) v[i] = raw[j][u * 16 + i];
+        }
+        q[j][u] = zero ? u32x4{0, 0, 0, 0} : quantise16(v, f);
+      }
+    }
+  }
+};
+
+// One unit of a row's integers to its place.
+template <bool VEC, int RT> __device__ inline void place(const QuantArgs& g, u32x4* a, int r, int u, const u32x4& q) {
+  const int lane = threadIdx.x % 64;
+  if constexpr (VEC) {
+    const int k = u * 64 + lane;
+    if (k < 2 * g.steps) a[k * RT + (r ^ (k & 7))] = q;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int c = (u * 16 + i) * 64 + lane, k = c / 16;
+      if (c < g.inner) reinterpret_cast<uint8_t*>(a + (k * RT + (r ^ (k & 7))))[c % 16] = (uint8_t)(q[i / 4] >> (i % 4 * 8));
+    }
+  }
+}
+
+// Rows row0 .. row0 + RT - 1 into LDS by WAVES waves, 64 registers of them at a time.
+template <typename T, bool VEC, int RT, int NU, int WAVES>
+__device__ inline void quantise_rows(const QuantArgs& g, int64_t row0, u32x4* a, float* scale) {
+  constexpr int PER = RT / WAVES, MOST = VEC ? 16 / (int)sizeof(T) / NU : 4 / NU, R = MOST < PER ? MOST : PER;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  for (int j = 0; j < PER; j += R) {
+    if (row0 + wave * PER + j >= g.rows) break;
+    RowChunk<T, VEC, R, NU> c;
+    c.load(g, row0 + wave * PER + j);
+    float sc[R];
+    u32x4 q[R][NU];
+    c.quantise(sc, q);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int r = wave * PER + j + i;
+      if (threadIdx.x % 64 == 0) scale[r] = sc[i];
+#pragma unroll
+      for (int u = 0; u < NU; ++u) place<VEC, RT>(g, a, r, u, q[i][u]);
+    }
+  }
+}
+
+// y of RB blocks of 32 rows by 64 channels a wave: lane l holds row l % 32 and, of each 32 channels, those
+// of which bit 2 is l / 32; they go through 2 KB of LDS a wave to leave as 64-byte pieces of rows. wl, bl:
+// the scale and bias of channel `lane` of the 64, handed out through the last 512 bytes of LDS.
+template <typename T, int RB>
+__device__ inline void quant_store(const QuantArgs& g, const i32x16 (&acc)[RB][2], const float (&xs)[RB], int64_t row0, int64_t n0,
+                                   float wl, float bl, uint8_t* scratch) {
+  const int lane = threadIdx.x % 64, l = lane % 32, h = lane / 32, turn = l >> 2 & 3;
+  constexpr int E = OP_VEC<T>, COLS = 4 * E, Q = COLS / 8;   // channels of a piece, and its groups of 8
+  const auto settle = []() {   // LDS between the lanes of the wave
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  float* channel = reinterpret_cast<float*>(scratch + 2048);
+  channel[lane] = wl;
+  channel[64 + lane] = bl;
+  settle();
+  // A piece's rows are read back while the next one is computed, and stored after that.
+  u32x4 held[2];
+  const auto flush = [&](int piece, int rb) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t row = row0 + rb * 32 + i * 16 + lane / 4, n = n0 + piece * COLS + lane % 4 * E;
+      if (row < g.rows && n < g.outer) *reinterpret_cast<u32x4*>(static_cast<T*>(g.y) + row * g.y_row + n) = held[i];
+    }
+  };
+#pragma unroll
+  for (int piece = 0; piece < 64 / COLS; ++piece) {
+    float sw[Q][4], bn[Q][4];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const f32x4 w = *reinterpret_cast<const f32x4*>(channel + piece * COLS + q * 8 + h * 4);
+      const f32x4 b = *reinterpret_cast<const f32x4*>(channel + 64 + piece * COLS + q * 8 + h * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { sw[q][i] = w[i]; bn[q][i] = b[i]; }
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int of = piece * Q + q;   // group of 8 channels of the 64
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = fmaf((float)acc[rb][of / 4][of % 4 * 4 + i], xs[rb] * sw[q][i], bn[q][i]);
+        if constexpr (sizeof(T) == 2)
+          *reinterpret_cast<u32x2*>(scratch + l * 64 + (q ^ turn) * 16 + h * 8) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        else
+          *reinterpret_cast<u32x4*>(scratch + l * 64 + ((2 * q + h) ^ turn) * 16) = pack(v);
+      }
+      settle();
+      if (g.y_vec) {
+        if (piece + rb > 0) flush(rb ? piece : piece - 1, rb ? rb - 1 : RB - 1);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = i * 16 + lane / 4, unit = lane % 4;
+          held[i] = *reinterpret_cast<const u32x4*>(scratch + r * 64 + (unit ^ (r >> 2 & 3)) * 16);
         }
       } else {
         for (int e = lane; e < 32 * COLS; e += 64) {
           const int r = e / COLS, c = e % COLS;
-          const T w = *reinterpret_cast<const T*>(scratch + r * 128 + ((c / E ^ (r & 7)) * 16) + c % E * sizeof(T));
-          const int64_t row = row0 + rb * 32 + r, n = base + c;
+          const T w = *reinterpret_cast<const T*>(scratch + r * 64 + (c / E ^ (r >> 2 & 3)) * 16 + c % E * sizeof(T));
+          const int64_t row = row0 + rb * 32 + r, n = n0 + piece * COLS + c;
           if (row < g.rows && n < g.outer) static_cast<T*>(g.y)[row * g.y_row + n] = w;
         }
       }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      settle();
     }
   }
+  if (g.y_vec) flush(64 / COLS - 1, RB - 1);
 }
 
-// A workgroup: RB blocks of 32 rows and its part of the channels; its waves take RBW blocks by 64 channels
-// at a time, each on its own once the rows are in LDS. 128 rows a workgroup (RB = RBW = 4) read the
-// weights from L2 at half the rate at which the vector L1 delivers; with two products a fragment
-// of x or four a fragment of weights LDS is at half its rate too.
-template <typename T, bool VEC, int RB, int RBW, int NU>
-__global__ __launch_bounds__(QUANT_THREADS, 2) void quant_wide(QuantArgs g) {
-  extern __shared__ u32x4 lds[];
-  constexpr int RT = RB * 32, WM = RB / RBW, WN = QUANT_WAVES / WM;
-  // Workgroups of the same rows on one XCD (workgroup b runs on XCD b % 8).
-  const int tile = blockIdx.x % 8 + blockIdx.x / 8 / g.parts * 8, part = blockIdx.x / 8 % g.parts;
-  if (tile >= g.row_tiles) return;
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = lane % 32, h = lane / 32;
-  uint8_t* scratch = reinterpret_cast<uint8_t*>(lds + 2 * g.steps * RT);
-  float* scale = reinterpret_cast<float*>(scratch);
-  const int64_t row0 = (int64_t)tile * RT;
-  quantise_rows<T, VEC, RT, NU>(g, row0, lds, scale);
-  __syncthreads();
-  const int wm = wave / WN, wn = wave % WN;
-  float xs[RBW];
-#pragma unroll
-  for (int rb = 0; rb < RBW; ++rb) xs[rb] = scale[(wm * RBW + rb) * 32 + l];
-  __syncthreads();   // the scratch holds the scales until here
-  scratch += wave * (QUANT_SCRATCH / QUANT_WAVES);
-
-  const int nb = (int)((g.outer + 31) / 32);
-  const int per = (g.units + g.parts - 1) / g.parts, u1 = (part + 1) * per < g.units ? (part + 1) * per : g.units;
-  // x fragments of step 4 s + j: unit 8 s + 2 j + h.
+// One wave: RB blocks of 32 rows in LDS by the units of 64 channels unit0, unit0 + by, ... below unit1.
+// Weights are loaded DEPTH steps ahead (L2's latency under load), the next unit's before the present
+// one is stored, rows XD - 1. A unit goes through whole turns of DEPTH steps: past the last step the
+// weights read as zeros (buffer loads, whose bounds end there; the step's offset is a scalar, so the
+// loop computes no addresses), and the rows whatever lies in LDS behind them: up to three steps, 6 RT units.
+template <typename T, int RB>
+__device__ inline void quant_units(const QuantArgs& g, const u32x4* lds, int unit0, int unit1, int by, const float (&xs)[RB],
+                                   int64_t row0, uint8_t* scratch) {
+  constexpr int RT = RB * 32, DEPTH = RB > 2 ? 4 : 8, XD = RB > 2 ? 2 : 4;
+  const int lane = threadIdx.x % 64, l = lane % 32, h = lane / 32, nb = (int)((g.outer + 31) / 32);
+  if (unit0 >= unit1) return;
+  // Rows of step 4 s + j: unit 8 s + 2 j + h.
   const u32x4* ax[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) ax[j] = lds + (2 * j + h) * RT + ((wm * RBW * 32 + l) ^ (2 * j + h));
-  for (int unit = part * per + wn; unit < u1; unit += WN) {
-    const u32x4* w[2];
+  for (int j = 0; j < 4; ++j) ax[j] = lds + (2 * j + h) * RT + (l ^ (2 * j + h));
+  __amdgpu_buffer_rsrc_t w[2];
+  i32x4 b[DEPTH][2], x[XD][RB];
+  const auto start = [&](int unit) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int n = unit * 2 + c < nb ? unit * 2 + c : nb - 1;
-      w[c] = reinterpret_cast<const u32x4*>(g.image) + (int64_t)n * g.steps * 64;
+      w[c] = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.image) + (int64_t)n * g.steps * FRAG, 0, g.steps * FRAG, 0x00027000);
     }
-    i32x16 acc[RBW][2] = {};
-    u32x4 b[4][2];
+  };
+  const auto weights = [&](int c, int s) {
+    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w[c], lane * 16, s * FRAG, 0));
+  };
+  const int last4 = (g.steps - 1) / 4 * 4;
+  const auto rows = [&](int s4, int j, int to) {   // of step s4 + j, s4 a multiple of 4
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int rb = 0; rb < RB; ++rb) x[to][rb] = __builtin_bit_cast(i32x4, ax[j][(s4 < last4 ? s4 : last4) * 2 * RT + rb * 32]);
+  };
+  const auto first = [&]() {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) b[j][c] = w[c][(j < g.steps ? j : 0) * 64 + lane];
-    const auto step = [&](int s, int j) {
-      u32x4 x[RBW];
+    for (int j = 0; j < DEPTH; ++j)
 #pragma unroll
-      for (int rb = 0; rb < RBW; ++rb) x[rb] = ax[j][s * 2 * RT + rb * 32];
-      u32x4 now[2];
+      for (int c = 0; c < 2; ++c) b[j][c] = weights(c, j);
+  };
+  start(unit0);
+  first();
+  for (int unit = unit0; unit < unit1; unit += by) {
+    const int64_t n = (int64_t)unit * 64 + lane, in = n < g.outer ? n : g.outer - 1;
+    const float wl = g.w_scale[in], bl = g.bias ? g.bias[in] : 0.0f;
+    i32x16 acc[RB][2] = {};
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        now[c] = b[j][c];
-        if (s + j + 4 < g.steps) b[j][c] = w[c][(s + j + 4) * 64 + lane];
+    for (int j = 0; j < XD - 1; ++j) rows(0, j, j);
+    for (int s = 0; s < g.steps; s += DEPTH) {
+#pragma unroll
+      for (int j = 0; j < DEPTH; ++j) {
+        rows(s + (j + XD - 1) / 4 * 4, (j + XD - 1) % 4, (j + XD - 1) % XD);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+            acc[rb][c] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[j][c], x[j % XD][rb], acc[rb][c], 0, 0, 0);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) b[j][c] = weights(c, s + j + DEPTH);
+        __builtin_amdgcn_sched_barrier(0);   // the order above is the order of issue
       }
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int rb = 0; rb < RBW; ++rb)
-          acc[rb][c] = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, now[c]), __builtin_bit_cast(i32x4, x[rb]), acc[rb][c], 0, 0, 0);
-    };
-    int s = 0;
-    for (; s + 4 <= g.steps; s += 4) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) step(s, j);
     }
+    if (unit + by < unit1) {
+      start(unit + by);
+      first();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    quant_store<T, RB>(g, acc, xs, row0, (int64_t)unit * 64, wl, bl, scratch);
+  }
+}
+
+// A workgroup: RT rows and its part of the channels, 64 a wave at a time, each wave on its own once the
+// rows are in LDS.
+template <typename T, bool VEC, int RB, int NU, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void quant_wide(QuantArgs g) {
+  extern __shared__ u32x4 lds[];
+  constexpr int RT = RB * 32;
+  // Workgroups of the same rows on one XCD (workgroup b runs on XCD b % 8).
+  const int tile = blockIdx.x % 8 + blockIdx.x / 8 / g.parts * 8, part = blockIdx.x / 8 % g.parts;
+  if (tile >= g.row_tiles) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x % 32;
+  uint8_t* scratch = reinterpret_cast<uint8_t*>(lds + 2 * g.steps * RT);
+  float* scale = reinterpret_cast<float*>(scratch);
+  const int64_t row0 = (int64_t)tile * RT;
+  quantise_rows<T, VEC, RT, NU, WAVES>(g, row0, lds, scale);
+  __syncthreads();
+  float xs[RB];
 #pragma unroll
-    for (int j = 0; j < 3; ++j)
-      if (s + j < g.steps) step(s, j);
-    quant_store<T, RBW>(g, acc, xs, row0 + wm * RBW * 32, (int64_t)unit * 64, scratch);
+  for (int rb = 0; rb < RB; ++rb) xs[rb] = scale[rb * 32 + l];
+  __syncthreads();   // the scratch holds the scales until here
+  const int per = (g.units + g.parts - 1) / g.parts, u1 = (part + 1) * per < g.units ? (part + 1) * per : g.units;
+  quant_units<T, RB>(g, lds, part * per + wave, u1, WAVES, xs, row0, scratch + wave * QUANT_SCRATCH);
+}
+
+// Many rows: workgroups stay, one a compute unit, and go from tile to tile of 128 rows, which fill LDS.
+// Half of the waves (one a SIMD) load and quantise the next tile and keep its integers in registers (128
+// of them) until the other half, which multiplies and stores the present tile, is done with LDS: reading,
+// quantising, matrix instructions and writing go on at the same time, and the weights come from L2
+// once for 128 rows (once for 64, two tiles in LDS at a time, took 260 against 204 us at
+// 131072 x 1024 x 1024 bf16).
+template <typename T>
+__global__ __launch_bounds__(QUANT_THREADS, 2) void quant_stream(QuantArgs g) {
+  extern __shared__ u32x4 lds[];
+  constexpr int RB = 4, RT = RB * 32, HALF = QUANT_WAVES / 2, PER = RT / HALF, R = 8 / (int)sizeof(T);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, of = wave % HALF;
+  uint8_t* scratch = reinterpret_cast<uint8_t*>(lds + 2 * g.steps * RT);
+  float* scale = reinterpret_cast<float*>(scratch + HALF * QUANT_SCRATCH);   // [RT]
+  const int stride = gridDim.x;
+  quantise_rows<T, true, RT, 1, QUANT_WAVES>(g, (int64_t)blockIdx.x * RT, lds, scale);   // the first tile: everyone
+  __syncthreads();
+  // Two barriers a tile for both halves: LDS is free, LDS is filled.
+  if (wave >= HALF) {
+    for (int tile = blockIdx.x; tile < g.row_tiles; tile += stride) {
+      const int next = tile + stride;
+      u32x4 q[PER / R][R][1];
+      float mine = 0.0f;   // lane j: the scale of row j
+      if (next < g.row_tiles) {
+#pragma unroll
+        for (int j = 0; j < PER / R; ++j) {
+          RowChunk<T, true, R, 1> c;
+          c.load(g, (int64_t)next * RT + of * PER + j * R);
+          float sc[R];
+          c.quantise(sc, q[j]);
+#pragma unroll
+          for (int i = 0; i < R; ++i) mine = lane == j * R + i ? sc[i] : mine;
+        }
+      }
+      __syncthreads();
+      if (next < g.row_tiles) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) place<true, RT>(g, lds, of * PER + j, 0, q[j / R][j % R][0]);
+        if (lane < PER) scale[of * PER + lane] = mine;
+      }
+      __syncthreads();
+    }
+  } else {
+    for (int tile = blockIdx.x; tile < g.row_tiles; tile += stride) {
+      float xs[RB];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) xs[rb] = scale[rb * 32 + lane % 32];
+      quant_units<T, RB>(g, lds, of, g.units, HALF, xs, (int64_t)tile * RT, scratch + of * QUANT_SCRATCH);
+      __syncthreads();
+      __syncthreads();
+    }
   }
 }
 
@@ -418,8 +529,8 @@ __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_few(QuantArgs g) {
     const int s = wave + j * QUANT_WAVES;
     b[j] = w[(s < g.steps ? s : 0) * 64];
   }
-  float* scale = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(lds) + (2 * g.steps * 512 > QUANT_SCRATCH ? 2 * g.steps * 512 : QUANT_SCRATCH));
-  quantise_rows<T, VEC, 32, NU>(g, row0, lds, scale);
+  float* scale = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(lds) + (g.steps > QUANT_WAVES * 4 ? g.steps : QUANT_WAVES * 4) * 1024);
+  quantise_rows<T, VEC, 32, NU, QUANT_WAVES>(g, row0, lds, scale);
   __syncthreads();
   i32x16 acc = {};
   for (int s0 = 0; s0 < g.steps; s0 += U * QUANT_WAVES) {
@@ -478,41 +589,47 @@ int64_t quant_workspace(int64_t rows, int64_t inner) {   // q as fragments, then
   return frag_blocks(rows) * frag_blocks(inner) * FRAG + op_div_up(rows, 4) * 16;
 }
 
-template <auto KERNEL> hipError_t quant_go(int64_t grid, size_t bytes, const QuantArgs& g, hipStream_t s) {
+template <auto KERNEL> hipError_t quant_go(int64_t grid, size_t bytes, const QuantArgs& g, hipStream_t s, int threads = QUANT_THREADS) {
   if (bytes > 65536) {
     const hipError_t e = quant_lds_limit<KERNEL>();
     if (e != hipSuccess) return e;
   }
-  KERNEL<<<dim3((unsigned)grid), QUANT_THREADS, bytes, s>>>(g);
+  KERNEL<<<dim3((unsigned)grid), threads, bytes, s>>>(g);
   return hipGetLastError();
 }
 
-// Rows of up to QUANT_LDS_INNER inputs. Few row tiles: quant_few's 32 x 32 tiles. Else the largest
-// tile of rows that still gives every compute unit one (and fits LDS); tiles of 32 rows share the
-// channels out over workgroups where there are too few of them.
+// Rows of up to QUANT_LDS_INNER inputs. Few row tiles: quant_few's 32 x 32 tiles. The largest
+// tiles of rows of which every compute unit gets one and LDS holds it: 128 (quant_stream), 64, 32; the
+// channels shared out over workgroups where tiles of 32 rows are still too few. (LDS is for what quant_units
+// reads past the rows, too.)
 template <typename T, bool VEC> hipError_t quant_launch_lds(QuantArgs g, hipStream_t s) {
   constexpr int64_t CUS = 256;
   const int64_t t32 = op_div_up(g.rows, 32), nb = op_div_up(g.outer, 32);
   const size_t unit32 = (size_t)g.steps * 1024;   // bytes of 32 rows
   if (t32 * op_div_up(g.outer, 512) < CUS / 2) {
-    const size_t bytes = (unit32 > (size_t)QUANT_SCRATCH ? unit32 : (size_t)QUANT_SCRATCH) + 128;
+    const size_t bytes = (g.steps > QUANT_WAVES * 4 ? g.steps : QUANT_WAVES * 4) * 1024 + 128;
     if (g.inner <= 1024) return quant_go<quant_few<T, VEC, 1>>(t32 * nb, bytes, g, s);
     return quant_go<quant_few<T, VEC, 4>>(t32 * nb, bytes, g, s);
   }
-  const int rb = g.inner <= 1024 && g.rows > 128 * (CUS - 1) ? 4 : g.inner <= 2048 && g.rows > 64 * (CUS - 1) ? 2 : 1;
+  g.units = (int)op_div_up(g.outer, 64);
+  if constexpr (VEC) {
+    if (g.inner <= 1024 && g.rows > 128 * (CUS - 1)) {
+      g.row_tiles = (int)op_div_up(g.rows, 128);
+      return quant_go<quant_stream<T>>(CUS, unit32 * 4 + QUANT_SCRATCH * QUANT_WAVES / 2 + 512 + 2048, g, s);
+    }
+  }
+  const int rb = g.inner <= 2048 && g.rows > 64 * (CUS - 1) ? 2 : 1;
   const int64_t tiles = op_div_up(g.rows, rb * 32);
   g.row_tiles = (int)tiles;
-  g.units = (int)op_div_up(g.outer, 64);
   g.parts = 1;
   while (tiles * g.parts < CUS && g.parts * QUANT_WAVES < g.units) ++g.parts;
   const int64_t grid = op_div_up(tiles, 8) * 8 * g.parts;
-  const size_t bytes = unit32 * rb + QUANT_SCRATCH;
-  if (rb == 4 && g.outer > 128) return quant_go<quant_wide<T, VEC, 4, 4, 1>>(grid, bytes, g, s);
-  if (rb == 4) return quant_go<quant_wide<T, VEC, 4, 1, 1>>(grid, bytes, g, s);
-  if (rb == 2 && g.inner <= 1024) return quant_go<quant_wide<T, VEC, 2, 2, 1>>(grid, bytes, g, s);
-  if (rb == 2) return quant_go<quant_wide<T, VEC, 2, 2, 2>>(grid, bytes, g, s);
-  if (g.inner <= 1024) return quant_go<quant_wide<T, VEC, 1, 1, 1>>(grid, bytes, g, s);
-  return quant_go<quant_wide<T, VEC, 1, 1, 4>>(grid, bytes, g, s);
+  const size_t bytes = unit32 * rb + QUANT_SCRATCH * QUANT_WAVES;
+  if (rb == 2 && g.inner <= 1024)
+    return quant_go<quant_wide<T, VEC, 2, 1, 4>>(grid, unit32 * 2 + QUANT_SCRATCH * 4, g, s, 256);
+  if (rb == 2) return quant_go<quant_wide<T, VEC, 2, 2, QUANT_WAVES>>(grid, bytes, g, s);
+  if (g.inner <= 1024) return quant_go<quant_wide<T, VEC, 1, 1, QUANT_WAVES>>(grid, bytes, g, s);
+  return quant_go<quant_wide<T, VEC, 1, 4, QUANT_WAVES>>(grid, bytes, g, s);
 }
 
 template <typename T>
@@ -527,7 +644,6 @@ hipError_t quant_launch(int64_t rows, int64_t outer, int64_t inner, const void* 
     g.y = y; g.y_row = y_row;
     g.rows = rows; g.outer = outer; g.inner = (int)inner; g.steps = (int)steps;
     g.y_vec = outer % E == 0 && op_vec_ok(y, y_row, sizeof(T));
-    g.w_vec = op_aligned(w_scale, 16) && op_aligned(bias, 16);
     if (inner % 16 == 0 && op_vec_ok(x, x_row, sizeof(T))) return quant_launch_lds<T, true>(g, s);
     return quant_launch_lds<T, false>(g, s);
   }
