@@ -30,11 +30,14 @@ template <int CTRL> __device__ inline uint32_t dpp_max(uint32_t x) {
   const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
   return o > x ? o : x;
 }
-__device__ inline uint32_t wave_max(uint32_t x) {
+__device__ inline uint32_t max16(uint32_t x) {   // of 16 lanes
   x = dpp_max<0xB1>(x);    // neighbours, pairs, the halves of 16 lanes mirrored, the 16 mirrored
   x = dpp_max<0x4E>(x);
   x = dpp_max<0x141>(x);
-  x = dpp_max<0x140>(x);
+  return dpp_max<0x140>(x);
+}
+__device__ inline uint32_t wave_max(uint32_t x) {
+  x = max16(x);
   auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
   x = r[0] > r[1] ? r[0] : r[1];
   r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
@@ -180,19 +183,23 @@ template <typename T> __device__ inline uint32_t largest(const u32x4& w, uint32_
   return m;
 }
 
-// R rows of x as a wave loads them, NU units of 16 inputs a lane (up to 1024 NU inputs), and their way
-// into LDS: unit k of the workgroup's row r at k RT + (r ^ (k & 7)), so that 32 rows of a unit are contiguous
-// for the products and eight units of a row fall on different banks here. What lies past a row's
-// inputs within its last step meets zero weights; what lies past the rows is not stored.
-template <typename T, bool VEC, int R, int NU> struct RowChunk {
-  static constexpr int E = OP_VEC<T>, W = 16 / E;
+// Rows of x as a wave loads them: LPR lanes a row (64, or 16: four rows at once, for up to 256 inputs),
+// R times, NU units of 16 inputs a lane (up to 16 LPR NU inputs); and their way into LDS: unit k of the
+// workgroup's row r at k RT + (r ^ (k & 7)), so that 32 rows of a unit are contiguous for the products and
+// eight units of a row fall on different banks here. What lies past a row's inputs within its last
+// step meets zero weights; what lies past the rows is not stored. VEC: 16-byte loads, a unit is 16
+// adjacent inputs; else its inputs are LPR apart, so that a row's lanes still read neighbours.
+template <typename T, bool VEC, int R, int NU, int LPR> struct RowChunk {
+  static constexpr int E = OP_VEC<T>, W = 16 / E, ROWS = R * (64 / LPR);
   typename std::conditional<VEC, u32x4[R][NU][W], float[R][NU * 16]>::type raw;
 
+  static __device__ int row_of(int j) { return LPR == 64 ? j : j * (64 / LPR) + (int)(threadIdx.x % 64) / LPR; }
+
   __device__ void load(const QuantArgs& g, int64_t row0) {
-    const int lane = threadIdx.x % 64;
+    const int lane = threadIdx.x % LPR;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-      const int64_t row = row0 + j < g.rows ? row0 + j : g.rows - 1;
+      const int64_t want = row0 + row_of(j), row = want < g.rows ? want : g.rows - 1;
       const T* p = static_cast<const T*>(g.x) + row * g.x_row;
       if constexpr (VEC) {
 #pragma unroll
@@ -200,13 +207,13 @@ template <typename T, bool VEC, int R, int NU> struct RowChunk {
 #pragma unroll
           for (int k = 0; k < W; ++k) {
             raw[j][u][k] = u32x4{0, 0, 0, 0};
-            const uint32_t c = (u * 64 + lane) * 16;
-            if (c < (uint32_t)g.inner) raw[j][u][k] = *reinterpret_cast<const u32x4*>(p + c + k * E);
+            const uint32_t c = (u * LPR + lane) * 16 + k * E;
+            if (c < (uint32_t)g.inner) raw[j][u][k] = *reinterpret_cast<const u32x4*>(p + c);
           }
       } else {
 #pragma unroll
         for (int i = 0; i < NU * 16; ++i) {
-          const int c = i * 64 + lane;
+          const int c = i * LPR + lane;
           raw[j][i] = c < g.inner ? to_f<T>(p[c]) : 0.0f;
         }
       }
@@ -232,7 +239,8 @@ template <typename T, bool VEC, int R, int NU> struct RowChunk {
           m[j] = b > m[j] ? b : m[j];
         }
       }
-      m[j] = __builtin_amdgcn_readfirstlane(wave_max(m[j]));
+      if (LPR == 64) m[j] = __builtin_amdgcn_readfirstlane(wave_max(m[j]));
+      else m[j] = max16(m[j]);
     }
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -258,41 +266,42 @@ template <typename T, bool VEC, int R, int NU> struct RowChunk {
       }
     }
   }
-};
 
-// One unit of a row's integers to its place.
-template <bool VEC, int RT> __device__ inline void place(const QuantArgs& g, u32x4* a, int r, int u, const u32x4& q) {
-  const int lane = threadIdx.x % 64;
-  if constexpr (VEC) {
-    const int k = u * 64 + lane;
-    if (k < 2 * g.steps) a[k * RT + (r ^ (k & 7))] = q;
-  } else {
+  // One unit of a row's integers to its place: unit u of the lane, row r of the RT.
+  template <int RT> static __device__ void place(const QuantArgs& g, u32x4* a, int r, int u, const u32x4& q) {
+    const int lane = threadIdx.x % LPR;
+    if constexpr (VEC) {
+      const int k = u * LPR + lane;
+      if (k < 2 * g.steps) a[k * RT + (r ^ (k & 7))] = q;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int c = (u * 16 + i) * 64 + lane, k = c / 16;
-      if (c < g.inner) reinterpret_cast<uint8_t*>(a + (k * RT + (r ^ (k & 7))))[c % 16] = (uint8_t)(q[i / 4] >> (i % 4 * 8));
+      for (int i = 0; i < 16; ++i) {
+        const int c = (u * 16 + i) * LPR + lane, k = c / 16;
+        if (c < g.inner) reinterpret_cast<uint8_t*>(a + (k * RT + (r ^ (k & 7))))[c % 16] = (uint8_t)(q[i / 4] >> (i % 4 * 8));
+      }
     }
   }
-}
+};
 
 // Rows row0 .. row0 + RT - 1 into LDS by WAVES waves, 64 registers of them at a time.
-template <typename T, bool VEC, int RT, int NU, int WAVES>
+template <typename T, bool VEC, int RT, int NU, int LPR, int WAVES>
 __device__ inline void quantise_rows(const QuantArgs& g, int64_t row0, u32x4* a, float* scale) {
-  constexpr int PER = RT / WAVES, MOST = VEC ? 16 / (int)sizeof(T) / NU : 4 / NU, R = MOST < PER ? MOST : PER;
+  constexpr int PER = RT / WAVES, TIMES = PER / (64 / LPR), MOST = VEC ? 16 / (int)sizeof(T) / NU : 4 / NU, R = MOST < TIMES ? MOST : TIMES;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  for (int j = 0; j < PER; j += R) {
+  using C = RowChunk<T, VEC, R, NU, LPR>;
+  for (int j = 0; j < PER; j += C::ROWS) {
     if (row0 + wave * PER + j >= g.rows) break;
-    RowChunk<T, VEC, R, NU> c;
+    C c;
     c.load(g, row0 + wave * PER + j);
     float sc[R];
     u32x4 q[R][NU];
     c.quantise(sc, q);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const int r = wave * PER + j + i;
-      if (threadIdx.x % 64 == 0) scale[r] = sc[i];
+      const int r = wave * PER + j + C::row_of(i);
+      if (threadIdx.x % LPR == 0) scale[r] = sc[i];
 #pragma unroll
-      for (int u = 0; u < NU; ++u) place<VEC, RT>(g, a, r, u, q[i][u]);
+      for (int u = 0; u < NU; ++u) C::template place<RT>(g, a, r, u, q[i][u]);
     }
   }
 }
@@ -439,7 +448,7 @@ __device__ inline void quant_units(const QuantArgs& g, const u32x4* lds, int uni
 
 // A workgroup: RT rows and its part of the channels, 64 a wave at a time, each wave on its own once the
 // rows are in LDS.
-template <typename T, bool VEC, int RB, int NU, int WAVES>
+template <typename T, bool VEC, int RB, int NU, int LPR, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void quant_wide(QuantArgs g) {
   extern __shared__ u32x4 lds[];
   constexpr int RT = RB * 32;
@@ -450,7 +459,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void quant_wide(QuantArgs g) {
   uint8_t* scratch = reinterpret_cast<uint8_t*>(lds + 2 * g.steps * RT);
   float* scale = reinterpret_cast<float*>(scratch);
   const int64_t row0 = (int64_t)tile * RT;
-  quantise_rows<T, VEC, RT, NU, WAVES>(g, row0, lds, scale);
+  quantise_rows<T, VEC, RT, NU, LPR, WAVES>(g, row0, lds, scale);
   __syncthreads();
   float xs[RB];
 #pragma unroll
@@ -474,7 +483,8 @@ __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_stream(QuantArgs g) {
   uint8_t* scratch = reinterpret_cast<uint8_t*>(lds + 2 * g.steps * RT);
   float* scale = reinterpret_cast<float*>(scratch + HALF * QUANT_SCRATCH);   // [RT]
   const int stride = gridDim.x;
-  quantise_rows<T, true, RT, 1, QUANT_WAVES>(g, (int64_t)blockIdx.x * RT, lds, scale);   // the first tile: everyone
+  using C = RowChunk<T, true, R, 1, 64>;
+  quantise_rows<T, true, RT, 1, 64, QUANT_WAVES>(g, (int64_t)blockIdx.x * RT, lds, scale);   // the first tile: everyone
   __syncthreads();
   // Two barriers a tile for both halves: LDS is free, LDS is filled.
   if (wave >= HALF) {
@@ -485,7 +495,7 @@ __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_stream(QuantArgs g) {
       if (next < g.row_tiles) {
 #pragma unroll
         for (int j = 0; j < PER / R; ++j) {
-          RowChunk<T, true, R, 1> c;
+          C c;
           c.load(g, (int64_t)next * RT + of * PER + j * R);
           float sc[R];
           c.quantise(sc, q[j]);
@@ -496,7 +506,7 @@ __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_stream(QuantArgs g) {
       __syncthreads();
       if (next < g.row_tiles) {
 #pragma unroll
-        for (int j = 0; j < PER; ++j) place<true, RT>(g, lds, of * PER + j, 0, q[j / R][j % R][0]);
+        for (int j = 0; j < PER; ++j) C::template place<RT>(g, lds, of * PER + j, 0, q[j / R][j % R][0]);
         if (lane < PER) scale[of * PER + lane] = mine;
       }
       __syncthreads();
@@ -516,7 +526,7 @@ __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_stream(QuantArgs g) {
 // Few rows: 32 rows by 32 channels a workgroup, whose waves share the inputs out (every eighth step each) and add
 // their sums in LDS: the weights' loads of a call are spread over the whole device and are in flight
 // while the rows are quantised (by every workgroup for itself, from L2).
-template <typename T, bool VEC, int NU>
+template <typename T, bool VEC, int NU, int LPR>
 __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_few(QuantArgs g) {
   extern __shared__ u32x4 lds[];
   const int nb = (int)((g.outer + 31) / 32), lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -530,7 +540,7 @@ __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_few(QuantArgs g) {
     b[j] = w[(s < g.steps ? s : 0) * 64];
   }
   float* scale = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(lds) + (g.steps > QUANT_WAVES * 4 ? g.steps : QUANT_WAVES * 4) * 1024);
-  quantise_rows<T, VEC, 32, NU, QUANT_WAVES>(g, row0, lds, scale);
+  quantise_rows<T, VEC, 32, NU, LPR, QUANT_WAVES>(g, row0, lds, scale);
   __syncthreads();
   i32x16 acc = {};
   for (int s0 = 0; s0 < g.steps; s0 += U * QUANT_WAVES) {
@@ -608,12 +618,13 @@ template <typename T, bool VEC> hipError_t quant_launch_lds(QuantArgs g, hipStre
   const size_t unit32 = (size_t)g.steps * 1024;   // bytes of 32 rows
   if (t32 * op_div_up(g.outer, 512) < CUS / 2) {
     const size_t bytes = (g.steps > QUANT_WAVES * 4 ? g.steps : QUANT_WAVES * 4) * 1024 + 128;
-    if (g.inner <= 1024) return quant_go<quant_few<T, VEC, 1>>(t32 * nb, bytes, g, s);
-    return quant_go<quant_few<T, VEC, 4>>(t32 * nb, bytes, g, s);
+    if (g.inner <= 256) return quant_go<quant_few<T, VEC, 1, 16>>(t32 * nb, bytes, g, s);
+    if (g.inner <= 1024) return quant_go<quant_few<T, VEC, 1, 64>>(t32 * nb, bytes, g, s);
+    return quant_go<quant_few<T, VEC, 4, 64>>(t32 * nb, bytes, g, s);
   }
   g.units = (int)op_div_up(g.outer, 64);
   if constexpr (VEC) {
-    if (g.inner <= 1024 && g.rows > 128 * (CUS - 1)) {
+    if (g.inner > 256 && g.inner <= 1024 && g.rows > 128 * (CUS - 1)) {
       g.row_tiles = (int)op_div_up(g.rows, 128);
       return quant_go<quant_stream<T>>(CUS, unit32 * 4 + QUANT_SCRATCH * QUANT_WAVES / 2 + 512 + 2048, g, s);
     }
@@ -625,11 +636,15 @@ template <typename T, bool VEC> hipError_t quant_launch_lds(QuantArgs g, hipStre
   while (tiles * g.parts < CUS && g.parts * QUANT_WAVES < g.units) ++g.parts;
   const int64_t grid = op_div_up(tiles, 8) * 8 * g.parts;
   const size_t bytes = unit32 * rb + QUANT_SCRATCH * QUANT_WAVES;
-  if (rb == 2 && g.inner <= 1024)
-    return quant_go<quant_wide<T, VEC, 2, 1, 4>>(grid, unit32 * 2 + QUANT_SCRATCH * 4, g, s, 256);
-  if (rb == 2) return quant_go<quant_wide<T, VEC, 2, 2, QUANT_WAVES>>(grid, bytes, g, s);
-  if (g.inner <= 1024) return quant_go<quant_wide<T, VEC, 1, 1, QUANT_WAVES>>(grid, bytes, g, s);
-  return quant_go<quant_wide<T, VEC, 1, 4, QUANT_WAVES>>(grid, bytes, g, s);
+  if (rb == 2 && g.inner <= 1024) {
+    const size_t four = unit32 * 2 + QUANT_SCRATCH * 4;   // four waves: two workgroups a compute unit
+    if (g.inner <= 256) return quant_go<quant_wide<T, VEC, 2, 1, 16, 4>>(grid, four, g, s, 256);
+    return quant_go<quant_wide<T, VEC, 2, 1, 64, 4>>(grid, four, g, s, 256);
+  }
+  if (rb == 2) return quant_go<quant_wide<T, VEC, 2, 2, 64, QUANT_WAVES>>(grid, bytes, g, s);
+  if (g.inner <= 256) return quant_go<quant_wide<T, VEC, 1, 1, 16, QUANT_WAVES>>(grid, bytes, g, s);
+  if (g.inner <= 1024) return quant_go<quant_wide<T, VEC, 1, 1, 64, QUANT_WAVES>>(grid, bytes, g, s);
+  return quant_go<quant_wide<T, VEC, 1, 4, 64, QUANT_WAVES>>(grid, bytes, g, s);
 }
 
 template <typename T>
@@ -644,7 +659,7 @@ hipError_t quant_launch(int64_t rows, int64_t outer, int64_t inner, const void* 
     g.y = y; g.y_row = y_row;
     g.rows = rows; g.outer = outer; g.inner = (int)inner; g.steps = (int)steps;
     g.y_vec = outer % E == 0 && op_vec_ok(y, y_row, sizeof(T));
-    if (inner % 16 == 0 && op_vec_ok(x, x_row, sizeof(T))) return quant_launch_lds<T, true>(g, s);
+    if (inner % E == 0 && op_vec_ok(x, x_row, sizeof(T))) return quant_launch_lds<T, true>(g, s);
     return quant_launch_lds<T, false>(g, s);
   }
   int8_t* q = static_cast<int8_t*>(ws);

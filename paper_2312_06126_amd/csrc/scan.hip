@@ -650,19 +650,26 @@ template <typename T, int V, int CL> __global__ __launch_bounds__(TILE_THREADS, 
   if (a.dh0 && n == 0 && threadIdx.x < CL) store_s<V>(a.dh0 + st, vec && op_aligned16(a.dh0), c);
 }
 
-// How a call is spread over the threads, by its sizes alone:
-//   serial: a thread walks the whole sequence: sequences of at most SCAN_SHORT steps, or channels
-//     enough for SCAN_FILL threads (eight waves a compute unit);
-//   tiles: a workgroup walks it in tiles of time: SCAN_TILES workgroups or more, or so few tiles that
-//     one launch is shorter than the three of
-//   pieces: time cut into pieces, for SCAN_FILL threads but of at least SCAN_MIN_LEN steps each.
-constexpr int64_t SCAN_SHORT = 16, SCAN_FILL = 131072, SCAN_MIN_LEN = 32, SCAN_TILES = 128, SCAN_FEW_STEPS = 1024;
+// How a call is spread over the threads, by its sizes alone, from what the ways cost (microseconds
+// forward, both sides measured from 16 x 40 x 256 to 27 x 13250 x 56):
+//   serial: a thread walks the whole sequence: 0.26 a step, as long as there are threads for it;
+//   tiles: a workgroup walks it in tiles of time, 512 workgroups at a time: 3 a round and 3.7 a tile of it
+//     (64 x 64 x 256: 7 against 17 serially; 270 x 23 x 536: 64 against 12);
+//   pieces: time cut into pieces, for SCAN_FILL threads but of at least SCAN_MIN_LEN steps each: 24 for
+//     three launches and 1.6 a million elements for reading twice (1 x 4096 x 256: 26 against 59 in
+//     tiles; 8 x 2216 x 624: 54 against 43).
+constexpr int64_t SCAN_FILL = 131072, SCAN_MIN_LEN = 32;
 enum ScanWay { SCAN_SERIAL, SCAN_TILED, SCAN_PIECES };
 struct ScanPlan { ScanWay way; int64_t pieces, len; };
 ScanPlan scan_plan(const spz_scan_args& a) {
   const int64_t threads = a.batch * op_div_up(a.width, SCAN_V);
-  if (a.steps <= SCAN_SHORT || threads * 2 > SCAN_FILL) return {SCAN_SERIAL, 1, a.steps};
-  if (a.steps <= SCAN_FEW_STEPS || a.batch * op_div_up(a.width, 32) >= SCAN_TILES) return {SCAN_TILED, 1, a.steps};
+  const bool narrow = a.width <= 8, vectors = a.width % SCAN_V == 0;
+  const int64_t tile = (narrow ? 1024 : 256) / (vectors ? 1 : SCAN_V);   // steps of one
+  const int64_t rounds = op_div_up(a.batch * op_div_up(a.width, narrow ? 8 : 32), 512);
+  const int64_t turns = rounds * op_div_up(a.steps, tile);
+  if (threads * 2 > SCAN_FILL || a.steps <= 14 * turns + 11 * rounds) return {SCAN_SERIAL, 1, a.steps};
+  const int64_t millions = a.batch * a.steps * a.width >> 20;
+  if (turns <= 6 + millions / 2 || a.steps < 2 * SCAN_MIN_LEN) return {SCAN_TILED, 1, a.steps};
   int64_t pieces = op_div_up(SCAN_FILL, threads);
   const int64_t most = a.steps / SCAN_MIN_LEN;
   if (pieces > most) pieces = most;

@@ -274,8 +274,10 @@ def block_norm_backward(dx_out, du, x, h=None, z=None, w_post=None, b_post=None,
     def call(s):
         g = {"dx": x.new_empty(x.shape), "dh": None if h is None else x.new_empty(x.shape),
              "dz": x.new_empty(x.shape) if h is not None and gate != "none" else None}
-        for k, t in (("dw_post", w_post), ("dscale", scale), ("dw_pre", w_pre), ("db_post", b_post), ("db_pre", b_pre)):
-            g[k] = None if t is None else x.new_empty(t.shape, dtype=_F32)
+        wanted = (("dw_post", w_post), ("dscale", scale), ("dw_pre", w_pre), ("db_post", b_post), ("db_pre", b_pre))
+        sums = iter(x.new_empty((sum(t is not None for _, t in wanted), x.shape[1]), dtype=_F32).unbind(0))
+        for k, t in wanted:
+            g[k] = None if t is None else next(sums)
         a = _block_pack(x, h, z, vectors, valid, (None, None),
                         (dx_out, du, g["dx"], g["dh"], g["dz"], g["dw_post"], g["db_post"], g["dscale"], g["dw_pre"], g["db_pre"]),
                         drop, eps, post, pre, gate)
