@@ -78,60 +78,53 @@ template <int TPR> struct WideSum {
 };
 
 // ----------------------------------------------------------------------------- a row in registers
-// Thread `lane` of TPR holds K chunks of NORM_CHUNK elements. VEC: chunk j is the columns from
-// (j TPR + lane) NORM_CHUNK on, in 16-byte accesses; else its elements are TPR columns apart, so that
-// the threads of a row still read neighbours.
-template <typename T, bool VEC, int TPR, int K> struct RowMap {
-  static constexpr int VW = NORM_CHUNK, N = K * VW;
+// Thread `lane` of TPR holds K chunks of NORM_CHUNK adjacent elements, chunk j from column
+// (j TPR + lane) NORM_CHUNK on, in 16-byte accesses at whatever alignment the rows have. EVEN: the width
+// is a multiple of the chunk; else the row's last chunk has a part of its elements.
+template <typename T, bool EVEN, int TPR, int K> struct RowMap {
+  static constexpr int VW = NORM_CHUNK, N = K * VW, E = OP_VEC<T>, P = VW / E;
   static constexpr int MASK = TPR * K + 2;   // bytes of a row's dropout mask: its Philox blocks
   uint32_t lane, D;
-  __device__ uint32_t col(int j, int i) const { return VEC ? (j * TPR + lane) * VW + i : (j * VW + i) * TPR + lane; }
-  // Element i of chunk j exists (VEC: whole chunks do; the width is a multiple of theirs).
-  __device__ bool in(int j, int i) const { return col(j, VEC ? 0 : i) < D; }
+  __device__ uint32_t col(int j, int i) const { return (j * TPR + lane) * VW + i; }
+  // Element i of chunk j exists.
+  __device__ bool in(int j, int i) const { return col(j, EVEN ? 0 : i) < D; }
   // Element c of a row. The row's address is the same for a whole wave (where it is one): with a 32-bit
   // byte offset beside it no thread needs 64-bit arithmetic or registers for its addresses.
-  template <typename E> static __device__ E* at(E* row, uint32_t c) {
-    return reinterpret_cast<E*>(reinterpret_cast<char*>(const_cast<typename std::remove_const<E>::type*>(row)) + c * (uint32_t)sizeof(E));
+  template <typename V> static __device__ V* at(V* row, uint32_t c) {
+    return reinterpret_cast<V*>(reinterpret_cast<char*>(const_cast<typename std::remove_const<V>::type*>(row)) + c * (uint32_t)sizeof(V));
   }
   // The thread's part of a row as it is stored. Elements past the width are set to zero once (clear)
   // and never loaded, so that they add nothing to a sum.
   struct Raw {
-    static constexpr int WORDS = N * (int)sizeof(T) / 16;
-    typename std::conditional<VEC, u32x4[WORDS], T[N]>::type w;
+    u32x4 w[K * P];
     __device__ void clear() {
 #pragma unroll
-      for (int i = 0; i < (VEC ? WORDS : N); ++i) w[i] = decltype(+w[0]){};
+      for (int i = 0; i < K * P; ++i) w[i] = u32x4{0, 0, 0, 0};
     }
   };
+  // access(index, first column, elements) over the thread's accesses.
+  template <typename F> __device__ void each(F&& access) const {
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        const uint32_t c = col(j, k * E);
+        if (c < D) access(j * P + k, c, EVEN || c + E <= D ? E : (int)(D - c));
+      }
+  }
   __device__ void load(const T* p, Raw& r) const {
-    if constexpr (VEC) {
-      constexpr int E = OP_VEC<T>, P = VW / E;
-#pragma unroll
-      for (int j = 0; j < K; ++j)
-#pragma unroll
-        for (int k = 0; k < P; ++k)
-          if (in(j, 0)) r.w[j * P + k] = *reinterpret_cast<const u32x4*>(at(p, col(j, k * E)));
-    } else {
-#pragma unroll
-      for (int j = 0; j < K; ++j)
-#pragma unroll
-        for (int i = 0; i < VW; ++i)
-          if (in(j, i)) r.w[j * VW + i] = *at(p, col(j, i));
-    }
+    each([&](int i, uint32_t c, int n) {
+      if (n == E) r.w[i] = load16(at(p, c));
+      else r.w[i] = load_part(at(p, c), n);
+    });
   }
   __device__ void floats(const Raw& r, float (&x)[N]) const {
-    if constexpr (VEC) {
-      constexpr int E = OP_VEC<T>;
 #pragma unroll
-      for (int k = 0; k < N / E; ++k) {
-        float t[E];
-        unpack(r.w[k], t);
+    for (int k = 0; k < N / E; ++k) {
+      float t[E];
+      unpack(r.w[k], t);
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[k * E + i] = t[i];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = to_f<T>(r.w[i]);
+      for (int i = 0; i < E; ++i) x[k * E + i] = t[i];
     }
   }
   __device__ void load(const T* p, float (&x)[N]) const {
@@ -141,52 +134,47 @@ template <typename T, bool VEC, int TPR, int K> struct RowMap {
     floats(r, x);
   }
   __device__ void store(T* p, const float (&x)[N]) const {
-    if constexpr (VEC) {
-      constexpr int E = OP_VEC<T>, P = VW / E;
+    each([&](int i, uint32_t c, int n) {
+      float t[E];
 #pragma unroll
-      for (int j = 0; j < K; ++j)
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-          float t[E];
-#pragma unroll
-          for (int i = 0; i < E; ++i) t[i] = x[j * VW + k * E + i];
-          if (in(j, 0)) *reinterpret_cast<u32x4*>(at(p, col(j, k * E))) = pack(t);
-        }
-    } else {
-#pragma unroll
-      for (int j = 0; j < K; ++j)
-#pragma unroll
-        for (int i = 0; i < VW; ++i)
-          if (in(j, i)) *at(p, col(j, i)) = from_f<T>(x[j * VW + i]);
-    }
+      for (int k = 0; k < E; ++k) t[k] = x[i * E + k];
+      if (n == E) store16(at(p, c), pack(t));
+      else store_part(at(p, c), pack(t), n);
+    });
   }
   // A parameter vector; NULL: `other`, also past the width.
   __device__ void vec(const float* p, float other, float (&x)[N]) const {
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      if constexpr (VEC) {
+    for (int i = 0; i < N; ++i) x[i] = other;
+    if (!p) return;
 #pragma unroll
-        for (int i = 0; i < VW; i += 4) {
-          f32x4 w = {other, other, other, other};
-          if (p && in(j, 0)) w = *reinterpret_cast<const f32x4*>(at(p, col(j, i)));
+    for (int j = 0; j < K; ++j)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) x[j * VW + i + k] = w[k];
+      for (int i = 0; i < VW; i += 4) {
+        const uint32_t c = col(j, i);
+        if (EVEN ? c < D : c + 4 <= D) {
+          const u32x4 w = load16(at(p, c));
+          float t[4];
+          unpack(w, t);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[j * VW + i + k] = t[k];
+        } else if (!EVEN) {
+#pragma unroll
+          for (int k = 0; k < 3; ++k)
+            if (c + k < D) x[j * VW + i + k] = *at(p, c + k);
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < VW; ++i) x[j * VW + i] = p && in(j, i) ? *at(p, col(j, i)) : other;
       }
-    }
   }
-  // Dropout of the thread's elements. VEC: a chunk is one Philox block, whose words are kept. Else the
-  // row's threads take a block each and hand its bits over through LDS (`mask`, MASK bytes, a buffer
-  // that no thread of the row reads any more; one barrier where the row is more than a wave).
+  // Dropout of the thread's elements. EVEN: a chunk is one Philox block, whose words are kept. Else it lies
+  // across two, and the row's threads take a block each and hand its bits over through LDS (`mask`,
+  // MASK bytes, a buffer that no thread of the row reads any more; one barrier where the row is more
+  // than a wave).
   struct Kept {
-    U4 w[VEC ? K : 1];
+    U4 w[EVEN ? K : 1];
     uint32_t bits;   // bit j VW + i
     uint32_t d;
     __device__ float pass(int e, float x) const {
-      const bool keep = VEC ? drop_half(w[e / VW], e % VW) >= d : (bits >> e & 1) != 0;
+      const bool keep = EVEN ? drop_half(w[e / VW], e % VW) >= d : (bits >> e & 1) != 0;
       return keep ? x : 0.0f;
     }
   };
@@ -194,7 +182,7 @@ template <typename T, bool VEC, int TPR, int K> struct RowMap {
     const uint64_t e0 = (uint64_t)row * D;
     q.d = d;
     q.bits = 0;
-    if constexpr (VEC) {
+    if constexpr (EVEN) {
 #pragma unroll
       for (int j = 0; j < K; ++j) q.w[j] = drop_words((e0 + col(j, 0)) >> 3, a.seed, a.step, a.tensor);
     } else {
@@ -213,11 +201,11 @@ template <typename T, bool VEC, int TPR, int K> struct RowMap {
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
       }
-      const uint32_t first = (uint32_t)(e0 & 7);
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const uint32_t c = first + (in(e / VW, e % VW) ? col(e / VW, e % VW) : D - 1);
-        q.bits |= (uint32_t)(mask[c >> 3] >> (c & 7) & 1) << e;
+      for (int j = 0; j < K; ++j) {
+        const uint32_t c = (uint32_t)(e0 & 7) + (in(j, 0) ? col(j, 0) : 0);
+        const uint32_t two = mask[c >> 3] | (uint32_t)mask[(c >> 3) + 1] << 8;
+        q.bits |= (two >> (c & 7) & 0xFFu) << (j * VW);
       }
     }
   }
@@ -315,11 +303,11 @@ template <int TPR> constexpr int norm_threads = TPR > 64 ? TPR : NORM_THREADS;
   __shared__ float buf[2][TPR > 64 ? TPR / 64 : 1];                                                     \
   typename std::conditional<(TPR > 64), WideSum<(TPR > 64 ? TPR : 128)>, RowSum<TPR>>::type sum{};      \
   if constexpr (TPR > 64) sum.buf = buf;                                                                \
-  __shared__ uint8_t masks[2][VEC ? 1 : GROUPS][VEC ? 1 : M::MASK]
+  __shared__ uint8_t masks[2][EVEN ? 1 : GROUPS][EVEN ? 1 : M::MASK]
 
-template <typename T, bool VEC, int TPR, int K>
+template <typename T, bool EVEN, int TPR, int K>
 __global__ __launch_bounds__(norm_threads<TPR>) void norm_forward(NormArgs g) {
-  using M = RowMap<T, VEC, TPR, K>;
+  using M = RowMap<T, EVEN, TPR, K>;
   constexpr int N = M::N, GROUPS = norm_threads<TPR> / TPR;
   const spz_block_norm_args& a = g.a;
   const M m{threadIdx.x % TPR, (uint32_t)a.width};
@@ -342,7 +330,7 @@ __global__ __launch_bounds__(norm_threads<TPR>) void norm_forward(NormArgs g) {
     m.load(static_cast<const T*>(a.h) + row * a.h_row, h);
     if (a.gate != SPZ_GATE_NONE) m.load(static_cast<const T*>(a.z) + row * a.z_row, z);
     typename M::Kept kept;
-    if (g.drop.on) m.kept(a, g.drop.d, row, masks[0][VEC ? 0 : threadIdx.x / TPR], kept);
+    if (g.drop.on) m.kept(a, g.drop.d, row, masks[0][EVEN ? 0 : threadIdx.x / TPR], kept);
     m.norm(a.post, a.eps, inv_d, sum, h);
     if (a.post != SPZ_NORM_NONE) {
       if (a.w_post) {
@@ -387,9 +375,9 @@ __global__ __launch_bounds__(norm_threads<TPR>) void norm_forward(NormArgs g) {
   m.store(u, x);
 }
 
-template <typename T, bool VEC, int TPR, int K>
+template <typename T, bool EVEN, int TPR, int K>
 __global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g) {
-  using M = RowMap<T, VEC, TPR, K>;
+  using M = RowMap<T, EVEN, TPR, K>;
   constexpr int N = M::N, GROUPS = norm_threads<TPR> / TPR;
   const spz_block_norm_args& a = g.a;
   const M m{threadIdx.x % TPR, (uint32_t)a.width};
@@ -397,16 +385,26 @@ __global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g
   NORM_ROW_SUM();
   int slot = 0;
   const bool gated = a.h && a.gate != SPZ_GATE_NONE, has_du = a.du && a.pre != SPZ_NORM_NONE;
-  float acc[NORM_VECTORS][N], wq[N], bq[N], sc[N], wp[N];
+  // More than a chunk a thread (rows above 4096): registers hold the sums, but neither the vectors nor a
+  // second row beside them (with both, 600 of them spilled: 461 against 292 us at 4096 x 6000 bf16).
+  constexpr bool LEAN = K > 1;
+  float acc[NORM_VECTORS][N], kept_w[4][LEAN ? 1 : N];
 #pragma unroll
   for (int k = 0; k < NORM_VECTORS; ++k)
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[k][i] = 0.0f;
   const bool post = a.post != SPZ_NORM_NONE;
-  m.vec(post ? a.w_post : nullptr, 1.0f, wq);
-  m.vec(post ? a.b_post : nullptr, 0.0f, bq);
-  m.vec(a.scale, 1.0f, sc);
-  m.vec(a.w_pre, 1.0f, wp);
+  const float* const params[4] = {post ? a.w_post : nullptr, post ? a.b_post : nullptr, a.scale, a.w_pre};
+  constexpr int WQ = 0, BQ = 1, SC = 2, WP = 3;
+  if constexpr (!LEAN)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m.vec(params[k], k == BQ ? 0.0f : 1.0f, kept_w[k]);
+  const auto vec = [&](int k, float (&w)[N]) {
+    if constexpr (LEAN) m.vec(params[k], k == BQ ? 0.0f : 1.0f, w);
+    else
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = kept_w[k][i];
+  };
 
   struct Rows { typename M::Raw x, h, z, d, du; bool on; };
   const auto load = [&](int64_t row, Rows& r) {
@@ -434,7 +432,7 @@ __global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g
     m.floats(now.x, x);
     if (a.h) {
       if (g.drop.on) {
-        m.kept(a, g.drop.d, row, masks[slot][VEC ? 0 : threadIdx.x / TPR], kept);
+        m.kept(a, g.drop.d, row, masks[slot][EVEN ? 0 : threadIdx.x / TPR], kept);
         slot ^= 1;
       }
       m.floats(now.h, h);
@@ -447,6 +445,10 @@ __global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g
 #pragma unroll
         for (int i = 0; i < N; ++i) { gt[i] = 1.0f; slope[i] = 0.0f; }
       }
+      float wq[N], bq[N], sc[N];
+      vec(WQ, wq);
+      vec(BQ, bq);
+      vec(SC, sc);
       if (g.drop.on) {
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = fmaf(sc[i], kept.pass(i, gt[i] * fmaf(h[i], wq[i], bq[i]) * g.drop.gain), x[i]);
@@ -465,6 +467,8 @@ __global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g
       float du[N];
       m.floats(now.du, du);
       const float rx = m.norm(a.pre, a.eps, inv_d, sum, x);
+      float wp[N];
+      vec(WP, wp);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         acc[3][i] = fmaf(du[i], x[i], acc[3][i]);
@@ -481,6 +485,10 @@ __global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g
 #pragma unroll
       for (int i = 0; i < N; ++i) d[i] = kept.pass(i, d[i] * g.drop.gain);
     }
+    float wq[N], bq[N], sc[N];
+    vec(WQ, wq);
+    vec(BQ, bq);
+    vec(SC, sc);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float t = fmaf(h[i], wq[i], bq[i]);
@@ -502,21 +510,33 @@ __global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g
     m.norm_back(a.post, rh, inv_d, sum, h, d);
     m.store(static_cast<T*>(a.dh) + row * a.dh_row, d);
   };
-  // Two rows in turn, so that none is copied: the other one's loads are in flight.
   const int64_t stride = (int64_t)gridDim.x * GROUPS;
-  Rows r0, r1;
-  for (Rows* r : {&r0, &r1})
-    for (typename M::Raw* w : {&r->x, &r->h, &r->z, &r->d, &r->du}) w->clear();
-  int64_t row = first_row<TPR>();
-  if (row < a.rows) load(row, r0);
-  while (row < a.rows) {
-    if (row + stride < a.rows) load(row + stride, r1);
-    take(row, r0);
-    row += stride;
-    if (row >= a.rows) break;
-    if (row + stride < a.rows) load(row + stride, r0);
-    take(row, r1);
-    row += stride;
+  const auto clear = [](Rows& r) {
+    for (typename M::Raw* w : {&r.x, &r.h, &r.z, &r.d, &r.du}) w->clear();
+  };
+  if constexpr (LEAN) {
+    Rows r;
+    clear(r);
+    for (int64_t row = first_row<TPR>(); row < a.rows; row += stride) {
+      load(row, r);
+      take(row, r);
+    }
+  } else {
+    // Two rows in turn, so that none is copied: the other one's loads are in flight.
+    Rows r0, r1;
+    clear(r0);
+    clear(r1);
+    int64_t row = first_row<TPR>();
+    if (row < a.rows) load(row, r0);
+    while (row < a.rows) {
+      if (row + stride < a.rows) load(row + stride, r1);
+      take(row, r0);
+      row += stride;
+      if (row >= a.rows) break;
+      if (row + stride < a.rows) load(row + stride, r0);
+      take(row, r1);
+      row += stride;
+    }
   }
 
   // Column sums of the workgroup's rows, in their order.
@@ -699,8 +719,8 @@ template <typename T, bool BACK> __global__ __launch_bounds__(WIDE_THREADS) void
 }
 
 // ----------------------------------------------------------------------------- dropout
-// Eight elements a thread: one Philox block. FLAT: rows follow each other without a gap and the
-// arrays are 16-byte aligned, so that they are one row of eights with a ragged end.
+// Eight elements a thread: one Philox block. FLAT: rows follow each other without a gap, so that they
+// are one row of eights with a ragged end.
 template <typename T, bool FLAT>
 __global__ __launch_bounds__(256) void dropout(const T* x, int64_t x_row, T* y, int64_t y_row, int64_t width, int64_t n,
                                                Drop d, uint64_t seed, uint32_t step, uint32_t tensor) {
@@ -710,13 +730,13 @@ __global__ __launch_bounds__(256) void dropout(const T* x, int64_t x_row, T* y, 
   if (FLAT && i0 + 8 <= n) {
     float v[8 / VW][VW];
 #pragma unroll
-    for (int j = 0; j < 8 / VW; ++j) unpack(*reinterpret_cast<const u32x4*>(x + i0 + j * VW), v[j]);
+    for (int j = 0; j < 8 / VW; ++j) unpack(load16(x + i0 + j * VW), v[j]);
     const U4 w = drop_words((uint64_t)blk, seed, step, tensor);
 #pragma unroll
     for (int j = 0; j < 8 / VW; ++j) {
 #pragma unroll
       for (int i = 0; i < VW; ++i) v[j][i] = drop_half(w, j * VW + i) >= d.d ? v[j][i] * d.gain : 0.0f;
-      *reinterpret_cast<u32x4*>(y + i0 + j * VW) = pack(v[j]);
+      store16(y + i0 + j * VW, pack(v[j]));
     }
     return;
   }
@@ -758,18 +778,18 @@ int64_t norm_blocks(const spz_block_norm_args& a) {   // of the backward pass
   return n < most ? n : most;
 }
 
-template <typename T, bool VEC> void norm_dispatch(const NormArgs& g, bool back, int64_t blocks, hipStream_t s) {
+template <typename T, bool EVEN> void norm_dispatch(const NormArgs& g, bool back, int64_t blocks, hipStream_t s) {
   const NormWay way = norm_way(g.a.width, back);
   const auto go = [&](auto tpr, auto k) {
     constexpr int TPR = decltype(tpr)::value, K = decltype(k)::value;
     if constexpr (K == 1 || TPR == 512) {
       if (back) {
-        norm_backward<T, VEC, TPR, K><<<dim3((unsigned)blocks), norm_threads<TPR>, 0, s>>>(g);
+        norm_backward<T, EVEN, TPR, K><<<dim3((unsigned)blocks), norm_threads<TPR>, 0, s>>>(g);
         return;
       }
     }
     if constexpr ((K > 1 && TPR != 512) || TPR <= 64)
-      norm_forward<T, VEC, TPR, K><<<dim3((unsigned)op_div_up(g.a.rows, norm_threads<TPR> / TPR)), norm_threads<TPR>, 0, s>>>(g);
+      norm_forward<T, EVEN, TPR, K><<<dim3((unsigned)op_div_up(g.a.rows, norm_threads<TPR> / TPR)), norm_threads<TPR>, 0, s>>>(g);
   };
   using std::integral_constant;
   const auto is = [&](int tpr, int k) { return way.tpr == tpr && way.k == k; };
@@ -833,20 +853,6 @@ const char* norm_check_arrays(const spz_block_norm_args& a, bool back) {
   return nullptr;
 }
 
-// 16-byte accesses everywhere: every array that the call touches is aligned for them.
-bool norm_vec(const spz_block_norm_args& a, bool back) {
-  const int e = op_size(a.prec);
-  if (a.width % NORM_CHUNK) return false;
-  const auto ok = [&](const void* p, int64_t s) { return !p || op_vec_ok(p, s, e); };
-  for (const float* p : {a.w_post, a.b_post, a.scale, a.w_pre, a.b_pre})
-    if (!op_aligned(p, 16)) return false;
-  const bool z = a.h && a.gate != SPZ_GATE_NONE, pre = a.pre != SPZ_NORM_NONE;
-  if (!ok(a.x, a.x_row) || !ok(a.h, a.h_row) || (z && !ok(a.z, a.z_row))) return false;
-  if (!back) return (!a.h || ok(a.x_out, a.x_out_row)) && (!pre || ok(a.u, a.u_row));
-  return ok(a.dx_out, a.dx_out_row) && (!pre || ok(a.du, a.du_row)) && ok(a.dx, a.dx_row) &&
-         (!a.h || ok(a.dh, a.dh_row)) && (!z || ok(a.dz, a.dz_row));
-}
-
 int norm_run(const char* call, const spz_block_norm_args* args, bool back, void* ws, int64_t ws_bytes, void* stream) {
   const char* bad = norm_check(args);
   if (!bad) bad = norm_check_arrays(*args, back);
@@ -866,15 +872,15 @@ int norm_run(const char* call, const spz_block_norm_args* args, bool back, void*
   g.drop.d = drop_threshold(a.drop_p);
   g.drop.gain = drop_gain(g.drop.d);
   g.drop.on = g.drop.d > 0;
-  const bool vec = norm_vec(a, back);
+  const bool even = a.width % NORM_CHUNK == 0;
   const SumArgs o{{a.dw_post, a.db_post, a.dscale, a.dw_pre, a.db_pre}};
   for (int k = 0; k < NORM_VECTORS; ++k) g.wants[k] = o.out[k] != nullptr;
   if (a.rows > 0) {
     if (a.prec == SPZ_PREC_BF16) {
-      if (vec) norm_dispatch<bf16_t, true>(g, back, blocks, s);
+      if (even) norm_dispatch<bf16_t, true>(g, back, blocks, s);
       else norm_dispatch<bf16_t, false>(g, back, blocks, s);
     } else {
-      if (vec) norm_dispatch<float, true>(g, back, blocks, s);
+      if (even) norm_dispatch<float, true>(g, back, blocks, s);
       else norm_dispatch<float, false>(g, back, blocks, s);
     }
   }
@@ -922,7 +928,7 @@ int spz_dropout(int32_t prec, int64_t rows, int64_t width, const void* x, int64_
     return op_error(SPZ_EINVAL, call, "stride out of range");
   if (n == 0) return SPZ_OK;
   const Drop d{drop_threshold(p), drop_gain(drop_threshold(p)), true};
-  const bool flat = (rows == 1 || (x_row == width && y_row == width)) && op_aligned(x, 16) && op_aligned(y, 16);
+  const bool flat = rows == 1 || (x_row == width && y_row == width);
   const dim3 grid((unsigned)op_div_up(op_div_up(n, 8), 256));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const auto go = [&](auto kernel, auto tag) {

@@ -30,8 +30,6 @@ inline bool op_out_strides_ok(int64_t n0, int64_t n1, int64_t width, int64_t s0,
   // The inner dimension's span fits between two elements of the outer one.
   return s0 >= s1 ? s0 >= (n1 - 1) * s1 + width : s1 >= (n0 - 1) * s0 + width;
 }
-// 16-byte vectors of this array's rows: base and row distance (elements of e bytes).
-inline bool op_vec_ok(const void* p, int64_t stride, int e) { return op_aligned(p, 16) && stride * e % 16 == 0; }
 
 inline int64_t op_div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -73,6 +71,35 @@ __device__ inline u32x4 pack(const float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
   return w;
+}
+
+// Sixteen bytes at any alignment of the element type (the hardware takes 16-byte accesses of global
+// memory at any address; ones that straddle cache lines cost an access more), or the first n < OP_VEC
+// elements of them, with zeros behind.
+template <typename T> __device__ inline u32x4 load16(const T* p) {
+  u32x4 w;
+  __builtin_memcpy(&w, p, 16);
+  return w;
+}
+template <typename T> __device__ inline void store16(T* p, const u32x4& w) { __builtin_memcpy(p, &w, 16); }
+template <typename T> __device__ inline u32x4 load_part(const T* p, int n) {
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < OP_VEC<T> - 1; ++i)
+    if (i < n) {
+      if (sizeof(T) == 4) w[i & 3] = __builtin_bit_cast(uint32_t, to_f<T>(p[i]));
+      else w[(i / 2) & 3] |= (__builtin_bit_cast(uint32_t, to_f<T>(p[i])) >> 16) << (16 * (i & 1));
+    }
+  return u32x4{w[0], w[1], w[2], w[3]};
+}
+template <typename T> __device__ inline void store_part(T* p, const u32x4& v, int n) {
+  const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+  for (int i = 0; i < OP_VEC<T> - 1; ++i)
+    if (i < n) {
+      const uint32_t bits = sizeof(T) == 4 ? w[i & 3] : (i & 1) ? w[(i / 2) & 3] & 0xFFFF0000u : w[(i / 2) & 3] << 16;
+      p[i] = from_f<T>(__builtin_bit_cast(float, bits));   // exact: the value is one of T
+    }
 }
 
 // ----------------------------------------------------------------------------- arithmetic

@@ -123,7 +123,6 @@ struct QuantArgs {
   int64_t rows, outer;
   int inner, steps;         // steps of 32 inputs
   int row_tiles, parts, units;  // quant_wide: units of 64 channels, shared out over `parts` workgroups
-  bool y_vec;               // 16-byte stores of y
 };
 
 // Sixteen elements over s, rounded to integers, as bytes. r is 1 / s correctly rounded; then, with q = x r
@@ -187,11 +186,10 @@ template <typename T> __device__ inline uint32_t largest(const u32x4& w, uint32_
 // R times, NU units of 16 inputs a lane (up to 16 LPR NU inputs); and their way into LDS: unit k of the
 // workgroup's row r at k RT + (r ^ (k & 7)), so that 32 rows of a unit are contiguous for the products and
 // eight units of a row fall on different banks here. What lies past a row's inputs within its last
-// step meets zero weights; what lies past the rows is not stored. VEC: 16-byte loads, a unit is 16
-// adjacent inputs; else its inputs are LPR apart, so that a row's lanes still read neighbours.
-template <typename T, bool VEC, int R, int NU, int LPR> struct RowChunk {
+// step meets zero weights; what lies past the rows is not stored.
+template <typename T, int R, int NU, int LPR> struct RowChunk {
   static constexpr int E = OP_VEC<T>, W = 16 / E, ROWS = R * (64 / LPR);
-  typename std::conditional<VEC, u32x4[R][NU][W], float[R][NU * 16]>::type raw;
+  u32x4 raw[R][NU][W];
 
   static __device__ int row_of(int j) { return LPR == 64 ? j : j * (64 / LPR) + (int)(threadIdx.x % 64) / LPR; }
 
@@ -201,20 +199,24 @@ template <typename T, bool VEC, int R, int NU, int LPR> struct RowChunk {
     for (int j = 0; j < R; ++j) {
       const int64_t want = row0 + row_of(j), row = want < g.rows ? want : g.rows - 1;
       const T* p = static_cast<const T*>(g.x) + row * g.x_row;
-      if constexpr (VEC) {
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
+      for (int u = 0; u < NU; ++u)
 #pragma unroll
-          for (int k = 0; k < W; ++k) {
-            raw[j][u][k] = u32x4{0, 0, 0, 0};
-            const uint32_t c = (u * LPR + lane) * 16 + k * E;
-            if (c < (uint32_t)g.inner) raw[j][u][k] = *reinterpret_cast<const u32x4*>(p + c);
-          }
-      } else {
+        for (int k = 0; k < W; ++k) {
+          raw[j][u][k] = u32x4{0, 0, 0, 0};
+          const int c = (u * LPR + lane) * 16 + k * E;
+          if (c + E <= g.inner) raw[j][u][k] = load16(p + (uint32_t)c);
+        }
+      // The last elements of a row of no whole number of accesses: one lane's, one access.
+      if (g.inner % E) {
+        const int last = g.inner / E, u0 = last / W, k0 = last % W;
+        if (u0 % LPR == lane) {
+          const u32x4 w = load_part(p + last * E, g.inner % E);
 #pragma unroll
-        for (int i = 0; i < NU * 16; ++i) {
-          const int c = i * LPR + lane;
-          raw[j][i] = c < g.inner ? to_f<T>(p[c]) : 0.0f;
+          for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int k = 0; k < W; ++k)
+              if (u == u0 / LPR && k == k0) raw[j][u][k] = w;
         }
       }
     }
@@ -226,19 +228,11 @@ template <typename T, bool VEC, int R, int NU, int LPR> struct RowChunk {
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       m[j] = 0;
-      if constexpr (VEC) {
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
+      for (int u = 0; u < NU; ++u)
 #pragma unroll
-          for (int k = 0; k < W; ++k) m[j] = largest<T>(raw[j][u][k], m[j]);
-        if (sizeof(T) == 2) m[j] = (m[j] << 16) > (m[j] & 0xFFFF0000u) ? m[j] << 16 : m[j] & 0xFFFF0000u;
-      } else {
-#pragma unroll
-        for (int i = 0; i < NU * 16; ++i) {
-          const uint32_t b = __builtin_bit_cast(uint32_t, raw[j][i]) & 0x7FFFFFFFu;
-          m[j] = b > m[j] ? b : m[j];
-        }
-      }
+        for (int k = 0; k < W; ++k) m[j] = largest<T>(raw[j][u][k], m[j]);
+      if (sizeof(T) == 2) m[j] = (m[j] << 16) > (m[j] & 0xFFFF0000u) ? m[j] << 16 : m[j] & 0xFFFF0000u;
       if (LPR == 64) m[j] = __builtin_amdgcn_readfirstlane(wave_max(m[j]));
       else m[j] = max16(m[j]);
     }
@@ -250,17 +244,12 @@ template <typename T, bool VEC, int R, int NU, int LPR> struct RowChunk {
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         float v[16];
-        if constexpr (VEC) {
 #pragma unroll
-          for (int k = 0; k < W; ++k) {
-            float t[E];
-            unpack(raw[j][u][k], t);
+        for (int k = 0; k < W; ++k) {
+          float t[E];
+          unpack(raw[j][u][k], t);
 #pragma unroll
-            for (int i = 0; i < E; ++i) v[k * E + i] = t[i];
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = raw[j][u * 16 + i];
+          for (int i = 0; i < E; ++i) v[k * E + i] = t[i];
         }
         q[j][u] = zero ? u32x4{0, 0, 0, 0} : quantise16(v, f);
       }
@@ -269,26 +258,17 @@ template <typename T, bool VEC, int R, int NU, int LPR> struct RowChunk {
 
   // One unit of a row's integers to its place: unit u of the lane, row r of the RT.
   template <int RT> static __device__ void place(const QuantArgs& g, u32x4* a, int r, int u, const u32x4& q) {
-    const int lane = threadIdx.x % LPR;
-    if constexpr (VEC) {
-      const int k = u * LPR + lane;
-      if (k < 2 * g.steps) a[k * RT + (r ^ (k & 7))] = q;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int c = (u * 16 + i) * LPR + lane, k = c / 16;
-        if (c < g.inner) reinterpret_cast<uint8_t*>(a + (k * RT + (r ^ (k & 7))))[c % 16] = (uint8_t)(q[i / 4] >> (i % 4 * 8));
-      }
-    }
+    const int k = u * LPR + threadIdx.x % LPR;
+    if (k < 2 * g.steps) a[k * RT + (r ^ (k & 7))] = q;
   }
 };
 
 // Rows row0 .. row0 + RT - 1 into LDS by WAVES waves, 64 registers of them at a time.
-template <typename T, bool VEC, int RT, int NU, int LPR, int WAVES>
+template <typename T, int RT, int NU, int LPR, int WAVES>
 __device__ inline void quantise_rows(const QuantArgs& g, int64_t row0, u32x4* a, float* scale) {
-  constexpr int PER = RT / WAVES, TIMES = PER / (64 / LPR), MOST = VEC ? 16 / (int)sizeof(T) / NU : 4 / NU, R = MOST < TIMES ? MOST : TIMES;
+  constexpr int PER = RT / WAVES, TIMES = PER / (64 / LPR), MOST = 16 / (int)sizeof(T) / NU, R = MOST < 1 ? 1 : MOST < TIMES ? MOST : TIMES;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  using C = RowChunk<T, VEC, R, NU, LPR>;
+  using C = RowChunk<T, R, NU, LPR>;
   for (int j = 0; j < PER; j += C::ROWS) {
     if (row0 + wave * PER + j >= g.rows) break;
     C c;
@@ -329,7 +309,9 @@ __device__ inline void quant_store(const QuantArgs& g, const i32x16 (&acc)[RB][2
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t row = row0 + rb * 32 + i * 16 + lane / 4, n = n0 + piece * COLS + lane % 4 * E;
-      if (row < g.rows && n < g.outer) *reinterpret_cast<u32x4*>(static_cast<T*>(g.y) + row * g.y_row + n) = held[i];
+      T* p = static_cast<T*>(g.y) + row * g.y_row + n;
+      if (row < g.rows && n + E <= g.outer) store16(p, held[i]);
+      else if (row < g.rows && n < g.outer) store_part(p, held[i], (int)(g.outer - n));
     }
   };
 #pragma unroll
@@ -356,25 +338,16 @@ __device__ inline void quant_store(const QuantArgs& g, const i32x16 (&acc)[RB][2
           *reinterpret_cast<u32x4*>(scratch + l * 64 + ((2 * q + h) ^ turn) * 16) = pack(v);
       }
       settle();
-      if (g.y_vec) {
-        if (piece + rb > 0) flush(rb ? piece : piece - 1, rb ? rb - 1 : RB - 1);
+      if (piece + rb > 0) flush(rb ? piece : piece - 1, rb ? rb - 1 : RB - 1);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int r = i * 16 + lane / 4, unit = lane % 4;
-          held[i] = *reinterpret_cast<const u32x4*>(scratch + r * 64 + (unit ^ (r >> 2 & 3)) * 16);
-        }
-      } else {
-        for (int e = lane; e < 32 * COLS; e += 64) {
-          const int r = e / COLS, c = e % COLS;
-          const T w = *reinterpret_cast<const T*>(scratch + r * 64 + (c / E ^ (r >> 2 & 3)) * 16 + c % E * sizeof(T));
-          const int64_t row = row0 + rb * 32 + r, n = n0 + piece * COLS + c;
-          if (row < g.rows && n < g.outer) static_cast<T*>(g.y)[row * g.y_row + n] = w;
-        }
+      for (int i = 0; i < 2; ++i) {
+        const int r = i * 16 + lane / 4, unit = lane % 4;
+        held[i] = *reinterpret_cast<const u32x4*>(scratch + r * 64 + (unit ^ (r >> 2 & 3)) * 16);
       }
       settle();
     }
   }
-  if (g.y_vec) flush(64 / COLS - 1, RB - 1);
+  flush(64 / COLS - 1, RB - 1);
 }
 
 // One wave: RB blocks of 32 rows in LDS by the units of 64 channels unit0, unit0 + by, ... below unit1.
@@ -448,7 +421,7 @@ __device__ inline void quant_units(const QuantArgs& g, const u32x4* lds, int uni
 
 // A workgroup: RT rows and its part of the channels, 64 a wave at a time, each wave on its own once the
 // rows are in LDS.
-template <typename T, bool VEC, int RB, int NU, int LPR, int WAVES>
+template <typename T, int RB, int NU, int LPR, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void quant_wide(QuantArgs g) {
   extern __shared__ u32x4 lds[];
   constexpr int RT = RB * 32;
@@ -459,7 +432,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void quant_wide(QuantArgs g) {
   uint8_t* scratch = reinterpret_cast<uint8_t*>(lds + 2 * g.steps * RT);
   float* scale = reinterpret_cast<float*>(scratch);
   const int64_t row0 = (int64_t)tile * RT;
-  quantise_rows<T, VEC, RT, NU, LPR, WAVES>(g, row0, lds, scale);
+  quantise_rows<T, RT, NU, LPR, WAVES>(g, row0, lds, scale);
   __syncthreads();
   float xs[RB];
 #pragma unroll
@@ -483,8 +456,8 @@ __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_stream(QuantArgs g) {
   uint8_t* scratch = reinterpret_cast<uint8_t*>(lds + 2 * g.steps * RT);
   float* scale = reinterpret_cast<float*>(scratch + HALF * QUANT_SCRATCH);   // [RT]
   const int stride = gridDim.x;
-  using C = RowChunk<T, true, R, 1, 64>;
-  quantise_rows<T, true, RT, 1, 64, QUANT_WAVES>(g, (int64_t)blockIdx.x * RT, lds, scale);   // the first tile: everyone
+  using C = RowChunk<T, R, 1, 64>;
+  quantise_rows<T, RT, 1, 64, QUANT_WAVES>(g, (int64_t)blockIdx.x * RT, lds, scale);   // the first tile: everyone
   __syncthreads();
   // Two barriers a tile for both halves: LDS is free, LDS is filled.
   if (wave >= HALF) {
@@ -526,7 +499,7 @@ __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_stream(QuantArgs g) {
 // Few rows: 32 rows by 32 channels a workgroup, whose waves share the inputs out (every eighth step each) and add
 // their sums in LDS: the weights' loads of a call are spread over the whole device and are in flight
 // while the rows are quantised (by every workgroup for itself, from L2).
-template <typename T, bool VEC, int NU, int LPR>
+template <typename T, int NU, int LPR>
 __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_few(QuantArgs g) {
   extern __shared__ u32x4 lds[];
   const int nb = (int)((g.outer + 31) / 32), lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -540,7 +513,7 @@ __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_few(QuantArgs g) {
     b[j] = w[(s < g.steps ? s : 0) * 64];
   }
   float* scale = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(lds) + (g.steps > QUANT_WAVES * 4 ? g.steps : QUANT_WAVES * 4) * 1024);
-  quantise_rows<T, VEC, 32, NU, LPR, QUANT_WAVES>(g, row0, lds, scale);
+  quantise_rows<T, 32, NU, LPR, QUANT_WAVES>(g, row0, lds, scale);
   __syncthreads();
   i32x16 acc = {};
   for (int s0 = 0; s0 < g.steps; s0 += U * QUANT_WAVES) {
@@ -612,22 +585,20 @@ template <auto KERNEL> hipError_t quant_go(int64_t grid, size_t bytes, const Qua
 // tiles of rows of which every compute unit gets one and LDS holds it: 128 (quant_stream), 64, 32; the
 // channels shared out over workgroups where tiles of 32 rows are still too few. (LDS is for what quant_units
 // reads past the rows, too.)
-template <typename T, bool VEC> hipError_t quant_launch_lds(QuantArgs g, hipStream_t s) {
+template <typename T> hipError_t quant_launch_lds(QuantArgs g, hipStream_t s) {
   constexpr int64_t CUS = 256;
   const int64_t t32 = op_div_up(g.rows, 32), nb = op_div_up(g.outer, 32);
   const size_t unit32 = (size_t)g.steps * 1024;   // bytes of 32 rows
   if (t32 * op_div_up(g.outer, 512) < CUS / 2) {
     const size_t bytes = (g.steps > QUANT_WAVES * 4 ? g.steps : QUANT_WAVES * 4) * 1024 + 128;
-    if (g.inner <= 256) return quant_go<quant_few<T, VEC, 1, 16>>(t32 * nb, bytes, g, s);
-    if (g.inner <= 1024) return quant_go<quant_few<T, VEC, 1, 64>>(t32 * nb, bytes, g, s);
-    return quant_go<quant_few<T, VEC, 4, 64>>(t32 * nb, bytes, g, s);
+    if (g.inner <= 256) return quant_go<quant_few<T, 1, 16>>(t32 * nb, bytes, g, s);
+    if (g.inner <= 1024) return quant_go<quant_few<T, 1, 64>>(t32 * nb, bytes, g, s);
+    return quant_go<quant_few<T, 4, 64>>(t32 * nb, bytes, g, s);
   }
   g.units = (int)op_div_up(g.outer, 64);
-  if constexpr (VEC) {
-    if (g.inner > 256 && g.inner <= 1024 && g.rows > 128 * (CUS - 1)) {
-      g.row_tiles = (int)op_div_up(g.rows, 128);
-      return quant_go<quant_stream<T>>(CUS, unit32 * 4 + QUANT_SCRATCH * QUANT_WAVES / 2 + 512 + 2048, g, s);
-    }
+  if (g.inner > 256 && g.inner <= 1024 && g.rows > 128 * (CUS - 1)) {
+    g.row_tiles = (int)op_div_up(g.rows, 128);
+    return quant_go<quant_stream<T>>(CUS, unit32 * 4 + QUANT_SCRATCH * QUANT_WAVES / 2 + 512 + 2048, g, s);
   }
   const int rb = g.inner <= 2048 && g.rows > 64 * (CUS - 1) ? 2 : 1;
   const int64_t tiles = op_div_up(g.rows, rb * 32);
@@ -638,13 +609,13 @@ template <typename T, bool VEC> hipError_t quant_launch_lds(QuantArgs g, hipStre
   const size_t bytes = unit32 * rb + QUANT_SCRATCH * QUANT_WAVES;
   if (rb == 2 && g.inner <= 1024) {
     const size_t four = unit32 * 2 + QUANT_SCRATCH * 4;   // four waves: two workgroups a compute unit
-    if (g.inner <= 256) return quant_go<quant_wide<T, VEC, 2, 1, 16, 4>>(grid, four, g, s, 256);
-    return quant_go<quant_wide<T, VEC, 2, 1, 64, 4>>(grid, four, g, s, 256);
+    if (g.inner <= 256) return quant_go<quant_wide<T, 2, 1, 16, 4>>(grid, four, g, s, 256);
+    return quant_go<quant_wide<T, 2, 1, 64, 4>>(grid, four, g, s, 256);
   }
-  if (rb == 2) return quant_go<quant_wide<T, VEC, 2, 2, 64, QUANT_WAVES>>(grid, bytes, g, s);
-  if (g.inner <= 256) return quant_go<quant_wide<T, VEC, 1, 1, 16, QUANT_WAVES>>(grid, bytes, g, s);
-  if (g.inner <= 1024) return quant_go<quant_wide<T, VEC, 1, 1, 64, QUANT_WAVES>>(grid, bytes, g, s);
-  return quant_go<quant_wide<T, VEC, 1, 4, 64, QUANT_WAVES>>(grid, bytes, g, s);
+  if (rb == 2) return quant_go<quant_wide<T, 2, 2, 64, QUANT_WAVES>>(grid, bytes, g, s);
+  if (g.inner <= 256) return quant_go<quant_wide<T, 1, 1, 16, QUANT_WAVES>>(grid, bytes, g, s);
+  if (g.inner <= 1024) return quant_go<quant_wide<T, 1, 1, 64, QUANT_WAVES>>(grid, bytes, g, s);
+  return quant_go<quant_wide<T, 1, 4, 64, QUANT_WAVES>>(grid, bytes, g, s);
 }
 
 template <typename T>
@@ -652,15 +623,12 @@ hipError_t quant_launch(int64_t rows, int64_t outer, int64_t inner, const void* 
                         const float* w_scale, const float* bias, void* y, int64_t y_row, void* ws, hipStream_t s) {
   const int64_t mb = frag_blocks(rows), nb = frag_blocks(outer), steps = frag_blocks(inner);
   if (quant_in_lds(inner)) {
-    constexpr int E = OP_VEC<T>;
     QuantArgs g{};
     g.x = x; g.x_row = x_row;
     g.image = static_cast<const int8_t*>(image); g.w_scale = w_scale; g.bias = bias;
     g.y = y; g.y_row = y_row;
     g.rows = rows; g.outer = outer; g.inner = (int)inner; g.steps = (int)steps;
-    g.y_vec = outer % E == 0 && op_vec_ok(y, y_row, sizeof(T));
-    if (inner % E == 0 && op_vec_ok(x, x_row, sizeof(T))) return quant_launch_lds<T, true>(g, s);
-    return quant_launch_lds<T, false>(g, s);
+    return quant_launch_lds<T>(g, s);
   }
   int8_t* q = static_cast<int8_t*>(ws);
   float* xs = reinterpret_cast<float*>(q + mb * steps * FRAG);
