@@ -80,23 +80,30 @@ def _operand(t, name: str, dims: int) -> int:
     return t.get_device()
 
 
-def _on_stream(stream, gpu: int, tensors, call):
-    """call(stream address) with the tensors' device current and allocations on the stream."""
+_device = torch._C._cuda_getDevice
+_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _elsewhere(stream, gpu: int, tensors, call):
+    """call() with the tensors' device and the given stream current, so that what it allocates belongs to
+    that stream; the tensors stay alive until the stream has run."""
     if stream is None:
-        if gpu == torch.cuda.current_device():
-            return call(torch._C._cuda_getCurrentRawStream(gpu))
         with torch.cuda.device(gpu):
-            return call(torch._C._cuda_getCurrentRawStream(gpu))
+            return call()
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=gpu) if stream else torch.cuda.default_stream(gpu)
     elif stream.device.index != gpu:
         _refuse("the stream is on %s, the tensors are on cuda:%d" % (stream.device, gpu))
     with torch.cuda.stream(stream):
-        out = call(stream.cuda_stream)
+        out = call()
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
     return out
+
+
+def _empty(x: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
 
 
 def _workspace(n: int, ref: torch.Tensor) -> Optional[torch.Tensor]:
@@ -155,19 +162,20 @@ def scan(f, v, h0=None, *, reset=None, lengths=None, save: bool = False, out=Non
     _like(hT, "hT", gpu, (B, D), _F32, contiguous=True)
     n_saved, n, _ = _scan_sizes(B, T, D, prec)
 
-    def call(s):
-        y = out if out is not None else _sequences(f)
-        last = hT if hT is not None else f.new_empty((B, D), dtype=_F32)
-        saved = f.new_empty((n_saved,), dtype=_F32) if save else None
-        ws = _workspace(n, f)
-        a = pack_scan(B, T, D, f.data_ptr(), v.data_ptr(), *_outer(f), *_outer(v), _ptr(reset), *_outer(reset), _ptr(lengths),
-                      _ptr(h0), y.data_ptr(), *_outer(y), last.data_ptr(), _ptr(saved), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, prec)
-        rc = lib.spz_scan_forward(a, _ptr(ws), n, s)
-        if rc:
-            _done(rc)
-        return (y, last, saved) if save else (y, last)
-
-    return _on_stream(stream, gpu, (f, v, h0, reset, lengths, out, hT), call)
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (f, v, h0, reset, lengths, out, hT),
+                          lambda: scan(f, v, h0, reset=reset, lengths=lengths, save=save, out=out, hT=hT))
+    s = _stream(gpu)
+    y = out if out is not None else _sequences(f)
+    last = hT if hT is not None else torch.empty_like(h0) if h0 is not None else f.new_empty((B, D), dtype=_F32)
+    saved = f.new_empty((n_saved,), dtype=_F32) if save else None
+    ws = _workspace(n, f)
+    a = pack_scan(B, T, D, f.data_ptr(), v.data_ptr(), *_outer(f), *_outer(v), _ptr(reset), *_outer(reset), _ptr(lengths),
+                  _ptr(h0), y.data_ptr(), *_outer(y), last.data_ptr(), _ptr(saved), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, prec)
+    rc = lib.spz_scan_forward(a, _ptr(ws), n, s)
+    if rc:
+        _done(rc)
+    return (y, last, saved) if save else (y, last)
 
 
 def scan_backward(f, v, dy, saved, *, dhT=None, reset=None, lengths=None, out=None, stream=None):
@@ -189,17 +197,18 @@ def scan_backward(f, v, dy, saved, *, dhT=None, reset=None, lengths=None, out=No
                 _refuse("out holds df and dv")
             _like(t, name, gpu, f.shape, f.dtype)
 
-    def call(s):
-        df, dv = out if out is not None else (_sequences(f), _sequences(f))
-        dh0 = f.new_empty((B, D), dtype=_F32)
-        ws = _workspace(n, f)
-        a = pack_scan(B, T, D, f.data_ptr(), v.data_ptr(), *_outer(f), *_outer(v), _ptr(reset), *_outer(reset), _ptr(lengths),
-                      0, 0, 0, 0, 0, saved.data_ptr(), _ptr(dy), *_outer(dy), _ptr(dhT), df.data_ptr(), dv.data_ptr(),
-                      *_outer(df), *_outer(dv), dh0.data_ptr(), prec)
-        _done(lib.spz_scan_backward(a, _ptr(ws), n, s))
-        return df, dv, dh0
-
-    return _on_stream(stream, gpu, (f, v, dy, saved, dhT, reset, lengths) + tuple(out or ()), call)
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (f, v, dy, saved, dhT, reset, lengths) + tuple(out or ()),
+                          lambda: scan_backward(f, v, dy, saved, dhT=dhT, reset=reset, lengths=lengths, out=out))
+    s = _stream(gpu)
+    df, dv = out if out is not None else (_sequences(f), _sequences(f))
+    dh0 = f.new_empty((B, D), dtype=_F32)
+    ws = _workspace(n, f)
+    a = pack_scan(B, T, D, f.data_ptr(), v.data_ptr(), *_outer(f), *_outer(v), _ptr(reset), *_outer(reset), _ptr(lengths),
+                  0, 0, 0, 0, 0, saved.data_ptr(), _ptr(dy), *_outer(dy), _ptr(dhT), df.data_ptr(), dv.data_ptr(),
+                  *_outer(df), *_outer(dv), dh0.data_ptr(), prec)
+    _done(lib.spz_scan_backward(a, _ptr(ws), n, s))
+    return df, dv, dh0
 
 
 # ----------------------------------------------------------------------------- block norm
@@ -215,8 +224,9 @@ def _block_check(x, h, z, vectors, post, pre, gate, valid) -> int:
     if gate != "none" and h is not None and z is None:
         _refuse("the gate needs z")
     _like(z, "z", gpu, shape, x.dtype)
-    for name, t in zip(("w_post", "b_post", "scale", "w_pre", "b_pre"), vectors):
-        _like(t, name, gpu, (D,), _F32)
+    for i, t in enumerate(vectors):
+        if t is not None and not (t.dtype is _F32 and t.dim() == 1 and t.numel() == D and t.get_device() == gpu and t.is_contiguous()):
+            _like(t, ("w_post", "b_post", "scale", "w_pre", "b_pre")[i], gpu, (D,), _F32)
     if valid is not None:
         _like(valid, "valid", gpu, (R,), torch.bool if getattr(valid, "dtype", None) is torch.bool else torch.uint8, contiguous=True)
     return gpu
@@ -249,16 +259,19 @@ def block_norm(x, h=None, z=None, w_post=None, b_post=None, scale=None, w_pre=No
     vectors = (w_post, b_post, scale, w_pre, b_pre)
     gpu = _block_check(x, h, z, vectors, post, pre, gate, valid)
 
-    def call(s):
-        x_out = x.new_empty(x.shape) if h is not None else None
-        u = x.new_empty(x.shape) if pre != "none" else None
-        a = _block_pack(x, h, z, vectors, valid, (x_out, u), (None,) * 10, drop, eps, post, pre, gate)
-        rc = lib.spz_block_norm_forward(a, s)
-        if rc:
-            _done(rc)
-        return (x if h is None else x_out), u
-
-    return _on_stream(stream, gpu, (x, h, z, *vectors, valid), call)
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (x, h, z, *vectors, valid),
+                          lambda: block_norm(x, h, z,
+                              w_post, b_post, scale, w_pre, b_pre, post=post, pre=pre, gate=gate, eps=eps,
+                              drop=drop, valid=valid))
+    s = _stream(gpu)
+    x_out = _empty(x) if h is not None else None
+    u = _empty(x) if pre != "none" else None
+    a = _block_pack(x, h, z, vectors, valid, (x_out, u), (None,) * 10, drop, eps, post, pre, gate)
+    rc = lib.spz_block_norm_forward(a, s)
+    if rc:
+        _done(rc)
+    return (x if h is None else x_out), u
 
 
 def block_norm_backward(dx_out, du, x, h=None, z=None, w_post=None, b_post=None, scale=None, w_pre=None, b_pre=None, *,
@@ -271,22 +284,25 @@ def block_norm_backward(dx_out, du, x, h=None, z=None, w_post=None, b_post=None,
     _like(dx_out, "dx_out", gpu, x.shape, x.dtype)
     _like(du, "du", gpu, x.shape, x.dtype)
 
-    def call(s):
-        g = {"dx": x.new_empty(x.shape), "dh": None if h is None else x.new_empty(x.shape),
-             "dz": x.new_empty(x.shape) if h is not None and gate != "none" else None}
-        wanted = (("dw_post", w_post), ("dscale", scale), ("dw_pre", w_pre), ("db_post", b_post), ("db_pre", b_pre))
-        sums = iter(x.new_empty((sum(t is not None for _, t in wanted), x.shape[1]), dtype=_F32).unbind(0))
-        for k, t in wanted:
-            g[k] = None if t is None else next(sums)
-        a = _block_pack(x, h, z, vectors, valid, (None, None),
-                        (dx_out, du, g["dx"], g["dh"], g["dz"], g["dw_post"], g["db_post"], g["dscale"], g["dw_pre"], g["db_pre"]),
-                        drop, eps, post, pre, gate)
-        n = _size(lib.spz_block_norm_workspace(a))
-        ws = _workspace(n, x)
-        _done(lib.spz_block_norm_backward(a, _ptr(ws), n, s))
-        return g
-
-    return _on_stream(stream, gpu, (x, dx_out, du, h, z, *vectors, valid), call)
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (x, dx_out, du, h, z, *vectors, valid),
+                          lambda: block_norm_backward(dx_out, du, x, h, z,
+                              w_post, b_post, scale, w_pre, b_pre, post=post, pre=pre, gate=gate, eps=eps,
+                              drop=drop, valid=valid))
+    s = _stream(gpu)
+    g = {"dx": _empty(x), "dh": None if h is None else _empty(x),
+         "dz": _empty(x) if h is not None and gate != "none" else None}
+    wanted = (("dw_post", w_post), ("dscale", scale), ("dw_pre", w_pre), ("db_post", b_post), ("db_pre", b_pre))
+    sums = iter(x.new_empty((sum(t is not None for _, t in wanted), x.shape[1]), dtype=_F32).unbind(0))
+    for k, t in wanted:
+        g[k] = None if t is None else next(sums)
+    a = _block_pack(x, h, z, vectors, valid, (None, None),
+                    (dx_out, du, g["dx"], g["dh"], g["dz"], g["dw_post"], g["db_post"], g["dscale"], g["dw_pre"], g["db_pre"]),
+                    drop, eps, post, pre, gate)
+    n = _size(lib.spz_block_norm_workspace(a))
+    ws = _workspace(n, x)
+    _done(lib.spz_block_norm_backward(a, _ptr(ws), n, s))
+    return g
 
 
 def dropout(x, p: float, seed: int, step: int, tensor: int = 0, *, out=None, stream=None):
@@ -297,16 +313,16 @@ def dropout(x, p: float, seed: int, step: int, tensor: int = 0, *, out=None, str
     gpu = _operand(x, "x", 2)
     _like(out, "out", gpu, x.shape, x.dtype)
 
-    def call(s):
-        rows, width = x.shape
-        y = out if out is not None else x.new_empty((rows, width))
-        rc = lib.spz_dropout(_PREC[x.dtype], rows, width, x.data_ptr(), x.stride(0), y.data_ptr(), y.stride(0), p,
-                             int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(tensor) & 0xFFFFFFFF, s)
-        if rc:
-            _done(rc)
-        return y
-
-    return _on_stream(stream, gpu, (x, out), call)
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (x, out), lambda: dropout(x, p, seed, step, tensor, out=out))
+    s = _stream(gpu)
+    rows, width = x.shape
+    y = out if out is not None else _empty(x)
+    rc = lib.spz_dropout(_PREC[x.dtype], rows, width, x.data_ptr(), x.stride(0), y.data_ptr(), y.stride(0), p,
+                         int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(tensor) & 0xFFFFFFFF, s)
+    if rc:
+        _done(rc)
+    return y
 
 
 # ----------------------------------------------------------------------------- 8-bit product
@@ -331,15 +347,15 @@ def quant_rows(x, *, stream=None):
     lib = load()
     gpu = _operand(x, "x", 2)
 
-    def call(s):
-        rows, width = x.shape
-        q = x.new_empty((rows, width), dtype=torch.int8)
-        scale = x.new_empty((rows,), dtype=_F32)
-        _done(lib.spz_quant_rows(_PREC[x.dtype], rows, width, x.data_ptr(), x.stride(0), q.data_ptr(), q.stride(0),
-                                 scale.data_ptr(), s))
-        return q, scale
-
-    return _on_stream(stream, gpu, (x,), call)
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (x,), lambda: quant_rows(x))
+    s = _stream(gpu)
+    rows, width = x.shape
+    q = x.new_empty((rows, width), dtype=torch.int8)
+    scale = x.new_empty((rows,), dtype=_F32)
+    _done(lib.spz_quant_rows(_PREC[x.dtype], rows, width, x.data_ptr(), x.stride(0), q.data_ptr(), q.stride(0),
+                             scale.data_ptr(), s))
+    return q, scale
 
 
 def quant_pack(q, scale, *, stream=None) -> QuantWeights:
@@ -356,12 +372,12 @@ def quant_pack(q, scale, *, stream=None) -> QuantWeights:
     _like(scale, "scale", gpu, (outer,), _F32, contiguous=True)
     n = _size(lib.spz_quant_image_bytes(outer, inner))
 
-    def call(s):
-        image = q.new_empty((n,))
-        _done(lib.spz_quant_pack(outer, inner, q.data_ptr(), q.stride(0), image.data_ptr(), s))
-        return QuantWeights(image, scale, outer, inner)
-
-    return _on_stream(stream, gpu, (q, scale), call)
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (q, scale), lambda: quant_pack(q, scale))
+    s = _stream(gpu)
+    image = q.new_empty((n,))
+    _done(lib.spz_quant_pack(outer, inner, q.data_ptr(), q.stride(0), image.data_ptr(), s))
+    return QuantWeights(image, scale, outer, inner)
 
 
 def quant_linear(x, weights: QuantWeights, *, bias=None, out=None, stream=None):
@@ -380,13 +396,13 @@ def quant_linear(x, weights: QuantWeights, *, bias=None, out=None, stream=None):
     _like(bias, "bias", gpu, (N,), _F32)
     _like(out, "out", gpu, (M, N), x.dtype)
 
-    def call(s):
-        y = out if out is not None else x.new_empty((M, N))
-        ws = _workspace(n, x)
-        rc = lib.spz_quant_linear(prec, M, N, K, x.data_ptr(), x.stride(0), image.data_ptr(), scale.data_ptr(), _ptr(bias),
-                                  y.data_ptr(), y.stride(0), _ptr(ws), n, s)
-        if rc:
-            _done(rc)
-        return y
-
-    return _on_stream(stream, gpu, (x, image, scale, bias, out), call)
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (x, image, scale, bias, out), lambda: quant_linear(x, weights, bias=bias, out=out))
+    s = _stream(gpu)
+    y = out if out is not None else x.new_empty((M, N))
+    ws = _workspace(n, x)
+    rc = lib.spz_quant_linear(prec, M, N, K, x.data_ptr(), x.stride(0), image.data_ptr(), scale.data_ptr(), _ptr(bias),
+                              y.data_ptr(), y.stride(0), _ptr(ws), n, s)
+    if rc:
+        _done(rc)
+    return y
