@@ -192,9 +192,9 @@ def scan_backward(f, v, dy, saved, *, dhT=None, reset=None, lengths=None, out=No
         _refuse("saved is missing: scan(..., save=True) makes it")
     _like(saved, "saved", gpu, (n_saved,), _F32, contiguous=True)
     if out is not None:
+        if len(out) != 2 or out[0] is None or out[1] is None:
+            _refuse("out holds df and dv")
         for name, t in zip(("df", "dv"), out):
-            if t is None:
-                _refuse("out holds df and dv")
             _like(t, name, gpu, f.shape, f.dtype)
 
     if stream is not None or gpu != _device():

@@ -517,3 +517,72 @@ def test_quant_refuses():
         with pytest.raises(SpzError) as e:
             call()
         assert e.value.code == SPZ_EINVAL
+
+
+# ----------------------------------------------------------------------------- across the operators
+
+def test_offsets_past_32_bits():
+    """Rows 2^32 elements apart give what the same rows side by side give."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(21)
+    B, T, D, far = 2, 40, 64, 1 << 32
+    big = torch.empty(far + T * D, dtype=torch.bfloat16, device="cuda")
+    f = gpu(rng.standard_normal((B, T, D)), "bf16")
+    v = gpu(rng.standard_normal((B, T, D)), "bf16")
+    apart = big.as_strided((B, T, D), (far, D, 1))
+    apart.copy_(f)
+    y, hT, saved = ops.scan(f, v, save=True)
+    y2, hT2, saved2 = ops.scan(apart, v, save=True)
+    assert torch.equal(y, y2) and torch.equal(hT, hT2)
+    for a, b in zip(ops.scan_backward(f, v, y, saved), ops.scan_backward(apart, v, y, saved2)):
+        assert torch.equal(a, b)
+    ops.scan(f, v, out=apart)                  # now the far rows are outputs
+    assert torch.equal(apart, y)
+    rows = big.as_strided((B, D), (far, 1))
+    x = rows.contiguous()
+    h = v[0, :B].contiguous()
+    for a, b in zip(ops.block_norm(x, h), ops.block_norm(rows, h)):
+        assert torch.equal(a, b)
+    assert torch.equal(ops.block_norm_backward(x, h, x, h)["dx"], ops.block_norm_backward(rows, h, rows, h)["dx"])
+    w = ops.quant_pack(*ops.quant_rows(gpu(rng.standard_normal((48, D)))))
+    assert torch.equal(ops.quant_linear(x, w), ops.quant_linear(rows, w))
+    assert all(torch.equal(a, b) for a, b in zip(ops.quant_rows(x), ops.quant_rows(rows)))
+
+
+@pytest.mark.parametrize("rows,inner", [(40, 4096), (33000, 512)])
+def test_graphs_replay_the_eager_results(rows, inner):
+    """A captured block (8-bit product, norm with dropout and gradients, scan in pieces) on new inputs, replayed
+    between eager work: every replay equals the eager calls."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(22)
+    D = 64
+    w = ops.quant_pack(*ops.quant_rows(gpu(rng.standard_normal((D, inner)))))
+    ones = torch.ones(D, device="cuda")
+    x = torch.empty((rows, inner), dtype=torch.bfloat16, device="cuda")
+    history = torch.empty((1, 4096, D), dtype=torch.bfloat16, device="cuda")
+
+    def block():
+        u = ops.quant_linear(x, w)
+        x_out, n = ops.block_norm(u, u, u, w_post=ones, scale=ones, w_pre=ones, gate="silu", drop=(0.2, 1, 2, 3))
+        g = ops.block_norm_backward(x_out, n, u, u, u, w_post=ones, scale=ones, w_pre=ones, gate="silu", drop=(0.2, 1, 2, 3))
+        y, hT, saved = ops.scan(history, history, save=True)
+        df, dv, dh0 = ops.scan_backward(history, history, y, saved)
+        return [u, x_out, n, y, hT, df, dv, dh0, ops.dropout(n, 0.5, 4, 5, 6)] + list(g[k] for k in ("dx", "dh", "dz", "dw_post", "dscale", "dw_pre"))
+
+    x.normal_()
+    history.normal_()
+    block()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = block()
+    for i in range(4):
+        x.copy_(gpu(rng.standard_normal((rows, inner)), "bf16"))
+        history.copy_(gpu(rng.standard_normal((1, 4096, D)), "bf16"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(captured, block()):
+            assert torch.equal(a, b), i
+        torch.cuda.synchronize()
