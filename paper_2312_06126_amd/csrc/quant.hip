@@ -36,11 +36,14 @@ __device__ inline uint32_t max16(uint32_t x) {   // of 16 lanes
   x = dpp_max<0x141>(x);
   return dpp_max<0x140>(x);
 }
-__device__ inline uint32_t wave_max(uint32_t x) {
+__device__ inline uint32_t max32(uint32_t x) {   // of 32 lanes
   x = max16(x);
-  auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  x = r[0] > r[1] ? r[0] : r[1];
-  r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return r[0] > r[1] ? r[0] : r[1];
+}
+__device__ inline uint32_t wave_max(uint32_t x) {
+  x = max32(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
   return r[0] > r[1] ? r[0] : r[1];
 }
 // The row's scale from the largest |x| as bits, and whether the row quantises to zeros: infinity and
@@ -182,8 +185,8 @@ template <typename T> __device__ inline uint32_t largest(const u32x4& w, uint32_
   return m;
 }
 
-// Rows of x as a wave loads them: LPR lanes a row (64, or 16: four rows at once, for up to 256 inputs),
-// R times, NU units of 16 inputs a lane (up to 16 LPR NU inputs); and their way into LDS: unit k of the
+// Rows of x as a wave loads them: LPR lanes a row (64; 16 or 32 for up to 256 or 512 inputs: four or two
+// rows at once), R times, NU units of 16 inputs a lane (up to 16 LPR NU inputs); and their way into LDS: unit k of the
 // workgroup's row r at k RT + (r ^ (k & 7)), so that 32 rows of a unit are contiguous for the products and
 // eight units of a row fall on different banks here. What lies past a row's inputs within its last
 // step meets zero weights; what lies past the rows is not stored.
@@ -234,7 +237,7 @@ template <typename T, int R, int NU, int LPR> struct RowChunk {
         for (int k = 0; k < W; ++k) m[j] = largest<T>(raw[j][u][k], m[j]);
       if (sizeof(T) == 2) m[j] = (m[j] << 16) > (m[j] & 0xFFFF0000u) ? m[j] << 16 : m[j] & 0xFFFF0000u;
       if (LPR == 64) m[j] = __builtin_amdgcn_readfirstlane(wave_max(m[j]));
-      else m[j] = max16(m[j]);
+      else m[j] = LPR == 32 ? max32(m[j]) : max16(m[j]);
     }
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -358,7 +361,7 @@ __device__ inline void quant_store(const QuantArgs& g, const i32x16 (&acc)[RB][2
 template <typename T, int RB>
 __device__ inline void quant_units(const QuantArgs& g, const u32x4* lds, int unit0, int unit1, int by, const float (&xs)[RB],
                                    int64_t row0, uint8_t* scratch) {
-  constexpr int RT = RB * 32, DEPTH = RB > 2 ? 4 : 8, XD = RB > 2 ? 2 : 4;
+  constexpr int RT = RB * 32, DEPTH = 8, XD = 4;
   const int lane = threadIdx.x % 64, l = lane % 32, h = lane / 32, nb = (int)((g.outer + 31) / 32);
   if (unit0 >= unit1) return;
   // Rows of step 4 s + j: unit 8 s + 2 j + h.
@@ -425,8 +428,11 @@ template <typename T, int RB, int NU, int LPR, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void quant_wide(QuantArgs g) {
   extern __shared__ u32x4 lds[];
   constexpr int RT = RB * 32;
-  // Workgroups of the same rows on one XCD (workgroup b runs on XCD b % 8).
-  const int tile = blockIdx.x % 8 + blockIdx.x / 8 / g.parts * 8, part = blockIdx.x / 8 % g.parts;
+  // Workgroup b runs on XCD b % 8: there are the workgroups of the same channels (eight parts or more:
+  // few rows, to which the weights are the larger part) or of the same rows.
+  const bool many = g.parts >= 8;
+  const int tile = many ? blockIdx.x / g.parts : blockIdx.x % 8 + blockIdx.x / 8 / g.parts * 8;
+  const int part = many ? blockIdx.x % g.parts : blockIdx.x / 8 % g.parts;
   if (tile >= g.row_tiles) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x % 32;
   uint8_t* scratch = reinterpret_cast<uint8_t*>(lds + 2 * g.steps * RT);
@@ -440,60 +446,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void quant_wide(QuantArgs g) {
   __syncthreads();   // the scratch holds the scales until here
   const int per = (g.units + g.parts - 1) / g.parts, u1 = (part + 1) * per < g.units ? (part + 1) * per : g.units;
   quant_units<T, RB>(g, lds, part * per + wave, u1, WAVES, xs, row0, scratch + wave * QUANT_SCRATCH);
-}
-
-// Many rows: workgroups stay, one a compute unit, and go from tile to tile of 128 rows, which fill LDS.
-// Half of the waves (one a SIMD) load and quantise the next tile and keep its integers in registers (128
-// of them) until the other half, which multiplies and stores the present tile, is done with LDS: reading,
-// quantising, matrix instructions and writing go on at the same time, and the weights come from L2
-// once for 128 rows (once for 64, two tiles in LDS at a time, took 260 against 204 us at
-// 131072 x 1024 x 1024 bf16).
-template <typename T>
-__global__ __launch_bounds__(QUANT_THREADS, 2) void quant_stream(QuantArgs g) {
-  extern __shared__ u32x4 lds[];
-  constexpr int RB = 4, RT = RB * 32, HALF = QUANT_WAVES / 2, PER = RT / HALF, R = 8 / (int)sizeof(T);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, of = wave % HALF;
-  uint8_t* scratch = reinterpret_cast<uint8_t*>(lds + 2 * g.steps * RT);
-  float* scale = reinterpret_cast<float*>(scratch + HALF * QUANT_SCRATCH);   // [RT]
-  const int stride = gridDim.x;
-  using C = RowChunk<T, R, 1, 64>;
-  quantise_rows<T, RT, 1, 64, QUANT_WAVES>(g, (int64_t)blockIdx.x * RT, lds, scale);   // the first tile: everyone
-  __syncthreads();
-  // Two barriers a tile for both halves: LDS is free, LDS is filled.
-  if (wave >= HALF) {
-    for (int tile = blockIdx.x; tile < g.row_tiles; tile += stride) {
-      const int next = tile + stride;
-      u32x4 q[PER / R][R][1];
-      float mine = 0.0f;   // lane j: the scale of row j
-      if (next < g.row_tiles) {
-#pragma unroll
-        for (int j = 0; j < PER / R; ++j) {
-          C c;
-          c.load(g, (int64_t)next * RT + of * PER + j * R);
-          float sc[R];
-          c.quantise(sc, q[j]);
-#pragma unroll
-          for (int i = 0; i < R; ++i) mine = lane == j * R + i ? sc[i] : mine;
-        }
-      }
-      __syncthreads();
-      if (next < g.row_tiles) {
-#pragma unroll
-        for (int j = 0; j < PER; ++j) C::template place<RT>(g, lds, of * PER + j, 0, q[j / R][j % R][0]);
-        if (lane < PER) scale[of * PER + lane] = mine;
-      }
-      __syncthreads();
-    }
-  } else {
-    for (int tile = blockIdx.x; tile < g.row_tiles; tile += stride) {
-      float xs[RB];
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) xs[rb] = scale[rb * 32 + lane % 32];
-      quant_units<T, RB>(g, lds, of, g.units, HALF, xs, (int64_t)tile * RT, scratch + of * QUANT_SCRATCH);
-      __syncthreads();
-      __syncthreads();
-    }
-  }
 }
 
 // Few rows: 32 rows by 32 channels a workgroup, whose waves share the inputs out (every eighth step each) and add
@@ -581,39 +533,43 @@ template <auto KERNEL> hipError_t quant_go(int64_t grid, size_t bytes, const Qua
   return hipGetLastError();
 }
 
-// Rows of up to QUANT_LDS_INNER inputs. Few row tiles: quant_few's 32 x 32 tiles. The largest
-// tiles of rows of which every compute unit gets one and LDS holds it: 128 (quant_stream), 64, 32; the
-// channels shared out over workgroups where tiles of 32 rows are still too few. (LDS is for what quant_units
-// reads past the rows, too.)
+// Rows of up to QUANT_LDS_INNER inputs, by what a compute unit gets (microseconds, bf16, both sides
+// measured):
+//   quant_few, while its 32 x 32 tiles are at most one a compute unit (64 x 2048 x 2048: 12 against 15 of
+//     quant_wide; 512 x 512 x 2048, four each: 15 against 7);
+//   quant_wide of 64 rows, two workgroups of four waves a compute unit (above 1024 inputs one of eight),
+//     where LDS holds them and every compute unit gets rows or some 2^27 multiplications
+//     (8192 x 1024 x 4096: 48 against 57 of 32 rows; 16384 x 2048 x 512: 33 against 45);
+//   else of 32 rows (5000 x 1024 x 800: 16 against 19).
+// Its channels are shared out over as many workgroups as run at once: one more a tile would be a second
+// round (2000 x 4096 x 4001: 57 in 4 parts, 100 in 5).
 template <typename T> hipError_t quant_launch_lds(QuantArgs g, hipStream_t s) {
   constexpr int64_t CUS = 256;
   const int64_t t32 = op_div_up(g.rows, 32), nb = op_div_up(g.outer, 32);
   const size_t unit32 = (size_t)g.steps * 1024;   // bytes of 32 rows
-  if (t32 * op_div_up(g.outer, 512) < CUS / 2) {
+  if (t32 * nb <= CUS) {
     const size_t bytes = (g.steps > QUANT_WAVES * 4 ? g.steps : QUANT_WAVES * 4) * 1024 + 128;
     if (g.inner <= 256) return quant_go<quant_few<T, 1, 16>>(t32 * nb, bytes, g, s);
+    if (g.inner <= 512) return quant_go<quant_few<T, 1, 32>>(t32 * nb, bytes, g, s);
     if (g.inner <= 1024) return quant_go<quant_few<T, 1, 64>>(t32 * nb, bytes, g, s);
     return quant_go<quant_few<T, 4, 64>>(t32 * nb, bytes, g, s);
   }
   g.units = (int)op_div_up(g.outer, 64);
-  if (g.inner > 256 && g.inner <= 1024 && g.rows > 128 * (CUS - 1)) {
-    g.row_tiles = (int)op_div_up(g.rows, 128);
-    return quant_go<quant_stream<T>>(CUS, unit32 * 4 + QUANT_SCRATCH * QUANT_WAVES / 2 + 512 + 2048, g, s);
-  }
-  const int rb = g.inner <= 2048 && g.rows > 64 * (CUS - 1) ? 2 : 1;
-  const int64_t tiles = op_div_up(g.rows, rb * 32);
+  const bool two = g.inner <= 2048 && (g.rows > 64 * (CUS - 1) || t32 * g.units * g.steps >= 512 * CUS);
+  const bool four = two && g.inner <= 1024;   // waves
+  const int64_t tiles = op_div_up(g.rows, two ? 64 : 32), at_once = four ? 2 * CUS : CUS;
   g.row_tiles = (int)tiles;
-  g.parts = 1;
-  while (tiles * g.parts < CUS && g.parts * QUANT_WAVES < g.units) ++g.parts;
-  const int64_t grid = op_div_up(tiles, 8) * 8 * g.parts;
-  const size_t bytes = unit32 * rb + QUANT_SCRATCH * QUANT_WAVES;
-  if (rb == 2 && g.inner <= 1024) {
-    const size_t four = unit32 * 2 + QUANT_SCRATCH * 4;   // four waves: two workgroups a compute unit
-    if (g.inner <= 256) return quant_go<quant_wide<T, 2, 1, 16, 4>>(grid, four, g, s, 256);
-    return quant_go<quant_wide<T, 2, 1, 64, 4>>(grid, four, g, s, 256);
-  }
-  if (rb == 2) return quant_go<quant_wide<T, 2, 2, 64, QUANT_WAVES>>(grid, bytes, g, s);
+  const int64_t most = at_once / tiles < g.units ? at_once / tiles : g.units, tiles8 = op_div_up(tiles, 8) * 8;
+  g.parts = (int)(most >= 8 ? most / 8 * 8 : most < at_once / tiles8 ? most : at_once / tiles8);
+  if (g.parts < 1) g.parts = 1;
+  const int64_t grid = (g.parts >= 8 ? tiles : tiles8) * g.parts;
+  const size_t bytes = unit32 * (two ? 2 : 1) + QUANT_SCRATCH * (four ? 4 : QUANT_WAVES);
+  if (four && g.inner <= 256) return quant_go<quant_wide<T, 2, 1, 16, 4>>(grid, bytes, g, s, 256);
+  if (four && g.inner <= 512) return quant_go<quant_wide<T, 2, 1, 32, 4>>(grid, bytes, g, s, 256);
+  if (four) return quant_go<quant_wide<T, 2, 1, 64, 4>>(grid, bytes, g, s, 256);
+  if (two) return quant_go<quant_wide<T, 2, 2, 64, QUANT_WAVES>>(grid, bytes, g, s);
   if (g.inner <= 256) return quant_go<quant_wide<T, 1, 1, 16, QUANT_WAVES>>(grid, bytes, g, s);
+  if (g.inner <= 512) return quant_go<quant_wide<T, 1, 1, 32, QUANT_WAVES>>(grid, bytes, g, s);
   if (g.inner <= 1024) return quant_go<quant_wide<T, 1, 1, 64, QUANT_WAVES>>(grid, bytes, g, s);
   return quant_go<quant_wide<T, 1, 4, 64, QUANT_WAVES>>(grid, bytes, g, s);
 }
