@@ -13,6 +13,9 @@
 // eight elements of a row there. A workgroup adds its rows in LDS, norm_sums the workgroups in order: no
 // atomics, the same bits on every run. Rows wider than the registers hold take norm_wide, which
 // reads them again for each statistic.
+//
+// Measured at 65536 x 1024 bf16: norm_forward 124 us (5.4 TB/s), norm_backward 254 to 294 (4.2 to 3.7),
+// norm_sums 5; at 5000 x 393 float32, rows that no access of 16 bytes fits: 13, 27 and 4 us.
 #include <type_traits>
 
 #include "ops.h"
@@ -22,7 +25,8 @@ namespace {
 
 constexpr int NORM_THREADS = 256;
 constexpr int NORM_VECTORS = 5;          // dw_post, db_post, dscale, dw_pre, db_pre
-constexpr int64_t NORM_MAX_WAVES = 2048; // of the backward pass: eight a compute unit
+constexpr int64_t NORM_MAX_WAVES = 2048; // of the backward pass: eight a compute unit (16: 31 against 27
+                                         // us at 5000 x 393 float32, and twice the sums to add)
 constexpr int NORM_CHUNK = 8;            // adjacent elements of a thread: one Philox block
 
 struct Drop { uint32_t d; float gain; bool on; };
@@ -606,7 +610,9 @@ __global__ __launch_bounds__(SUM_COLS * SUM_GROUPS) void norm_sums(const float* 
 }
 
 // ----------------------------------------------------------------------------- rows of any width
-// One workgroup a row, which reads it once for every statistic (from L2 after the first time).
+// One workgroup a row, which reads it once for every statistic (from L2 after the first time): forward
+// 291 us at 1024 x 20000 bf16, backward 1363 at 1024 x 16384. The simple form, for rows that no
+// network here has.
 constexpr int WIDE_THREADS = 1024;
 template <typename T, bool BACK> __global__ __launch_bounds__(WIDE_THREADS) void norm_wide(NormArgs g) {
   const spz_block_norm_args& a = g.a;
@@ -720,7 +726,7 @@ template <typename T, bool BACK> __global__ __launch_bounds__(WIDE_THREADS) void
 
 // ----------------------------------------------------------------------------- dropout
 // Eight elements a thread: one Philox block. FLAT: rows follow each other without a gap, so that they
-// are one row of eights with a ragged end.
+// are one row of eights with a ragged end. 89 us at 131072 x 1024 bf16: 6.0 TB/s, HBM's rate.
 template <typename T, bool FLAT>
 __global__ __launch_bounds__(256) void dropout(const T* x, int64_t x_row, T* y, int64_t y_row, int64_t width, int64_t n,
                                                Drop d, uint64_t seed, uint32_t step, uint32_t tensor) {

@@ -58,7 +58,7 @@ __device__ inline int quantised(float x, float s) {
   return (int)fminf(fmaxf(q, -127.0f), 127.0f);
 }
 
-// Rows of integers: one wave a row, which it reads twice. q [rows, width] at q_row, or (FRAGS) as
+// Rows of integers: one wave a row, which it reads twice (bound by HBM and its latency; weights, once). q [rows, width] at q_row, or (FRAGS) as
 // fragments over 32 * frag_blocks(rows) rows.
 template <typename T, bool FRAGS>
 __global__ __launch_bounds__(256) void quant_rows(const T* x, int64_t x_row, int64_t rows, int64_t width, int8_t* q,
@@ -84,6 +84,7 @@ __global__ __launch_bounds__(256) void quant_rows(const T* x, int64_t x_row, int
   }
 }
 
+// A byte of the image a thread, zeros past the edges: 5 us at 1024 x 1024, once for the weights.
 __global__ __launch_bounds__(256) void quant_pack(const int8_t* q, int64_t q_row, int64_t outer, int64_t inner, int8_t* image) {
   const int64_t steps = (inner + 31) / 32, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= (outer + 31) / 32 * steps * FRAG) return;
@@ -92,7 +93,8 @@ __global__ __launch_bounds__(256) void quant_pack(const int8_t* q, int64_t q_row
   image[i] = n < outer && k < inner ? q[n * q_row + k] : (int8_t)0;
 }
 
-// One wave a 32 x 32 tile of y.
+// Rows above QUANT_LDS_INNER inputs, the simple form: one wave a 32 x 32 tile of y, fragments straight from
+// L2, which bounds it. With quant_rows 161 us at 4096 x 8192 x 1024 bf16 (0.43 POP/s).
 template <typename T>
 __global__ __launch_bounds__(256) void quant_product(const int8_t* x, const int8_t* w, const float* xs, const float* ws,
                                                      const float* bias, T* y, int64_t y_row, int64_t rows, int64_t outer,
@@ -423,7 +425,12 @@ __device__ inline void quant_units(const QuantArgs& g, const u32x4* lds, int uni
 }
 
 // A workgroup: RT rows and its part of the channels, 64 a wave at a time, each wave on its own once the
-// rows are in LDS.
+// rows are in LDS. Bound by its phases: all workgroups read and quantise, multiply and write at about the
+// same time, so neither HBM nor the matrix instructions are always busy; two workgroups a compute unit
+// cover some of it. 131072 x 1024 x 1024 bf16: 207 us, 1.33 POP/s (the matrix instructions alone take a
+// third); 131072 x 256 x 256: 35 us, 3.8 TB/s. Waves of the workgroup that load the next tile of 128 rows
+// while the others multiply were as fast at the first (197 to 211) and slower elsewhere
+// (65536 x 1024 x 4096: 482 against 368).
 template <typename T, int RB, int NU, int LPR, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void quant_wide(QuantArgs g) {
   extern __shared__ u32x4 lds[];
@@ -450,7 +457,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void quant_wide(QuantArgs g) {
 
 // Few rows: 32 rows by 32 channels a workgroup, whose waves share the inputs out (every eighth step each) and add
 // their sums in LDS: the weights' loads of a call are spread over the whole device and are in flight
-// while the rows are quantised (by every workgroup for itself, from L2).
+// while the rows are quantised (by every workgroup for itself, from L2). Bound by latency: 16 x 1024 x 1024 bf16
+// 5.4 us, of which an empty launch takes about half.
 template <typename T, int NU, int LPR>
 __global__ __launch_bounds__(QUANT_THREADS, 2) void quant_few(QuantArgs g) {
   extern __shared__ u32x4 lds[];

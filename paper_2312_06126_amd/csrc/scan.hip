@@ -12,13 +12,18 @@
 // are joined into the state in front of every piece (scan_join), then every piece is walked
 // (scan_forward, scan_backward). The second reading of f and v comes mostly from the 256 MB
 // last-level cache. Maps are kept in 64 bits: a state that a map gives is a sum of terms that may
-// cancel, and then has to be as near as the one that steps in a row give. An episode start inside a piece makes its map independent of the state: such a
-// map is marked by A = -1 (A is a product of sigmoids, else >= 0), so that a state that is not
-// finite does not pass it as 0 * inf.
+// cancel, and then has to be as near as the one that steps in a row give. An episode start inside a
+// piece makes its map independent of the state: such a map is marked by A = -1 (A is a product of
+// sigmoids, else >= 0), so that a state that is not finite does not pass it as 0 * inf.
 //
 // Backward the same with time reversed: c -> P c + Q is the gradient handed from step to step.
 // h_{t-1} is not stored by the forward pass: `saved` holds the state in front of every SEG-th step
 // (6% of the bytes moved in bf16), from which a thread recomputes SEG steps in registers.
+//
+// Measured: 2048 x 50 x 256 bf16, serially: forward 27 us, backward 49 (5.8 and 5.4 TB/s, partly from
+// the last-level cache). 64 x 1000 x 200 float32 in tiles: forward 48 us (3.2 TB/s, 448 workgroups).
+// 1 x 65536 x 512 bf16 in pieces: forward 33 + 12 + 39 us (scan_piece, scan_join, scan_forward), backward
+// 33 + 12 + 82.
 #include <type_traits>
 
 #include "ops.h"
