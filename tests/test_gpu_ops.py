@@ -519,6 +519,32 @@ def test_quant_refuses():
         assert e.value.code == SPZ_EINVAL
 
 
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("shape", [(129, 500, 1100), (256, 260, 1024), (257, 260, 1024), (96, 700, 4000), (300, 500, 1100), (270, 200, 1500),
+                                   (300, 4096, 4001), (3000, 1025, 2100), (3000, 2048, 1500), (8200, 1000, 2000), (16400, 300, 100),
+                                   (16400, 100, 130), (16400, 1700, 65), (20000, 1024, 130), (300, 5000, 200)], ids=str)
+def test_quant_ways(shape, prec):
+    """Each way of spreading a product, at shares that do not divide, against exact sums. Rounded to 24 bits: the
+    sum, the product of the scales, the result; then once to the output's bits."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    M, K, N = shape
+    rng = np.random.default_rng(31)
+    x = gpu(rng.standard_normal((M, K)).astype(np.float32), prec)
+    q, s = ops.quant_rows(x)
+    wq, ws = ops.quant_rows(gpu(rng.standard_normal((N, K)).astype(np.float32)))
+    bias = gpu(rng.standard_normal(N).astype(np.float32))
+    room = torch.full((M + 2, N + 3), 7.0, dtype=x.dtype, device="cuda")
+    y = room[1:M + 1, 1:N + 1]
+    ops.quant_linear(x, ops.quant_pack(wq, ws), bias=bias, out=y)
+    product = (q.double() @ wq.double().t().contiguous()) * s.double()[:, None] * ws.double()
+    want = product + bias.double()
+    bound = 2.0 ** -22 * (product.abs() + want.abs()) + (2.0 ** -8 if prec == "bf16" else 2.0 ** -24) * 1.01 * want.abs() + 1e-37
+    assert bool(((y.double() - want).abs() <= bound).all())
+    y.fill_(7.0)
+    assert bool((room == 7.0).all())
+
+
 # ----------------------------------------------------------------------------- across the operators
 
 def test_offsets_past_32_bits():
