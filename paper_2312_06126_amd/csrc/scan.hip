@@ -22,8 +22,8 @@
 //
 // Measured: 2048 x 50 x 256 bf16, serially: forward 27 us, backward 49 (5.8 and 5.4 TB/s, partly from
 // the last-level cache). 64 x 1000 x 200 float32 in tiles: forward 48 us (3.2 TB/s, 448 workgroups).
-// 1 x 65536 x 512 bf16 in pieces: forward 33 + 12 + 39 us (scan_piece, scan_join, scan_forward), backward
-// 33 + 12 + 82.
+// 1 x 65536 x 512 bf16 in pieces: forward 33 + 10 + 39 us (scan_piece, scan_join, scan_forward), backward
+// 33 + 10 + 82.
 #include <type_traits>
 
 #include "ops.h"
@@ -245,7 +245,9 @@ __device__ inline double apply_map(double A, double H, double h) { return A == -
 
 // map_h[p] <- the state in front of piece p (backward: behind it), from the maps and the first
 // state (`first`, NULL: zeros). 8 channels a workgroup; 128 groups of threads each join a range of
-// pieces, the ranges' maps are joined by doubling, then each range is walked from its first state.
+// pieces, the ranges' maps are joined by doubling, then each range is walked from its first state. Bound by
+// latency: 1024 pieces of 512 channels 10 us, with ranges of up to U kept in registers (12 when read again;
+// 4 or 2 channels a workgroup: 15, 16).
 __global__ __launch_bounds__(JOIN_CH * JOIN_GROUPS) void scan_join(const double* map_a, double* map_h, const float* first,
                                                                    int64_t channels, int64_t pieces, bool back) {
   __shared__ double sa[JOIN_GROUPS][JOIN_CH], sh[JOIN_GROUPS][JOIN_CH];
@@ -256,21 +258,25 @@ __global__ __launch_bounds__(JOIN_CH * JOIN_GROUPS) void scan_join(const double*
   const int64_t p0 = gr * per < pieces ? gr * per : pieces, p1 = on ? (p0 + per < pieces ? p0 + per : pieces) : p0;
   const auto at = [&](int64_t p) { return (back ? pieces - 1 - p : p) * channels + ch; };
   constexpr int U = 8;   // maps loaded at once
-  double A = 1.0, H = 0.0;
-  for (int64_t p = p0; p < p1; p += U) {
-    double ma[U], mh[U];
+  double ma[U], mh[U];
+  const auto load = [&](int64_t p) {
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int64_t o = at(p + j < p1 ? p + j : p1 - 1);
       ma[j] = map_a[o];
       mh[j] = map_h[o];
     }
+  };
+  double A = 1.0, H = 0.0;
+  for (int64_t p = p0; p < p1; p += U) {
+    load(p);
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       if (p + j >= p1) continue;
-      join_maps(A, H, ma[j], mh[j]);
-      A = ma[j];
-      H = mh[j];
+      double A2 = ma[j], H2 = mh[j];
+      join_maps(A, H, A2, H2);
+      A = A2;
+      H = H2;
     }
   }
   for (int d = 1; d < JOIN_GROUPS; d *= 2) {
@@ -287,13 +293,7 @@ __global__ __launch_bounds__(JOIN_CH * JOIN_GROUPS) void scan_join(const double*
   double h = first ? first[ch] : 0.0;
   if (gr) h = apply_map(sa[gr - 1][c], sh[gr - 1][c], h);
   for (int64_t p = p0; p < p1; p += U) {
-    double ma[U], mh[U];
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int64_t o = at(p + j < p1 ? p + j : p1 - 1);
-      ma[j] = map_a[o];
-      mh[j] = map_h[o];
-    }
+    if (per > U) load(p);
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       if (p + j >= p1) continue;
