@@ -21,7 +21,7 @@
 // (6% of the bytes moved in bf16), from which a thread recomputes SEG steps in registers.
 //
 // Measured: 2048 x 50 x 256 bf16, serially: forward 27 us, backward 49 (5.8 and 5.4 TB/s, partly from
-// the last-level cache). 64 x 1000 x 200 float32 in tiles: forward 48 us (3.2 TB/s, 448 workgroups).
+// the last-level cache). 64 x 1000 x 200 float32 in tiles: forward 39 us (3.9 TB/s).
 // 1 x 65536 x 512 bf16 in pieces: forward 33 + 10 + 39 us (scan_piece, scan_join, scan_forward), backward
 // 33 + 10 + 82.
 #include <type_traits>
@@ -445,6 +445,10 @@ template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS, 2) void 
 // launch. Order position (wave, time lane) runs with time, backward against it.
 constexpr int TILE_THREADS = 256, TILE_WAVES = TILE_THREADS / 64;
 
+// Workgroup b runs on XCD b % 8: neighbours in width, whose 128 bytes a step share cache lines where rows
+// are not whole lines, on the same one (64 x 1000 x 200 float32: 39 against 48 us).
+__device__ inline int64_t tile_block() { return blockIdx.x % 8 * (int64_t)(gridDim.x / 8) + blockIdx.x / 8; }
+
 template <int V, int CL, bool BACK> struct Tile {
   static constexpr int TL = 64 / CL, LANES = TILE_WAVES * TL;
   double (*maps)[TILE_WAVES][CL][2 * V];   // [2]: the waves' maps, two buffers in turn
@@ -488,8 +492,9 @@ template <typename T, int V, int CL> __global__ __launch_bounds__(TILE_THREADS, 
   using Ti = Tile<V, CL, false>;
   __shared__ double maps[2][TILE_WAVES][CL][2 * V];
   Ti tile{maps, (int)threadIdx.x / 64, (int)threadIdx.x % 64 / CL, (int)threadIdx.x % CL};
-  const int64_t groups = (g.chunks + CL - 1) / CL, b = blockIdx.x / groups;
-  const int64_t chunk = blockIdx.x % groups * CL + tile.cl, c = chunk * V;
+  const int64_t groups = (g.chunks + CL - 1) / CL, at = tile_block(), b = at / groups;
+  const int64_t chunk = at % groups * CL + tile.cl, c = chunk * V;
+  if (b >= a.batch) return;
   const bool on = chunk < g.chunks, vec = a.width % 4 == 0;
   const int64_t n = scan_length(a, b), saves = (a.steps + SEG - 1) / SEG, st = b * a.width + c;
   const T* const p[2] = {static_cast<const T*>(a.f) + b * a.f_batch + c, static_cast<const T*>(a.v) + b * a.v_batch + c};
@@ -560,8 +565,9 @@ template <typename T, int V, int CL> __global__ __launch_bounds__(TILE_THREADS, 
   using Ti = Tile<V, CL, true>;
   __shared__ double maps[2][TILE_WAVES][CL][2 * V];
   Ti tile{maps, (int)threadIdx.x / 64, (int)threadIdx.x % 64 / CL, (int)threadIdx.x % CL};
-  const int64_t groups = (g.chunks + CL - 1) / CL, b = blockIdx.x / groups;
-  const int64_t chunk = blockIdx.x % groups * CL + tile.cl, c0 = chunk * V;
+  const int64_t groups = (g.chunks + CL - 1) / CL, at = tile_block(), b = at / groups;
+  const int64_t chunk = at % groups * CL + tile.cl, c0 = chunk * V;
+  if (b >= a.batch) return;
   const bool on = chunk < g.chunks, vec = a.width % 4 == 0;
   const int64_t n = scan_length(a, b), st = b * a.width + c0;
   const T* const p[3] = {static_cast<const T*>(a.f) + b * a.f_batch + c0, static_cast<const T*>(a.v) + b * a.v_batch + c0,
@@ -717,7 +723,7 @@ template <typename T, int V, bool BACK> void scan_launch(const ScanArgs& g, Scan
   if (way == SCAN_TILED) {
     const auto tiles = [&](auto lanes) {
       constexpr int CL = decltype(lanes)::value;
-      const dim3 grid((unsigned)(g.a.batch * op_div_up(g.chunks, CL)));
+      const dim3 grid((unsigned)(op_div_up(g.a.batch * op_div_up(g.chunks, CL), 8) * 8));
       if constexpr (BACK) scan_tile_backward<T, V, CL><<<grid, TILE_THREADS, 0, s>>>(g);
       else scan_tile_forward<T, V, CL><<<grid, TILE_THREADS, 0, s>>>(g);
     };
