@@ -343,7 +343,7 @@ def _quant_sizes(prec: int, rows: int, outer: int, inner: int):
 
 
 def quant_rows(x, *, stream=None):
-    """x [rows, width] -> (q, scale): int8 q = x / scale rounded, scale = max |x| / 127 a row."""
+    """x [rows, width] -> (q, scale): int8 q = x / scale rounded, scale = max |x| * float32(1 / 127) a row."""
     lib = load()
     gpu = _operand(x, "x", 2)
 

@@ -177,10 +177,10 @@ def block_norm(x, h=None, z=None, w_post=None, b_post=None, scale=None, w_pre=No
 
 
 def quant_rows(x):
-    """float32 rows -> (q, scale): the scale is a float32 number; the quotient rounds to float32
-    before it rounds to an integer, as the operator states it."""
+    """float32 rows -> (q, scale): the scale is a float32 number, the largest magnitude times the float32
+    next to 1 / 127; the quotient rounds to float32 before it rounds to an integer, as the operator states it."""
     m = np.abs(x).max(1) if x.shape[1] else np.zeros(len(x), np.float32)
-    s = (m.astype(np.float32) / np.float32(127.0)).astype(np.float32)
+    s = (m.astype(np.float32) * (np.float32(1.0) / np.float32(127.0))).astype(np.float32)
     q = np.zeros(x.shape)
     with np.errstate(all="ignore"):
         on = s > 0

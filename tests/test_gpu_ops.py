@@ -490,6 +490,20 @@ def test_quant_rows_values(prec):
     assert e.shape == (8, 0) and not f.any()
 
 
+def test_quant_rows_like_torch():
+    """The integers and scales of 20 million elements are those of the same formula in torch on the GPU."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    x = torch.randn((100000, 200), generator=gen, device="cuda")
+    q, s = ops.quant_rows(x)
+    want = x.abs().amax(1) / 127.0
+    assert torch.equal(s, want) and torch.equal(q.float(), torch.round(x / want[:, None]))
+    w = ops.quant_pack(torch.eye(200, dtype=torch.int8, device="cuda"), torch.ones(200, device="cuda"))
+    assert torch.equal(ops.quant_linear(x, w), torch.round(x / want[:, None]) * want[:, None])
+
+
 def test_quant_largest_sums_and_empty_inner():
     """Sums of the greatest length stay exact in 32 bits; no inputs leave the bias."""
     from paper_2312_06126_amd import ops
