@@ -33,6 +33,15 @@ inline bool op_out_strides_ok(int64_t n0, int64_t n1, int64_t width, int64_t s0,
 
 inline int64_t op_div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// launch(first, grid) over `blocks` workgroups of `threads`, as many dispatches as it takes. A dispatch counts its
+// work-items in 32 bits: of a grid with more of them only a part runs, and no call reports it.
+constexpr int64_t OP_DISPATCH = (int64_t)1 << 31;
+template <typename F> void op_dispatch(int64_t blocks, int64_t threads, F&& launch) {
+  const int64_t most = OP_DISPATCH / threads;
+  for (int64_t first = 0; first < blocks; first += most)
+    launch(first, dim3((unsigned)(blocks - first < most ? blocks - first : most)));
+}
+
 inline int op_launched(const char* call) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SPZ_OK : op_error(SPZ_EHIP, call, hipGetErrorString(e));

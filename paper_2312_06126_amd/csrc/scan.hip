@@ -40,6 +40,7 @@ constexpr int JOIN_CH = 8, JOIN_GROUPS = 128;
 struct ScanArgs {
   spz_scan_args a;
   int64_t chunks;       // of V channels
+  int64_t first;        // workgroup of the call that the dispatch starts with (scan_pos)
   int64_t pieces, len;  // time pieces and their steps (a multiple of SEG)
   double *map_a, *map_h; // [pieces, batch, width]: maps; map_h then the states between the pieces
 };
@@ -110,7 +111,7 @@ __device__ inline bool op_aligned16(const void* p) { return op_aligned(p, 16); }
 
 struct ScanPos { int64_t b, c, p; };
 template <int V> __device__ inline bool scan_pos(const ScanArgs& g, ScanPos& q) {
-  const int64_t i = (int64_t)blockIdx.x * SCAN_THREADS + threadIdx.x;
+  const int64_t i = (g.first + blockIdx.x) * SCAN_THREADS + threadIdx.x;
   if (i >= g.chunks * g.a.batch * g.pieces) return false;
   q.c = i % g.chunks * V;
   q.b = i / g.chunks % g.a.batch;
@@ -692,7 +693,7 @@ const char* scan_check(const spz_scan_args* a) {
   if (!a) return "NULL arguments";
   if (!op_prec_ok(a->prec)) return "unknown precision";
   if (!op_extent_ok(a->batch) || !op_extent_ok(a->steps) || !op_extent_ok(a->width)) return "extent out of range";
-  // Bounds every index and the grid.
+  // No device holds more; keeps every index and count within 62 bits.
   if (a->width && a->batch && a->batch > ((int64_t)1 << 38) / a->width) return "batch * width out of range";
   if (a->width && a->batch && a->steps > ((int64_t)1 << 44) / (a->batch * a->width)) return "extents out of range";
   return nullptr;
@@ -732,15 +733,20 @@ template <typename T, int V, bool BACK> void scan_launch(const ScanArgs& g, Scan
     else tiles(std::integral_constant<int, 32 / V>{});
     return;
   }
-  const dim3 grid((unsigned)op_div_up(g.chunks * g.a.batch * g.pieces, SCAN_THREADS));
-  if (way == SCAN_PIECES) {
+  const int64_t blocks = op_div_up(g.chunks * g.a.batch * g.pieces, SCAN_THREADS);
+  if (way == SCAN_PIECES) {   // SCAN_FILL threads or some more: one dispatch
+    const dim3 grid((unsigned)blocks);
     const int64_t channels = g.a.batch * g.a.width;
     scan_piece<T, V, BACK><<<grid, SCAN_THREADS, 0, s>>>(g);
     scan_join<<<dim3((unsigned)op_div_up(channels, JOIN_CH)), JOIN_CH * JOIN_GROUPS, 0, s>>>(
         g.map_a, g.map_h, BACK ? g.a.dhT : g.a.h0, channels, g.pieces, BACK);
   }
-  if constexpr (BACK) scan_backward<T, V><<<grid, SCAN_THREADS, 0, s>>>(g);
-  else scan_forward<T, V><<<grid, SCAN_THREADS, 0, s>>>(g);
+  op_dispatch(blocks, SCAN_THREADS, [&](int64_t first, dim3 grid) {
+    ScanArgs part = g;
+    part.first = first;
+    if constexpr (BACK) scan_backward<T, V><<<grid, SCAN_THREADS, 0, s>>>(part);
+    else scan_forward<T, V><<<grid, SCAN_THREADS, 0, s>>>(part);
+  });
 }
 
 template <typename T> void scan_dispatch(const ScanArgs& g, ScanWay way, bool back, bool vectors, hipStream_t s) {
@@ -782,8 +788,6 @@ int scan_run(const char* call, const spz_scan_args* args, bool back, void* ws, i
                   (back ? vec(a.dy, a.dy_batch, a.dy_step) && vec(a.df, a.df_batch, a.df_step) && vec(a.dv, a.dv_batch, a.dv_step)
                         : vec(a.y, a.y_batch, a.y_step));
   g.chunks = vectors ? a.width / v : a.width;
-  if (op_div_up(g.chunks * a.batch * g.pieces, SCAN_THREADS) >= OP_MAX_EXTENT)
-    return op_error(SPZ_EINVAL, call, "extents out of range");
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (a.prec == SPZ_PREC_BF16) scan_dispatch<bf16_t>(g, plan.way, back, vectors, s);
   else scan_dispatch<float>(g, plan.way, back, vectors, s);
