@@ -34,6 +34,7 @@ struct Drop { uint32_t d; float gain; bool on; };
 struct NormArgs {
   spz_block_norm_args a;
   Drop drop;
+  int64_t first;      // workgroup of the forward call that the dispatch starts with
   float* part;        // backward: [blocks, NORM_VECTORS, width]
   bool wants[NORM_VECTORS];
 };
@@ -291,12 +292,12 @@ template <int N> __device__ inline void gate_row(int kind, const float (&z)[N], 
   }
 }
 
-// The first row of a thread: uniform over its wave where the row fills one.
-template <int TPR> __device__ inline int64_t first_row() {
+// The first row of a thread in workgroup b: uniform over its wave where the row fills one.
+template <int TPR> __device__ inline int64_t first_row(int64_t b) {
   constexpr int GROUPS = TPR > 64 ? 1 : NORM_THREADS / TPR;
-  if constexpr (GROUPS == 1) return blockIdx.x;
+  if constexpr (GROUPS == 1) return b;
   const int sub = threadIdx.x / TPR;
-  return (int64_t)blockIdx.x * GROUPS + (TPR == 64 ? __builtin_amdgcn_readfirstlane(sub) : sub);
+  return b * GROUPS + (TPR == 64 ? __builtin_amdgcn_readfirstlane(sub) : sub);
 }
 
 // Workgroups: rows of more than a wave have one to themselves (its barriers are the row's).
@@ -315,7 +316,7 @@ __global__ __launch_bounds__(norm_threads<TPR>) void norm_forward(NormArgs g) {
   constexpr int N = M::N, GROUPS = norm_threads<TPR> / TPR;
   const spz_block_norm_args& a = g.a;
   const M m{threadIdx.x % TPR, (uint32_t)a.width};
-  const int64_t row = first_row<TPR>();
+  const int64_t row = first_row<TPR>(g.first + blockIdx.x);
   if (row >= a.rows) return;
   T* xo = a.h ? static_cast<T*>(a.x_out) + row * a.x_out_row : nullptr;
   T* u = a.pre != SPZ_NORM_NONE ? static_cast<T*>(a.u) + row * a.u_row : nullptr;
@@ -521,7 +522,7 @@ __global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g
   if constexpr (LEAN) {
     Rows r;
     clear(r);
-    for (int64_t row = first_row<TPR>(); row < a.rows; row += stride) {
+    for (int64_t row = first_row<TPR>(blockIdx.x); row < a.rows; row += stride) {
       load(row, r);
       take(row, r);
     }
@@ -530,7 +531,7 @@ __global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g
     Rows r0, r1;
     clear(r0);
     clear(r1);
-    int64_t row = first_row<TPR>();
+    int64_t row = first_row<TPR>(blockIdx.x);
     if (row < a.rows) load(row, r0);
     while (row < a.rows) {
       if (row + stride < a.rows) load(row + stride, r1);
@@ -580,12 +581,15 @@ __global__ __launch_bounds__(norm_threads<TPR>, 2) void norm_backward(NormArgs g
 // out[k][c] = sum over the workgroups b of part[b][k][c]: 32 threads a column take every 32nd each.
 struct SumArgs { float* out[NORM_VECTORS]; };
 constexpr int SUM_COLS = 32, SUM_GROUPS = 32;
-__global__ __launch_bounds__(SUM_COLS * SUM_GROUPS) void norm_sums(const float* part, SumArgs o, int64_t width, int blocks) {
+__global__ __launch_bounds__(SUM_COLS * SUM_GROUPS) void norm_sums(const float* part, SumArgs o, int64_t width, int blocks,
+                                                                   int64_t first) {
   __shared__ float s[SUM_GROUPS][SUM_COLS];
-  const int c = threadIdx.x % SUM_COLS, gr = threadIdx.x / SUM_COLS, k = blockIdx.x % NORM_VECTORS;
+  const int c = threadIdx.x % SUM_COLS, gr = threadIdx.x / SUM_COLS;
+  const int64_t block = first + blockIdx.x;
+  const int k = (int)(block % NORM_VECTORS);
   float* out = o.out[k];
   if (!out) return;
-  const int64_t col = (int64_t)(blockIdx.x / NORM_VECTORS) * SUM_COLS + c;
+  const int64_t col = block / NORM_VECTORS * SUM_COLS + c;
   float x = 0.0f;
   if (col < width) {
     const float* p = part + k * width + col;
@@ -795,7 +799,11 @@ template <typename T, bool EVEN> void norm_dispatch(const NormArgs& g, bool back
       }
     }
     if constexpr ((K > 1 && TPR != 512) || TPR <= 64)
-      norm_forward<T, EVEN, TPR, K><<<dim3((unsigned)op_div_up(g.a.rows, norm_threads<TPR> / TPR)), norm_threads<TPR>, 0, s>>>(g);
+      op_dispatch(op_div_up(g.a.rows, norm_threads<TPR> / TPR), norm_threads<TPR>, [&](int64_t first, dim3 grid) {
+        NormArgs part = g;
+        part.first = first;
+        norm_forward<T, EVEN, TPR, K><<<grid, norm_threads<TPR>, 0, s>>>(part);
+      });
   };
   using std::integral_constant;
   const auto is = [&](int tpr, int k) { return way.tpr == tpr && way.k == k; };
@@ -892,8 +900,9 @@ int norm_run(const char* call, const spz_block_norm_args* args, bool back, void*
   }
   if (back) {
     if (a.dw_post || a.db_post || a.dscale || a.dw_pre || a.db_pre)
-      norm_sums<<<dim3((unsigned)(op_div_up(a.width, SUM_COLS) * NORM_VECTORS)), SUM_COLS * SUM_GROUPS, 0, s>>>(
-          g.part, o, a.width, (int)blocks);
+      op_dispatch(op_div_up(a.width, SUM_COLS) * NORM_VECTORS, SUM_COLS * SUM_GROUPS, [&](int64_t first, dim3 grid) {
+        norm_sums<<<grid, SUM_COLS * SUM_GROUPS, 0, s>>>(g.part, o, a.width, (int)blocks, first);
+      });
   }
   return op_launched(call);
 }

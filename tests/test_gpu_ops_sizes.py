@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from .helpers import log
-from .test_gpu_ops import gpu, torch_
+from .test_gpu_ops import gpu, host, torch_
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,54 @@ def test_scan_of_many_states():
     got, want = ops.scan_backward(t["f"], t["v"], t["dy"], saved), ops.scan_backward(one["f"], one["v"], one["dy"], saved1)
     for g, w in zip(got, want):
         assert all_equal(g.reshape(B, D), w.reshape(D), 1 << 20)
+
+
+def philox_tail(first, count, step, tensor, seed):
+    """Dropout's 16-bit words of elements first .. first + count - 1 (multiples of 8)."""
+    from oracle import philox
+    u = np.uint64
+    blk = np.arange(first // 8, (first + count) // 8, dtype=np.uint64)
+    w = np.stack(philox.block(blk, u(step), u(5) + ((blk >> u(32)) << u(8)), u(tensor), u(seed), u(0)), 1)
+    return np.stack([w & u(0xFFFF), w >> u(16)], 2).reshape(-1)
+
+
+def test_block_norm_of_many_rows():
+    """2^28 rows, 16 of them a workgroup; dropout counts elements over all rows."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    R, D = (1 << 28) + 24, 2
+    log("block_norm %d x %d" % (R, D))
+    x = torch.empty((R, D), dtype=torch.bfloat16, device="cuda").uniform_(-1, 1)
+    x_out, u = ops.block_norm(x, x, pre="layer")
+    for part in (slice(0, 1 << 20), slice(R // 2, R // 2 + 4099), slice((1 << 28) - 4096, R)):
+        a, b = ops.block_norm(x[part], x[part], pre="layer")
+        assert torch.equal(x_out[part], a) and torch.equal(u[part], b)
+    del x_out, u
+    zero, one = (torch.full((1, D), c, dtype=torch.bfloat16, device="cuda").expand(R, D) for c in (0.0, 1.0))
+    x_out, _ = ops.block_norm(zero, one, post="none", pre="none", drop=(0.25, 11, 12, 13))
+    n = 4096
+    assert np.array_equal(host(x_out[-n // D:]).reshape(-1) != 0, philox_tail(R * D - n, n, 12, 13, 11) >= 16384)
+
+
+def test_block_norm_of_many_rows_of_a_wave():
+    """2^26 rows of a wave each."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    R, D = (1 << 26) + 5, 264
+    log("block_norm %d x %d" % (R, D))
+    x = gpu(np.random.default_rng(52).standard_normal((1, D)), "bf16")
+    _, u = ops.block_norm(x.expand(R, D))
+    assert all_equal(u, ops.block_norm(x)[1][0], 1 << 22)
+
+
+def test_block_norm_gradients_of_many_columns():
+    """The vectors' gradients of more columns than one dispatch sums. Sums of small integers are exact."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    R, D = 2, (1 << 25) + 7
+    log("block_norm backward %d x %d" % (R, D))
+    x = torch.empty((R, D), dtype=torch.bfloat16, device="cuda").uniform_(-1, 1)
+    du = torch.randint(-4, 5, (R, D), device="cuda").bfloat16()
+    zero = torch.zeros(D, device="cuda")
+    g = ops.block_norm_backward(None, du, x, b_pre=zero)
+    assert torch.equal(g["db_pre"], du.float().sum(0))
