@@ -733,9 +733,9 @@ template <typename T, bool BACK> __global__ __launch_bounds__(WIDE_THREADS) void
 // are one row of eights with a ragged end. 89 us at 131072 x 1024 bf16: 6.0 TB/s, HBM's rate.
 template <typename T, bool FLAT>
 __global__ __launch_bounds__(256) void dropout(const T* x, int64_t x_row, T* y, int64_t y_row, int64_t width, int64_t n,
-                                               Drop d, uint64_t seed, uint32_t step, uint32_t tensor) {
+                                               Drop d, uint64_t seed, uint32_t step, uint32_t tensor, int64_t first) {
   constexpr int VW = OP_VEC<T>;
-  const int64_t blk = (int64_t)blockIdx.x * 256 + threadIdx.x, i0 = blk * 8;
+  const int64_t blk = (first + blockIdx.x) * 256 + threadIdx.x, i0 = blk * 8;
   if (i0 >= n) return;
   if (FLAT && i0 + 8 <= n) {
     float v[8 / VW][VW];
@@ -944,11 +944,12 @@ int spz_dropout(int32_t prec, int64_t rows, int64_t width, const void* x, int64_
   if (n == 0) return SPZ_OK;
   const Drop d{drop_threshold(p), drop_gain(drop_threshold(p)), true};
   const bool flat = rows == 1 || (x_row == width && y_row == width);
-  const dim3 grid((unsigned)op_div_up(op_div_up(n, 8), 256));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const auto go = [&](auto kernel, auto tag) {
     using T = decltype(tag);
-    kernel<<<grid, 256, 0, s>>>(static_cast<const T*>(x), x_row, static_cast<T*>(y), y_row, width, n, d, seed, step, tensor);
+    op_dispatch(op_div_up(op_div_up(n, 8), 256), 256, [&](int64_t first, dim3 grid) {
+      kernel<<<grid, 256, 0, s>>>(static_cast<const T*>(x), x_row, static_cast<T*>(y), y_row, width, n, d, seed, step, tensor, first);
+    });
   };
   if (prec == SPZ_PREC_BF16) {
     if (flat) go(dropout<bf16_t, true>, bf16_t{});

@@ -88,3 +88,25 @@ def test_block_norm_gradients_of_many_columns():
     zero = torch.zeros(D, device="cuda")
     g = ops.block_norm_backward(None, du, x, b_pre=zero)
     assert torch.equal(g["db_pre"], du.float().sum(0))
+
+
+def test_dropout_of_many_elements():
+    """2^35 elements, in place: the words of the last ones are those of their 64-bit index."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    R, D, n = (1 << 15) + 1, 1 << 20, 4096
+    log("dropout %d x %d" % (R, D))
+    x = torch.ones((R, D), dtype=torch.bfloat16, device="cuda")
+    ops.dropout(x, 0.25, 11, 12, 13, out=x)
+    assert np.array_equal(host(x[-1, -n:]) != 0, philox_tail(R * D - n, n, 12, 13, 11) >= 16384)
+    assert np.array_equal(host(x[0, :n]) != 0, philox_tail(0, n, 12, 13, 11) >= 16384)
+
+
+def test_dropout_of_many_elements_of_rows_apart():
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    R, D, n = (1 << 15) + 1, 1 << 20, 4096
+    log("dropout %d x %d, rows apart" % (R, D))
+    x = torch.ones((1, D), dtype=torch.bfloat16, device="cuda").expand(R, D)
+    y = ops.dropout(x, 0.25, 11, 12, 13)
+    assert np.array_equal(host(y[-1, -n:]) != 0, philox_tail(R * D - n, n, 12, 13, 11) >= 16384)
