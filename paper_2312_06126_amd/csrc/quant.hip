@@ -67,8 +67,8 @@ __device__ inline int quantised(float x, float s) {
 // fragments over 32 * frag_blocks(rows) rows.
 template <typename T, bool FRAGS>
 __global__ __launch_bounds__(256) void quant_rows(const T* x, int64_t x_row, int64_t rows, int64_t width, int8_t* q,
-                                                  int64_t q_row, float* scale) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+                                                  int64_t q_row, float* scale, int64_t first) {
+  const int64_t row = (first + blockIdx.x) * 4 + threadIdx.x / 64;
   const int lane = threadIdx.x % 64;
   const int64_t steps = (width + 31) / 32;
   if (row >= (FRAGS ? (rows + 31) / 32 * 32 : rows)) return;
@@ -90,8 +90,9 @@ __global__ __launch_bounds__(256) void quant_rows(const T* x, int64_t x_row, int
 }
 
 // A byte of the image a thread, zeros past the edges: 5 us at 1024 x 1024, once for the weights.
-__global__ __launch_bounds__(256) void quant_pack(const int8_t* q, int64_t q_row, int64_t outer, int64_t inner, int8_t* image) {
-  const int64_t steps = (inner + 31) / 32, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void quant_pack(const int8_t* q, int64_t q_row, int64_t outer, int64_t inner, int8_t* image,
+                                                  int64_t first) {
+  const int64_t steps = (inner + 31) / 32, i = (first + blockIdx.x) * 256 + threadIdx.x;
   if (i >= (outer + 31) / 32 * steps * FRAG) return;
   const int64_t frag = i / FRAG, lane = i % FRAG / 16;
   const int64_t n = frag / steps * 32 + lane % 32, k = frag % steps * 32 + lane / 32 * 16 + i % 16;
@@ -103,8 +104,8 @@ __global__ __launch_bounds__(256) void quant_pack(const int8_t* q, int64_t q_row
 template <typename T>
 __global__ __launch_bounds__(256) void quant_product(const int8_t* x, const int8_t* w, const float* xs, const float* ws,
                                                      const float* bias, T* y, int64_t y_row, int64_t rows, int64_t outer,
-                                                     int64_t steps) {
-  const int64_t nb = (outer + 31) / 32, tile = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+                                                     int64_t steps, int64_t first) {
+  const int64_t nb = (outer + 31) / 32, tile = (first + blockIdx.x) * 4 + threadIdx.x / 64;
   if (tile >= (rows + 31) / 32 * nb) return;
   const int lane = threadIdx.x % 64;
   const i32x4* a = reinterpret_cast<const i32x4*>(x) + tile / nb * steps * 64 + lane;
@@ -593,17 +594,30 @@ hipError_t quant_launch(int64_t rows, int64_t outer, int64_t inner, const void* 
   const int64_t mb = frag_blocks(rows), nb = frag_blocks(outer), steps = frag_blocks(inner);
   if (quant_in_lds(inner)) {
     QuantArgs g{};
-    g.x = x; g.x_row = x_row;
+    g.x_row = x_row;
     g.image = static_cast<const int8_t*>(image); g.w_scale = w_scale; g.bias = bias;
-    g.y = y; g.y_row = y_row;
-    g.rows = rows; g.outer = outer; g.inner = (int)inner; g.steps = (int)steps;
-    return quant_launch_lds<T>(g, s);
+    g.y_row = y_row;
+    g.outer = outer; g.inner = (int)inner; g.steps = (int)steps;
+    // A part of the rows at a time, such that its workgroups (512 threads for 32 rows at most) are one dispatch.
+    constexpr int64_t PART = OP_DISPATCH / 512 * 32;
+    hipError_t e = hipSuccess;
+    for (int64_t r = 0; r < rows && e == hipSuccess; r += PART) {
+      g.x = static_cast<const T*>(x) + r * x_row;
+      g.y = static_cast<T*>(y) + r * y_row;
+      g.rows = rows - r < PART ? rows - r : PART;
+      e = quant_launch_lds<T>(g, s);
+    }
+    return e;
   }
   int8_t* q = static_cast<int8_t*>(ws);
   float* xs = reinterpret_cast<float*>(q + mb * steps * FRAG);
-  quant_rows<T, true><<<dim3((unsigned)op_div_up(mb * 32, 4)), 256, 0, s>>>(static_cast<const T*>(x), x_row, rows, inner, q, 0, xs);
-  quant_product<T><<<dim3((unsigned)op_div_up(mb * nb, 4)), 256, 0, s>>>(q, static_cast<const int8_t*>(image), xs, w_scale, bias,
-                                                                       static_cast<T*>(y), y_row, rows, outer, steps);
+  op_dispatch(op_div_up(mb * 32, 4), 256, [&](int64_t first, dim3 grid) {
+    quant_rows<T, true><<<grid, 256, 0, s>>>(static_cast<const T*>(x), x_row, rows, inner, q, 0, xs, first);
+  });
+  op_dispatch(op_div_up(mb * nb, 4), 256, [&](int64_t first, dim3 grid) {
+    quant_product<T><<<grid, 256, 0, s>>>(q, static_cast<const int8_t*>(image), xs, w_scale, bias, static_cast<T*>(y), y_row, rows,
+                                          outer, steps, first);
+  });
   return hipGetLastError();
 }
 
@@ -625,12 +639,13 @@ int spz_quant_rows(int32_t prec, int64_t rows, int64_t width, const void* x, int
   if (!op_in_stride_ok(x_row)) return op_error(SPZ_EINVAL, call, "input stride out of range");
   if (!op_out_stride_ok(rows, width, q_row)) return op_error(SPZ_EINVAL, call, "rows of q overlap");
   if (rows == 0) return SPZ_OK;
-  const dim3 grid((unsigned)op_div_up(rows, 4));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (prec == SPZ_PREC_BF16)
-    quant_rows<bf16_t, false><<<grid, 256, 0, s>>>(static_cast<const bf16_t*>(x), x_row, rows, width, q, q_row, scale);
-  else
-    quant_rows<float, false><<<grid, 256, 0, s>>>(static_cast<const float*>(x), x_row, rows, width, q, q_row, scale);
+  op_dispatch(op_div_up(rows, 4), 256, [&](int64_t first, dim3 grid) {
+    if (prec == SPZ_PREC_BF16)
+      quant_rows<bf16_t, false><<<grid, 256, 0, s>>>(static_cast<const bf16_t*>(x), x_row, rows, width, q, q_row, scale, first);
+    else
+      quant_rows<float, false><<<grid, 256, 0, s>>>(static_cast<const float*>(x), x_row, rows, width, q, q_row, scale, first);
+  });
   return op_launched(call);
 }
 
@@ -648,10 +663,10 @@ int spz_quant_pack(int64_t outer, int64_t inner, const int8_t* q, int64_t q_row,
   if (bytes > 0 && (!q || !image)) return op_error(SPZ_EINVAL, call, "NULL array");
   if (!op_aligned(image, 16)) return op_error(SPZ_EINVAL, call, "image not aligned to 16 bytes");
   if (!op_in_stride_ok(q_row)) return op_error(SPZ_EINVAL, call, "input stride out of range");
-  if (bytes / 256 >= OP_MAX_EXTENT) return op_error(SPZ_EINVAL, call, "extents out of range");
   if (bytes == 0) return SPZ_OK;
-  quant_pack<<<dim3((unsigned)op_div_up(bytes, 256)), 256, 0, static_cast<hipStream_t>(hip_stream)>>>(
-      q, q_row, outer, inner, static_cast<int8_t*>(image));
+  op_dispatch(op_div_up(bytes, 256), 256, [&](int64_t first, dim3 grid) {
+    quant_pack<<<grid, 256, 0, static_cast<hipStream_t>(hip_stream)>>>(q, q_row, outer, inner, static_cast<int8_t*>(image), first);
+  });
   return op_launched(call);
 }
 

@@ -110,3 +110,56 @@ def test_dropout_of_many_elements_of_rows_apart():
     x = torch.ones((1, D), dtype=torch.bfloat16, device="cuda").expand(R, D)
     y = ops.dropout(x, 0.25, 11, 12, 13)
     assert np.array_equal(host(y[-1, -n:]) != 0, philox_tail(R * D - n, n, 12, 13, 11) >= 16384)
+
+
+def test_quant_rows_of_many_rows():
+    """2^26 rows, a wave each."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    R, D = (1 << 26) + 5, 3
+    log("quant_rows %d x %d" % (R, D))
+    x = torch.empty((R, D), dtype=torch.bfloat16, device="cuda").uniform_(-1, 1)
+    q, s = ops.quant_rows(x)
+    for part in (slice(0, R // 2), slice(R // 2, R)):
+        a, b = ops.quant_rows(x[part])
+        assert torch.equal(q[part], a) and torch.equal(s[part], b)
+
+
+def test_quant_pack_of_a_large_image():
+    """An image of more than 4 GiB: the images of parts of the channels, one after the other."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    N, K = (1 << 15) + 40, 131072
+    log("quant_pack %d x %d" % (N, K))
+    q = torch.randint(-127, 128, (N, K), dtype=torch.int8, device="cuda")
+    s = torch.ones(N, device="cuda")
+    image = ops.quant_pack(q, s).image
+    for n0, n1 in ((0, 1 << 14), (1 << 14, N)):
+        part = ops.quant_pack(q[n0:n1], s[n0:n1]).image
+        assert torch.equal(image[n0 * K:n0 * K + part.numel()], part)
+
+
+@pytest.mark.parametrize("R,K,N", [((1 << 30) + 70, 8, 1), ((1 << 28) + 70, 2056, 1), ((1 << 26) + 70, 0, 2)])
+def test_quant_linear_of_many_rows(R, K, N):
+    """64 or 32 rows a workgroup in LDS, and a wave a row where there are no inputs."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(53)
+    log("quant_linear %d x %d x %d" % (R, K, N))
+    x = gpu(rng.standard_normal((1, K)), "bf16")
+    w = ops.quant_pack(torch.from_numpy(rng.integers(-127, 128, (N, K)).astype(np.int8)).cuda(), torch.ones(N, device="cuda"))
+    bias = gpu(rng.standard_normal(N))
+    y = ops.quant_linear(x.expand(R, K), w, bias=bias)
+    assert all_equal(y, ops.quant_linear(x, w, bias=bias)[0])
+
+
+def test_quant_linear_of_many_tiles():
+    """The simple form's 32 x 32 tiles, a wave each, without inputs: 2^26 of them leave the bias everywhere."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    R, N = (1 << 21) + 33, 1 << 15
+    log("quant_linear %d x 0 x %d" % (R, N))
+    bias = gpu(np.random.default_rng(54).standard_normal(N))
+    w = ops.quant_pack(torch.zeros((N, 0), dtype=torch.int8, device="cuda"), torch.ones(N, device="cuda"))
+    y = ops.quant_linear(torch.empty((R, 0), dtype=torch.bfloat16, device="cuda"), w, bias=bias)
+    assert all_equal(y, bias.bfloat16(), 1 << 16)
