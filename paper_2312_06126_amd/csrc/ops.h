@@ -112,14 +112,19 @@ template <typename T> __device__ inline void store_part(T* p, const u32x4& v, in
 }
 
 // ----------------------------------------------------------------------------- arithmetic
-// a = 1 / (1 + exp(-x)) and b = 1 - a = exp(-x) / (1 + exp(-x)), each to float32's relative precision:
-// 1 - a by subtraction only where a < 1/2, which is also where exp(-x) may overflow. The
-// hardware's exponential and reciprocal (1 ulp) serve; the exponential's argument is rounded, which
-// costs b some |x| / 2 ulp where it is small.
+// a = 1 / (1 + exp(-x)) and b = 1 - a, each to 7 units of 2^-24 of itself: with e = exp(-|x|), which cannot overflow, the
+// larger one is 1 / (1 + e) and the other one e / (1 + e). The hardware's exponential and reciprocal (1 ulp) serve. The
+// exponential's argument t = -|x| log2(e) would lose |t| 2^-24 to its rounding (62 units at |x| = 80), so what e lacks, the
+// factor exp(s), s = -|x| - t ln 2, is put back as 1 + s. The constant is two ulp above log2(e), so that s >= 0 whatever t's
+// rounding: held to [0, 1], which costs no instruction, it is 0 instead of NaN where x is infinite.
 __device__ inline void sigmoid2(float x, float& a, float& b) {
-  const float e = __builtin_amdgcn_exp2f(x * -1.44269504f);
-  a = __builtin_amdgcn_rcpf(1.0f + e);
-  b = x < 0.0f ? 1.0f - a : e * a;
+  constexpr float LOG2E_ABOVE = 0x1.71547ap+0f, LN2 = 0x1.62e43p-1f, LN2_LOW = -0x1.05c61p-29f;
+  const float m = __builtin_fabsf(x), t = m * -LOG2E_ABOVE;
+  const float s = __builtin_amdgcn_fmed3f(fmaf(t, -LN2_LOW, fmaf(t, -LN2, -m)), 0.0f, 1.0f);
+  const float p = __builtin_amdgcn_exp2f(t), e = fmaf(p, s, p);
+  const float big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;
+  a = x < 0.0f ? small : big;
+  b = x < 0.0f ? big : small;
 }
 
 // Dropout's 16-bit words of elements 8 blk .. 8 blk + 7 (two to a word, low half first).

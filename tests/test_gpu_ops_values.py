@@ -1,0 +1,68 @@
+"""Values of the recurrent block's operators where float32 has to be used with care: sigmoids far from
+zero, and the state behind sequences that end before the last step."""
+import numpy as np
+import pytest
+
+from . import ops_reference as ref
+from .helpers import log
+from .test_gpu_ops import gpu, host, torch_
+
+pytestmark = pytest.mark.gpu
+
+
+def sigmoid_arguments():
+    rng = np.random.default_rng(41)
+    x = np.concatenate([np.linspace(-80, 80, 4001), rng.uniform(-80, 80, 4000), rng.standard_normal(186), [0.0, -0.0, 1e-30, -1e-30, 0.5]])
+    return x.astype(np.float32)   # 8192 of them
+
+
+def relative(name, got, want, units):
+    off = np.abs(got - want) / np.abs(want)
+    log("%s: at most %.2f of %g units" % (name, off.max() / ref.U, units))
+    assert (off <= units * ref.U).all(), (name, off.max() / ref.U, units)
+
+
+# In units of 2^-24. e = exp(-|x|): the hardware's 2^t (1 ulp: 2) and a product by fma (1): 3. The larger of a = sigmoid(x) and 1 - a
+# is 1 / (1 + e): at most half of e's 3, 1 of the sum, 2 of the reciprocal (1 ulp). The other one is e / (1 + e): 3 / (1 + e) of
+# e, 1 + 2 of the quotient, 1 of the product: less than 7. 1 - a may be 2 more, for ways whose e and 1 + e are off
+# on the same side; a product of both is 7 + 9 + 1.
+A, B, AB = 7, 9, 17
+
+
+def test_sigmoids_of_the_scan():
+    """a, 1 - a and both gradients of single steps, each to a few units of its own size over |f| <= 80."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    f = sigmoid_arguments().reshape(8, 1, -1)
+    a, b = ref.sigmoid(f.astype(np.float64))
+    one, zero = torch.ones(f.shape, device="cuda"), torch.zeros(f.shape, device="cuda")
+    keep, hT, saved = ops.scan(gpu(f), zero, one[:, 0].contiguous(), save=True)
+    relative("a", host(keep), a, A)
+    relative("1 - a", host(ops.scan(gpu(f), one)[0]), b, B)
+    df, dv, dh0 = ops.scan_backward(gpu(f), zero, one, saved)
+    relative("df", host(df), a * b, AB)
+    relative("dv", host(dv), b, B)
+    relative("dh0", host(dh0), a[:, 0], A)
+
+
+@pytest.mark.parametrize("width", [64, 16392])
+def test_sigmoids_of_the_gates(width):
+    """Gates and their slopes the same, in rows that stay in registers and in rows read again."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rows = 2 * 8192 // width if width < 8192 else 1
+    z = np.resize(sigmoid_arguments(), (rows, width))
+    s, t = ref.sigmoid(z.astype(np.float64))
+    one, zero = torch.ones(z.shape, device="cuda"), torch.zeros(z.shape, device="cuda")
+    for gate in ("sigmoid", "silu"):
+        x_out, _ = ops.block_norm(zero, one, gpu(z), post="none", pre="none", gate=gate)
+        dz = ops.block_norm_backward(one, None, zero, one, gpu(z), post="none", pre="none", gate=gate)["dz"]
+        if gate == "sigmoid":
+            relative("gate", host(x_out), s, A)
+            relative("slope", host(dz), s * t, AB)
+        else:
+            # z s is one rounding more; the slope s (1 + z t) is a sum of s and z s t, which may cancel.
+            some = z != 0
+            relative("silu", host(x_out)[some], (z * s)[some], A + 1)
+            off = np.abs(host(dz) - s * (1.0 + z * t))
+            assert (off <= ((A + 1) * s + (A + B + 2) * s * t * np.abs(z)) * ref.U * 1.01).all()
