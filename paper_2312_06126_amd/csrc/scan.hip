@@ -355,7 +355,8 @@ template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS, 2) void 
 #pragma unroll
   for (int i = 0; i < V; ++i) zero[i] = 0.0f;
   for (int64_t t = t1 > t0 ? t1 : t0; t < t2; ++t) store_v<T, V>(y + t * a.y_step, zero);
-  if (a.hT && q.p == g.pieces - 1) store_s<V>(a.hT + st, vec && op_aligned16(a.hT), h);
+  // hT from the piece with the last step (the joint maps' state behind it may differ in its last bits); h0 without steps.
+  if (a.hT && (n ? t0 < n && n <= end : q.p == 0)) store_s<V>(a.hT + st, vec && op_aligned16(a.hT), h);
 }
 
 template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS, 2) void scan_backward(ScanArgs g) {

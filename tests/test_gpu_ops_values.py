@@ -66,3 +66,15 @@ def test_sigmoids_of_the_gates(width):
             relative("silu", host(x_out)[some], (z * s)[some], A + 1)
             off = np.abs(host(dz) - s * (1.0 + z * t))
             assert (off <= ((A + 1) * s + (A + B + 2) * s * t * np.abs(z)) * ref.U * 1.01).all()
+
+
+@pytest.mark.parametrize("B,T,D", [(2, 6000, 40), (1, 3001, 7), (3, 300, 24), (200, 40, 513)])
+def test_last_state_is_that_of_the_last_step(B, T, D):
+    """hT and y's last row are one number, whichever way the sequence is walked and wherever it ends."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(42)
+    f, v, h0 = gpu(rng.standard_normal((B, T, D)) * 2 + 1), gpu(rng.standard_normal((B, T, D))), gpu(rng.standard_normal((B, D)))
+    for n in (0, 1, T // 3, T - 1, T):
+        y, hT = ops.scan(f, v, h0, lengths=torch.full((B,), n, dtype=torch.int32, device="cuda"))
+        assert torch.equal(hT, y[:, n - 1] if n else h0), n
