@@ -7,6 +7,10 @@ torch.cuda.Stream or a hipStream_t address (default: the device's current stream
 enqueued on it, and tensors that belong to another stream are kept alive until it has run; what
 was enqueued elsewhere is the caller's to order. Nothing waits for the GPU, so calls may be
 captured into a HIP graph. Errors: SpzError.
+
+torch's autograd does not record the calls: gradients come from scan_backward, block_norm_backward and, for dropout,
+the same call on the gradient (quant_linear has none). Tensors that require a gradient are refused, so that none is
+lost; within torch.no_grad() they are taken. The calls work on data pointers: they are not for tracing or vmap.
 """
 from __future__ import annotations
 
@@ -41,6 +45,13 @@ def _ptr(t: Optional[torch.Tensor]) -> int:
     return _NULL if t is None else t.data_ptr()
 
 
+_grad_on = torch.is_grad_enabled
+
+
+def _refuse_grad(name: str):
+    _refuse("%s requires a gradient, which autograd would not record here: call within torch.no_grad() or detach it" % name)
+
+
 def _like(t, name: str, gpu: int, shape, dtype, contiguous: bool = False):
     """Checks an argument's device, shape, type and layout (None passes)."""
     if t is None:
@@ -53,6 +64,8 @@ def _like(t, name: str, gpu: int, shape, dtype, contiguous: bool = False):
         _refuse("%s has shape %s, not %s" % (name, tuple(t.shape), tuple(shape)))
     if t.dtype is not dtype:
         _refuse("%s has type %s, not %s" % (name, t.dtype, dtype))
+    if t.requires_grad and _grad_on():
+        _refuse_grad(name)
     if t.is_contiguous():
         return
     if contiguous:
@@ -75,6 +88,8 @@ def _operand(t, name: str, dims: int) -> int:
         _refuse("%s has type %s" % (name, t.dtype))
     if t.dim() != dims:
         _refuse("%s has %d dimensions, not %d" % (name, t.dim(), dims))
+    if t.requires_grad and _grad_on():
+        _refuse_grad(name)
     if not t.is_contiguous() and t.shape[-1] > 1 and t.stride(-1) != 1:
         _refuse("%s is not contiguous in its last dimension" % name)
     return t.get_device()
@@ -225,7 +240,8 @@ def _block_check(x, h, z, vectors, post, pre, gate, valid) -> int:
         _refuse("the gate needs z")
     _like(z, "z", gpu, shape, x.dtype)
     for i, t in enumerate(vectors):
-        if t is not None and not (t.dtype is _F32 and t.dim() == 1 and t.numel() == D and t.get_device() == gpu and t.is_contiguous()):
+        if t is not None and not (t.dtype is _F32 and t.dim() == 1 and t.numel() == D and t.get_device() == gpu and t.is_contiguous()
+                                  and not t.requires_grad):
             _like(t, ("w_post", "b_post", "scale", "w_pre", "b_pre")[i], gpu, (D,), _F32)
     if valid is not None:
         _like(valid, "valid", gpu, (R,), torch.bool if getattr(valid, "dtype", None) is torch.bool else torch.uint8, contiguous=True)

@@ -1,0 +1,48 @@
+"""What the recurrent block's calls on torch tensors refuse, beyond shapes, types and layouts."""
+import pytest
+
+from .test_gpu_ops import torch_
+
+pytestmark = pytest.mark.gpu
+
+
+def test_tensors_that_require_a_gradient():
+    """Any operand: refused where autograd would lose its gradient, taken where it is off."""
+    from paper_2312_06126_amd import ops
+    from paper_2312_06126_amd.spz import SPZ_EINVAL, SpzError
+    torch = torch_()
+
+    def calls(t):
+        """Each call with one operand replaced by what t(operand) gives."""
+        f, x = torch.ones((2, 3, 8), device="cuda"), torch.ones((4, 8), device="cuda")
+        state, w = torch.ones((2, 8), device="cuda"), torch.ones(8, device="cuda")
+        saved = ops.scan(f, f, save=True)[2]
+        weights = ops.quant_pack(*ops.quant_rows(x))
+        block = dict(x=x, h=x, z=x, w_post=w, b_post=w, scale=w, w_pre=w, b_pre=w, gate="silu")
+        for k in ("f", "v", "h0", "out", "hT"):
+            a = dict(f=f, v=f, h0=state, out=f.clone(), hT=state.clone())
+            yield lambda: ops.scan(**dict(a, **{k: t(a[k])}))
+        for k in ("f", "v", "dy", "dhT", "saved"):
+            a = dict(f=f, v=f, dy=f, dhT=state, saved=saved)
+            yield lambda: ops.scan_backward(**dict(a, **{k: t(a[k])}))
+        for k in ("x", "h", "z", "w_post", "b_post", "scale", "w_pre", "b_pre"):
+            yield lambda: ops.block_norm(**dict(block, **{k: t(block[k])}))
+            yield lambda: ops.block_norm_backward(x, x, **dict(block, **{k: t(block[k])}))
+        yield lambda: ops.block_norm_backward(t(x), x, **block)
+        yield lambda: ops.block_norm_backward(x, t(x), **block)
+        yield lambda: ops.dropout(t(x), 0.5, 1, 2)
+        yield lambda: ops.quant_rows(t(x))
+        yield lambda: ops.quant_linear(t(x), weights)
+        yield lambda: ops.quant_linear(x, weights, bias=t(torch.ones(4, device="cuda")))
+        yield lambda: ops.quant_linear(x, weights._replace(scale=t(weights.scale)))
+
+    def leaf(x):
+        return x.clone().requires_grad_()
+
+    for call in calls(leaf):
+        with pytest.raises(SpzError) as e:
+            call()
+        assert e.value.code == SPZ_EINVAL and "gradient" in str(e.value)
+    with torch.no_grad():
+        for call in calls(leaf):
+            call()
