@@ -11,7 +11,7 @@ int op_error(int code, const char* call, const char* what) noexcept;
 
 // ----------------------------------------------------------------------------- checks
 constexpr int64_t OP_MAX_EXTENT = (int64_t)1 << 31;   // extents are below this
-constexpr int64_t OP_MAX_STRIDE = (int64_t)1 << 42;   // keeps every byte offset within 62 bits
+constexpr int64_t OP_MAX_STRIDE = (int64_t)1 << 42;   // strides in bytes do not wrap
 
 inline bool op_prec_ok(int32_t prec) { return prec == SPZ_PREC_FP32 || prec == SPZ_PREC_BF16; }
 inline int op_size(int32_t prec) { return prec == SPZ_PREC_BF16 ? 2 : 4; }
@@ -27,8 +27,9 @@ inline bool op_out_strides_ok(int64_t n0, int64_t n1, int64_t width, int64_t s0,
   if (n0 == 0 || n1 == 0 || width == 0) return op_in_stride_ok(s0) && op_in_stride_ok(s1);
   if (!op_out_stride_ok(n0, width, s0) || !op_out_stride_ok(n1, width, s1)) return false;
   if (n0 <= 1 || n1 <= 1) return true;
-  // The inner dimension's span fits between two elements of the outer one.
-  return s0 >= s1 ? s0 >= (n1 - 1) * s1 + width : s1 >= (n0 - 1) * s0 + width;
+  // The inner dimension's span, (n - 1) strides and a row, fits between two elements of the outer one. (By
+  // division, as the product may wrap; the strides are at least `width` here.)
+  return s0 >= s1 ? (s0 - width) / s1 >= n1 - 1 : (s1 - width) / s0 >= n0 - 1;
 }
 
 inline int64_t op_div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
