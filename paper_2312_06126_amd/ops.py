@@ -14,7 +14,9 @@ lost; within torch.no_grad() they are taken. The calls work on data pointers: th
 """
 from __future__ import annotations
 
+import ctypes
 import functools
+import struct
 from typing import NamedTuple, Optional
 
 import torch
@@ -240,8 +242,8 @@ def _block_check(x, h, z, vectors, post, pre, gate, valid) -> int:
         _refuse("the gate needs z")
     _like(z, "z", gpu, shape, x.dtype)
     for i, t in enumerate(vectors):
-        if t is not None and not (t.dtype is _F32 and t.dim() == 1 and t.numel() == D and t.get_device() == gpu and t.is_contiguous()
-                                  and not t.requires_grad):
+        if t is not None and not (isinstance(t, torch.Tensor) and t.dtype is _F32 and t.dim() == 1 and t.numel() == D
+                                  and t.get_device() == gpu and t.is_contiguous() and not t.requires_grad):
             _like(t, ("w_post", "b_post", "scale", "w_pre", "b_pre")[i], gpu, (D,), _F32)
     if valid is not None:
         _like(valid, "valid", gpu, (R,), torch.bool if getattr(valid, "dtype", None) is torch.bool else torch.uint8, contiguous=True)
@@ -252,17 +254,23 @@ def _row(t) -> int:
     return 0 if t is None else t.stride(0)
 
 
+_NOT_NUMBERS = (struct.error, ctypes.ArgumentError, TypeError, ValueError, OverflowError)
+
+
 def _block_pack(x, h, z, vectors, valid, outs, backs, drop, eps, post, pre, gate) -> bytes:
     """The argument block; outs: x_out, u, backs: dx_out, du, then the gradients."""
     x_out, u = outs
     dx_out, du, dx, dh, dz, dw_post, db_post, dscale, dw_pre, db_pre = backs
-    p, seed, step, tensor = drop if drop is not None else (0.0, 0, 0, 0)
-    return pack_block_norm(
-        x.shape[0], x.shape[1], x.data_ptr(), _ptr(h), _ptr(z), x.stride(0), _row(h), _row(z), *map(_ptr, vectors), _ptr(valid),
-        _ptr(x_out), _ptr(u), _row(x_out), _row(u), _ptr(dx_out), _ptr(du), _row(dx_out), _row(du), _ptr(dx), _ptr(dh),
-        _ptr(dz), _row(dx), _row(dh), _row(dz), _ptr(dw_post), _ptr(db_post), _ptr(dscale), _ptr(dw_pre), _ptr(db_pre),
-        int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(tensor) & 0xFFFFFFFF, p, eps, NORMS[post], NORMS[pre],
-        GATES[gate], _PREC[x.dtype])
+    try:
+        p, seed, step, tensor = drop if drop is not None else (0.0, 0, 0, 0)
+        return pack_block_norm(
+            x.shape[0], x.shape[1], x.data_ptr(), _ptr(h), _ptr(z), x.stride(0), _row(h), _row(z), *map(_ptr, vectors), _ptr(valid),
+            _ptr(x_out), _ptr(u), _row(x_out), _row(u), _ptr(dx_out), _ptr(du), _row(dx_out), _row(du), _ptr(dx), _ptr(dh),
+            _ptr(dz), _row(dx), _row(dh), _row(dz), _ptr(dw_post), _ptr(db_post), _ptr(dscale), _ptr(dw_pre), _ptr(db_pre),
+            int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(tensor) & 0xFFFFFFFF, p, eps, NORMS[post], NORMS[pre],
+            GATES[gate], _PREC[x.dtype])
+    except _NOT_NUMBERS as e:
+        _refuse("drop is not (p, seed, step, tensor) or eps no number: %s" % e)
 
 
 def block_norm(x, h=None, z=None, w_post=None, b_post=None, scale=None, w_pre=None, b_pre=None, *, post="rms", pre="rms",
@@ -334,8 +342,11 @@ def dropout(x, p: float, seed: int, step: int, tensor: int = 0, *, out=None, str
     s = _stream(gpu)
     rows, width = x.shape
     y = out if out is not None else _empty(x)
-    rc = lib.spz_dropout(_PREC[x.dtype], rows, width, x.data_ptr(), x.stride(0), y.data_ptr(), y.stride(0), p,
-                         int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(tensor) & 0xFFFFFFFF, s)
+    try:
+        rc = lib.spz_dropout(_PREC[x.dtype], rows, width, x.data_ptr(), x.stride(0), y.data_ptr(), y.stride(0), p,
+                             int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(tensor) & 0xFFFFFFFF, s)
+    except _NOT_NUMBERS as e:
+        _refuse("p, seed, step or tensor is no number: %s" % e)
     if rc:
         _done(rc)
     return y
@@ -401,6 +412,8 @@ def quant_linear(x, weights: QuantWeights, *, bias=None, out=None, stream=None):
     at a time within the call, products and sums are exact integers, y has x's type."""
     lib = load()
     gpu = _operand(x, "x", 2)
+    if not isinstance(weights, tuple) or len(weights) != 4:
+        _refuse("weights are not those of quant_pack")
     image, scale, N, K = weights
     M = x.shape[0]
     if x.shape[1] != K:

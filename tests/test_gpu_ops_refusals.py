@@ -46,3 +46,23 @@ def test_tensors_that_require_a_gradient():
     with torch.no_grad():
         for call in calls(leaf):
             call()
+
+
+def test_arguments_of_other_kinds():
+    """What is no tensor, no number or no packed weights is an SpzError as well."""
+    from paper_2312_06126_amd import ops
+    from paper_2312_06126_amd.spz import SPZ_EINVAL, SpzError
+    torch = torch_()
+    x = torch.ones((4, 8), device="cuda")
+    f = torch.ones((2, 3, 8), device="cuda")
+    q, s = ops.quant_rows(x)
+    for call in (lambda: ops.block_norm(x, w_pre=[1.0] * 8), lambda: ops.block_norm(x, x, scale=2.0), lambda: ops.block_norm(x, valid=[1] * 4),
+                 lambda: ops.block_norm(x, x, drop=0.5), lambda: ops.block_norm(x, x, drop=(0.5, 1, 2)), lambda: ops.block_norm(x, x, drop=(1e39, 1, 2, 3)),
+                 lambda: ops.block_norm(x, x, drop=(0.5, "a", 2, 3)), lambda: ops.block_norm(x, eps=None), lambda: ops.block_norm(x, eps="a"),
+                 lambda: ops.block_norm_backward(x, x, x, x, w_post=1), lambda: ops.block_norm_backward(None, [0.0], x),
+                 lambda: ops.dropout(x, "a", 1, 2), lambda: ops.dropout(x, 0.5, None, 2), lambda: ops.dropout(x, 1e39, 1, 2),
+                 lambda: ops.quant_linear(x, q), lambda: ops.quant_linear(x, None), lambda: ops.quant_linear(x, (q, s, 4, 8)),
+                 lambda: ops.quant_pack(q, 1.0), lambda: ops.scan(f, f, lengths=[1, 2]), lambda: ops.scan(f, f, 0.0), lambda: ops.scan(f, None)):
+        with pytest.raises(SpzError) as e:
+            call()
+        assert e.value.code == SPZ_EINVAL
