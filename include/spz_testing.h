@@ -22,6 +22,8 @@
 
 #include <stdint.h>
 
+#include "spz.h"
+
 #ifdef __cplusplus
 extern "C" {
 #endif
@@ -105,6 +107,12 @@ int spzt_row_workspace(int32_t td3, int32_t bf16, int32_t obs_dim, int32_t act_d
  */
 int spzt_row_range(int32_t td3, int32_t bf16, int32_t sequential, int32_t n_streams, int32_t graphs, int32_t obs_dim,
                    int32_t act_dim, const int32_t* hidden, int32_t n_hidden, int32_t* lo, int32_t* hi);
+/*
+ * How spz_scan_forward (backward = 0) or spz_scan_backward spreads a call: 0 a thread walks a whole sequence, 1
+ * a workgroup walks it in tiles of time, 2 time is cut into pieces; + 4 where a thread takes vectors of channels.
+ * Runs on the host alone.
+ */
+int spzt_scan_way(const spz_scan_args* args, int32_t backward);
 
 #ifdef __cplusplus
 }

@@ -26,6 +26,7 @@
 // 33 + 10 + 82.
 #include <type_traits>
 
+#include "../../include/spz_testing.h"
 #include "ops.h"
 
 namespace spz {
@@ -757,6 +758,17 @@ template <typename T> void scan_dispatch(const ScanArgs& g, ScanWay way, bool ba
   else scan_launch<T, 1, false>(g, way, s);
 }
 
+// Vectors of channels need every touched row aligned for them.
+bool scan_vectors(const spz_scan_args& a, bool back) {
+  const int e = op_size(a.prec), v = back ? SCAN_V_BACK : SCAN_V;
+  const auto vec = [&](const void* p, int64_t s0, int64_t s1) {
+    return !p || (op_aligned(p, v * e) && s0 % v == 0 && s1 % v == 0);
+  };
+  return a.width % v == 0 && vec(a.f, a.f_batch, a.f_step) && vec(a.v, a.v_batch, a.v_step) &&
+         (back ? vec(a.dy, a.dy_batch, a.dy_step) && vec(a.df, a.df_batch, a.df_step) && vec(a.dv, a.dv_batch, a.dv_step)
+               : vec(a.y, a.y_batch, a.y_step));
+}
+
 int64_t scan_workspace(const spz_scan_args& a) {
   const ScanPlan p = scan_plan(a);
   return p.way == SCAN_PIECES ? 2 * p.pieces * a.batch * a.width * 8 : 0;
@@ -780,14 +792,8 @@ int scan_run(const char* call, const spz_scan_args* args, bool back, void* ws, i
     g.map_a = static_cast<double*>(ws);
     g.map_h = g.map_a + plan.pieces * a.batch * a.width;
   }
-  // Vectors of channels need every touched row aligned for them.
-  const int e = op_size(a.prec), v = back ? SCAN_V_BACK : SCAN_V;
-  const auto vec = [&](const void* p, int64_t s0, int64_t s1) {
-    return !p || (op_aligned(p, v * e) && s0 % v == 0 && s1 % v == 0);
-  };
-  const bool vectors = a.width % v == 0 && vec(a.f, a.f_batch, a.f_step) && vec(a.v, a.v_batch, a.v_step) &&
-                  (back ? vec(a.dy, a.dy_batch, a.dy_step) && vec(a.df, a.df_batch, a.df_step) && vec(a.dv, a.dv_batch, a.dv_step)
-                        : vec(a.y, a.y_batch, a.y_step));
+  const int v = back ? SCAN_V_BACK : SCAN_V;
+  const bool vectors = scan_vectors(a, back);
   g.chunks = vectors ? a.width / v : a.width;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (a.prec == SPZ_PREC_BF16) scan_dispatch<bf16_t>(g, plan.way, back, vectors, s);
@@ -821,6 +827,11 @@ int spz_scan_forward(const spz_scan_args* args, void* workspace, int64_t workspa
 
 int spz_scan_backward(const spz_scan_args* args, void* workspace, int64_t workspace_bytes, void* hip_stream) {
   return scan_run("spz_scan_backward", args, true, workspace, workspace_bytes, hip_stream);
+}
+
+int spzt_scan_way(const spz_scan_args* args, int32_t backward) {
+  if (scan_check(args)) return SPZ_EINVAL;
+  return (int)scan_plan(*args).way + (scan_vectors(*args, backward != 0) ? 4 : 0);
 }
 
 }  // extern "C"
