@@ -485,7 +485,8 @@ int spz_dropout(int32_t prec, int64_t rows, int64_t width, const void* x, int64_
 
 /* 8-bit integers with a scale for each row: scale[r] = max_c |x[r, c]| * (1 / 127), the
  * factor and the product rounded to float32, and q[r, c] = x[r, c] / scale[r] (float32)
- * rounded to the nearest integer, ties to even, within +-127; 0 and 0 for a row of zeros. A row with an infinity or NaN gets a NaN scale and zeros. */
+ * rounded to the nearest integer, ties to even, within +-127; 0 and 0 for a row of zeros. A row with an
+ * infinity or NaN gets a NaN scale and zeros. */
 int spz_quant_rows(int32_t prec, int64_t rows, int64_t width, const void* x, int64_t x_row, int8_t* q, int64_t q_row,
                    float* scale, void* hip_stream);
 

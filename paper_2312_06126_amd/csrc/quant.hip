@@ -1,7 +1,7 @@
 // The 8-bit integer product with a scale for each row of the input and each output channel
 // (spz_quant_*).
 //
-//   y[m, n] = s[m] w_scale[n] sum_k q[m, k] w[n, k] + bias[n],   s[m] = max_k |x[m, k]| / 127
+//   y[m, n] = s[m] w_scale[n] sum_k q[m, k] w[n, k] + bias[n],   s[m] = max_k |x[m, k]| float32(1 / 127)
 //
 // Weights are kept as fragments: 1 KB pieces of 32 channels by 32 bytes of k in the order in which
 // one wave feeds v_mfma_i32_32x32x32_i8 (lane l: 16 bytes of channel l % 32, k from 16 (l / 32)), zeros
@@ -46,10 +46,10 @@ __device__ inline uint32_t wave_max(uint32_t x) {
   const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
   return r[0] > r[1] ? r[0] : r[1];
 }
-// A scale is the row's largest |x| times the float32 next to 1 / 127: within an ulp of the quotient, and what
-// dividing a float32 tensor on the GPU by the number 127 gives in torch, so that a quantisation written
-// there rounds the same elements up (4% of scales differ by an ulp from the quotient, which moves
-// 1 element in 10 million across a tie).
+// A scale is the row's largest |x| times the float32 next to 1 / 127: what dividing a float32 tensor on the GPU by the
+// number 127 gives in torch, so that a quantisation written there rounds the same elements up. In 5% of rows it is an ulp from
+// the rounded quotient max |x| / 127, which moves elements that lie at a tie: of a million normal ones (rows of 512) less than
+// 0.1 in float32, but 40 to 80 in bfloat16, where ties are common.
 constexpr float QUANT_STEP = 1.0f / 127.0f;
 // The row's scale from the largest |x| as bits, and whether the row quantises to zeros: infinity and
 // NaN have the largest bits.
@@ -63,8 +63,8 @@ __device__ inline int quantised(float x, float s) {
   return (int)fminf(fmaxf(q, -127.0f), 127.0f);
 }
 
-// Rows of integers: one wave a row, which it reads twice (bound by HBM and its latency; weights, once). q [rows, width] at q_row, or (FRAGS) as
-// fragments over 32 * frag_blocks(rows) rows.
+// Rows of integers: one wave a row, which it reads twice (bound by HBM and its latency; weights, once). q [rows, width]
+// at q_row, or (FRAGS) as fragments over 32 * frag_blocks(rows) rows.
 template <typename T, bool FRAGS>
 __global__ __launch_bounds__(256) void quant_rows(const T* x, int64_t x_row, int64_t rows, int64_t width, int8_t* q,
                                                   int64_t q_row, float* scale, int64_t first) {

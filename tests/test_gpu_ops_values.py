@@ -78,3 +78,21 @@ def test_last_state_is_that_of_the_last_step(B, T, D):
     for n in (0, 1, T // 3, T - 1, T):
         y, hT = ops.scan(f, v, h0, lengths=torch.full((B,), n, dtype=torch.int32, device="cuda"))
         assert torch.equal(hT, y[:, n - 1] if n else h0), n
+
+
+@pytest.mark.parametrize("kind", ["normal", "relu"])
+def test_quant_of_bfloat16_like_torch(kind):
+    """bfloat16 rows, where ties are common: scales, integers and products are those of the same formula in torch."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(43)
+    x = torch.randn((100000, 200), generator=gen, device="cuda").bfloat16()
+    if kind == "relu":
+        x = torch.relu(x)
+    q, s = ops.quant_rows(x)
+    scale = x.float().abs().amax(1) / 127.0
+    want = torch.round(x.float() / scale[:, None])
+    assert torch.equal(s, scale) and torch.equal(q.float(), want)
+    w = ops.quant_pack(torch.eye(200, dtype=torch.int8, device="cuda"), torch.ones(200, device="cuda"))
+    assert torch.equal(ops.quant_linear(x, w), (want * scale[:, None]).bfloat16())
