@@ -359,9 +359,10 @@ int spz_profile_read(spz_ctx* ctx, spz_kernel_stat* out, int32_t max, int32_t* n
 
 /* ---------------------------------------------------------------------------------------
  * Operators of a recurrent residual block. The policy of a task that one observation does
- * not describe acts on a history: sequences of the shared pool's transitions when the
- * update process trains it (Section 3.2), one step a call for the N samplers (Section
- * 3.1.1). One block of such a network is
+ * not describe acts on a history: sequences of transitions in training (beside Section
+ * 3.2's update process), one step a call for N samplers (as in Section 3.1.1). They are for
+ * a learner that the caller builds: a context's networks are feed-forward, its ring holds
+ * single transitions, and none of its calls uses them. One block of such a network is
  *     u = norm(x);  f, v, z = products of u;  h = scan(f, v);
  *     x' = x + scale * dropout(gate(z) * norm(h));  u' = norm(x')  (the next block's)
  * Conventions of all of them
@@ -379,7 +380,8 @@ int spz_profile_read(spz_ctx* ctx, spz_kernel_stat* out, int32_t max, int32_t* n
  *     apart (inputs: 0 repeats a row); an output's rows must not overlap each other, nor
  *     any other array of the call unless said otherwise. Any alignment of the element
  *     type is taken; 16-byte aligned rows are faster.
- *   - Every extent may be 0 and is below 2^31; a call without elements checks its
+ *   - Every extent may be 0 and is below 2^31, and their product within what a device may
+ *     hold (2^38 states, 2^40 to 2^44 elements); a call without elements checks its
  *     arguments and writes what remains (zero sums, the state).
  *   - Results depend on the arguments alone: sums are taken in a fixed order.
  *   - Errors: SPZ_EINVAL (NULL where an array is needed, an extent, stride, selector or

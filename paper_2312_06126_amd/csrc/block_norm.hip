@@ -14,8 +14,9 @@
 // atomics, the same bits on every run. Rows wider than the registers hold take norm_wide, which
 // reads them again for each statistic.
 //
-// Measured at 65536 x 1024 bf16: norm_forward 124 us (5.4 TB/s), norm_backward 254 to 294 (4.2 to 3.7),
-// norm_sums 5; at 5000 x 393 float32, rows that no access of 16 bytes fits: 13, 27 and 4 us.
+// Measured at 65536 x 1024 bf16: norm_forward 120 us (5.6 TB/s), norm_backward 253 to 266 (4.2 to 4.0), norm_sums 5;
+// without a block in front (h NULL) 51, 107 (from memory; 5.3 and 3.8 TB/s) and 5. At 5000 x 393 float32, rows
+// that no access of 16 bytes fits: 15, 29 and 4 us from memory.
 #include <type_traits>
 
 #include "ops.h"
@@ -730,7 +731,8 @@ template <typename T, bool BACK> __global__ __launch_bounds__(WIDE_THREADS) void
 
 // ----------------------------------------------------------------------------- dropout
 // Eight elements a thread: one Philox block. FLAT: rows follow each other without a gap, so that they
-// are one row of eights with a ragged end. 89 us at 131072 x 1024 bf16: 6.0 TB/s, HBM's rate.
+// are one row of eights with a ragged end. 88 us at 131072 x 1024 bf16: 6.1 TB/s, HBM's rate. Else each element by itself:
+// 71 us at 131072 rows of 256 out of 768 bf16 (1.9 TB/s; rows without gaps 22).
 template <typename T, bool FLAT>
 __global__ __launch_bounds__(256) void dropout(const T* x, int64_t x_row, T* y, int64_t y_row, int64_t width, int64_t n,
                                                Drop d, uint64_t seed, uint32_t step, uint32_t tensor, int64_t first) {

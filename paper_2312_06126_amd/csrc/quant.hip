@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256) void quant_pack(const int8_t* q, int64_t q_row
 }
 
 // Rows above QUANT_LDS_INNER inputs, the simple form: one wave a 32 x 32 tile of y, fragments straight from
-// L2, which bounds it. With quant_rows 161 us at 4096 x 8192 x 1024 bf16 (0.43 POP/s).
+// L2, which bounds it. With quant_rows 160 us at 4096 x 8192 x 1024 bf16 (0.43 POP/s), 220 where all comes from memory.
 template <typename T>
 __global__ __launch_bounds__(256) void quant_product(const int8_t* x, const int8_t* w, const float* xs, const float* ws,
                                                      const float* bias, T* y, int64_t y_row, int64_t rows, int64_t outer,
@@ -433,8 +433,8 @@ __device__ inline void quant_units(const QuantArgs& g, const u32x4* lds, int uni
 // A workgroup: RT rows and its part of the channels, 64 a wave at a time, each wave on its own once the
 // rows are in LDS. Bound by its phases: all workgroups read and quantise, multiply and write at about the
 // same time, so neither HBM nor the matrix instructions are always busy; two workgroups a compute unit
-// cover some of it. 131072 x 1024 x 1024 bf16: 207 us, 1.33 POP/s (the matrix instructions alone take a
-// third); 131072 x 256 x 256: 35 us, 3.8 TB/s. Waves of the workgroup that load the next tile of 128 rows
+// cover some of it. 131072 x 1024 x 1024 bf16: 200 us at the least, 1.37 POP/s (the matrix instructions alone take a
+// third), 232 in the median of calls without a pause; 131072 x 256 x 256: 39 us, 3.4 TB/s, from memory. Waves of the workgroup that load the next tile of 128 rows
 // while the others multiply were as fast at the first (197 to 211) and slower elsewhere
 // (65536 x 1024 x 4096: 482 against 368).
 template <typename T, int RB, int NU, int LPR, int WAVES>

@@ -2,8 +2,8 @@
 //
 //   h_t = a_t k_t h_{t-1} + (1 - a_t) v_t,  a_t = sigmoid(f_t), k_t = 0 at an episode start.
 //
-// Both directions are bound by HBM: 3 elements moved a step and channel forward, 5 backward
-// (f, v, dy, df, dv), for some 15 and 40 instructions. A thread owns SCAN_V adjacent channels of
+// Forward moves 3 elements a step and channel, backward 5 (f, v, dy, df, dv), for some 20 and 45 instructions, which
+// take nearly as long: bound by HBM where enough steps are in flight, in pieces by both. A thread owns SCAN_V adjacent channels of
 // one sequence (8 or 16 bytes a step, so a wave reads whole cache lines) and walks time with the
 // next steps' loads in flight; states stay in registers in float32.
 //
@@ -20,10 +20,12 @@
 // h_{t-1} is not stored by the forward pass: `saved` holds the state in front of every SEG-th step
 // (6% of the bytes moved in bf16), from which a thread recomputes SEG steps in registers.
 //
-// Measured: 2048 x 50 x 256 bf16, serially: forward 27 us, backward 49 (5.8 and 5.4 TB/s, partly from
-// the last-level cache). 64 x 1000 x 200 float32 in tiles: forward 39 us (3.9 TB/s).
-// 1 x 65536 x 512 bf16 in pieces: forward 33 + 10 + 39 us (scan_piece, scan_join, scan_forward), backward
-// 33 + 10 + 82.
+// Measured, on arrays that come from memory (in brackets: on the same arrays again and again, which the last-level cache
+// holds in part or, in tiles, whole): 2048 x 50 x 256 bf16, serially: forward 49 us, backward 72 (39, 71; 3.2 and
+// 3.6 TB/s), with lengths of half as many steps 39 and 57 (28, 49). 64 x 1000 x 200 float32 in tiles: forward 49 us,
+// 3.2 TB/s (41); backward 74, 3.5 TB/s (74).
+// 1 x 65536 x 512 bf16 in pieces: forward 42 + 10 + 40 us (36 + 10 + 41; scan_piece, scan_join, scan_forward), backward
+// 37 + 10 + 82 (39 + 10 + 83).
 #include <type_traits>
 
 #include "../../include/spz_testing.h"
@@ -449,7 +451,7 @@ template <typename T, int V> __global__ __launch_bounds__(SCAN_THREADS, 2) void 
 constexpr int TILE_THREADS = 256, TILE_WAVES = TILE_THREADS / 64;
 
 // Workgroup b runs on XCD b % 8: neighbours in width, whose 128 bytes a step share cache lines where rows
-// are not whole lines, on the same one (64 x 1000 x 200 float32: 39 against 48 us).
+// are not whole lines, on the same one (64 x 1000 x 200 float32, in the last-level cache: 39 against 48 us).
 __device__ inline int64_t tile_block() { return blockIdx.x % 8 * (int64_t)(gridDim.x / 8) + blockIdx.x / 8; }
 
 template <int V, int CL, bool BACK> struct Tile {

@@ -4,7 +4,7 @@ include/spz.h): argument checks, outputs and workspaces; every step runs in the 
 Tensors are on one GPU; float32 or bfloat16 as the header says, states, scales and parameter vectors
 float32. The last dimension is contiguous, the others have any strides. `stream`: a
 torch.cuda.Stream or a hipStream_t address (default: the device's current stream); the call is
-enqueued on it, and tensors that belong to another stream are kept alive until it has run; what
+enqueued on it, and where `stream` is given tensors that belong to another one are kept alive until it has run; what
 was enqueued elsewhere is the caller's to order. Nothing waits for the GPU, so calls may be
 captured into a HIP graph. Errors: SpzError.
 
