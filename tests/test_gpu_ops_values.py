@@ -96,3 +96,26 @@ def test_quant_of_bfloat16_like_torch(kind):
     assert torch.equal(s, scale) and torch.equal(q.float(), want)
     w = ops.quant_pack(torch.eye(200, dtype=torch.int8, device="cuda"), torch.ones(200, device="cuda"))
     assert torch.equal(ops.quant_linear(x, w), (want * scale[:, None]).bfloat16())
+
+
+@pytest.mark.parametrize("B,T,D", [(2, 0, 4), (0, 3, 4), (2, 3, 0), (0, 0, 0)])
+def test_scan_without_elements(B, T, D):
+    """No steps leave the state and its gradient as they are; no sequences or channels leave nothing."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    f, state = torch.ones((B, T, D), device="cuda"), torch.randn((B, D), device="cuda")
+    y, hT, saved = ops.scan(f, f, state, save=True)
+    df, dv, dh0 = ops.scan_backward(f, f, y, saved, dhT=state)
+    assert y.shape == df.shape == dv.shape == (B, T, D)
+    assert hT.shape == dh0.shape == (B, D)
+    if T == 0:
+        assert torch.equal(hT, state) and torch.equal(dh0, state)
+    x = torch.ones((B * T, D), device="cuda")
+    x_out, u = ops.block_norm(x, x)
+    assert x_out.shape == u.shape == ops.dropout(x, 0.5, 1, 2).shape == x.shape
+    g = ops.block_norm_backward(x_out, u, x, x, w_post=torch.ones(D, device="cuda"))
+    assert g["dh"].shape == x.shape and g["dw_post"].shape == (D,) and not g["dw_post"].any()
+    q, s = ops.quant_rows(x)
+    assert q.shape == x.shape and not s.any()
+    w = ops.quant_pack(torch.ones((3, D), dtype=torch.int8, device="cuda"), torch.ones(3, device="cuda"))
+    assert ops.quant_linear(x, w).shape == (B * T, 3) and not ops.quant_linear(x, w).any() or D
