@@ -506,6 +506,140 @@ int spz_quant_linear(int32_t prec, int64_t rows, int64_t outer, int64_t inner, c
                      const void* image, const float* w_scale, const float* bias, void* y, int64_t y_row,
                      void* workspace, int64_t workspace_bytes, void* hip_stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators of a block whose memory is a matrix, and an optimizer for a learner's own
+ * tensors, under the conventions above: norms and rotation of queries and keys, linear
+ * attention that forgets at a rate of its own in each head, AdamW over many tensors.
+ */
+
+/* Norms of each head of queries and keys, and their rotation by position, in one pass:
+ *     n = norm(x) * w + b over the `dim` columns of a head (norm as in spz_block_norm, or none,
+ *         where w and b still apply);
+ *     pair i < pairs of n is turned by the angle t = positions[row] * freqs[i]:
+ *         (a, b) -> (a cos t - b sin t, a sin t + b cos t), and the columns behind stay.
+ * layout SPZ_PAIRS_HALVES: pair i is columns i and pairs + i; SPZ_PAIRS_NEIGHBOURS: 2 i and
+ * 2 i + 1. 2 pairs <= dim <= 1024. Angles are taken in 64 bits, so positions may be far
+ * (off by 2^-52 of the angle, 1e-6 at 2^31 and a frequency of 1). heads_k may be 0 (no
+ * keys: any heads' norms). Rows r with valid[r] == 0 are not read: their outputs are zero
+ * and they give no gradient. q_out may be q and k_out may be k (with the same strides), as
+ * dq may be dq_out and dk dk_out.
+ *
+ * Backward, from dq_out and dk_out (NULL: zeros): dq, dk (NULL: not wanted) and the sums over
+ * rows and heads dw_q, db_q, dw_k, db_k (float32 [dim], written; NULL: not wanted). */
+#define SPZ_PAIRS_HALVES 0
+#define SPZ_PAIRS_NEIGHBOURS 1
+typedef struct spz_head_norm_args {
+  int64_t rows, heads_q, heads_k, dim, pairs;
+  const void *q, *k;                       /* [rows, heads, dim]                                 */
+  int64_t q_row, q_head, k_row, k_head;
+  const float *w_q, *b_q, *w_k, *b_k;      /* [dim]; NULL: ones and zeros                        */
+  const int32_t* positions;                /* [rows]; needed where pairs > 0                     */
+  const double* freqs;                     /* [pairs], radians a position                        */
+  const uint8_t* valid;                    /* [rows] or NULL (all of them)                       */
+  void *q_out, *k_out;                     /* forward: [rows, heads, dim]                        */
+  int64_t q_out_row, q_out_head, k_out_row, k_out_head;
+  const void *dq_out, *dk_out;             /* backward: [rows, heads, dim]                       */
+  int64_t dq_out_row, dq_out_head, dk_out_row, dk_out_head;
+  void *dq, *dk;                           /* backward: [rows, heads, dim]                       */
+  int64_t dq_row, dq_head, dk_row, dk_head;
+  float *dw_q, *db_q, *dw_k, *db_k;        /* backward: [dim]                                    */
+  float eps;                               /* a normal number > 0                                */
+  int32_t norm, layout;
+  int32_t prec;                            /* of q, k, their outputs and gradients               */
+} spz_head_norm_args;
+
+/* Bytes of the backward call's workspace (negative code on error). */
+int64_t spz_head_norm_workspace(const spz_head_norm_args* args);
+int spz_head_norm_forward(const spz_head_norm_args* args, void* hip_stream);
+int spz_head_norm_backward(const spz_head_norm_args* args, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* Linear attention over `steps` of each of `batch` sequences, in each of `heads` heads with a
+ * state of key_width x value_width (both at most 256):
+ *     S_t = d k_t S_{t-1} + key_t^T value_t,   y_t = scale query_t S_t,   d = exp(-rate[head])
+ * with S_{-1} = state and k_t = 0 where reset[t] != 0 (step t starts an episode: nothing of the
+ * state before it, finite or not, passes), else 1. An infinite rate is d = 0. Sequence b has
+ * lengths[b] steps (clamped to [0, steps]): behind them nothing is read, y is 0 and the state
+ * stays, so last = S of the last step (`state` of an empty sequence). The states are float32
+ * throughout. steps = 1 is the samplers' form; last may be state (updated in place).
+ * Queries, keys or values may be shared by heads (stride 0).
+ *
+ * Backward, from dy and dlast (the gradient to last): with C = dlast behind the last step,
+ *     G_t = C + scale query_t^T dy_t,  dquery_t = scale dy_t S_t^T,
+ *     dkey_t = value_t G_t^T,  dvalue_t = key_t G_t,  C = d k_t G_t;   dstate = C in front of the first step
+ * dq, dk, dv are 0 behind a sequence's length; those of shared heads are one for each head. It
+ * takes the forward call's `state`; the rates get no gradient. */
+typedef struct spz_linear_attention_args {
+  int64_t batch, steps, heads, key_width, value_width;
+  const void *q, *k, *v;                   /* [batch, steps, heads, key_width or value_width]    */
+  int64_t q_batch, q_step, q_head, k_batch, k_step, k_head, v_batch, v_step, v_head;
+  const float* rate;                       /* [heads] or NULL (zeros: nothing is forgotten)      */
+  const uint8_t* reset;                    /* [batch, steps] or NULL (no episode starts)         */
+  int64_t reset_batch, reset_step;
+  const int32_t* lengths;                  /* [batch] or NULL (all of them `steps`)              */
+  const float* state;                      /* [batch, heads, key_width, value_width] contiguous, or NULL (zeros) */
+  void* y;                                 /* forward: [batch, steps, heads, value_width]        */
+  int64_t y_batch, y_step, y_head;
+  float* last;                             /* forward: as state, or NULL                         */
+  const void* dy;                          /* backward: as y, or NULL (zeros)                    */
+  int64_t dy_batch, dy_step, dy_head;
+  const float* dlast;                      /* backward: as state, or NULL (zeros)                */
+  void *dq, *dk, *dv;                      /* backward: as q, k, v                               */
+  int64_t dq_batch, dq_step, dq_head, dk_batch, dk_step, dk_head, dv_batch, dv_step, dv_head;
+  float* dstate;                           /* backward: as state, or NULL                        */
+  float scale;                             /* finite                                             */
+  int32_t prec;                            /* of q, k, v, y and their gradients                  */
+} spz_linear_attention_args;
+
+/* Bytes of the workspace (negative code on error). Only the extents and prec are read. */
+int64_t spz_linear_attention_workspace(const spz_linear_attention_args* args, int32_t backward);
+int spz_linear_attention_forward(const spz_linear_attention_args* args, void* workspace, int64_t workspace_bytes,
+                                 void* hip_stream);
+int spz_linear_attention_backward(const spz_linear_attention_args* args, void* workspace, int64_t workspace_bytes,
+                                  void* hip_stream);
+
+/* An AdamW step over `count` tensors at once, each element by itself:
+ *     g = grad_scale grad,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *     p = p - lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p)
+ * in float32; p is rounded once to its type, and so is the bfloat16 copy for products to read. m
+ * and v are two arrays of `moments` elements for all tensors: tensor i has elements at ..
+ * at + n - 1 of both, `at` a multiple of SPZ_ADAMW_BLOCK; what lies between is left as it is.
+ * Two tensors may share no element.
+ *
+ * bits 32: m and v are float32. bits 8: m holds codes of m and v codes of sqrt(v) in the 8-bit
+ * floating point type e4m3 (1 sign, 4 exponent, 3 mantissa bits, largest 448), m_scale and v_scale
+ * a float32 for each SPZ_ADAMW_BLOCK of them: m = code m_scale, v = (code v_scale)^2. A step
+ * writes scale = max * (1 / 448) over the block's elements of the tensor (the factor and the
+ * product rounded to float32) and rounds x = |m| / scale and sqrt(v) / scale (at most 448) up or
+ * down to a value of the type with the probability of its distance: x below 2^-6 has 2^-6 added
+ * and taken off again; to its float32 bits 16 w + 8 is added and the low 20 bits are cleared. w is
+ * a 16-bit word of Philox4x32-10 (key seed; element e: counter (e >> 2 low 32 bits, low 32 bits of
+ * t, 6 + 256 (e >> 34), 0); words 2 (e & 3) for m and the one behind it for v, low half of each 32-bit word
+ * first). So small steps count on average, which rounding to nearest would lose. A positive
+ * sqrt(v) is at least 2^-9. A scale of 0 gives zeros, a maximum that is not finite a NaN scale and
+ * zeros. The step itself uses m and v before they are rounded. */
+#define SPZ_ADAMW_BLOCK 256
+typedef struct spz_adamw_tensor {
+  void* p;                                 /* [n], p_prec: updated in place                      */
+  const void* g;                           /* [n], g_prec                                        */
+  uint16_t* copy;                          /* bfloat16 [n], written, or NULL                     */
+  int64_t n, at;
+  double weight_decay;
+} spz_adamw_tensor;
+typedef struct spz_adamw_args {
+  int64_t count, moments;
+  const spz_adamw_tensor* tensors;         /* HOST [count], read within the call                 */
+  void *m, *v;                             /* [moments]: float32, or 8-bit codes                 */
+  float *m_scale, *v_scale;                /* bits 8: [moments / SPZ_ADAMW_BLOCK]                */
+  const float* grad_scale;                 /* device [1], or NULL (1)                            */
+  const int64_t* step_at;                  /* device [1]: t, read when the kernel runs, or NULL  */
+  const float* lr_at;                      /* device [1], as step_at, or NULL                    */
+  int64_t step;                            /* t >= 1 where step_at is NULL                       */
+  double lr, beta1, beta2, eps;            /* lr where lr_at is NULL; betas in [0, 1), eps >= 0  */
+  uint64_t seed;
+  int32_t bits, p_prec, g_prec, reserved;  /* reserved: 0                                        */
+} spz_adamw_args;
+int spz_adamw(const spz_adamw_args* args, void* hip_stream);
+
 /* Message of the last failure: of ctx, or of the calling thread when ctx is
  * NULL. Never NULL; empty when there was none. Valid until the next call. */
 const char* spz_last_error(const spz_ctx* ctx);

@@ -1,5 +1,5 @@
-"""The operators of a recurrent residual block on torch tensors (spz_scan_* .. spz_quant_* of
-include/spz.h): argument checks, outputs and workspaces; every step runs in the HIP library.
+"""The operators of recurrent and linear-attention blocks and their optimizer on torch tensors (spz_scan_* .. spz_adamw
+of include/spz.h): argument checks, outputs and workspaces; every step runs in the HIP library.
 
 Tensors are on one GPU; float32 or bfloat16 as the header says, states, scales and parameter vectors
 float32. The last dimension is contiguous, the others have any strides. `stream`: a
@@ -8,20 +8,22 @@ enqueued on it, and where `stream` is given tensors that belong to another one a
 was enqueued elsewhere is the caller's to order. Nothing waits for the GPU, so calls may be
 captured into a HIP graph. Errors: SpzError.
 
-torch's autograd does not record the calls: gradients come from scan_backward, block_norm_backward and, for dropout,
-the same call on the gradient (quant_linear has none). Tensors that require a gradient are refused, so that none is
+torch's autograd does not record the calls: gradients come from scan_backward, block_norm_backward, head_norm_backward,
+linear_attention_backward and, for dropout, the same call on the gradient (quant_linear has none). Tensors that require a gradient are refused, so that none is
 lost; within torch.no_grad() they are taken. The calls work on data pointers: they are not for tracing or vmap.
 """
 from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import struct
-from typing import NamedTuple, Optional
+from typing import NamedTuple, Optional, Sequence
 
 import torch
 
-from .spz import GATES, NORMS, SPZ_EINVAL, SPZ_OK, SpzError, load, pack_block_norm, pack_scan
+from .spz import (ADAMW_BLOCK, GATES, NORMS, PAIRS, SPZ_EINVAL, SPZ_OK, SpzError, load, pack_adamw, pack_adamw_tensor,
+                  pack_block_norm, pack_head_norm, pack_linear_attention, pack_scan)
 
 _PREC = {torch.float32: 0, torch.bfloat16: 1}
 _F32 = torch.float32
@@ -435,3 +437,360 @@ def quant_linear(x, weights: QuantWeights, *, bias=None, out=None, stream=None):
     if rc:
         _done(rc)
     return y
+
+
+# ----------------------------------------------------------------------------- head norms
+
+def rotation_freqs(dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """Angles a position for head_norm: base^(-2 i / dim), i < dim / 2 (float64)."""
+    return torch.tensor([base ** (-2.0 * i / dim) for i in range(dim // 2)], dtype=torch.float64, device=device)
+
+
+def _head_check(q, k, vectors, norm, positions, freqs, pairs, valid) -> int:
+    gpu = _operand(q, "q", 3)
+    R, _, D = q.shape
+    if norm not in NORMS:
+        _refuse("norms are %s" % ", ".join(NORMS))
+    if pairs not in PAIRS:
+        _refuse("pairs are %s" % ", ".join(PAIRS))
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 3:
+            _refuse("k is no tensor [rows, heads, dim]")
+        _like(k, "k", gpu, (R, k.shape[1], D), q.dtype)
+    for i, t in enumerate(vectors):
+        if t is not None:
+            _like(t, ("w_q", "b_q", "w_k", "b_k")[i], gpu, (D,), _F32)
+    if (positions is None) != (freqs is None):
+        _refuse("positions and freqs come together")
+    if freqs is not None:
+        _like(positions, "positions", gpu, (R,), torch.int32, contiguous=True)
+        if not isinstance(freqs, torch.Tensor) or freqs.dim() != 1 or 2 * freqs.shape[0] > D:
+            _refuse("freqs is no tensor of at most dim / 2 angles")
+        _like(freqs, "freqs", gpu, freqs.shape, torch.float64, contiguous=True)
+    if valid is not None:
+        _like(valid, "valid", gpu, (R,), torch.bool if getattr(valid, "dtype", None) is torch.bool else torch.uint8, contiguous=True)
+    return gpu
+
+
+def _two(t):
+    """Strides of the rows and heads (no tensor: 0)."""
+    return (0, 0) if t is None else t.stride()[:2]
+
+
+def _pair_out(out, q, k, gpu, names):
+    """The two tensors of an `out` argument, checked (none: two None)."""
+    if out is None:
+        return None, None
+    if not isinstance(out, (tuple, list)) or len(out) != 2 or out[0] is None or (out[1] is None) != (k is None):
+        _refuse("out holds %s and %s" % names)
+    _like(out[0], names[0], gpu, q.shape, q.dtype)
+    if k is not None:
+        _like(out[1], names[1], gpu, k.shape, q.dtype)
+    return out
+
+
+def _head_pack(q, k, vectors, positions, freqs, valid, outs, back, grads, eps, norm, pairs) -> bytes:
+    """The argument block; outs: q_out, k_out; back: dq_out, dk_out, dq, dk; grads: dw_q, db_q, dw_k, db_k."""
+    R, H, D = q.shape
+    try:
+        return pack_head_norm(
+            R, H, 0 if k is None else k.shape[1], D, 0 if freqs is None else freqs.shape[0], q.data_ptr(), _ptr(k), *_two(q), *_two(k),
+            *map(_ptr, vectors), _ptr(positions), _ptr(freqs), _ptr(valid), _ptr(outs[0]), _ptr(outs[1]), *_two(outs[0]), *_two(outs[1]),
+            _ptr(back[0]), _ptr(back[1]), *_two(back[0]), *_two(back[1]), _ptr(back[2]), _ptr(back[3]), *_two(back[2]), *_two(back[3]),
+            *map(_ptr, grads), eps, NORMS[norm], PAIRS[pairs], _PREC[q.dtype])
+    except _NOT_NUMBERS as e:
+        _refuse("eps is no number: %s" % e)
+
+
+def head_norm(q, k=None, w_q=None, w_k=None, b_q=None, b_k=None, *, norm="rms", eps=1e-6, positions=None, freqs=None, pairs="halves",
+              valid=None, out=None, stream=None):
+    """norm(x) * w + b of each head of q [rows, heads, dim] and k [rows, other heads, dim] (None: no keys), with the
+    first 2 len(freqs) columns turned in pairs by the angle positions[row] * freqs[i] -> (q', k').
+
+    norm "none", "rms", "layer"; pairs "halves" (columns i and len(freqs) + i) or "neighbours" (2 i and 2 i + 1).
+    positions int32 [rows] and freqs float64 (rotation_freqs makes some) come together. Rows with valid == 0 are
+    not read, their outputs are zero. `out`: (q', k'); they may be q and k."""
+    lib = load()
+    vectors = (w_q, b_q, w_k, b_k)
+    gpu = _head_check(q, k, vectors, norm, positions, freqs, pairs, valid)
+    q_out, k_out = _pair_out(out, q, k, gpu, ("q'", "k'"))
+
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (q, k, *vectors, positions, freqs, valid, q_out, k_out),
+                          lambda: head_norm(q, k, w_q, w_k, b_q, b_k, norm=norm, eps=eps, positions=positions, freqs=freqs, pairs=pairs,
+                                            valid=valid, out=out))
+    s = _stream(gpu)
+    if q_out is None:
+        q_out, k_out = q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)
+    rc = lib.spz_head_norm_forward(_head_pack(q, k, vectors, positions, freqs, valid, (q_out, k_out), (None,) * 4, (None,) * 4, eps, norm, pairs), s)
+    if rc:
+        _done(rc)
+    return q_out, k_out
+
+
+def head_norm_backward(dq_out, dk_out, q, k=None, w_q=None, w_k=None, b_q=None, b_k=None, *, norm="rms", eps=1e-6, positions=None,
+                       freqs=None, pairs="halves", valid=None, out=None, stream=None):
+    """Gradients of head_norm from those of q' and k' (None: zeros): a dict of dq, dk and, for the vectors that were
+    given, dw_q, db_q, dw_k, db_k (float32, summed over rows and heads). `out`: (dq, dk), e.g. two parts of one."""
+    lib = load()
+    vectors = (w_q, b_q, w_k, b_k)
+    gpu = _head_check(q, k, vectors, norm, positions, freqs, pairs, valid)
+    _like(dq_out, "dq_out", gpu, q.shape, q.dtype)
+    if k is None and dk_out is not None:
+        _refuse("dk_out without k")
+    if k is not None:
+        _like(dk_out, "dk_out", gpu, k.shape, q.dtype)
+    dq, dk = _pair_out(out, q, k, gpu, ("dq", "dk"))
+
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (dq_out, dk_out, q, k, *vectors, positions, freqs, valid, dq, dk),
+                          lambda: head_norm_backward(dq_out, dk_out, q, k, w_q, w_k, b_q, b_k, norm=norm, eps=eps, positions=positions, freqs=freqs,
+                                                     pairs=pairs, valid=valid, out=out))
+    s = _stream(gpu)
+    if dq is None:
+        dq, dk = q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)
+    g = {"dq": dq, "dk": dk}
+    sums = iter(q.new_empty((4, q.shape[2]), dtype=_F32).unbind(0))
+    for name, t in zip(("dw_q", "db_q", "dw_k", "db_k"), vectors):
+        g[name] = None if t is None else next(sums)
+    a = _head_pack(q, k, vectors, positions, freqs, valid, (None, None), (dq_out, dk_out, dq, dk),
+                   (g["dw_q"], g["db_q"], g["dw_k"], g["db_k"]), eps, norm, pairs)
+    n = _size(lib.spz_head_norm_workspace(a))
+    ws = _workspace(n, q)
+    _done(lib.spz_head_norm_backward(a, _ptr(ws), n, s))
+    return g
+
+
+# ----------------------------------------------------------------------------- linear attention
+
+@functools.lru_cache(maxsize=4096)
+def _attention_sizes(B: int, T: int, H: int, K: int, V: int, prec: int):
+    """Bytes of the workspaces, forward and backward: functions of the sizes alone."""
+    lib = load()
+    a = pack_linear_attention(B, T, H, K, V, *([0] * 41), 0.0, prec)
+    return _size(lib.spz_linear_attention_workspace(a, 0)), _size(lib.spz_linear_attention_workspace(a, 1))
+
+
+def _attention_check(q, k, v, rate, state, reset, lengths) -> int:
+    gpu = _operand(q, "q", 4)
+    B, T, H, K = q.shape
+    if k is None or v is None:
+        _refuse("k or v is missing")
+    _like(k, "k", gpu, q.shape, q.dtype)
+    if not isinstance(v, torch.Tensor) or v.dim() != 4:
+        _refuse("v is no tensor [batch, steps, heads, width]")
+    _like(v, "v", gpu, (B, T, H, v.shape[3]), q.dtype)
+    _like(rate, "rate", gpu, (H,), _F32, contiguous=True)
+    _like(state, "state", gpu, (B, H, K, v.shape[3]), _F32, contiguous=True)
+    _like(lengths, "lengths", gpu, (B,), torch.int32, contiguous=True)
+    if reset is not None:
+        _flags_2d(reset, "reset", gpu, (B, T))
+    return gpu
+
+
+def _three(t):
+    """Strides of the batch, time and head dimensions (no tensor: 0)."""
+    return (0, 0, 0) if t is None else t.stride()[:3]
+
+
+def _steps(like: torch.Tensor, width: int) -> torch.Tensor:
+    """An empty [batch, steps, heads, width] tensor with the outer two dimensions in the order of like's."""
+    B, T, H, _ = like.shape
+    s = like.stride()
+    if s[0] < s[1] and B > 1:
+        return like.new_empty((T, B, H, width)).transpose(0, 1)
+    return like.new_empty((B, T, H, width))
+
+
+def linear_attention(q, k, v, rate=None, state=None, *, scale=None, reset=None, lengths=None, out=None, last=None, stream=None):
+    """S_t = exp(-rate) S_{t-1} + k_t^T v_t, y_t = scale q_t S_t in each head of q, k [batch, steps, heads, width] and
+    v [batch, steps, heads, other width] (at most 256 wide) -> (y, last).
+
+    rate: float32 [heads] (default zeros). state, last: float32 [batch, heads, width, other width], S in front
+    (default zeros) and behind; pass last=state to update a state in place. scale: default 1 / sqrt(width). reset
+    [batch, steps] (uint8 or bool): steps that start an episode, cut off from the state before. lengths [batch]
+    (int32): steps of each sequence; y is 0 behind it. Heads may share q, k or v (stride 0). `out`: y."""
+    lib = load()
+    gpu = _attention_check(q, k, v, rate, state, reset, lengths)
+    B, T, H, K = q.shape
+    V = v.shape[3]
+    _like(out, "out", gpu, v.shape, q.dtype)
+    _like(last, "last", gpu, (B, H, K, V), _F32, contiguous=True)
+    n = _attention_sizes(B, T, H, K, V, _PREC[q.dtype])[0]
+
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (q, k, v, rate, state, reset, lengths, out, last),
+                          lambda: linear_attention(q, k, v, rate, state, scale=scale, reset=reset, lengths=lengths, out=out, last=last))
+    s = _stream(gpu)
+    y = out if out is not None else _steps(q, V)
+    end = last if last is not None else q.new_empty((B, H, K, V), dtype=_F32)
+    ws = _workspace(n, q)
+    try:
+        a = pack_linear_attention(
+            B, T, H, K, V, q.data_ptr(), k.data_ptr(), v.data_ptr(), *_three(q), *_three(k), *_three(v), _ptr(rate), _ptr(reset), *_outer(reset),
+            _ptr(lengths), _ptr(state), y.data_ptr(), *_three(y), end.data_ptr(), *([0] * 18),
+            1.0 / math.sqrt(max(K, 1)) if scale is None else scale, _PREC[q.dtype])
+    except _NOT_NUMBERS as e:
+        _refuse("scale is no number: %s" % e)
+    rc = lib.spz_linear_attention_forward(a, _ptr(ws), n, s)
+    if rc:
+        _done(rc)
+    return y, end
+
+
+def linear_attention_backward(q, k, v, dy, rate=None, state=None, *, scale=None, dlast=None, reset=None, lengths=None, out=None, stream=None):
+    """Gradients (dq, dk, dv, dstate) of linear_attention's (y, last) from dy and dlast (None: zeros), with the forward
+    call's other arguments (`state` as it was before the call). Those of shared heads are one for each
+    head. `out`: the tensors (dq, dk, dv) to write, e.g. three parts of one."""
+    lib = load()
+    gpu = _attention_check(q, k, v, rate, state, reset, lengths)
+    B, T, H, K = q.shape
+    V = v.shape[3]
+    _like(dy, "dy", gpu, v.shape, q.dtype)
+    _like(dlast, "dlast", gpu, (B, H, K, V), _F32, contiguous=True)
+    if out is not None:
+        if not isinstance(out, (tuple, list)) or len(out) != 3 or any(t is None for t in out):
+            _refuse("out holds dq, dk and dv")
+        for name, t, w in zip(("dq", "dk", "dv"), out, (q, k, v)):
+            _like(t, name, gpu, w.shape, q.dtype)
+    n = _attention_sizes(B, T, H, K, V, _PREC[q.dtype])[1]
+
+    if stream is not None or gpu != _device():
+        return _elsewhere(stream, gpu, (q, k, v, dy, rate, state, dlast, reset, lengths) + tuple(out or ()),
+                          lambda: linear_attention_backward(q, k, v, dy, rate, state, scale=scale, dlast=dlast, reset=reset, lengths=lengths, out=out))
+    s = _stream(gpu)
+    dq, dk, dv = out if out is not None else (_steps(q, K), _steps(q, K), _steps(q, V))
+    dstate = q.new_empty((B, H, K, V), dtype=_F32)
+    ws = _workspace(n, q)
+    try:
+        a = pack_linear_attention(
+            B, T, H, K, V, q.data_ptr(), k.data_ptr(), v.data_ptr(), *_three(q), *_three(k), *_three(v), _ptr(rate), _ptr(reset), *_outer(reset),
+            _ptr(lengths), _ptr(state), 0, 0, 0, 0, 0, _ptr(dy), *_three(dy), _ptr(dlast), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+            *_three(dq), *_three(dk), *_three(dv), dstate.data_ptr(), 1.0 / math.sqrt(max(K, 1)) if scale is None else scale, _PREC[q.dtype])
+    except _NOT_NUMBERS as e:
+        _refuse("scale is no number: %s" % e)
+    _done(lib.spz_linear_attention_backward(a, _ptr(ws), n, s))
+    return dq, dk, dv, dstate
+
+
+# ----------------------------------------------------------------------------- AdamW
+
+class AdamW:
+    """AdamW over a list of contiguous float32 or bfloat16 GPU tensors, which step() updates in place.
+
+    bits=32: the moments are float32. bits=8: e4m3 codes (of the second moment's root, for v) with a scale for
+    each 256 of them, rounded at random by `seed` and the step, so that small changes count on average. `m`, `v` and,
+    for 8 bits, `m_scale`, `v_scale` hold the moments of all tensors one after the other, each from places[i] on, and are
+    the state to save; they start as zeros and may be copied into. copies: bfloat16 tensors that get each new value as
+    well (a list with None for none). weight_decay: a number, or one for each tensor."""
+
+    def __init__(self, params: Sequence[torch.Tensor], *, bits: int = 32, copies=None, weight_decay=0.0, seed: int = 0):
+        params = list(params)
+        if not params:
+            _refuse("no parameters")
+        if bits not in (8, 32):
+            _refuse("bits are 8 or 32")
+        first = params[0]
+        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+            _refuse("params[0] is no GPU tensor")
+        self._gpu = gpu = first.get_device()
+        copies = [None] * len(params) if copies is None else list(copies)
+        try:
+            decay = [float(d) for d in weight_decay] if hasattr(weight_decay, "__len__") else [float(weight_decay)] * len(params)
+            self._seed = int(seed) & 0xFFFFFFFFFFFFFFFF
+        except _NOT_NUMBERS as e:
+            _refuse("weight_decay or seed is no number: %s" % e)
+        if len(copies) != len(params) or len(decay) != len(params):
+            _refuse("copies and weight_decay have one entry for each tensor")
+        spans, at, self.places = [], 0, []
+        for i, (p, c, d) in enumerate(zip(params, copies, decay)):
+            self._tensor(p, "params[%d]" % i)
+            if c is not None:
+                if p.dtype is not _F32:
+                    _refuse("copies[%d] of a tensor that is not float32" % i)
+                if not isinstance(c, torch.Tensor) or c.requires_grad:
+                    _refuse("copies[%d] is no tensor, or requires a gradient" % i)
+                _like(c, "copies[%d]" % i, gpu, p.shape, torch.bfloat16, contiguous=True)
+            if not math.isfinite(d):
+                _refuse("weight_decay of params[%d] is not finite" % i)
+            spans += [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in (p, c) if t is not None and t.numel()]
+            self.places.append(at)
+            at += -(-p.numel() // ADAMW_BLOCK) * ADAMW_BLOCK
+        spans.sort()
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            _refuse("two of the tensors share elements")
+        self.params, self.copies, self.bits, self.weight_decay = params, copies, bits, decay
+        kind = torch.float8_e4m3fn if bits == 8 else _F32
+        dev = first.device
+        self.m, self.v = (torch.zeros(at, dtype=kind, device=dev) for _ in range(2))
+        self.m_scale, self.v_scale = (torch.zeros(at // ADAMW_BLOCK, device=dev) if bits == 8 else None for _ in range(2))
+        self._moments = at
+        self._layout = [(p.shape, p.dtype, p.data_ptr(), 0 if c is None else c.data_ptr()) for p, c in zip(params, copies)]
+
+    def _tensor(self, p, name):
+        if not isinstance(p, torch.Tensor) or p.get_device() != self._gpu or p.dtype not in _PREC or not p.is_contiguous():
+            _refuse("%s is no contiguous float32 or bfloat16 tensor on cuda:%d" % (name, self._gpu))
+        if p.requires_grad and not p.is_leaf:
+            _refuse("%s is not a leaf" % name)
+
+    def _state(self):
+        """The moments, which a user may have replaced by tensors of their own."""
+        kind = torch.float8_e4m3fn if self.bits == 8 else _F32
+        _like(self.m, "m", self._gpu, (self._moments,), kind, contiguous=True)
+        _like(self.v, "v", self._gpu, (self._moments,), kind, contiguous=True)
+        if self.bits == 8:
+            _like(self.m_scale, "m_scale", self._gpu, (self._moments // ADAMW_BLOCK,), _F32, contiguous=True)
+            _like(self.v_scale, "v_scale", self._gpu, (self._moments // ADAMW_BLOCK,), _F32, contiguous=True)
+
+    def step(self, grads, *, step, lr, betas=(0.9, 0.999), eps: float = 1e-8, grad_scale=None, stream=None):
+        """One update with the gradients (float32 or bfloat16, a list with None for tensors that stay as they are).
+
+        step: the count of this update, from 1, or an int64 GPU tensor of one element; lr: a number, or a float32
+        GPU tensor of one element. Tensors are read when the kernel runs, so that a captured graph follows them.
+        grad_scale: a float32 GPU tensor of one element that multiplies the gradients (a clip, a loss scale)."""
+        lib = load()
+        gpu = self._gpu
+        if not isinstance(grads, (tuple, list)) or len(grads) != len(self.params):
+            _refuse("grads is no list of %d" % len(self.params))
+        self._state()
+        for name, t, kind in (("step", step, torch.int64), ("lr", lr, _F32), ("grad_scale", grad_scale, _F32)):
+            if isinstance(t, torch.Tensor):
+                if t.numel() != 1:
+                    _refuse("%s has more than one element, or none" % name)
+                _like(t, name, gpu, t.shape, kind, contiguous=True)
+        if grad_scale is not None and not isinstance(grad_scale, torch.Tensor):
+            _refuse("grad_scale is no tensor")
+        groups = {}
+        for i, (p, c, g) in enumerate(zip(self.params, self.copies, grads)):
+            if g is None:
+                continue
+            if not isinstance(g, torch.Tensor) or g.dtype not in _PREC or g.shape != p.shape or g.get_device() != gpu or not g.is_contiguous():
+                _refuse("grads[%d] is no contiguous float32 or bfloat16 tensor %s on cuda:%d" % (i, tuple(p.shape), gpu))
+            if g.requires_grad and _grad_on():
+                _refuse_grad("grads[%d]" % i)
+            shape, kind, at, to = self._layout[i]
+            if p.shape != shape or p.dtype is not kind or p.data_ptr() != at or (c is not None and c.data_ptr() != to):
+                _refuse("params[%d] or its copy is not where it was: make another AdamW of the new tensors" % i)
+            groups.setdefault((_PREC[kind], _PREC[g.dtype]), []).append(
+                pack_adamw_tensor(at, g.data_ptr(), to, p.numel(), self.places[i], self.weight_decay[i]))
+
+        if stream is not None or gpu != _device():
+            tensors = [*self.params, *self.copies, *grads, self.m, self.v, self.m_scale, self.v_scale, grad_scale]
+            tensors += [t for t in (step, lr) if isinstance(t, torch.Tensor)]
+            return _elsewhere(stream, gpu, tensors, lambda: self.step(grads, step=step, lr=lr, betas=betas, eps=eps, grad_scale=grad_scale))
+        s = _stream(gpu)
+        on_step, on_lr = isinstance(step, torch.Tensor), isinstance(lr, torch.Tensor)
+        for (p_prec, g_prec), entries in groups.items():
+            block = b"".join(entries)
+            host = ctypes.create_string_buffer(block, len(block))
+            try:
+                b1, b2 = betas
+                a = pack_adamw(len(entries), self._moments, ctypes.addressof(host), self.m.data_ptr(), self.v.data_ptr(), _ptr(self.m_scale),
+                               _ptr(self.v_scale), _ptr(grad_scale), step.data_ptr() if on_step else 0, lr.data_ptr() if on_lr else 0,
+                               0 if on_step else step, 0.0 if on_lr else lr, b1, b2, eps, self._seed, self.bits, p_prec, g_prec, 0)
+            except _NOT_NUMBERS as e:
+                _refuse("step, lr, betas or eps is no number: %s" % e)
+            rc = lib.spz_adamw(a, s)
+            if rc:
+                _done(rc)
+        torch.autograd.graph.increment_version([p for p, g in zip(self.params, grads) if g is not None])

@@ -37,9 +37,12 @@ EXPORTS = ["spz_hparams_default", "spz_create", "spz_destroy", "spz_buffer_push"
            "spz_scan_saved", "spz_scan_workspace", "spz_scan_forward", "spz_scan_backward",
            "spz_block_norm_workspace", "spz_block_norm_forward", "spz_block_norm_backward", "spz_dropout",
            "spz_quant_rows", "spz_quant_image_bytes", "spz_quant_pack", "spz_quant_linear_workspace",
-           "spz_quant_linear"]
+           "spz_quant_linear", "spz_head_norm_workspace", "spz_head_norm_forward", "spz_head_norm_backward",
+           "spz_linear_attention_workspace", "spz_linear_attention_forward", "spz_linear_attention_backward", "spz_adamw"]
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 GATES = {"none": 0, "sigmoid": 1, "silu": 2}
+PAIRS = {"halves": 0, "neighbours": 1}
+ADAMW_BLOCK = 256
 
 
 class SpzError(RuntimeError):
@@ -69,7 +72,7 @@ class KernelStat(ctypes.Structure):
 def _fields(**groups):
     """ctypes fields, a type's names after each other: I64="a b" etc., in the given order."""
     types = {"I64": ctypes.c_int64, "P": ctypes.c_void_p, "I32": ctypes.c_int32, "U64": ctypes.c_uint64,
-             "U32": ctypes.c_uint32, "F32": ctypes.c_float}
+             "U32": ctypes.c_uint32, "F32": ctypes.c_float, "F64": ctypes.c_double}
     return [(n, types[k.split("_")[0]]) for k, names in groups.items() for n in names.split()]
 
 
@@ -88,16 +91,44 @@ class BlockNormArgs(ctypes.Structure):
                        I32="post pre gate prec")
 
 
+class HeadNormArgs(ctypes.Structure):
+    _fields_ = _fields(I64="rows heads_q heads_k dim pairs", P="q k", I64_1="q_row q_head k_row k_head",
+                       P_1="w_q b_q w_k b_k positions freqs valid q_out k_out",
+                       I64_2="q_out_row q_out_head k_out_row k_out_head", P_2="dq_out dk_out",
+                       I64_3="dq_out_row dq_out_head dk_out_row dk_out_head", P_3="dq dk",
+                       I64_4="dq_row dq_head dk_row dk_head", P_4="dw_q db_q dw_k db_k", F32="eps", I32="norm layout prec")
+
+
+class LinearAttentionArgs(ctypes.Structure):
+    _fields_ = _fields(I64="batch steps heads key_width value_width", P="q k v",
+                       I64_1="q_batch q_step q_head k_batch k_step k_head v_batch v_step v_head", P_1="rate reset",
+                       I64_2="reset_batch reset_step", P_2="lengths state y", I64_3="y_batch y_step y_head", P_3="last dy",
+                       I64_4="dy_batch dy_step dy_head", P_4="dlast dq dk dv",
+                       I64_5="dq_batch dq_step dq_head dk_batch dk_step dk_head dv_batch dv_step dv_head", P_5="dstate",
+                       F32="scale", I32="prec")
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = _fields(P="p g copy", I64="n at", F64="weight_decay")
+
+
+class AdamwArgs(ctypes.Structure):
+    _fields_ = _fields(I64="count moments", P="tensors m v m_scale v_scale grad_scale step_at lr_at", I64_1="step",
+                       F64="lr beta1 beta2 eps", U64="seed", I32="bits p_prec g_prec reserved")
+
+
 def _packer(c) -> struct.Struct:
     """The struct as bytes from all its fields in order: a tenth of the time of setting them."""
     codes = {ctypes.c_int64: "q", ctypes.c_void_p: "P", ctypes.c_int32: "i", ctypes.c_uint64: "Q",
-             ctypes.c_uint32: "I", ctypes.c_float: "f"}
+             ctypes.c_uint32: "I", ctypes.c_float: "f", ctypes.c_double: "d"}
     p = struct.Struct("@" + "".join(codes[t] for _, t in c._fields_) + "0q")
     assert p.size == ctypes.sizeof(c)
     return p
 
 
 pack_scan, pack_block_norm = _packer(ScanArgs).pack, _packer(BlockNormArgs).pack
+pack_head_norm, pack_linear_attention = _packer(HeadNormArgs).pack, _packer(LinearAttentionArgs).pack
+pack_adamw, pack_adamw_tensor = _packer(AdamwArgs).pack, _packer(AdamwTensor).pack
 
 _lib = None
 
@@ -161,6 +192,13 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "spz_quant_pack": (ctypes.c_int, [I64, I64, P, I64, P, P]),
         "spz_quant_linear_workspace": (I64, [I32, I64, I64, I64]),
         "spz_quant_linear": (ctypes.c_int, [I32, I64, I64, I64, P, I64, P, P, P, P, I64, P, I64, P]),
+        "spz_head_norm_workspace": (I64, [na]),
+        "spz_head_norm_forward": (ctypes.c_int, [na, P]),
+        "spz_head_norm_backward": (ctypes.c_int, [na, P, I64, P]),
+        "spz_linear_attention_workspace": (I64, [sa, I32]),
+        "spz_linear_attention_forward": (ctypes.c_int, [sa, P, I64, P]),
+        "spz_linear_attention_backward": (ctypes.c_int, [sa, P, I64, P]),
+        "spz_adamw": (ctypes.c_int, [P, P]),
     })
     for name, (res, args) in sig.items():
         f = getattr(lib, name)

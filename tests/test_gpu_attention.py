@@ -1,0 +1,295 @@
+"""Linear attention on the GPU against float64 (more_ops_reference.py), with its bounds.
+
+Sizes cover one step, every remainder of a chunk of 64 steps, odd head widths up to the largest, sequences of no
+steps, episode starts everywhere, rates from none to infinite, strides, shared heads, values that are not finite in
+masked places, streams and graphs.
+"""
+import numpy as np
+import pytest
+
+from . import more_ops_reference as ref
+from .helpers import log
+from .test_gpu_ops import PRECS, check, gpu, host, torch_
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(rng, B, T, H, K, V, prec, resets=True, ragged=True, p_reset=0.08):
+    t = {n: gpu(rng.standard_normal((B, T, H, w)), prec) for n, w in (("q", K), ("k", K), ("v", V), ("dy", V))}
+    t.update(state=gpu(rng.standard_normal((B, H, K, V))), dlast=gpu(rng.standard_normal((B, H, K, V))),
+             rate=gpu(np.array([0.7 * 0.1 ** h for h in range(H)])))
+    reset = (rng.random((B, T)) < p_reset).astype(np.uint8) if resets else None
+    lengths = None
+    if ragged:
+        lengths = rng.integers(0, T + 1, B).astype(np.int32)
+        lengths[0] = T
+        if B > 1:
+            lengths[-1] = 0
+    return t, reset, lengths
+
+
+def run(t, reset=None, lengths=None, layout=lambda x: x, scale=None, outs=None, **kw):
+    """All results of a forward and a backward call."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    a = dict(rate=t.get("rate"), state=t.get("state"), scale=scale, reset=None if reset is None else torch.from_numpy(reset).cuda(),
+             lengths=None if lengths is None else torch.from_numpy(lengths).cuda(), **kw)
+    q, k, v, dy = (layout(t[n]) for n in ("q", "k", "v", "dy"))
+    y, last = ops.linear_attention(q, k, v, out=None if outs is None else outs[0], **a)
+    dq, dk, dv, dstate = ops.linear_attention_backward(q, k, v, dy, dlast=t.get("dlast"), out=None if outs is None else outs[1:], **a)
+    return dict(y=y, last=last, dq=dq, dk=dk, dv=dv, dstate=dstate)
+
+
+def check_all(got, t, reset, lengths, prec, scale=None):
+    x = {n: host(t[n]) for n in t}
+    want = ref.attention(x["q"], x["k"], x["v"], x.get("rate"), x.get("state"), x["q"].shape[3] ** -0.5 if scale is None else scale, reset, lengths,
+                         x["dy"], x.get("dlast"), prec)
+    for n, v in got.items():
+        check(n, v, want[n], "fp32" if n in ("last", "dstate") else prec)
+
+
+SHAPES = [(1, 1, 1, 1, 1), (3, 1, 2, 16, 16), (2, 2, 1, 5, 3), (2, 17, 2, 8, 24), (3, 50, 2, 64, 64), (1, 63, 1, 32, 33), (2, 64, 2, 40, 39),
+          (2, 65, 1, 64, 64), (1, 130, 2, 7, 64), (2, 200, 1, 128, 64), (1, 129, 1, 64, 128), (1, 70, 1, 256, 256), (2, 96, 1, 100, 200),
+          (1, 1000, 1, 16, 16), (5, 33, 3, 24, 8), (40, 5, 4, 64, 64), (1, 300, 2, 33, 65), (2, 8, 1, 256, 7), (1, 128, 1, 96, 160)]
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_attention(shape, prec):
+    log("attention %s %s" % (shape, prec))
+    rng = np.random.default_rng(sum(shape))
+    for resets, ragged in ((False, False), (True, True)):
+        t, reset, lengths = inputs(rng, *shape, prec, resets, ragged)
+        got = run(t, reset, lengths)
+        check_all(got, t, reset, lengths, prec)
+        again = run(t, reset, lengths)
+        assert all(torch_().equal(got[n], again[n]) for n in got)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("T", [3, 90, 200])
+def test_attention_rates_scales_and_absent_states(T, prec):
+    """Rates from none to infinite, scales of 0 and below, no state in front, no gradient behind."""
+    rng = np.random.default_rng(T)
+    t, reset, lengths = inputs(rng, 3, T, 5, 24, 40, prec)
+    t["rate"] = gpu(np.array([0.0, 1e-4, 0.5, 30.0, np.inf]))
+    for scale in (None, -0.3, 0.0):
+        check_all(run(t, reset, lengths, scale=scale), t, reset, lengths, prec, scale)
+    for gone in (("rate",), ("state", "dlast"), ("rate", "state", "dlast")):
+        u = {n: x for n, x in t.items() if n not in gone}
+        check_all(run(u, reset, lengths), u, reset, lengths, prec)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("T", [5, 64, 150])
+def test_attention_starts_everywhere(T, prec):
+    """Each step an episode of its own; the first step of all only; the first of each chunk; bool flags in columns."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(7)
+    t, _, lengths = inputs(rng, 2, T, 2, 32, 48, prec)
+    for marks in (np.ones(T), np.arange(T) == 0, np.arange(T) % 64 == 0, np.arange(T) == T - 1, np.arange(T) % 64 == 63):
+        reset = np.tile(marks.astype(np.uint8), (2, 1))
+        check_all(run(t, reset, lengths), t, reset, lengths, prec)
+    flags = torch.from_numpy(reset.T.copy()).cuda().bool().t()
+    n = torch.from_numpy(lengths).cuda()
+    y, last = ops.linear_attention(t["q"], t["k"], t["v"], t["rate"], t["state"], reset=flags, lengths=n)
+    want = run(t, reset, lengths)
+    assert torch.equal(y, want["y"]) and torch.equal(last, want["last"])
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("shape", [(3, 20, 2, 64, 64), (2, 100, 3, 40, 24), (2, 70, 2, 13, 9)], ids=str)
+def test_attention_layouts(shape, prec):
+    """Time-major arrays, heads in front of time, parts of one projection, odd distances and starts; outputs in such places."""
+    torch = torch_()
+    rng = np.random.default_rng(8)
+    B, T, H, K, V = shape
+    t, reset, lengths = inputs(rng, *shape, prec)
+    want = run(t, reset, lengths)
+    check_all(want, t, reset, lengths, prec)
+
+    def time_major(x):
+        return x.transpose(0, 1).contiguous().transpose(0, 1)
+
+    def heads_first(x):
+        return x.transpose(1, 2).contiguous().transpose(1, 2)
+
+    def part(x):
+        w = torch.full((B, T, H * x.shape[3] * 3), float("nan"), dtype=x.dtype, device="cuda")
+        w = w[..., H * x.shape[3]:2 * H * x.shape[3]].unflatten(2, (H, x.shape[3]))
+        return w.copy_(x)
+
+    def odd(x):
+        w = torch.full((B, T + 1, H + 1, x.shape[3] + 3), float("nan"), dtype=x.dtype, device="cuda")
+        w = w[:, 1:, :H, 1:x.shape[3] + 1]
+        return w.copy_(x)
+
+    for layout in (time_major, heads_first, part, odd):
+        log("attention %s %s %s" % (layout.__name__, shape, prec))
+        outs = tuple(layout(torch.zeros((B, T, H, w), dtype=t["q"].dtype, device="cuda")) for w in (V, K, K, V))
+        for o in (None, outs):
+            got = run(t, reset, lengths, layout, outs=o)
+            assert all(torch.equal(got[n], want[n]) for n in want), layout.__name__
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("T", [1, 100])
+def test_attention_shared_heads(T, prec):
+    """Keys and values that heads share (stride 0) give what copies of them do; gradients are one for each head."""
+    torch = torch_()
+    rng = np.random.default_rng(9)
+    t, reset, lengths = inputs(rng, 2, T, 4, 32, 32, prec)
+    for n in "kv":
+        t[n] = t[n][:, :, :1].expand(-1, -1, 4, -1)
+    u = dict(t, k=t["k"].contiguous(), v=t["v"].contiguous())
+    got, want = run(t, reset, lengths), run(u, reset, lengths)
+    assert all(torch.equal(got[n], want[n]) for n in want)
+    check_all(got, u, reset, lengths, prec)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("T,K,V", [(7, 24, 40), (100, 24, 40), (192, 64, 64)])
+def test_attention_masked_values_do_not_matter(T, K, V, prec):
+    """Infinities and NaN behind a sequence's length, and in front of an episode start in the forward results and behind one's
+    end in the gradients; the step that holds them is not finite, and none in front of it is affected."""
+    torch = torch_()
+    rng = np.random.default_rng(10)
+    t, _, _ = inputs(rng, 4, T, 2, K, V, prec)
+    lengths = np.array([T, T - 1, T // 2 + 1, 0], np.int32)
+    reset = np.zeros((4, T), np.uint8)
+    reset[:, T // 2] = 1
+    clean = {n: x.clone() for n, x in t.items()}
+    for b in range(4):
+        for n in ("q", "k", "v", "dy"):
+            t[n][b, lengths[b]:] = float("nan")
+            t[n][b, lengths[b] + 1:] = float("-inf")
+    got, want = run(t, reset, lengths), run(clean, reset, lengths)
+    assert all(torch.equal(got[n], want[n]) for n in want)
+    check_all(got, clean, reset, lengths, prec)
+    bad = T // 2 - 1                                    # the last step of the first episode
+    for n, value in (("k", float("inf")), ("v", float("nan")), ("q", float("nan"))):
+        u = dict(clean, **{n: clean[n].clone()})
+        u[n][0, bad, 0, 0] = value
+        got = run(u, reset, lengths)
+        assert torch.isfinite(got["last"]).all()
+        same = torch.ones((T,), dtype=torch.bool)
+        same[bad] = False
+        if n == "q":                                    # only its own row, and the gradients of its episode
+            assert torch.equal(got["y"][0, same], want["y"][0, same])
+        else:
+            check("last", got["last"], ref_of(clean, reset, lengths, prec)["last"], "fp32")
+            check("y in front", got["y"][:, :bad], tuple(x[:, :bad] for x in ref_of(clean, reset, lengths, prec)["y"]), prec)
+        check("y behind", got["y"][:, T // 2:], tuple(x[:, T // 2:] for x in ref_of(clean, reset, lengths, prec)["y"]), prec)
+        assert not torch.isfinite(got["y"][0, bad, 0].float()).all()
+        for g in ("dq", "dk", "dv"):                    # steps of the episode behind
+            check(g, got[g][:, T // 2:], tuple(x[:, T // 2:] for x in ref_of(clean, reset, lengths, prec)[g]), prec)
+    u = dict(clean, state=clean["state"] * float("nan"), dlast=clean["dlast"] * float("inf"))
+    got = run(u, reset, lengths)
+    w = ref_of(clean, reset, lengths, prec)
+    check("y", got["y"][:2, T // 2:], tuple(x[:2, T // 2:] for x in w["y"]), prec)
+    check("last", got["last"][:2], tuple(x[:2] for x in w["last"]), "fp32")
+    check("dk", got["dk"][:2, :T // 2], tuple(x[:2, :T // 2] for x in w["dk"]), prec)
+    check("dstate", got["dstate"][:2], tuple(x[:2] for x in w["dstate"]), "fp32")
+
+
+def ref_of(t, reset, lengths, prec):
+    x = {n: host(t[n]) for n in t}
+    return ref.attention(x["q"], x["k"], x["v"], x["rate"], x["state"], x["q"].shape[3] ** -0.5, reset, lengths, x["dy"], x["dlast"], prec)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("K,V", [(64, 64), (13, 40)])
+def test_attention_steps_in_place_are_the_sequence(K, V, prec):
+    """40 single steps that update a state in place, as samplers take them, against one call."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(11)
+    t, reset, _ = inputs(rng, 16, 40, 2, K, V, prec, ragged=False)
+    want = ref_of(t, reset, None, prec)
+    flags = torch.from_numpy(reset).cuda()
+    state = t["state"].clone()
+    ys = []
+    for i in range(40):
+        y, s = ops.linear_attention(*(t[n][:, i:i + 1] for n in ("q", "k", "v")), t["rate"], state, reset=flags[:, i:i + 1], last=state)
+        assert s is state
+        ys.append(y)
+    check("y", torch.cat(ys, 1), want["y"], prec)
+    check("last", state, want["last"], "fp32")
+
+
+def test_attention_of_nothing():
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    for B, T, H, K, V in ((0, 5, 2, 8, 8), (2, 0, 2, 8, 8), (2, 5, 0, 8, 8), (2, 5, 2, 0, 8), (2, 5, 2, 8, 0), (2, 70, 1, 0, 3), (2, 70, 1, 3, 0)):
+        q, v = torch.ones((B, T, H, K), device="cuda"), torch.ones((B, T, H, V), device="cuda")
+        s = torch.ones((B, H, K, V), device="cuda")
+        y, last = ops.linear_attention(q, q, v, state=s)
+        dq, dk, dv, ds = ops.linear_attention_backward(q, q, v, v, state=s, dlast=s)
+        assert y.shape == v.shape and dq.shape == q.shape and dv.shape == v.shape
+        if T == 0:
+            assert torch.equal(last, s) and torch.equal(ds, s)
+        if K == 0:
+            assert not y.any() and not dv.any()
+        if V == 0:
+            assert not dq.any() and not dk.any()
+
+
+def test_attention_lengths_are_clamped():
+    torch = torch_()
+    rng = np.random.default_rng(12)
+    t, reset, _ = inputs(rng, 3, 70, 1, 16, 16, "fp32", ragged=False)
+    a = run(t, reset, np.array([-5, 1000, 70], np.int32))
+    b = run(t, reset, np.array([0, 70, 70], np.int32))
+    assert all(torch.equal(a[n], b[n]) for n in a)
+
+
+def test_attention_gradient_against_differences():
+    """Float32: y and last are linear in each of q, k, v and the state by itself, so a difference has no error but rounding
+    (2^-24 of the sum of the terms, a hundred times over)."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(13)
+    t, reset, lengths = inputs(rng, 2, 75, 2, 24, 17, "fp32")
+    r, n = torch.from_numpy(reset).cuda(), torch.from_numpy(lengths).cuda()
+    got = run(t, reset, lengths)
+    live = (torch.arange(75, device="cuda")[None] < n[:, None])[..., None, None]
+
+    def loss(x):
+        y, last = ops.linear_attention(x["q"], x["k"], x["v"], x["rate"], x["state"], reset=r, lengths=n)
+        return float((y.double() * torch.where(live, t["dy"], 0.0).double()).sum() + (last.double() * t["dlast"].double()).sum())
+
+    for name in ("q", "k", "v", "state"):
+        d = gpu(rng.standard_normal(t[name].shape))
+        up, down = dict(t, **{name: t[name] + d}), dict(t, **{name: t[name] - d})
+        terms = got["d" + name].double() * d.double()
+        assert abs((loss(up) - loss(down)) / 2 - float(terms.sum())) < 1e-4 * float(terms.abs().sum()), name
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("shape", [(4, 1, 2, 64, 64), (2, 150, 2, 64, 64), (1, 1500, 1, 32, 32)], ids=str)
+def test_attention_streams_and_graphs(shape, prec):
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(14)
+    t, reset, lengths = inputs(rng, *shape, prec)
+    want = run(t, reset, lengths)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = run(t, reset, lengths, stream=side)
+    side.synchronize()
+    assert all(torch.equal(got[n], want[n]) for n in want)
+    r, n = torch.from_numpy(reset).cuda(), torch.from_numpy(lengths).cuda()
+    a = dict(rate=t["rate"], state=t["state"], reset=r, lengths=n)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, last = ops.linear_attention(t["q"], t["k"], t["v"], **a)
+        grads = ops.linear_attention_backward(t["q"], t["k"], t["v"], t["dy"], dlast=t["dlast"], **a)
+    for _ in range(3):
+        for x in (y, last, *grads):
+            x.fill_(7.0)
+        graph.replay()
+        again = run(t, reset, lengths)
+        torch.cuda.synchronize()
+        for name, x in zip(("y", "last", "dq", "dk", "dv", "dstate"), (y, last, *grads)):
+            assert torch.equal(x, want[name]) and torch.equal(again[name], want[name]), name
