@@ -23,8 +23,11 @@ struct LinRole {
 };
 struct LinArgs {
   LinRole role[3];
-  int roles;
+  int roles, units;                          // units: workgroups of a piece of a head
   int64_t batch, steps, heads, first;
+  int64_t pieces, len;                       // of time, len steps each
+  const float* inits[3];                     // states in front of the pieces [batch, heads, pieces, ..], or NULL
+  float *adds[2], *keeps[2];                 // what the pieces add, and keep, of the states of the first two roles
   const float* rate;
   const uint8_t* reset; int64_t reset_batch, reset_step;
   const int32_t* lengths;
@@ -114,6 +117,416 @@ template <typename T, int KR> __global__ __launch_bounds__(STEP_THREADS) void li
     }
 }
 
+// ----------------------------------------------------------------------------- chunks of steps
+// CL steps at a time on the matrix cores. Within a chunk, with s <= t steps of one episode, e(n) = exp(-rate n) and
+// n the chunk's steps:
+//     o_t = out (sum_s e(t - s) in (a_t b_s) c_s + e(t + 1) a_t R),   R' = e(n) R + sum_s e(n - 1 - s) in b_s^T c_s.
+// A workgroup of four waves holds the state of 64 columns in the matrix instructions' accumulators, a wave 16 of them.
+// The scores a_t b_s are shared through LDS; everything else is a wave's own. All products are taken so that a lane
+// ends with four consecutive elements of what it stores (o as its transpose), and the accumulators of the state are
+// operands of the next product as they stand: the order of the contraction is the same for both operands.
+// bfloat16 operands: the scores and the state enter a product as two bfloat16 numbers each (2^-17 of each is lost, less
+// than an output's rounding), the weighted c, from which the state is summed, as three (all 24 bits).
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+#define LDS_PTR(T) __attribute__((address_space(3))) T*
+
+constexpr int CHUNK_THREADS = 256, CHUNK_COLS = 64;
+
+template <typename T> struct Mat;
+template <> struct Mat<bf16_t> {
+  static constexpr int KB = 32, PAD = 8;               // contraction of one instruction; LDS elements behind a row
+  static constexpr int SCORE_PARTS = 2, STATE_PARTS = 2, VALUE_PARTS = 3;
+  typedef bf16x8 frag;
+  static constexpr int N = 8;                          // elements of a lane's fragment
+  static __device__ inline void mma(f32x4& acc, const frag& a, const frag& b) { acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0); }
+  // Row row0 + lane % 16, columns k0 + 8 (lane / 16) ..
+  static __device__ inline frag row(const bf16_t* p, int pitch, int row0, int k0, int i, int g) {
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + (row0 + i) * pitch + k0 + 8 * g));
+  }
+  // The same row, in the state's order: columns k0 + 4 (lane / 16) .. and the same 16 further.
+  static __device__ inline frag row_state(const bf16_t* p, int pitch, int row0, int k0, int i, int g) {
+    const bf16_t* q = p + (row0 + i) * pitch + k0 + 4 * g;
+    const u32x2 lo = *reinterpret_cast<const u32x2*>(q), hi = *reinterpret_cast<const u32x2*>(q + 16);
+    return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+  }
+  // Column col0 + lane % 16, rows k0 + 8 (lane / 16) ..: 16 lanes read four rows of 16 elements, each lane four of one
+  // row, and the instruction hands lane i column i.
+  static __device__ inline frag col(const bf16_t* p, int pitch, int k0, int col0, int i, int g) {
+    const bf16_t* q = p + (k0 + 8 * g + (i >> 2)) * pitch + col0 + 4 * (i & 3);
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(q));
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(q + 4 * pitch));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  static __device__ inline float at(const frag& f, int j) { return (float)f[j]; }
+  // x as PARTS fragments whose sum it is (to 8 bits more with each).
+  template <int PARTS> static __device__ inline void split(const float (&x)[8], frag (&f)[PARTS]) {
+    float r[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = x[j];
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[j] = pack_bf16x2(r[2 * j], r[2 * j + 1]);
+        r[2 * j] -= __builtin_bit_cast(float, w[j] << 16);
+        r[2 * j + 1] -= __builtin_bit_cast(float, w[j] & 0xFFFF0000u);
+      }
+      f[k] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+    }
+  }
+  // Four scores to each of the parts' arrays.
+  static __device__ inline void put(bf16_t* p, int part_size, const f32x4& x) {
+    float r[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+    for (int k = 0; k < SCORE_PARTS; ++k) {
+      const u32x2 w = {pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
+      *reinterpret_cast<u32x2*>(p + k * part_size) = w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r[j] -= __builtin_bit_cast(float, j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+    }
+  }
+  // Largest magnitudes of two elements a word, as their bits.
+  static __device__ inline uint32_t most(uint32_t m, uint32_t w) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)));
+  }
+  static __device__ inline bool finite(uint32_t m) { return (m & 0xFFFFu) < 0x7F80u && (m >> 16) < 0x7F80u; }
+};
+template <> struct Mat<float> {
+  static constexpr int KB = 16, PAD = 4;
+  static constexpr int SCORE_PARTS = 1, STATE_PARTS = 1, VALUE_PARTS = 1;
+  typedef f32x4 frag;
+  static constexpr int N = 4;
+  static __device__ inline void mma(f32x4& acc, const frag& a, const frag& b) {   // four instructions of four elements
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], acc, 0, 0, 0);
+  }
+  static __device__ inline frag row(const float* p, int pitch, int row0, int k0, int i, int g) {
+    return *reinterpret_cast<const f32x4*>(p + (row0 + i) * pitch + k0 + 4 * g);
+  }
+  static __device__ inline frag row_state(const float* p, int pitch, int row0, int k0, int i, int g) { return row(p, pitch, row0, k0, i, g); }
+  static __device__ inline frag col(const float* p, int pitch, int k0, int col0, int i, int g) {
+    const float* q = p + (k0 + 4 * g) * pitch + col0 + i;
+    return f32x4{q[0], q[pitch], q[2 * pitch], q[3 * pitch]};
+  }
+  static __device__ inline float at(const frag& f, int j) { return f[j]; }
+  template <int PARTS> static __device__ inline void split(const float (&x)[4], frag (&f)[PARTS]) { f[0] = f32x4{x[0], x[1], x[2], x[3]}; }
+  static __device__ inline void put(float* p, int, const f32x4& x) { *reinterpret_cast<f32x4*>(p) = x; }
+  static __device__ inline uint32_t most(uint32_t m, uint32_t w) {
+    w &= 0x7FFFFFFFu;
+    return w > m ? w : m;
+  }
+  static __device__ inline bool finite(uint32_t m) { return m < 0x7F800000u; }
+};
+
+// CL steps of W columns (zeros past `width` and past the sequence) on their way from memory to LDS.
+template <typename T, int W, int CL> struct Tile {
+  static constexpr int VW = OP_VEC<T>, VR = W / VW, N = CL * VR / CHUNK_THREADS, PITCH = W + Mat<T>::PAD;
+  static_assert(CL * VR % CHUNK_THREADS == 0, "whole vectors a thread");
+  u32x4 v[N];
+  // t(p): the step at place p; places from n on are behind the sequence.
+  template <typename F> __device__ inline void load(const T* base, int64_t step, int64_t p0, int64_t n, int width, F&& t) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int e = threadIdx.x + CHUNK_THREADS * j, c = e % VR * VW;
+      const int64_t p = p0 + e / VR;
+      v[j] = u32x4{0, 0, 0, 0};
+      if (p < n && c < width) {
+        const T* q = base + t(p) * step + c;
+        v[j] = c + VW <= width ? load16(q) : load_part(q, width - c);
+      }
+    }
+  }
+  __device__ inline void clear() {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = u32x4{0, 0, 0, 0};
+  }
+  __device__ inline void store(T* lds) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int e = threadIdx.x + CHUNK_THREADS * j;
+      *reinterpret_cast<u32x4*>(lds + e / VR * PITCH + e % VR * VW) = v[j];
+    }
+  }
+  __device__ inline uint32_t most(uint32_t m) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m = Mat<T>::most(m, v[j][k]);
+    return m;
+  }
+};
+
+// log2 of d, kept finite, so that no steps are a factor of 1 at an infinite rate too (NaN stays).
+__device__ inline float lin_log2(float rate) {
+  const float x = rate * -1.44269504088896341f;
+  return x < -1e30f ? -1e30f : x > 1e30f ? 1e30f : x;
+}
+__device__ inline float lin_power(float log2d, int n) { return __builtin_amdgcn_exp2f(log2d * (float)n); }
+
+// The workgroups of a launch: the slices of all roles of a piece of a head follow each other on one XCD, whose L2 holds
+// what they share.
+// A workgroup: slice of a role, head, sequence, piece of time. STATE: only what the piece adds to the state.
+template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(CHUNK_THREADS, 2) void lin_chunks(LinArgs g) {
+  using M = Mat<T>;
+  typedef typename M::frag frag;
+  constexpr int TILES = KP / 16, ROWS = CL / 16, PA = KP + M::PAD, PC = CHUNK_COLS + M::PAD, PS = CL + M::PAD, SCORES = CL * PS;
+  __shared__ __align__(16) T lds_a[STATE ? 1 : CL * PA];
+  __shared__ __align__(16) T lds_b[CL * PA];
+  __shared__ __align__(16) T lds_c[CL * PC];
+  __shared__ __align__(16) T lds_p[STATE ? 1 : M::SCORE_PARTS * SCORES];
+  __shared__ int odd[2];
+  const int64_t block = g.first + blockIdx.x, group = block / 8 / g.units * 8 + block % 8;
+  if (group >= g.batch * g.heads * g.pieces) return;
+  int unit = (int)(block / 8 % g.units), which = 0;
+  while (unit >= (g.role[which].nc + CHUNK_COLS - 1) / CHUNK_COLS) unit -= (g.role[which++].nc + CHUNK_COLS - 1) / CHUNK_COLS;
+  const LinRole& r = g.role[which];
+  const int64_t piece = group % g.pieces, h = group / g.pieces % g.heads, b = group / g.pieces / g.heads;
+  const int c0 = unit * CHUNK_COLS, cols = r.nc - c0 < CHUNK_COLS ? r.nc - c0 : CHUNK_COLS, ka = r.ka;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+  const int64_t n = lin_length(g, b), begin = piece * g.len, stop = begin + g.len < n ? begin + g.len : n;
+  const bool back = r.back;
+  const float log2d = lin_log2(g.rate ? g.rate[h] : 0.0f);
+  const auto time = [&](int64_t p) { return back ? n - 1 - p : p; };
+  const T* pa = r.a ? static_cast<const T*>(r.a) + b * r.a_batch + h * r.a_head : nullptr;
+  const T* pb = r.b ? static_cast<const T*>(r.b) + b * r.b_batch + h * r.b_head : nullptr;
+  const T* pc = r.c ? static_cast<const T*>(r.c) + b * r.c_batch + h * r.c_head + c0 : nullptr;
+  T* po = STATE ? nullptr : static_cast<T*>(r.out) + b * r.out_batch + h * r.out_head + c0;
+  const uint8_t* flags = g.reset ? g.reset + b * g.reset_batch : nullptr;
+  // Whether place p starts an episode in the order of the walk (backward: whether the step behind it does).
+  const auto starts = [&](int64_t p) {
+    if (!flags || p >= stop) return 0;
+    if (back) return p == 0 ? 0 : (int)flags[(n - p) * g.reset_step];
+    return (int)flags[p * g.reset_step];
+  };
+
+  f32x4 S[TILES];
+  const int col = 16 * wave + i;
+  const bool mine = col < cols;
+#pragma unroll
+  for (int k = 0; k < TILES; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = 16 * k + 4 * q + e;
+      const float* init = g.inits[which] ? g.inits[which] + ((b * g.heads + h) * g.pieces + piece) * ka * r.nc : r.init ? r.init + (b * g.heads + h) * ka * r.nc : nullptr;
+      S[k][e] = !STATE && init && mine && row < ka ? init[row * r.row_stride + (c0 + col) * r.col_stride] : 0.0f;
+    }
+  if constexpr (!STATE && M::KB == 32) {   // scores above the diagonal that share an instruction with scores below it
+    for (int e = threadIdx.x; e < M::SCORE_PARTS * SCORES; e += CHUNK_THREADS) lds_p[e] = from_f<T>(0.0f);
+  }
+  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+  float keep = 1.0f;   // STATE: what is left of the state in front of the piece
+  Tile<T, KP, CL> ta, tb;
+  Tile<T, CHUNK_COLS, CL> tc;
+  const auto fetch = [&](int64_t p0) {
+    if constexpr (!STATE) {
+      if (pa) ta.load(pa, r.a_step, p0, stop, ka, time);
+      else ta.clear();
+    }
+    if (pb) tb.load(pb, r.b_step, p0, stop, ka, time);
+    else tb.clear();
+    if (pc) tc.load(pc, r.c_step, p0, stop, cols, time);
+    else tc.clear();
+  };
+  int flag = 0;
+  if (begin < stop) {
+    fetch(begin);
+    flag = lane < CL ? starts(begin + lane) : 0;
+  }
+  __syncthreads();
+  int turn = 0;
+  for (int64_t p0 = begin; p0 < stop; p0 += CL, turn ^= 1) {
+    const int cnt = stop - p0 < CL ? (int)(stop - p0) : CL;
+    const int lead = back && p0 == 0 ? 0 : 1;   // steps between the state in front and the first place
+    if constexpr (!STATE) ta.store(lds_a);
+    tb.store(lds_b);
+    tc.store(lds_c);
+    if (!M::finite(tc.most(tb.most(0)))) odd[turn] = 1;
+    const uint64_t cuts = __ballot(flag != 0);
+    const int first = cuts ? __builtin_ctzll(cuts) : CL, last = cuts ? 63 - __builtin_clzll(cuts) : 0;
+    __syncthreads();
+    if (p0 + CL < stop) {
+      fetch(p0 + CL);
+      flag = lane < CL ? starts(p0 + CL + lane) : 0;
+    }
+    const bool slow = odd[turn] != 0;
+    if constexpr (!STATE) {
+      if (!slow) {   // the scores below the diagonal, tile by tile
+#pragma unroll
+        for (int k = 0; k < (ROWS * (ROWS + 1) / 2 + 3) / 4; ++k) {
+          const int tile = wave + 4 * k;
+          const int ti = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, si = tile - ti * (ti + 1) / 2;
+          if (tile < ROWS * (ROWS + 1) / 2 && 16 * ti < cnt) {
+            f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int kk = 0; kk < KP; kk += M::KB)
+              M::mma(acc, M::row(lds_b, PA, 16 * si, kk, i, q), M::row(lds_a, PA, 16 * ti, kk, i, q));
+            const int t = 16 * ti + i, s = 16 * si + 4 * q;
+            const uint64_t before = cuts & ((2ull << t) - 1);
+            const int from = before ? 63 - __builtin_clzll(before) : 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc[e] = s + e <= t && s + e >= from ? acc[e] * (r.in * r.out_scale * lin_power(log2d, t - s - e)) : 0.0f;
+            M::put(lds_p + t * PS + s, SCORES, acc);
+          }
+        }
+      }
+      __syncthreads();
+    }
+    if (!slow && 16 * wave < cols) {
+      frag v[CL / M::KB];
+#pragma unroll
+      for (int kk = 0; kk < CL / M::KB; ++kk) v[kk] = M::col(lds_c, PC, M::KB * kk, 16 * wave, i, q);
+      if constexpr (!STATE) {
+        f32x4 o[ROWS];
+#pragma unroll
+        for (int ti = 0; ti < ROWS; ++ti) o[ti] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int kk = 0; kk < KP / M::KB; ++kk) {
+          float x[M::N];
+#pragma unroll
+          for (int e = 0; e < M::N; ++e) x[e] = S[kk * (M::KB / 16) + e / 4][e % 4];
+          frag f[M::STATE_PARTS];
+          M::template split<M::STATE_PARTS>(x, f);
+#pragma unroll
+          for (int ti = 0; ti < ROWS; ++ti) {
+            const frag a = M::row_state(lds_a, PA, 16 * ti, M::KB * kk, i, q);
+#pragma unroll
+            for (int k = M::STATE_PARTS - 1; k >= 0; --k) M::mma(o[ti], f[k], a);
+          }
+        }
+#pragma unroll
+        for (int ti = 0; ti < ROWS; ++ti) {
+          const int t = 16 * ti + i;
+          const float f = r.out_scale * lin_power(log2d, t + lead);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[ti][e] = t < first ? o[ti][e] * f : 0.0f;
+#pragma unroll
+          for (int kk = 0; kk < CL / M::KB; ++kk)
+            if (M::KB * kk <= 16 * ti) {
+#pragma unroll
+              for (int k = M::SCORE_PARTS - 1; k >= 0; --k) M::mma(o[ti], v[kk], M::row(lds_p + k * SCORES, PS, 16 * ti, M::KB * kk, i, q));
+            }
+          if (t < cnt) {
+            T* to = po + time(p0 + t) * r.out_step + 16 * wave + 4 * q;
+            const int left = cols - 16 * wave - 4 * q;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (e < left) to[e] = from_f<T>(o[ti][e]);
+          }
+        }
+      }
+      const float whole = cuts ? 0.0f : lin_power(log2d, cnt - 1 + lead);
+#pragma unroll
+      for (int k = 0; k < TILES; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[k][e] = cuts ? 0.0f : S[k][e] * whole;
+      keep = cuts ? 0.0f : keep * whole;
+#pragma unroll
+      for (int kk = 0; kk < CL / M::KB; ++kk) {
+        float x[M::N];
+#pragma unroll
+        for (int e = 0; e < M::N; ++e) {
+          const int s = M::KB * kk + M::N * q + e;
+          x[e] = s < cnt && s >= last ? M::at(v[kk], e) * (r.in * lin_power(log2d, cnt - 1 - s)) : 0.0f;
+        }
+        frag f[M::VALUE_PARTS];
+        M::template split<M::VALUE_PARTS>(x, f);
+#pragma unroll
+        for (int k = 0; k < TILES; ++k) {
+          const frag a = M::col(lds_b, PA, M::KB * kk, 16 * k, i, q);
+#pragma unroll
+          for (int e = M::VALUE_PARTS - 1; e >= 0; --e) M::mma(S[k], a, f[e]);
+        }
+      }
+    } else if (slow) {
+      // A value that is not finite: step by step, as a product with a weight of 0 would spread it.
+      for (int p = 0; p < cnt; ++p) {
+        const bool cut = (cuts >> p & 1) != 0;
+        const float d = p == 0 && lead == 0 ? 1.0f : lin_power(log2d, 1), c = mine ? to_f<T>(lds_c[p * PC + col]) : 0.0f;
+        float o = 0.0f;
+#pragma unroll
+        for (int k = 0; k < TILES; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int row = 16 * k + 4 * q + e;
+            if (row < ka) {
+              S[k][e] = fmaf(r.in * to_f<T>(lds_b[p * PA + row]), c, cut ? 0.0f : d * S[k][e]);
+              if constexpr (!STATE) o = fmaf(to_f<T>(lds_a[p * PA + row]), S[k][e], o);
+            }
+          }
+        keep = cut ? 0.0f : keep * d;
+        if constexpr (!STATE) {
+          o += __shfl_xor(o, 16);
+          o += __shfl_xor(o, 32);
+          if (q == 0 && mine) po[time(p0 + p) * r.out_step + col] = from_f<T>(r.out_scale * o);
+        }
+      }
+    }
+    __syncthreads();
+    if (slow && threadIdx.x == 0) odd[turn] = 0;
+  }
+  if constexpr (STATE) {
+    const int64_t at = (b * g.heads + h) * g.pieces + piece;
+    float* to = g.adds[which] + at * ka * r.nc;
+#pragma unroll
+    for (int k = 0; k < TILES; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = 16 * k + 4 * q + e;
+        if (mine && row < ka) to[row * r.nc + c0 + col] = S[k][e];
+      }
+    if (unit == 0 && threadIdx.x == 0) g.keeps[which][at] = keep;
+  } else {
+    // Steps behind the sequence.
+    const int64_t end = begin + g.len < g.steps ? begin + g.len : g.steps;
+    for (int64_t e = threadIdx.x, z = begin > n ? begin : n; z + e / CHUNK_COLS < end; e += CHUNK_THREADS)
+      if ((int)(e % CHUNK_COLS) < cols) po[(z + e / CHUNK_COLS) * r.out_step + e % CHUNK_COLS] = from_f<T>(0.0f);
+    if (r.last && (stop == n ? begin < n || piece == 0 : false)) {
+      const bool cut = back && n > 0 && flags && flags[0] != 0;
+      const float d = back && n > 0 ? lin_power(log2d, 1) : 1.0f;
+      float* to = r.last + (b * g.heads + h) * ka * r.nc;
+#pragma unroll
+      for (int k = 0; k < TILES; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = 16 * k + 4 * q + e;
+          if (mine && row < ka) to[row * r.row_stride + (c0 + col) * r.col_stride] = cut ? 0.0f : S[k][e] * d;
+        }
+    }
+  }
+}
+
+// The state in front of each piece, in the place of what the piece adds to it: a thread an element.
+constexpr int JOIN_THREADS = 256, JOIN_AHEAD = 8;
+__global__ __launch_bounds__(JOIN_THREADS) void lin_join(LinArgs g) {
+  const int which = blockIdx.y;
+  const int64_t size = (int64_t)g.role[which].ka * g.role[which].nc;
+  const int64_t at = (int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x;
+  if (at >= g.batch * g.heads * size) return;
+  const int64_t head = at / size, e = at - head * size;
+  float* u = g.adds[which] + head * g.pieces * size + e;
+  const float* keep = g.keeps[which] + head * g.pieces;
+  float s = g.role[which].init ? g.role[which].init[at] : 0.0f;
+  for (int64_t p = 0; p < g.pieces; p += JOIN_AHEAD) {
+    float x[JOIN_AHEAD], k[JOIN_AHEAD];
+#pragma unroll
+    for (int j = 0; j < JOIN_AHEAD; ++j) {
+      const bool on = p + j < g.pieces;
+      x[j] = on ? u[(p + j) * size] : 0.0f;
+      k[j] = on ? keep[p + j] : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < JOIN_AHEAD; ++j)
+      if (p + j < g.pieces) {
+        u[(p + j) * size] = s;
+        s = k[j] == 0.0f ? x[j] : fmaf(k[j], s, x[j]);   // nothing passes an episode's start, finite or not
+      }
+  }
+}
+
 // The elements of a [n0, n1, n2, width] output do not overlap: from the smallest stride up, each dimension's
 // stride is at least the span of those inside it.
 bool lin_out_strides_ok(int64_t n0, int64_t n1, int64_t n2, int64_t width, int64_t s0, int64_t s1, int64_t s2) {
@@ -190,6 +603,76 @@ template <typename T> void lin_steps_launch(const LinArgs& g, hipStream_t s) {
   });
 }
 
+// How a call is spread: by its sizes alone.
+//   steps: a thread keeps its part of the state and walks;
+//   chunks: a workgroup walks in chunks on the matrix cores; pieces > 1: time is cut into pieces whose sums are joined first.
+constexpr int64_t STEPS_MOST = 8, CHUNK_FILL = 1024, PIECE_LEAST = 256;
+struct LinPlan { bool chunks; int64_t pieces, len; };
+LinPlan lin_plan(const spz_linear_attention_args& a, bool back) {
+  if (a.steps <= STEPS_MOST || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
+  const int64_t k = op_div_up(a.key_width, CHUNK_COLS), v = op_div_up(a.value_width, CHUNK_COLS), units = back ? 2 * k + v : v;
+  const int64_t groups = a.batch * a.heads * units;
+  int64_t pieces = groups > 0 ? CHUNK_FILL / groups : 1;
+  if (pieces > a.steps / PIECE_LEAST) pieces = a.steps / PIECE_LEAST;
+  if (pieces < 2) return {true, 1, a.steps};
+  const int64_t len = op_div_up(op_div_up(a.steps, pieces), 64) * 64;
+  return {true, op_div_up(a.steps, len), len};
+}
+// Floats of one state of all pieces, and of what they keep, each at 16 bytes.
+int64_t lin_states(const spz_linear_attention_args& a, const LinPlan& p) {
+  return op_div_up(a.batch * a.heads * p.pieces * a.key_width * a.value_width, 4) * 4;
+}
+int64_t lin_keeps(const spz_linear_attention_args& a, const LinPlan& p) { return op_div_up(a.batch * a.heads * p.pieces, 4) * 4; }
+
+template <typename T, int KP, int CL, bool STATE> void lin_chunks_go(LinArgs g, hipStream_t s) {
+  g.units = 0;
+  for (int i = 0; i < g.roles; ++i) g.units += (g.role[i].nc + CHUNK_COLS - 1) / CHUNK_COLS;
+  const int64_t blocks = op_div_up(g.batch * g.heads * g.pieces, 8) * 8 * g.units;
+  op_dispatch(blocks, CHUNK_THREADS, [&](int64_t first, dim3 grid) {
+    g.first = first;
+    lin_chunks<T, KP, CL, STATE><<<grid, CHUNK_THREADS, 0, s>>>(g);
+  });
+}
+template <typename T, bool STATE> void lin_chunks_launch(const LinArgs& g, hipStream_t s) {
+  int ka = 0;
+  for (int i = 0; i < g.roles; ++i) ka = g.role[i].ka > ka ? g.role[i].ka : ka;
+  if (ka <= 32) lin_chunks_go<T, 32, 64, STATE>(g, s);
+  else if (ka <= 64) lin_chunks_go<T, 64, 64, STATE>(g, s);
+  else if (ka <= 128) lin_chunks_go<T, 128, 64, STATE>(g, s);
+  else lin_chunks_go<T, 256, sizeof(T) == 4 ? 32 : 64, STATE>(g, s);
+}
+
+template <typename T> void lin_launch(LinArgs& g, const LinPlan& plan, const spz_linear_attention_args& a, bool back, void* ws, hipStream_t s) {
+  if (!plan.chunks) return lin_steps_launch<T>(g, s);
+  g.pieces = plan.pieces;
+  g.len = plan.len;
+  if (plan.pieces > 1) {
+    LinArgs u = g;
+    u.roles = 1;
+    float* at = static_cast<float*>(ws);
+    const int K = (int)a.key_width, V = (int)a.value_width;
+    const auto state = [&](LinRole& r, int i, const void* x, int64_t x0, int64_t x1, int64_t x2, const void* y, int64_t y0, int64_t y1, int64_t y2,
+                           const float* init, bool rev) {
+      r = LinRole{};
+      r.b = x; r.b_batch = x0; r.b_step = x1; r.b_head = x2;
+      r.c = y; r.c_batch = y0; r.c_step = y1; r.c_head = y2;
+      r.init = init; r.row_stride = V; r.col_stride = 1; r.ka = K; r.nc = V; r.back = rev; r.in = rev ? a.scale : 1.0f;
+      u.adds[i] = at;
+      u.keeps[i] = at + lin_states(a, plan);
+      at += lin_states(a, plan) + lin_keeps(a, plan);
+    };
+    state(u.role[0], 0, a.k, a.k_batch, a.k_step, a.k_head, a.v, a.v_batch, a.v_step, a.v_head, a.state, false);
+    if (back) {
+      u.roles = 2;
+      state(u.role[1], 1, a.q, a.q_batch, a.q_step, a.q_head, a.dy, a.dy_batch, a.dy_step, a.dy_head, a.dlast, true);
+    }
+    lin_chunks_launch<T, true>(u, s);
+    lin_join<<<dim3((unsigned)op_div_up(a.batch * a.heads * K * V, JOIN_THREADS), (unsigned)u.roles), JOIN_THREADS, 0, s>>>(u);
+    for (int i = 0; i < g.roles; ++i) g.inits[i] = u.adds[g.role[i].back ? 1 : 0];
+  }
+  lin_chunks_launch<T, false>(g, s);
+}
+
 int lin_run(const char* call, const spz_linear_attention_args* args, bool back, void* ws, int64_t ws_bytes, void* stream) {
   const char* bad = lin_check(args);
   if (!bad) bad = lin_check_arrays(*args, back);
@@ -227,8 +710,9 @@ int lin_run(const char* call, const spz_linear_attention_args* args, bool back, 
   }
   if (g.roles == 0 || a.batch == 0 || a.heads == 0) return SPZ_OK;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (a.prec == SPZ_PREC_BF16) lin_steps_launch<bf16_t>(g, s);
-  else lin_steps_launch<float>(g, s);
+  const LinPlan plan = lin_plan(a, back);
+  if (a.prec == SPZ_PREC_BF16) lin_launch<bf16_t>(g, plan, a, back, ws, s);
+  else lin_launch<float>(g, plan, a, back, ws, s);
   return op_launched(call);
 }
 
@@ -240,10 +724,10 @@ using namespace spz;
 extern "C" {
 
 int64_t spz_linear_attention_workspace(const spz_linear_attention_args* args, int32_t backward) {
-  (void)backward;
   const char* bad = lin_check(args);
   if (bad) return op_error(SPZ_EINVAL, "spz_linear_attention_workspace", bad);
-  return 0;
+  const LinPlan plan = lin_plan(*args, backward != 0);
+  return plan.pieces > 1 ? 4 * (backward ? 2 : 1) * (lin_states(*args, plan) + lin_keeps(*args, plan)) : 0;
 }
 
 int spz_linear_attention_forward(const spz_linear_attention_args* args, void* workspace, int64_t workspace_bytes, void* hip_stream) {
