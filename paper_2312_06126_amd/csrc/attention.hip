@@ -21,10 +21,14 @@ struct LinRole {
   bool back;
   float in, out_scale;
 };
+struct Divisor { uint32_t mul; int shift; };
 struct LinArgs {
   LinRole role[3];
-  int roles, units;                          // units: workgroups of a piece of a head
-  int64_t batch, steps, heads, first;
+  int roles, units, slices[3];               // units: workgroups of a piece of a head, slices: of it for a role
+  uint32_t groups;                           // pieces of heads of a launch
+  Divisor by_units, by_pieces, by_heads;
+  bool far;                                  // 32 bits do not hold 16 steps of an output
+  int64_t batch, steps, heads, first;        // first: steps' kernel: workgroup; chunks' kernel: sequence
   int64_t pieces, len;                       // of time, len steps each
   const float* inits[3];                     // states in front of the pieces [batch, heads, pieces, ..], or NULL
   float *adds[2], *keeps[2];                 // what the pieces add, and keep, of the states of the first two roles
@@ -221,40 +225,96 @@ template <> struct Mat<float> {
   static __device__ inline bool finite(uint32_t m) { return m < 0x7F800000u; }
 };
 
-// CL steps of W columns (zeros past `width` and past the sequence) on their way from memory to LDS.
+// CL steps of W columns (zeros past `width` and past the sequence) on their way from memory to LDS. A thread's vectors
+// are of one column group and RI rows apart, so that one 32-bit offset from scalar addresses serves them all.
+struct Walk { int64_t n; bool back; };   // place p of a walk is step p, or n - 1 - p
 template <typename T, int W, int CL> struct Tile {
-  static constexpr int VW = OP_VEC<T>, VR = W / VW, N = CL * VR / CHUNK_THREADS, PITCH = W + Mat<T>::PAD;
-  static_assert(CL * VR % CHUNK_THREADS == 0, "whole vectors a thread");
+  static constexpr int VW = OP_VEC<T>, VR = W / VW, RI = CHUNK_THREADS / VR, N = CL / RI, PITCH = W + Mat<T>::PAD;
+  static_assert(CL % RI == 0, "whole vectors a thread");
   u32x4 v[N];
-  // t(p): the step at place p; places from n on are behind the sequence.
-  template <typename F> __device__ inline void load(const T* base, int64_t step, int64_t p0, int64_t n, int width, F&& t) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int e = threadIdx.x + CHUNK_THREADS * j, c = e % VR * VW;
-      const int64_t p = p0 + e / VR;
-      v[j] = u32x4{0, 0, 0, 0};
-      if (p < n && c < width) {
-        const T* q = base + t(p) * step + c;
-        v[j] = c + VW <= width ? load16(q) : load_part(q, width - c);
-      }
-    }
-  }
-  __device__ inline void clear() {
+  const char* base;          // of the sequence's first step
+  int64_t step;              // in bytes
+  uint32_t off;
+  int width, cnt, row, col;
+  bool plain;                // rows of a vector and more, and 32 bits hold a chunk's offsets
+  __device__ inline void init(const T* p, int64_t stride, int columns, bool back) {
+    base = reinterpret_cast<const char*>(p);
+    step = stride * (int)sizeof(T);
+    width = columns;
+    row = threadIdx.x / VR;
+    col = threadIdx.x % VR * VW;
+    plain = width >= VW && step < (int64_t)1 << 26;
+    off = (uint32_t)((back ? CL - 1 - row : row) * (uint32_t)step) + column() * (int)sizeof(T);
+    cnt = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = u32x4{0, 0, 0, 0};
   }
-  __device__ inline void store(T* lds) const {
+  // Where the thread's vector is read: the last one of a row that ends inside it is read whole, from further in front.
+  __device__ inline int column() const { return col + VW <= width ? col : col < width ? width - VW : 0; }
+  // Places p0 .. p0 + count - 1 (count > 0).
+  __device__ inline void load(const Walk& w, int64_t p0, int count) {
+    cnt = count;
+    if (!base) return;
+    if (plain && count == CL) {
+      const char* from = base + (w.back ? w.n - p0 - CL : p0) * step;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int e = threadIdx.x + CHUNK_THREADS * j;
-      *reinterpret_cast<u32x4*>(lds + e / VR * PITCH + e % VR * VW) = v[j];
+      for (int j = 0; j < N; ++j) v[j] = load16(reinterpret_cast<const T*>(from + (w.back ? -j : j) * RI * step + off));
+    } else if (plain) {      // rows behind the last one read that one again
+      const char* from = base + (w.back ? w.n - p0 - count : p0) * step;
+      const uint32_t c = column() * (int)sizeof(T);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int r = row + j * RI < count ? row + j * RI : count - 1;
+        v[j] = load16(reinterpret_cast<const T*>(from + ((uint32_t)(w.back ? count - 1 - r : r) * (uint32_t)step + c)));
+      }
     }
   }
-  __device__ inline uint32_t most(uint32_t m) const {
+  // Zeros where nothing is, and the ragged end of a row in its place.
+  __device__ inline void trim() {
+    if (!base) return;
+    if (width < W) {
+      const int part = col < width && col + VW > width ? col - (width - VW) : 0;   // elements to shift down
+      const bool none = col >= width;
 #pragma unroll
-    for (int j = 0; j < N; ++j)
+      for (int j = 0; j < N; ++j) {
+        if (width % VW != 0) {
+          constexpr int WORD = 4 / (int)sizeof(T);
+          if (WORD == 2 && part & 1) {
+            uint32_t u[4] = {v[j][0], v[j][1], v[j][2], v[j][3]};
+            v[j] = u32x4{u[0] >> 16 | u[1] << 16, u[1] >> 16 | u[2] << 16, u[2] >> 16 | u[3] << 16, u[3] >> 16};
+          }
+          if (part / WORD & 1) v[j] = u32x4{v[j][1], v[j][2], v[j][3], 0};
+          if (part / WORD & 2) v[j] = u32x4{v[j][2], v[j][3], 0, 0};
+        }
+        if (none) v[j] = u32x4{0, 0, 0, 0};
+      }
+    }
+    if (cnt < CL) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (row + j * RI >= cnt) v[j] = u32x4{0, 0, 0, 0};
+    }
+  }
+  // To LDS; returns the largest of the magnitudes and m. Rows that are not `plain` come from memory only here.
+  __device__ inline uint32_t store(T* lds, const Walk& w, int64_t p0, uint32_t m) {
+    if (base && !plain) {
+#pragma unroll 1
+      for (int e = threadIdx.x; e < CL * W; e += CHUNK_THREADS) {
+        const int r = e / W, c = e % W;
+        T x = from_f<T>(0.0f);
+        if (r < cnt && c < width) x = reinterpret_cast<const T*>(base + (w.back ? w.n - 1 - p0 - r : p0 + r) * step)[c];
+        lds[r * PITCH + c] = x;
+        m = Mat<T>::most(m, __builtin_bit_cast(uint32_t, to_f<T>(x)));   // a bfloat16 is the high half of its float32
+      }
+      return m;
+    }
+    trim();
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      *reinterpret_cast<u32x4*>(lds + (row + j * RI) * PITCH + col) = v[j];
 #pragma unroll
       for (int k = 0; k < 4; ++k) m = Mat<T>::most(m, v[j][k]);
+    }
     return m;
   }
 };
@@ -268,31 +328,86 @@ __device__ inline float lin_power(float log2d, int n) { return __builtin_amdgcn_
 
 // The workgroups of a launch: the slices of all roles of a piece of a head follow each other on one XCD, whose L2 holds
 // what they share.
+// The same number, of which the compiler does not know that it stays from chunk to chunk: else it keeps everything that
+// follows from it in registers throughout.
+__device__ inline int opaque(int x) {
+  asm("" : "+v"(x));
+  return x;
+}
+
+// x / d for x < 2^31 by a multiplication: 2^(31 + l) / d rounded up, l = ceil(log2 d).
+__device__ inline uint32_t divided(uint32_t x, const Divisor& d) { return (uint32_t)(((uint64_t)x * d.mul) >> d.shift); }
+
+// A lane's part of a state at row and column strides rs and cs: rows 16 k + 4 q .. of column c.
+template <int TILES>
+__device__ inline void state_load(const float* p, f32x4 (&S)[TILES], bool full, bool mine, int ka, int rs, int cs, int c, int q) {
+#pragma unroll
+  for (int k = 0; k < TILES; ++k) S[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (!p) return;
+  const uint32_t at = 4 * q * rs + c * cs;
+  if (full && rs == 1) {
+#pragma unroll
+    for (int k = 0; k < TILES; ++k) __builtin_memcpy(&S[k], p + 16 * k + at, 16);
+  } else if (full) {
+#pragma unroll
+    for (int k = 0; k < TILES; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[k][e] = (p + (16 * k + e) * rs)[at];
+  } else if (mine) {
+#pragma unroll
+    for (int k = 0; k < TILES; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (16 * k + 4 * q + e < ka) S[k][e] = (p + (16 * k + e) * rs)[at];
+  }
+}
+template <int TILES>
+__device__ inline void state_store(float* p, const f32x4 (&S)[TILES], bool full, bool mine, int ka, int rs, int cs, int c, int q) {
+  const uint32_t at = 4 * q * rs + c * cs;
+  if (full && rs == 1) {
+#pragma unroll
+    for (int k = 0; k < TILES; ++k) __builtin_memcpy(p + 16 * k + at, &S[k], 16);
+  } else if (full) {
+#pragma unroll
+    for (int k = 0; k < TILES; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) (p + (16 * k + e) * rs)[at] = S[k][e];
+  } else if (mine) {
+#pragma unroll
+    for (int k = 0; k < TILES; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (16 * k + 4 * q + e < ka) (p + (16 * k + e) * rs)[at] = S[k][e];
+  }
+}
+
 // A workgroup: slice of a role, head, sequence, piece of time. STATE: only what the piece adds to the state.
-template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(CHUNK_THREADS, 2) void lin_chunks(LinArgs g) {
+template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(CHUNK_THREADS, KP <= 64 ? 3 : 1) void lin_chunks(LinArgs g) {
   using M = Mat<T>;
   typedef typename M::frag frag;
   constexpr int TILES = KP / 16, ROWS = CL / 16, PA = KP + M::PAD, PC = CHUNK_COLS + M::PAD, PS = CL + M::PAD, SCORES = CL * PS;
+  constexpr int LOWER = ROWS * (ROWS + 1) / 2;         // tiles of scores on and below the diagonal
   __shared__ __align__(16) T lds_a[STATE ? 1 : CL * PA];
   __shared__ __align__(16) T lds_b[CL * PA];
   __shared__ __align__(16) T lds_c[CL * PC];
   __shared__ __align__(16) T lds_p[STATE ? 1 : M::SCORE_PARTS * SCORES];
   __shared__ int odd[2];
-  const int64_t block = g.first + blockIdx.x, group = block / 8 / g.units * 8 + block % 8;
-  if (group >= g.batch * g.heads * g.pieces) return;
-  int unit = (int)(block / 8 % g.units), which = 0;
-  while (unit >= (g.role[which].nc + CHUNK_COLS - 1) / CHUNK_COLS) unit -= (g.role[which++].nc + CHUNK_COLS - 1) / CHUNK_COLS;
+  __shared__ __align__(16) float fade[CL], enter[CL];    // of a place's c in the state behind the chunk, of the state in front in a place's o
+  __shared__ int start[CL];                              // first place of a place's episode within the chunk
+  const uint32_t block = (uint32_t)blockIdx.x, eighth = block / 8, set = divided(eighth, g.by_units);
+  const uint32_t group = set * 8 + block % 8;
+  if (group >= g.groups) return;
+  int unit = (int)(eighth - set * (uint32_t)g.units), which = 0;
+  while (unit >= g.slices[which]) unit -= g.slices[which++];
   const LinRole& r = g.role[which];
-  const int64_t piece = group % g.pieces, h = group / g.pieces % g.heads, b = group / g.pieces / g.heads;
+  const uint32_t seq = divided(group, g.by_pieces), bq = divided(seq, g.by_heads);
+  const int64_t piece = group - seq * (uint32_t)g.pieces, h = seq - bq * (uint32_t)g.heads, b = g.first + bq;
   const int c0 = unit * CHUNK_COLS, cols = r.nc - c0 < CHUNK_COLS ? r.nc - c0 : CHUNK_COLS, ka = r.ka;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i0 = lane & 15, q0 = lane >> 4;
   const int64_t n = lin_length(g, b), begin = piece * g.len, stop = begin + g.len < n ? begin + g.len : n;
   const bool back = r.back;
+  const Walk walk{n, back};
   const float log2d = lin_log2(g.rate ? g.rate[h] : 0.0f);
-  const auto time = [&](int64_t p) { return back ? n - 1 - p : p; };
-  const T* pa = r.a ? static_cast<const T*>(r.a) + b * r.a_batch + h * r.a_head : nullptr;
-  const T* pb = r.b ? static_cast<const T*>(r.b) + b * r.b_batch + h * r.b_head : nullptr;
-  const T* pc = r.c ? static_cast<const T*>(r.c) + b * r.c_batch + h * r.c_head + c0 : nullptr;
   T* po = STATE ? nullptr : static_cast<T*>(r.out) + b * r.out_batch + h * r.out_head + c0;
   const uint8_t* flags = g.reset ? g.reset + b * g.reset_batch : nullptr;
   // Whether place p starts an episode in the order of the walk (backward: whether the step behind it does).
@@ -302,73 +417,92 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
     return (int)flags[p * g.reset_step];
   };
 
+  Tile<T, KP, CL> ta, tb;
+  Tile<T, CHUNK_COLS, CL> tc;
+  if constexpr (!STATE) ta.init(r.a ? static_cast<const T*>(r.a) + b * r.a_batch + h * r.a_head : nullptr, r.a_step, ka, back);
+  tb.init(r.b ? static_cast<const T*>(r.b) + b * r.b_batch + h * r.b_head : nullptr, r.b_step, ka, back);
+  tc.init(r.c ? static_cast<const T*>(r.c) + b * r.c_batch + h * r.c_head + c0 : nullptr, r.c_step, cols, back);
+  int flag = 0;
+  const auto fetch = [&](int64_t p0) {
+    const int count = stop - p0 < CL ? (int)(stop - p0) : CL;
+    if constexpr (!STATE) ta.load(walk, p0, count);
+    tb.load(walk, p0, count);
+    tc.load(walk, p0, count);
+    flag = lane < CL ? starts(p0 + lane) : 0;
+  };
+  if (begin < stop) fetch(begin);
+
   f32x4 S[TILES];
-  const int col = 16 * wave + i;
+  const int col = 16 * wave + i0;
   const bool mine = col < cols;
-#pragma unroll
-  for (int k = 0; k < TILES; ++k)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int row = 16 * k + 4 * q + e;
-      const float* init = g.inits[which] ? g.inits[which] + ((b * g.heads + h) * g.pieces + piece) * ka * r.nc : r.init ? r.init + (b * g.heads + h) * ka * r.nc : nullptr;
-      S[k][e] = !STATE && init && mine && row < ka ? init[row * r.row_stride + (c0 + col) * r.col_stride] : 0.0f;
-    }
+  const int rs = (int)r.row_stride, cs = (int)r.col_stride, size = ka * r.nc;
+  const bool full = ka == KP && cols == CHUNK_COLS;   // every lane's part of the state exists
+  {
+    const float* init = nullptr;
+    if constexpr (!STATE)
+      init = g.inits[which] ? g.inits[which] + ((b * g.heads + h) * g.pieces + piece) * size : r.init ? r.init + (b * g.heads + h) * size : nullptr;
+    state_load<TILES>(init, S, full, mine, ka, rs, cs, c0 + col, q0);
+  }
   if constexpr (!STATE && M::KB == 32) {   // scores above the diagonal that share an instruction with scores below it
-    for (int e = threadIdx.x; e < M::SCORE_PARTS * SCORES; e += CHUNK_THREADS) lds_p[e] = from_f<T>(0.0f);
+    for (int e = threadIdx.x; e < M::SCORE_PARTS * SCORES / 8; e += CHUNK_THREADS) reinterpret_cast<u32x4*>(lds_p)[e] = u32x4{0, 0, 0, 0};
   }
   if (threadIdx.x < 2) odd[threadIdx.x] = 0;
   float keep = 1.0f;   // STATE: what is left of the state in front of the piece
-  Tile<T, KP, CL> ta, tb;
-  Tile<T, CHUNK_COLS, CL> tc;
-  const auto fetch = [&](int64_t p0) {
-    if constexpr (!STATE) {
-      if (pa) ta.load(pa, r.a_step, p0, stop, ka, time);
-      else ta.clear();
-    }
-    if (pb) tb.load(pb, r.b_step, p0, stop, ka, time);
-    else tb.clear();
-    if (pc) tc.load(pc, r.c_step, p0, stop, cols, time);
-    else tc.clear();
-  };
-  int flag = 0;
-  if (begin < stop) {
-    fetch(begin);
-    flag = lane < CL ? starts(begin + lane) : 0;
+  // Weights of the scores in a tile on the diagonal and in the one below it.
+  float on[4], below[4];
+  const float score = r.in * r.out_scale;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    on[e] = score * lin_power(log2d, i0 >= 4 * q0 + e ? i0 - 4 * q0 - e : 0);
+    below[e] = score * lin_power(log2d, 16 + i0 - 4 * q0 - e);
   }
+  const float two = lin_power(log2d, 16);
   __syncthreads();
   int turn = 0;
   for (int64_t p0 = begin; p0 < stop; p0 += CL, turn ^= 1) {
+    const int i = opaque(i0), q = opaque(q0);
     const int cnt = stop - p0 < CL ? (int)(stop - p0) : CL;
     const int lead = back && p0 == 0 ? 0 : 1;   // steps between the state in front and the first place
-    if constexpr (!STATE) ta.store(lds_a);
-    tb.store(lds_b);
-    tc.store(lds_c);
-    if (!M::finite(tc.most(tb.most(0)))) odd[turn] = 1;
+    if constexpr (!STATE) ta.store(lds_a, walk, p0, 0);
+    if (!M::finite(tc.store(lds_c, walk, p0, tb.store(lds_b, walk, p0, 0)))) odd[turn] = 1;
     const uint64_t cuts = __ballot(flag != 0);
-    const int first = cuts ? __builtin_ctzll(cuts) : CL, last = cuts ? 63 - __builtin_clzll(cuts) : 0;
-    __syncthreads();
-    if (p0 + CL < stop) {
-      fetch(p0 + CL);
-      flag = lane < CL ? starts(p0 + CL + lane) : 0;
+    if (wave == 0 && lane < CL) {
+      const uint64_t before = cuts & ((2ull << lane) - 1);
+      const int ahead = cnt - 1 - lane;
+      const float f = r.in * lin_power(log2d, ahead > 0 ? ahead : 0), o = r.out_scale * lin_power(log2d, lane + lead);
+      fade[lane] = ahead >= 0 && !(cuts >> lane >> 1) ? f : 0.0f;
+      enter[lane] = o;
+      start[lane] = before ? 63 - __builtin_clzll(before) : 0;
     }
-    const bool slow = odd[turn] != 0;
+    const int first = cuts ? __builtin_ctzll(cuts) : CL;
+    __syncthreads();
+    if (p0 + CL < stop) fetch(p0 + CL);
+    const bool slow = __builtin_amdgcn_readfirstlane(odd[turn]) != 0;
     if constexpr (!STATE) {
       if (!slow) {   // the scores below the diagonal, tile by tile
 #pragma unroll
-        for (int k = 0; k < (ROWS * (ROWS + 1) / 2 + 3) / 4; ++k) {
+        for (int k = 0; k < (LOWER + 3) / 4; ++k) {
           const int tile = wave + 4 * k;
           const int ti = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, si = tile - ti * (ti + 1) / 2;
-          if (tile < ROWS * (ROWS + 1) / 2 && 16 * ti < cnt) {
+          if (tile < LOWER && 16 * ti < cnt) {
             f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int kk = 0; kk < KP; kk += M::KB)
               M::mma(acc, M::row(lds_b, PA, 16 * si, kk, i, q), M::row(lds_a, PA, 16 * ti, kk, i, q));
             const int t = 16 * ti + i, s = 16 * si + 4 * q;
-            const uint64_t before = cuts & ((2ull << t) - 1);
-            const int from = before ? 63 - __builtin_clzll(before) : 0;
+            if (ti == si) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              acc[e] = s + e <= t && s + e >= from ? acc[e] * (r.in * r.out_scale * lin_power(log2d, t - s - e)) : 0.0f;
+              for (int e = 0; e < 4; ++e) acc[e] = 4 * q + e <= i ? acc[e] * on[e] : 0.0f;
+            } else {
+              const float f = ti - si == 1 ? 1.0f : ti - si == 2 ? two : two * two;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[e] *= below[e] * f;
+            }
+            if (cuts) {
+              const int from = start[t];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[e] = s + e >= from ? acc[e] : 0.0f;
+            }
             M::put(lds_p + t * PS + s, SCORES, acc);
           }
         }
@@ -383,24 +517,29 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
         f32x4 o[ROWS];
 #pragma unroll
         for (int ti = 0; ti < ROWS; ++ti) o[ti] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (first > 0) {
 #pragma unroll
-        for (int kk = 0; kk < KP / M::KB; ++kk) {
-          float x[M::N];
+          for (int kk = 0; kk < KP / M::KB; ++kk) {
+            float x[M::N];
 #pragma unroll
-          for (int e = 0; e < M::N; ++e) x[e] = S[kk * (M::KB / 16) + e / 4][e % 4];
-          frag f[M::STATE_PARTS];
-          M::template split<M::STATE_PARTS>(x, f);
+            for (int e = 0; e < M::N; ++e) x[e] = S[kk * (M::KB / 16) + e / 4][e % 4];
+            frag f[M::STATE_PARTS];
+            M::template split<M::STATE_PARTS>(x, f);
 #pragma unroll
-          for (int ti = 0; ti < ROWS; ++ti) {
-            const frag a = M::row_state(lds_a, PA, 16 * ti, M::KB * kk, i, q);
+            for (int ti = 0; ti < ROWS; ++ti) {
+              const frag a = M::row_state(lds_a, PA, 16 * ti, M::KB * kk, i, q);
 #pragma unroll
-            for (int k = M::STATE_PARTS - 1; k >= 0; --k) M::mma(o[ti], f[k], a);
+              for (int k = M::STATE_PARTS - 1; k >= 0; --k) M::mma(o[ti], f[k], a);
+            }
           }
         }
+        const uint32_t step = (uint32_t)(r.out_step * (int)sizeof(T));
+        const int left = cols - 16 * wave - 4 * q;
 #pragma unroll
         for (int ti = 0; ti < ROWS; ++ti) {
           const int t = 16 * ti + i;
-          const float f = r.out_scale * lin_power(log2d, t + lead);
+          if (16 * ti >= cnt) continue;
+          const float f = enter[t];
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[ti][e] = t < first ? o[ti][e] * f : 0.0f;
 #pragma unroll
@@ -409,16 +548,27 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
 #pragma unroll
               for (int k = M::SCORE_PARTS - 1; k >= 0; --k) M::mma(o[ti], v[kk], M::row(lds_p + k * SCORES, PS, 16 * ti, M::KB * kk, i, q));
             }
-          if (t < cnt) {
-            T* to = po + time(p0 + t) * r.out_step + 16 * wave + 4 * q;
-            const int left = cols - 16 * wave - 4 * q;
+          if (t < cnt && left > 0) {
+            const int64_t at = back ? n - 16 - 16 * ti - p0 : p0 + 16 * ti;   // of the tile's row with the lowest address
+            char* to = reinterpret_cast<char*>(po) + at * r.out_step * (int)sizeof(T);
+            to += g.far ? (int64_t)(back ? 15 - i : i) * r.out_step * (int)sizeof(T) : (int64_t)((uint32_t)(back ? 15 - i : i) * step);
+            T* y = reinterpret_cast<T*>(to) + 16 * wave + 4 * q;
+            if (left >= 4) {
+              if constexpr (sizeof(T) == 2) {
+                const u32x2 w = {pack_bf16x2(o[ti][0], o[ti][1]), pack_bf16x2(o[ti][2], o[ti][3])};
+                __builtin_memcpy(y, &w, 8);
+              } else {
+                __builtin_memcpy(y, &o[ti], 16);
+              }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (e < left) to[e] = from_f<T>(o[ti][e]);
+              for (int e = 0; e < 3; ++e)
+                if (e < left) y[e] = from_f<T>(o[ti][e]);
+            }
           }
         }
       }
-      const float whole = cuts ? 0.0f : lin_power(log2d, cnt - 1 + lead);
+      const float whole = lin_power(log2d, cnt - 1 + lead);
 #pragma unroll
       for (int k = 0; k < TILES; ++k)
 #pragma unroll
@@ -426,11 +576,13 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
       keep = cuts ? 0.0f : keep * whole;
 #pragma unroll
       for (int kk = 0; kk < CL / M::KB; ++kk) {
+        if (M::KB * kk >= cnt) continue;
         float x[M::N];
 #pragma unroll
-        for (int e = 0; e < M::N; ++e) {
-          const int s = M::KB * kk + M::N * q + e;
-          x[e] = s < cnt && s >= last ? M::at(v[kk], e) * (r.in * lin_power(log2d, cnt - 1 - s)) : 0.0f;
+        for (int e = 0; e < M::N; e += 4) {
+          const f32x4 w = *reinterpret_cast<const f32x4*>(fade + M::KB * kk + M::N * q + e);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[e + j] = M::at(v[kk], e + j) * w[j];
         }
         frag f[M::VALUE_PARTS];
         M::template split<M::VALUE_PARTS>(x, f);
@@ -461,7 +613,7 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
         if constexpr (!STATE) {
           o += __shfl_xor(o, 16);
           o += __shfl_xor(o, 32);
-          if (q == 0 && mine) po[time(p0 + p) * r.out_step + col] = from_f<T>(r.out_scale * o);
+          if (q == 0 && mine) po[(back ? n - 1 - p0 - p : p0 + p) * r.out_step + col] = from_f<T>(r.out_scale * o);
         }
       }
     }
@@ -470,31 +622,22 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
   }
   if constexpr (STATE) {
     const int64_t at = (b * g.heads + h) * g.pieces + piece;
-    float* to = g.adds[which] + at * ka * r.nc;
-#pragma unroll
-    for (int k = 0; k < TILES; ++k)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = 16 * k + 4 * q + e;
-        if (mine && row < ka) to[row * r.nc + c0 + col] = S[k][e];
-      }
+    state_store<TILES>(g.adds[which] + at * size, S, full, mine, ka, r.nc, 1, c0 + col, q0);
     if (unit == 0 && threadIdx.x == 0) g.keeps[which][at] = keep;
   } else {
     // Steps behind the sequence.
     const int64_t end = begin + g.len < g.steps ? begin + g.len : g.steps;
-    for (int64_t e = threadIdx.x, z = begin > n ? begin : n; z + e / CHUNK_COLS < end; e += CHUNK_THREADS)
-      if ((int)(e % CHUNK_COLS) < cols) po[(z + e / CHUNK_COLS) * r.out_step + e % CHUNK_COLS] = from_f<T>(0.0f);
-    if (r.last && (stop == n ? begin < n || piece == 0 : false)) {
+    for (int64_t t = (begin > n ? begin : n) + threadIdx.x / CHUNK_COLS; t < end; t += CHUNK_THREADS / CHUNK_COLS)
+      if ((int)threadIdx.x % CHUNK_COLS < cols) po[t * r.out_step + threadIdx.x % CHUNK_COLS] = from_f<T>(0.0f);
+    if (r.last && stop == n && (begin < n || piece == 0)) {
       const bool cut = back && n > 0 && flags && flags[0] != 0;
       const float d = back && n > 0 ? lin_power(log2d, 1) : 1.0f;
-      float* to = r.last + (b * g.heads + h) * ka * r.nc;
+      float* to = r.last + (b * g.heads + h) * size;
 #pragma unroll
       for (int k = 0; k < TILES; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = 16 * k + 4 * q + e;
-          if (mine && row < ka) to[row * r.row_stride + (c0 + col) * r.col_stride] = cut ? 0.0f : S[k][e] * d;
-        }
+        for (int e = 0; e < 4; ++e) S[k][e] = cut ? 0.0f : S[k][e] * d;
+      state_store<TILES>(to, S, full, mine, ka, rs, cs, c0 + col, q0);
     }
   }
 }
@@ -624,14 +767,29 @@ int64_t lin_states(const spz_linear_attention_args& a, const LinPlan& p) {
 }
 int64_t lin_keeps(const spz_linear_attention_args& a, const LinPlan& p) { return op_div_up(a.batch * a.heads * p.pieces, 4) * 4; }
 
+Divisor divisor(uint32_t d) {
+  int l = 0;
+  while (((uint64_t)1 << l) < d) ++l;
+  return {(uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), 31 + l};
+}
 template <typename T, int KP, int CL, bool STATE> void lin_chunks_go(LinArgs g, hipStream_t s) {
   g.units = 0;
-  for (int i = 0; i < g.roles; ++i) g.units += (g.role[i].nc + CHUNK_COLS - 1) / CHUNK_COLS;
-  const int64_t blocks = op_div_up(g.batch * g.heads * g.pieces, 8) * 8 * g.units;
-  op_dispatch(blocks, CHUNK_THREADS, [&](int64_t first, dim3 grid) {
+  g.far = false;
+  for (int i = 0; i < g.roles; ++i) {
+    g.units += g.slices[i] = (g.role[i].nc + CHUNK_COLS - 1) / CHUNK_COLS;
+    g.far = g.far || g.role[i].out_step > (int64_t)1 << 24;
+  }
+  g.by_units = divisor((uint32_t)g.units);
+  g.by_pieces = divisor((uint32_t)g.pieces);
+  g.by_heads = divisor((uint32_t)g.heads);
+  // Sequences whose workgroups one dispatch counts (a sequence has fewer than that: heads and pieces are limited).
+  const int64_t each = g.heads * g.pieces, most = (OP_DISPATCH / CHUNK_THREADS / g.units - 8) / each;
+  for (int64_t first = 0; first < g.batch; first += most) {
+    const int64_t count = g.batch - first < most ? g.batch - first : most;
     g.first = first;
-    lin_chunks<T, KP, CL, STATE><<<grid, CHUNK_THREADS, 0, s>>>(g);
-  });
+    g.groups = (uint32_t)(count * each);
+    lin_chunks<T, KP, CL, STATE><<<dim3((unsigned)(op_div_up(count * each, 8) * 8 * g.units)), CHUNK_THREADS, 0, s>>>(g);
+  }
 }
 template <typename T, bool STATE> void lin_chunks_launch(const LinArgs& g, hipStream_t s) {
   int ka = 0;
