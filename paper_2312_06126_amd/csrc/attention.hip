@@ -227,51 +227,54 @@ template <> struct Mat<float> {
 
 // CL steps of W columns (zeros past `width` and past the sequence) on their way from memory to LDS. A thread's vectors
 // are of one column group and RI rows apart, so that one 32-bit offset from scalar addresses serves them all.
-struct Walk { int64_t n; bool back; };   // place p of a walk is step p, or n - 1 - p
+struct Walk { int n; bool back; };   // place p of a walk is step p, or n - 1 - p
 template <typename T, int W, int CL> struct Tile {
   static constexpr int VW = OP_VEC<T>, VR = W / VW, RI = CHUNK_THREADS / VR, N = CL / RI, PITCH = W + Mat<T>::PAD;
   static_assert(CL % RI == 0, "whole vectors a thread");
   u32x4 v[N];
-  const char* base;          // of the sequence's first step
-  int64_t step;              // in bytes
+  const char* at;            // of the next chunk's place that comes first in memory, were the chunk whole
+  int64_t step;              // in bytes, forward in the walk
   uint32_t off;
   int width, cnt, row, col;
-  bool plain;                // rows of a vector and more, and 32 bits hold a chunk's offsets
-  __device__ inline void init(const T* p, int64_t stride, int columns, bool back) {
-    base = reinterpret_cast<const char*>(p);
+  bool some, plain;          // plain: rows of a vector and more, and 32 bits hold a chunk's offsets
+  __device__ inline void init(const T* p, int64_t stride, int columns, const Walk& w, int begin) {
+    some = p != nullptr;
     step = stride * (int)sizeof(T);
     width = columns;
     row = threadIdx.x / VR;
     col = threadIdx.x % VR * VW;
     plain = width >= VW && step < (int64_t)1 << 26;
-    off = (uint32_t)((back ? CL - 1 - row : row) * (uint32_t)step) + column() * (int)sizeof(T);
+    off = (uint32_t)((w.back ? CL - 1 - row : row) * (uint32_t)step) + column() * (int)sizeof(T);
+    at = reinterpret_cast<const char*>(p) + (w.back ? w.n - begin - CL : begin) * step;
+    if (w.back) step = -step;
     cnt = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = u32x4{0, 0, 0, 0};
   }
   // Where the thread's vector is read: the last one of a row that ends inside it is read whole, from further in front.
   __device__ inline int column() const { return col + VW <= width ? col : col < width ? width - VW : 0; }
-  // Places p0 .. p0 + count - 1 (count > 0).
-  __device__ inline void load(const Walk& w, int64_t p0, int count) {
+  // The next chunk, of which `count` > 0 places exist.
+  __device__ inline void load(bool back, int count) {
     cnt = count;
-    if (!base) return;
+    if (!some) return;
     if (plain && count == CL) {
-      const char* from = base + (w.back ? w.n - p0 - CL : p0) * step;
+      const char* from = at;
 #pragma unroll
-      for (int j = 0; j < N; ++j) v[j] = load16(reinterpret_cast<const T*>(from + (w.back ? -j : j) * RI * step + off));
+      for (int j = 0; j < N; ++j, from += RI * step) v[j] = load16(reinterpret_cast<const T*>(from + off));
     } else if (plain) {      // rows behind the last one read that one again
-      const char* from = base + (w.back ? w.n - p0 - count : p0) * step;
-      const uint32_t c = column() * (int)sizeof(T);
+      const char* from = back ? at - (CL - count) * step : at;
+      const uint32_t c = column() * (int)sizeof(T), up = (uint32_t)(back ? -step : step);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const int r = row + j * RI < count ? row + j * RI : count - 1;
-        v[j] = load16(reinterpret_cast<const T*>(from + ((uint32_t)(w.back ? count - 1 - r : r) * (uint32_t)step + c)));
+        v[j] = load16(reinterpret_cast<const T*>(from + ((uint32_t)(back ? count - 1 - r : r) * up + c)));
       }
     }
+    at += CL * step;
   }
   // Zeros where nothing is, and the ragged end of a row in its place.
   __device__ inline void trim() {
-    if (!base) return;
+    if (!some) return;
     if (width < W) {
       const int part = col < width && col + VW > width ? col - (width - VW) : 0;   // elements to shift down
       const bool none = col >= width;
@@ -296,13 +299,14 @@ template <typename T, int W, int CL> struct Tile {
     }
   }
   // To LDS; returns the largest of the magnitudes and m. Rows that are not `plain` come from memory only here.
-  __device__ inline uint32_t store(T* lds, const Walk& w, int64_t p0, uint32_t m) {
-    if (base && !plain) {
+  __device__ inline uint32_t store(T* lds, bool back, uint32_t m) {
+    if (some && !plain) {
+      const char* from = at - CL * step + (back ? -(CL - 1) * step : 0);   // of the chunk's first place
 #pragma unroll 1
       for (int e = threadIdx.x; e < CL * W; e += CHUNK_THREADS) {
         const int r = e / W, c = e % W;
         T x = from_f<T>(0.0f);
-        if (r < cnt && c < width) x = reinterpret_cast<const T*>(base + (w.back ? w.n - 1 - p0 - r : p0 + r) * step)[c];
+        if (r < cnt && c < width) x = reinterpret_cast<const T*>(from + r * step)[c];
         lds[r * PITCH + c] = x;
         m = Mat<T>::most(m, __builtin_bit_cast(uint32_t, to_f<T>(x)));   // a bfloat16 is the high half of its float32
       }
@@ -404,14 +408,13 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
   const int64_t piece = group - seq * (uint32_t)g.pieces, h = seq - bq * (uint32_t)g.heads, b = g.first + bq;
   const int c0 = unit * CHUNK_COLS, cols = r.nc - c0 < CHUNK_COLS ? r.nc - c0 : CHUNK_COLS, ka = r.ka;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i0 = lane & 15, q0 = lane >> 4;
-  const int64_t n = lin_length(g, b), begin = piece * g.len, stop = begin + g.len < n ? begin + g.len : n;
+  const int n = (int)lin_length(g, b), begin = (int)(piece * g.len), stop = n - begin > (int)g.len ? begin + (int)g.len : n;
   const bool back = r.back;
   const Walk walk{n, back};
   const float log2d = lin_log2(g.rate ? g.rate[h] : 0.0f);
-  T* po = STATE ? nullptr : static_cast<T*>(r.out) + b * r.out_batch + h * r.out_head + c0;
   const uint8_t* flags = g.reset ? g.reset + b * g.reset_batch : nullptr;
   // Whether place p starts an episode in the order of the walk (backward: whether the step behind it does).
-  const auto starts = [&](int64_t p) {
+  const auto starts = [&](int p) {
     if (!flags || p >= stop) return 0;
     if (back) return p == 0 ? 0 : (int)flags[(n - p) * g.reset_step];
     return (int)flags[p * g.reset_step];
@@ -419,18 +422,22 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
 
   Tile<T, KP, CL> ta, tb;
   Tile<T, CHUNK_COLS, CL> tc;
-  if constexpr (!STATE) ta.init(r.a ? static_cast<const T*>(r.a) + b * r.a_batch + h * r.a_head : nullptr, r.a_step, ka, back);
-  tb.init(r.b ? static_cast<const T*>(r.b) + b * r.b_batch + h * r.b_head : nullptr, r.b_step, ka, back);
-  tc.init(r.c ? static_cast<const T*>(r.c) + b * r.c_batch + h * r.c_head + c0 : nullptr, r.c_step, cols, back);
+  if constexpr (!STATE) ta.init(r.a ? static_cast<const T*>(r.a) + b * r.a_batch + h * r.a_head : nullptr, r.a_step, ka, walk, begin);
+  tb.init(r.b ? static_cast<const T*>(r.b) + b * r.b_batch + h * r.b_head : nullptr, r.b_step, ka, walk, begin);
+  tc.init(r.c ? static_cast<const T*>(r.c) + b * r.c_batch + h * r.c_head + c0 : nullptr, r.c_step, cols, walk, begin);
   int flag = 0;
-  const auto fetch = [&](int64_t p0) {
-    const int count = stop - p0 < CL ? (int)(stop - p0) : CL;
-    if constexpr (!STATE) ta.load(walk, p0, count);
-    tb.load(walk, p0, count);
-    tc.load(walk, p0, count);
+  const auto fetch = [&](int p0) {
+    const int count = stop - p0 < CL ? stop - p0 : CL;
+    if constexpr (!STATE) ta.load(back, count);
+    tb.load(back, count);
+    tc.load(back, count);
     flag = lane < CL ? starts(p0 + lane) : 0;
   };
   if (begin < stop) fetch(begin);
+  // The next place's row of o, or of 16 places the one that comes first in memory.
+  const int64_t out_step = STATE ? 0 : r.out_step * (int)sizeof(T), out_walk = back ? -out_step : out_step;
+  T* const po = STATE ? nullptr : static_cast<T*>(r.out) + b * r.out_batch + h * r.out_head + c0;
+  char* out = reinterpret_cast<char*>(po) + (back ? (int64_t)n - 16 - begin : (int64_t)begin) * out_step;
 
   f32x4 S[TILES];
   const int col = 16 * wave + i0;
@@ -459,12 +466,12 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
   const float two = lin_power(log2d, 16);
   __syncthreads();
   int turn = 0;
-  for (int64_t p0 = begin; p0 < stop; p0 += CL, turn ^= 1) {
+  for (int p0 = begin; p0 < stop; p0 += CL, turn ^= 1, out += CL * out_walk) {
     const int i = opaque(i0), q = opaque(q0);
-    const int cnt = stop - p0 < CL ? (int)(stop - p0) : CL;
+    const int cnt = stop - p0 < CL ? stop - p0 : CL;
     const int lead = back && p0 == 0 ? 0 : 1;   // steps between the state in front and the first place
-    if constexpr (!STATE) ta.store(lds_a, walk, p0, 0);
-    if (!M::finite(tc.store(lds_c, walk, p0, tb.store(lds_b, walk, p0, 0)))) odd[turn] = 1;
+    if constexpr (!STATE) ta.store(lds_a, back, 0);
+    if (!M::finite(tc.store(lds_c, back, tb.store(lds_b, back, 0)))) odd[turn] = 1;
     const uint64_t cuts = __ballot(flag != 0);
     if (wave == 0 && lane < CL) {
       const uint64_t before = cuts & ((2ull << lane) - 1);
@@ -533,7 +540,6 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
             }
           }
         }
-        const uint32_t step = (uint32_t)(r.out_step * (int)sizeof(T));
         const int left = cols - 16 * wave - 4 * q;
 #pragma unroll
         for (int ti = 0; ti < ROWS; ++ti) {
@@ -549,9 +555,8 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
               for (int k = M::SCORE_PARTS - 1; k >= 0; --k) M::mma(o[ti], v[kk], M::row(lds_p + k * SCORES, PS, 16 * ti, M::KB * kk, i, q));
             }
           if (t < cnt && left > 0) {
-            const int64_t at = back ? n - 16 - 16 * ti - p0 : p0 + 16 * ti;   // of the tile's row with the lowest address
-            char* to = reinterpret_cast<char*>(po) + at * r.out_step * (int)sizeof(T);
-            to += g.far ? (int64_t)(back ? 15 - i : i) * r.out_step * (int)sizeof(T) : (int64_t)((uint32_t)(back ? 15 - i : i) * step);
+            const int up = back ? 15 - i : i;
+            char* to = out + 16 * ti * out_walk + (g.far ? up * out_step : (int64_t)(uint32_t)(up * (uint32_t)out_step));
             T* y = reinterpret_cast<T*>(to) + 16 * wave + 4 * q;
             if (left >= 4) {
               if constexpr (sizeof(T) == 2) {
@@ -613,7 +618,7 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
         if constexpr (!STATE) {
           o += __shfl_xor(o, 16);
           o += __shfl_xor(o, 32);
-          if (q == 0 && mine) po[(back ? n - 1 - p0 - p : p0 + p) * r.out_step + col] = from_f<T>(r.out_scale * o);
+          if (q == 0 && mine) reinterpret_cast<T*>(out + (back ? 15 * out_step : 0) + p * out_walk)[col] = from_f<T>(r.out_scale * o);
         }
       }
     }
@@ -752,7 +757,8 @@ template <typename T> void lin_steps_launch(const LinArgs& g, hipStream_t s) {
 constexpr int64_t STEPS_MOST = 8, CHUNK_FILL = 1024, PIECE_LEAST = 256;
 struct LinPlan { bool chunks; int64_t pieces, len; };
 LinPlan lin_plan(const spz_linear_attention_args& a, bool back) {
-  if (a.steps <= STEPS_MOST || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
+  // (Places are counted in 31 bits, a chunk past the last one included.)
+  if (a.steps <= STEPS_MOST || a.steps > OP_MAX_EXTENT - 4096 || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
   const int64_t k = op_div_up(a.key_width, CHUNK_COLS), v = op_div_up(a.value_width, CHUNK_COLS), units = back ? 2 * k + v : v;
   const int64_t groups = a.batch * a.heads * units;
   int64_t pieces = groups > 0 ? CHUNK_FILL / groups : 1;
