@@ -1,14 +1,15 @@
 // Norms of each head of queries and keys, and their rotation by position, in one pass.
 //
-// A wave takes heads of rows one after the other: lane l holds columns l, l + 64, .. and, of columns that turn,
-// the partner's value as well, which it normalises itself, so that nothing crosses lanes but the two sums.
+// A group of lanes takes a row and walks over its heads (or some of them, where there are few rows), so that the row's
+// angles are taken once. Each lane holds pairs of columns that turn together: only the two sums of a norm cross lanes.
 #include "ops.h"
 
 namespace spz {
 namespace {
 
 constexpr int HEAD_MAX_DIM = 1024, HEAD_THREADS = 256, HEAD_WAVES = HEAD_THREADS / 64;
-constexpr int64_t HEAD_BLOCKS = 2048;   // most workgroups of a backward call: each leaves a row of partial sums
+constexpr int64_t HEAD_BLOCKS = 1024;   // most workgroups of a backward call's queries or keys: each leaves a row of partial sums
+constexpr int64_t HEAD_FILL = 4096;     // waves that fill the card: with fewer rows a row's heads are divided
 
 // Queries or keys.
 struct HeadPart {
@@ -16,8 +17,9 @@ struct HeadPart {
   const float *w, *b;
   const void* dy; int64_t dy_row, dy_head;   // backward
   void* out; int64_t out_row, out_head;      // forward: y; backward: dx
-  int64_t heads, items;                      // items: rows * heads
+  int64_t heads, items;                      // items: rows times shares of the heads
   int64_t first, blocks;                     // its workgroups
+  int share;                                 // heads of an item
 };
 struct HeadArgs {
   HeadPart part[2];
@@ -25,13 +27,16 @@ struct HeadArgs {
   const double* freqs;
   const uint8_t* valid;
   float* sums;                               // backward: [workgroups, 2, dim]
+  int64_t rows;
   int dim, pairs, norm, layout;
   float eps;
+  bool whole;                                // every column turns
 };
 
-__device__ inline float wave_sum(float x) {
+// Sum over groups of L lanes that follow each other.
+template <int L> __device__ inline float group_sum(float x) {
 #pragma unroll
-  for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
+  for (int m = L / 2; m; m >>= 1) x += __shfl_xor(x, m);
   return x;
 }
 
@@ -56,7 +61,9 @@ __device__ inline int partner_of(const HeadArgs& g, int c, int& pair, bool& seco
   return c ^ 1;
 }
 
-template <typename T, int K, bool BACK> __global__ __launch_bounds__(HEAD_THREADS) void head_norm(HeadArgs g, int64_t first) {
+// Any columns: a wave a row, lane l holds columns l, l + 64, .. and, of columns that turn, the partner's value as well,
+// which it normalises itself.
+template <typename T, int K, bool BACK> __global__ __launch_bounds__(HEAD_THREADS) void head_any(HeadArgs g, int64_t first) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t blk = first + blockIdx.x;
   const HeadPart& p = g.part[blk >= g.part[1].first];
@@ -76,82 +83,82 @@ template <typename T, int K, bool BACK> __global__ __launch_bounds__(HEAD_THREAD
     if (p.b) { b[i] = p.b[c]; bp[i] = p.b[other[i]]; }
   }
   for (int64_t it = (blk - p.first) * HEAD_WAVES + wave; it < p.items; it += p.blocks * HEAD_WAVES) {
-    const int64_t row = it / p.heads, head = it - row * p.heads;
-    T* out = static_cast<T*>(p.out) + row * p.out_row + head * p.out_head;
+    const int64_t share = p.items == g.rows ? 0 : it / g.rows, row = it - share * g.rows;
+    const int64_t h0 = share * p.share, h1 = h0 + p.share < p.heads ? h0 + p.share : p.heads;
+    T* out = static_cast<T*>(p.out) + row * p.out_row;
     if (g.valid && !g.valid[row]) {
       if (p.out)
-        for (int c = lane; c < D; c += 64) out[c] = from_f<T>(0.0f);
+        for (int64_t h = h0; h < h1; ++h)
+          for (int c = lane; c < D; c += 64) out[h * p.out_head + c] = from_f<T>(0.0f);
       continue;
     }
-    const T* x = static_cast<const T*>(p.x) + row * p.x_row + head * p.x_head;
-    float n[K], q[K];
-    float s1 = 0.0f;
+    float co[K], si[K];   // si: of the column's own value of the pair, so that y = y co + partner si
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-      const int c = lane + 64 * i;
-      n[i] = c < D ? to_f<T>(x[c]) : 0.0f;
-      q[i] = !BACK && pair[i] >= 0 ? to_f<T>(x[other[i]]) : 0.0f;
-      s1 += n[i];
-    }
-    float r = 1.0f;
-    if (g.norm != SPZ_NORM_NONE) {
-      const float mean = g.norm == SPZ_NORM_LAYER ? wave_sum(s1) * inv : 0.0f;
-      float s2 = 0.0f;
-#pragma unroll
-      for (int i = 0; i < K; ++i) {
-        n[i] -= mean;
-        q[i] -= mean;
-        s2 += lane + 64 * i < D ? n[i] * n[i] : 0.0f;
+      co[i] = 1.0f;
+      si[i] = 0.0f;
+      if (pair[i] >= 0) {
+        turn_of(g.positions[row], g.freqs[pair[i]], co[i], si[i]);
+        if (second[i] == BACK) si[i] = -si[i];
       }
-      r = 1.0f / sqrtf(wave_sum(s2) * inv + g.eps);
     }
-    if constexpr (!BACK) {
+    for (int64_t h = h0; h < h1; ++h) {
+      const T* x = static_cast<const T*>(p.x) + row * p.x_row + h * p.x_head;
+      const T* dy = BACK ? static_cast<const T*>(p.dy) + row * p.dy_row + h * p.dy_head : nullptr;
+      float n[K], q[K], d[K];
+      float s1 = 0.0f;
 #pragma unroll
       for (int i = 0; i < K; ++i) {
         const int c = lane + 64 * i;
-        if (c >= D) continue;
-        float y = fmaf(n[i] * r, w[i], b[i]);
-        if (pair[i] >= 0) {
-          float co, si;
-          turn_of(g.positions[row], g.freqs[pair[i]], co, si);
-          const float z = fmaf(q[i] * r, wp[i], bp[i]);
-          y = y * co + (second[i] ? z * si : -(z * si));
-        }
-        out[c] = from_f<T>(y);
+        n[i] = c < D ? to_f<T>(x[c]) : 0.0f;
+        q[i] = pair[i] >= 0 ? to_f<T>(BACK ? dy[other[i]] : x[other[i]]) : 0.0f;
+        if (BACK) d[i] = c < D ? to_f<T>(dy[c]) : 0.0f;
+        s1 += n[i];
       }
-    } else {
-      const T* dy = static_cast<const T*>(p.dy) + row * p.dy_row + head * p.dy_head;
-      float d[K], a1 = 0.0f, a2 = 0.0f;
+      float r = 1.0f;
+      if (g.norm != SPZ_NORM_NONE) {
+        const float mean = g.norm == SPZ_NORM_LAYER ? group_sum<64>(s1) * inv : 0.0f;
+        float s2 = 0.0f;
 #pragma unroll
-      for (int i = 0; i < K; ++i) {
-        const int c = lane + 64 * i;
-        d[i] = 0.0f;
-        if (c >= D) continue;
-        n[i] *= r;
-        d[i] = to_f<T>(dy[c]);
-        if (pair[i] >= 0) {   // turned back
-          float co, si;
-          turn_of(g.positions[row], g.freqs[pair[i]], co, si);
-          const float z = to_f<T>(dy[other[i]]);
-          d[i] = d[i] * co + (second[i] ? -(z * si) : z * si);
+        for (int i = 0; i < K; ++i) {
+          n[i] -= mean;
+          if (!BACK) q[i] -= mean;
+          s2 += lane + 64 * i < D ? n[i] * n[i] : 0.0f;
         }
-        dw[i] = fmaf(d[i], n[i], dw[i]);
-        db[i] += d[i];
-        d[i] *= w[i];
-        a1 += d[i];
-        a2 = fmaf(d[i], n[i], a2);
+        r = 1.0f / sqrtf(group_sum<64>(s2) * inv + g.eps);
       }
-      if (p.out) {
-        if (g.norm != SPZ_NORM_NONE) {
-          a1 = g.norm == SPZ_NORM_LAYER ? wave_sum(a1) * inv : 0.0f;
-          a2 = wave_sum(a2) * inv;
-        } else {
-          a1 = a2 = 0.0f;
-        }
+      if constexpr (!BACK) {
 #pragma unroll
         for (int i = 0; i < K; ++i) {
           const int c = lane + 64 * i;
-          if (c < D) out[c] = from_f<T>(r * (d[i] - fmaf(n[i], a2, a1)));
+          float y = fmaf(n[i] * r, w[i], b[i]);
+          if (pair[i] >= 0) y = fmaf(y, co[i], fmaf(q[i] * r, wp[i], bp[i]) * si[i]);
+          if (c < D) out[h * p.out_head + c] = from_f<T>(y);
+        }
+      } else {
+        float a1 = 0.0f, a2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+          n[i] = lane + 64 * i < D ? n[i] * r : 0.0f;
+          if (pair[i] >= 0) d[i] = fmaf(d[i], co[i], q[i] * si[i]);   // turned back
+          dw[i] = fmaf(d[i], n[i], dw[i]);
+          db[i] += d[i];
+          d[i] *= w[i];
+          a1 += d[i];
+          a2 = fmaf(d[i], n[i], a2);
+        }
+        if (p.out) {
+          if (g.norm != SPZ_NORM_NONE) {
+            a1 = g.norm == SPZ_NORM_LAYER ? group_sum<64>(a1) * inv : 0.0f;
+            a2 = group_sum<64>(a2) * inv;
+          } else {
+            a1 = a2 = 0.0f;
+          }
+#pragma unroll
+          for (int i = 0; i < K; ++i) {
+            const int c = lane + 64 * i;
+            if (c < D) out[h * p.out_head + c] = from_f<T>(r * (d[i] - fmaf(n[i], a2, a1)));
+          }
         }
       }
     }
@@ -174,28 +181,261 @@ template <typename T, int K, bool BACK> __global__ __launch_bounds__(HEAD_THREAD
   }
 }
 
-// The workgroups' partial sums, in a fixed order: thread (column, group) takes every 4th row.
-constexpr int HSUM_COLS = 64, HSUM_GROUPS = 4;
+// N elements at any alignment of the type, as loaded and as floats.
+template <typename T, int N> struct Run {
+  uint32_t w[N * sizeof(T) / 4];
+  __device__ inline void load(const T* p) { __builtin_memcpy(w, p, sizeof(w)); }
+  __device__ inline void clear() {
+#pragma unroll
+    for (uint32_t& u : w) u = 0;
+  }
+  __device__ inline void floats(float* x) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (sizeof(T) == 4) x[i] = __builtin_bit_cast(float, w[i % (N * sizeof(T) / 4)]);
+      else x[i] = __builtin_bit_cast(float, (i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    }
+  }
+};
+template <typename T, int N> __device__ inline void store_n(T* p, const float* x) {
+  uint32_t w[N * sizeof(T) / 4];
+#pragma unroll
+  for (int i = 0; i < (int)(N * sizeof(T) / 4); ++i) {
+    if (sizeof(T) == 4) w[i] = __builtin_bit_cast(uint32_t, x[i]);
+    else w[i] = pack_bf16x2(x[(2 * i) % N], x[(2 * i + 1) % N]);
+  }
+  __builtin_memcpy(p, w, sizeof(w));
+}
+
+// Columns in vectors: a group of L lanes a row, each lane two runs of SV columns, which turn together where pairs are
+// halves (columns c .. and pairs + c ..) and by themselves where they are neighbours.
+template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEAD_THREADS) void head_vectors(HeadArgs g, int64_t first) {
+  constexpr int N = 2 * SV, GROUPS = HEAD_THREADS / L;
+  const int j = threadIdx.x % L;
+  const int64_t blk = first + blockIdx.x;
+  const HeadPart& p = g.part[blk >= g.part[1].first];
+  const int D = g.dim;
+  const float inv = 1.0f / (float)D;
+  const bool halves = g.layout == SPZ_PAIRS_HALVES, on = j * N < D;
+  int ca = j * N, cb = ca + SV, pair = ca / 2, turning = SV;   // turning: the lane's pairs that turn
+  if (halves) {
+    if (j * SV < g.pairs) { ca = pair = j * SV; cb = g.pairs + ca; }
+    else { ca = 2 * g.pairs + (j - g.pairs / SV) * N; cb = ca + SV; turning = 0; }
+  } else {
+    turning = g.pairs - pair < 0 ? 0 : g.pairs - pair < SV ? g.pairs - pair : SV;
+  }
+  float w[N], b[N], dw[N], db[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = i < SV ? ca + i : cb + i - SV;
+    w[i] = on && p.w ? p.w[c] : 1.0f;
+    b[i] = on && p.b ? p.b[c] : 0.0f;
+    dw[i] = db[i] = 0.0f;
+  }
+  const auto turn = [&](float (&x)[N], const float (&co)[SV], const float (&si)[SV]) {
+#pragma unroll
+    for (int i = 0; i < SV; ++i) {
+      const int u = 2 * i, v = 2 * i + 1;   // of neighbours
+      const float a = halves ? x[i] : x[u], z = halves ? x[SV + i] : x[v];
+      const float na = fmaf(a, co[i], -(z * si[i])), nz = fmaf(a, si[i], z * co[i]);
+      if (halves) {
+        x[i] = g.whole || i < turning ? na : a;
+        x[SV + i] = g.whole || i < turning ? nz : z;
+      } else {
+        x[u] = g.whole || i < turning ? na : a;
+        x[v] = g.whole || i < turning ? nz : z;
+      }
+    }
+  };
+  for (int64_t it = (blk - p.first) * GROUPS + threadIdx.x / L; it < (p.items + GROUPS - 1) / GROUPS * GROUPS; it += p.blocks * GROUPS) {
+    const bool item = it < p.items;   // whole waves stay together for the sums
+    const int64_t share = !item || p.items == g.rows ? 0 : it / g.rows, row = item ? it - share * g.rows : 0;
+    const int64_t h0 = share * p.share;
+    const int count = !item ? 0 : h0 + p.share < p.heads ? p.share : (int)(p.heads - h0);
+    const bool live = item && (!g.valid || g.valid[row]);
+    float co[SV], si[SV];
+#pragma unroll
+    for (int i = 0; i < SV; ++i) {
+      co[i] = 1.0f;
+      si[i] = 0.0f;
+    }
+    if (g.pairs && live && on && turning) {
+      const int32_t at = g.positions[row];
+#pragma unroll
+      for (int i = 0; i < SV; ++i)
+        if (g.whole || i < turning) {
+          turn_of(at, g.freqs[pair + i], co[i], si[i]);
+          if (BACK) si[i] = -si[i];
+        }
+    }
+    const T* x = static_cast<const T*>(p.x) + row * p.x_row + h0 * p.x_head;
+    const T* dy = BACK ? static_cast<const T*>(p.dy) + row * p.dy_row + h0 * p.dy_head : nullptr;
+    T* out = static_cast<T*>(p.out) + row * p.out_row + h0 * p.out_head;
+    float n[N], d[N];
+    Run<T, SV> next[2], next_d[2];
+    const bool reads = live && on;
+    const auto fetch = [&](int h) {
+      if (reads && h < count) {
+        next[0].load(x + h * p.x_head + ca);
+        next[1].load(x + h * p.x_head + cb);
+        if (BACK) {
+          next_d[0].load(dy + h * p.dy_head + ca);
+          next_d[1].load(dy + h * p.dy_head + cb);
+        }
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      next[i].clear();
+      next_d[i].clear();
+    }
+    fetch(0);
+    for (int h = 0; h < p.share; ++h) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        next[i].floats(n + i * SV);
+        if (BACK) next_d[i].floats(d + i * SV);
+      }
+      fetch(h + 1);
+      float r = 1.0f;
+      if (g.norm != SPZ_NORM_NONE) {
+        if (g.norm == SPZ_NORM_LAYER) {
+          float s1 = 0.0f;
+#pragma unroll
+          for (int i = 0; i < N; ++i) s1 += n[i];
+          const float mean = group_sum<L>(s1) * inv;
+#pragma unroll
+          for (int i = 0; i < N; ++i) n[i] = on ? n[i] - mean : 0.0f;
+        }
+        float s2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) s2 = fmaf(n[i], n[i], s2);
+        r = 1.0f / sqrtf(group_sum<L>(s2) * inv + g.eps);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) n[i] *= r;
+      if constexpr (!BACK) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) n[i] = fmaf(n[i], w[i], b[i]);
+        if (g.pairs) turn(n, co, si);
+        if (on && h < count) {
+          if (!live) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) n[i] = 0.0f;
+          }
+          store_n<T, SV>(out + h * p.out_head + ca, n);
+          store_n<T, SV>(out + h * p.out_head + cb, n + SV);
+        }
+      } else {
+        if (g.pairs) turn(d, co, si);
+        float a1 = 0.0f, a2 = 0.0f;
+        const bool counts = reads && h < count;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          if (!counts) d[i] = n[i] = 0.0f;
+          dw[i] = fmaf(d[i], n[i], dw[i]);
+          db[i] += d[i];
+          d[i] *= w[i];
+          a1 += d[i];
+          a2 = fmaf(d[i], n[i], a2);
+        }
+        if (p.out) {
+          if (g.norm != SPZ_NORM_NONE) {
+            a1 = g.norm == SPZ_NORM_LAYER ? group_sum<L>(a1) * inv : 0.0f;
+            a2 = group_sum<L>(a2) * inv;
+#pragma unroll
+            for (int i = 0; i < N; ++i) d[i] = r * (d[i] - fmaf(n[i], a2, a1));
+          }
+          if (on && h < count) {
+            if (!live) {
+#pragma unroll
+              for (int i = 0; i < N; ++i) d[i] = 0.0f;
+            }
+            store_n<T, SV>(out + h * p.out_head + ca, d);
+            store_n<T, SV>(out + h * p.out_head + cb, d + SV);
+          }
+        }
+      }
+    }
+  }
+  if constexpr (BACK) {
+    // The groups of a wave, then the waves.
+    __shared__ float part[HEAD_WAVES][2][L * N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int m = L; m < 64; m <<= 1) {
+        dw[i] += __shfl_xor(dw[i], m);
+        db[i] += __shfl_xor(db[i], m);
+      }
+      if (threadIdx.x % 64 < L) {
+        part[threadIdx.x / 64][0][i * L + j] = dw[i];
+        part[threadIdx.x / 64][1][i * L + j] = db[i];
+      }
+    }
+    __syncthreads();
+    float* to = g.sums + blk * 2 * D;
+    if (threadIdx.x < L && on)
+      for (int i = 0; i < N; ++i)
+        for (int v = 0; v < 2; ++v) {
+          float s = 0.0f;
+          for (int k = 0; k < HEAD_WAVES; ++k) s += part[k][v][i * L + j];
+          to[v * D + (i < SV ? ca + i : cb + i - SV)] = s;
+        }
+  }
+}
+
+// The workgroups' partial sums, in a fixed order: thread (column, group) takes every 16th row.
+constexpr int HSUM_COLS = 64, HSUM_GROUPS = 16;
 struct HeadSums { float* out[2][2]; int64_t first[2], blocks[2]; };
 __global__ __launch_bounds__(HSUM_COLS* HSUM_GROUPS) void head_sums(const float* sums, HeadSums o, int dim) {
   __shared__ float part[HSUM_GROUPS][HSUM_COLS];
-  const int c = blockIdx.x * HSUM_COLS + threadIdx.x % HSUM_COLS, grp = threadIdx.x / HSUM_COLS;
+  const int col = threadIdx.x % HSUM_COLS, c = blockIdx.x * HSUM_COLS + col, grp = threadIdx.x / HSUM_COLS;
   const int which = blockIdx.y >> 1, v = blockIdx.y & 1;
   float* out = o.out[which][v];
+  if (!out) return;
   float s = 0.0f;
-  if (out && c < dim)
-    for (int64_t k = grp; k < o.blocks[which]; k += HSUM_GROUPS) s += sums[((o.first[which] + k) * 2 + v) * dim + c];
-  part[grp][threadIdx.x % HSUM_COLS] = s;
+  if (c < dim) {
+    const float* from = sums + (o.first[which] * 2 + v) * dim + c;
+#pragma unroll 8
+    for (int64_t k = grp; k < o.blocks[which]; k += HSUM_GROUPS) s += from[k * 2 * dim];
+  }
+  part[grp][col] = s;
   __syncthreads();
-  if (grp == 0 && out && c < dim) {
-    for (int k = 1; k < HSUM_GROUPS; ++k) s += part[k][threadIdx.x];
+  if (grp == 0 && c < dim) {
+#pragma unroll
+    for (int k = 1; k < HSUM_GROUPS; ++k) s += part[k][col];
     out[c] = s;
   }
 }
 
-int64_t head_blocks(int64_t items, bool back) {
-  const int64_t n = op_div_up(items, HEAD_WAVES);
-  return back && n > HEAD_BLOCKS ? HEAD_BLOCKS : n;
+// How columns are held: vectors of sv in groups of `lanes`, or (sv 0) any columns by whole waves.
+struct HeadWay { int sv, lanes; };
+HeadWay head_way(const spz_head_norm_args& a) {
+  const int vec = 16 / op_size(a.prec);
+  for (const int sv : {vec, vec / 2})
+    if (a.dim > 0 && a.dim % (2 * sv) == 0 && a.dim / (2 * sv) <= 64 && (a.layout == SPZ_PAIRS_NEIGHBOURS || a.pairs % sv == 0)) {
+      int lanes = 4;
+      while (lanes * 2 * sv < a.dim) lanes *= 2;
+      return {sv, lanes};
+    }
+  return {0, 64};
+}
+
+// Items and workgroups of the parts. A row's heads are divided where whole rows are too few waves.
+void head_spread(HeadArgs& g, const HeadWay& way, bool back) {
+  const int groups = HEAD_THREADS / way.lanes;
+  int64_t at = 0;
+  for (HeadPart& p : g.part) {
+    int64_t share = p.heads;
+    while (share > 1 && g.rows * op_div_up(p.heads, share) * way.lanes < HEAD_FILL * 64) share = (share + 1) / 2;
+    p.share = (int)share;
+    p.items = share > 0 ? g.rows * op_div_up(p.heads, share) : 0;
+    p.first = at;
+    p.blocks = op_div_up(p.items, groups);
+    if (back && p.blocks > HEAD_BLOCKS) p.blocks = HEAD_BLOCKS;
+    at += p.blocks;
+  }
 }
 
 const char* head_check(const spz_head_norm_args* p) {
@@ -238,40 +478,45 @@ const char* head_check_arrays(const spz_head_norm_args& a, bool back) {
   return nullptr;
 }
 
-// The work of a call: without a gradient of its outputs, a part's gradients are zeros, which its kernel does not compute.
 void head_parts(const spz_head_norm_args& a, bool back, HeadArgs& g) {
+  g.rows = a.rows;
   g.part[0] = {a.q, a.q_row, a.q_head, a.w_q, a.b_q, a.dq_out, a.dq_out_row, a.dq_out_head,
-               back ? a.dq : a.q_out, back ? a.dq_row : a.q_out_row, back ? a.dq_head : a.q_out_head, a.heads_q, a.rows * a.heads_q, 0, 0};
+               back ? a.dq : a.q_out, back ? a.dq_row : a.q_out_row, back ? a.dq_head : a.q_out_head, a.heads_q, 0, 0, 0, 0};
   g.part[1] = {a.k, a.k_row, a.k_head, a.w_k, a.b_k, a.dk_out, a.dk_out_row, a.dk_out_head,
-               back ? a.dk : a.k_out, back ? a.dk_row : a.k_out_row, back ? a.dk_head : a.k_out_head, a.heads_k, a.rows * a.heads_k, 0, 0};
-  int64_t at = 0;
-  for (HeadPart& p : g.part) {
-    p.first = at;
-    p.blocks = head_blocks(p.items, back);
-    at += p.blocks;
-  }
+               back ? a.dk : a.k_out, back ? a.dk_row : a.k_out_row, back ? a.dk_head : a.k_out_head, a.heads_k, 0, 0, 0, 0};
 }
 
 template <typename T> __global__ void head_zero(HeadPart p, int dim, int64_t first) {
   const int64_t i = (first + blockIdx.x) * HEAD_THREADS + threadIdx.x;
-  if (i >= p.items * dim) return;
+  if (i >= p.items) return;
   const int64_t it = i / dim, row = it / p.heads;
   static_cast<T*>(p.out)[row * p.out_row + (it - row * p.heads) * p.out_head + (i - it * dim)] = from_f<T>(0.0f);
 }
 
-template <typename T, bool BACK> void head_launch(const HeadArgs& g, hipStream_t s) {
+template <typename T, bool BACK> void head_launch(const HeadArgs& g, const HeadWay& way, hipStream_t s) {
   const int64_t blocks = g.part[1].first + g.part[1].blocks;
-  const auto go = [&](auto k) {
-    op_dispatch(blocks, HEAD_THREADS, [&](int64_t first, dim3 grid) {
-      head_norm<T, decltype(k)::value, BACK><<<grid, HEAD_THREADS, 0, s>>>(g, first);
-    });
-  };
   using std::integral_constant;
-  if (g.dim <= 64) go(integral_constant<int, 1>{});
-  else if (g.dim <= 128) go(integral_constant<int, 2>{});
-  else if (g.dim <= 256) go(integral_constant<int, 4>{});
-  else if (g.dim <= 512) go(integral_constant<int, 8>{});
-  else go(integral_constant<int, 16>{});
+  constexpr int VEC = OP_VEC<T>;
+  const auto dispatch = [&](auto kernel) {
+    op_dispatch(blocks, HEAD_THREADS, [&](int64_t first, dim3 grid) { kernel<<<grid, HEAD_THREADS, 0, s>>>(g, first); });
+  };
+  const auto lanes = [&](auto sv) {
+    constexpr int SV = decltype(sv)::value;
+    switch (way.lanes) {
+      case 4: return dispatch(head_vectors<T, SV, 4, BACK>);
+      case 8: return dispatch(head_vectors<T, SV, 8, BACK>);
+      case 16: return dispatch(head_vectors<T, SV, 16, BACK>);
+      case 32: return dispatch(head_vectors<T, SV, 32, BACK>);
+      default: return dispatch(head_vectors<T, SV, 64, BACK>);
+    }
+  };
+  if (way.sv == VEC) lanes(integral_constant<int, VEC>{});
+  else if (way.sv) lanes(integral_constant<int, VEC / 2>{});
+  else if (g.dim <= 64) dispatch(head_any<T, 1, BACK>);
+  else if (g.dim <= 128) dispatch(head_any<T, 2, BACK>);
+  else if (g.dim <= 256) dispatch(head_any<T, 4, BACK>);
+  else if (g.dim <= 512) dispatch(head_any<T, 8, BACK>);
+  else dispatch(head_any<T, 16, BACK>);
 }
 
 int head_run(const char* call, const spz_head_norm_args* args, bool back, void* ws, int64_t ws_bytes, void* stream) {
@@ -288,6 +533,7 @@ int head_run(const char* call, const spz_head_norm_args* args, bool back, void* 
   g.pairs = (int)a.pairs;
   g.norm = a.norm;
   g.layout = a.layout;
+  g.whole = 2 * a.pairs == a.dim;
   g.eps = a.eps;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (back) {
@@ -296,30 +542,27 @@ int head_run(const char* call, const spz_head_norm_args* args, bool back, void* 
     if (need > 0 && !op_aligned(ws, 16)) return op_error(SPZ_EINVAL, call, "workspace not aligned to 16 bytes");
     g.sums = static_cast<float*>(ws);
     for (HeadPart& p : g.part)
-      if (!p.dy && p.items > 0) {   // no gradient comes in
-        if (p.out && a.dim > 0)
-          op_dispatch(op_div_up(p.items * a.dim, HEAD_THREADS), HEAD_THREADS, [&](int64_t first, dim3 grid) {
+      if (!p.dy && p.heads > 0 && a.rows > 0) {   // no gradient comes in: zeros, and nothing for the kernel to do
+        p.items = a.rows * p.heads * a.dim;
+        if (p.out && p.items > 0)
+          op_dispatch(op_div_up(p.items, HEAD_THREADS), HEAD_THREADS, [&](int64_t first, dim3 grid) {
             if (a.prec == SPZ_PREC_BF16) head_zero<bf16_t><<<grid, HEAD_THREADS, 0, s>>>(p, g.dim, first);
             else head_zero<float><<<grid, HEAD_THREADS, 0, s>>>(p, g.dim, first);
           });
-        p.items = 0;
+        p.heads = 0;
       }
-    int64_t at = 0;
-    for (HeadPart& p : g.part) {
-      p.first = at;
-      p.blocks = head_blocks(p.items, back);
-      at += p.blocks;
-    }
   }
+  const HeadWay way = head_way(a);
+  head_spread(g, way, back);
   const int64_t blocks = g.part[1].first + g.part[1].blocks;
   if (a.dim == 0 || (!back && blocks == 0)) return SPZ_OK;
   if (blocks > 0) {
     if (a.prec == SPZ_PREC_BF16) {
-      if (back) head_launch<bf16_t, true>(g, s);
-      else head_launch<bf16_t, false>(g, s);
+      if (back) head_launch<bf16_t, true>(g, way, s);
+      else head_launch<bf16_t, false>(g, way, s);
     } else {
-      if (back) head_launch<float, true>(g, s);
-      else head_launch<float, false>(g, s);
+      if (back) head_launch<float, true>(g, way, s);
+      else head_launch<float, false>(g, way, s);
     }
   }
   if (back && (a.dw_q || a.db_q || a.dw_k || a.db_k)) {
@@ -341,6 +584,7 @@ int64_t spz_head_norm_workspace(const spz_head_norm_args* args) {
   if (bad) return op_error(SPZ_EINVAL, "spz_head_norm_workspace", bad);
   HeadArgs g{};
   head_parts(*args, true, g);
+  head_spread(g, head_way(*args), true);
   return (g.part[1].first + g.part[1].blocks) * 2 * args->dim * 4;
 }
 
