@@ -108,11 +108,7 @@ __device__ inline float block_max(const float (&x)[8]) {
     const uint32_t u = __builtin_bit_cast(uint32_t, x[i]) & 0x7FFFFFFFu;
     m = u > m ? u : m;
   }
-#pragma unroll
-  for (int k = 16; k; k >>= 1) {
-    const uint32_t u = (uint32_t)__shfl_xor((int)m, k);
-    m = u > m ? u : m;
-  }
+  m = max32(m);
   return __builtin_bit_cast(float, m);
 }
 

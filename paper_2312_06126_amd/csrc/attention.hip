@@ -92,8 +92,7 @@ template <typename T, int KR> __global__ __launch_bounds__(STEP_THREADS) void li
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      o[j] += __shfl_xor(o[j], 16);
-      o[j] += __shfl_xor(o[j], 32);
+      o[j] = add32(add16(o[j]));
       if (lane < 16) part[p & 1][wave][4 * lane + j] = o[j];
     }
     __syncthreads();
@@ -616,8 +615,7 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
           }
         keep = cut ? 0.0f : keep * d;
         if constexpr (!STATE) {
-          o += __shfl_xor(o, 16);
-          o += __shfl_xor(o, 32);
+          o = add32(add16(o));
           if (q == 0 && mine) reinterpret_cast<T*>(out + (back ? 15 * out_step : 0) + p * out_walk)[col] = from_f<T>(r.out_scale * o);
         }
       }

@@ -41,28 +41,6 @@ struct NormArgs {
 };
 
 // ----------------------------------------------------------------------------- sums over a row
-template <int CTRL> __device__ inline float dpp_add(float x) {
-  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
-}
-// Over 16 lanes (every lane gets it): neighbours, pairs, the halves mirrored, the row mirrored.
-__device__ inline float sum16(float x) {
-  x = dpp_add<0xB1>(x);
-  x = dpp_add<0x4E>(x);
-  x = dpp_add<0x141>(x);
-  return dpp_add<0x140>(x);
-}
-__device__ inline float sum32(float x) {
-  x = sum16(x);
-  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-  const uint32_t a = r[0], b = r[1];
-  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
-}
-__device__ inline float sum64(float x) {
-  x = sum32(x);
-  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-  const uint32_t a = r[0], b = r[1];
-  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
-}
 // Sums over the TPR threads of a row. More than a wave: through LDS, two buffers in turn so that one
 // barrier a sum is enough (a wave that writes a buffer again has passed the other one's barrier).
 template <int TPR> struct RowSum {

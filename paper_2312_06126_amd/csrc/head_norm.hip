@@ -35,9 +35,9 @@ struct HeadArgs {
 
 // Sum over groups of L lanes that follow each other.
 template <int L> __device__ inline float group_sum(float x) {
-#pragma unroll
-  for (int m = L / 2; m; m >>= 1) x += __shfl_xor(x, m);
-  return x;
+  if constexpr (L >= 16) return L == 16 ? sum16(x) : L == 32 ? sum32(x) : sum64(x);
+  x = dpp_add<0x4E>(dpp_add<0xB1>(x));
+  return L == 8 ? dpp_add<0x141>(x) : x;
 }
 
 // Cosine and sine of pos * freq: the angle in turns less the nearest whole number of them, in 64 bits, so that
@@ -59,6 +59,12 @@ __device__ inline int partner_of(const HeadArgs& g, int c, int& pair, bool& seco
   second = c & 1;
   pair = c >> 1;
   return c ^ 1;
+}
+
+// Which share of its row's heads an item is (64-bit divisions are slow).
+__device__ inline int64_t share_of(const HeadPart& p, int64_t rows, int64_t it) {
+  if (p.items == rows) return 0;
+  return p.items < (int64_t)1 << 32 ? (int64_t)((uint32_t)it / (uint32_t)rows) : it / rows;
 }
 
 // Any columns: a wave a row, lane l holds columns l, l + 64, .. and, of columns that turn, the partner's value as well,
@@ -83,7 +89,7 @@ template <typename T, int K, bool BACK> __global__ __launch_bounds__(HEAD_THREAD
     if (p.b) { b[i] = p.b[c]; bp[i] = p.b[other[i]]; }
   }
   for (int64_t it = (blk - p.first) * HEAD_WAVES + wave; it < p.items; it += p.blocks * HEAD_WAVES) {
-    const int64_t share = p.items == g.rows ? 0 : it / g.rows, row = it - share * g.rows;
+    const int64_t share = share_of(p, g.rows, it), row = it - share * g.rows;
     const int64_t h0 = share * p.share, h1 = h0 + p.share < p.heads ? h0 + p.share : p.heads;
     T* out = static_cast<T*>(p.out) + row * p.out_row;
     if (g.valid && !g.valid[row]) {
@@ -183,8 +189,12 @@ template <typename T, int K, bool BACK> __global__ __launch_bounds__(HEAD_THREAD
 
 // N elements at any alignment of the type, as loaded and as floats.
 template <typename T, int N> struct Run {
-  uint32_t w[N * sizeof(T) / 4];
-  __device__ inline void load(const T* p) { __builtin_memcpy(w, p, sizeof(w)); }
+  static constexpr int WORDS = (N * (int)sizeof(T) + 3) / 4;
+  uint32_t w[WORDS];
+  __device__ inline void load(const T* p) {
+    if constexpr (N * sizeof(T) % 4) w[0] = (uint32_t)*reinterpret_cast<const uint16_t*>(p);
+    else __builtin_memcpy(w, p, sizeof(w));
+  }
   __device__ inline void clear() {
 #pragma unroll
     for (uint32_t& u : w) u = 0;
@@ -192,13 +202,17 @@ template <typename T, int N> struct Run {
   __device__ inline void floats(float* x) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (sizeof(T) == 4) x[i] = __builtin_bit_cast(float, w[i % (N * sizeof(T) / 4)]);
+      if (sizeof(T) == 4) x[i] = __builtin_bit_cast(float, w[i % WORDS]);
       else x[i] = __builtin_bit_cast(float, (i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     }
   }
 };
 template <typename T, int N> __device__ inline void store_n(T* p, const float* x) {
-  uint32_t w[N * sizeof(T) / 4];
+  if constexpr (N == 1) {
+    *p = from_f<T>(x[0]);
+    return;
+  }
+  uint32_t w[(N * sizeof(T) + 3) / 4];
 #pragma unroll
   for (int i = 0; i < (int)(N * sizeof(T) / 4); ++i) {
     if (sizeof(T) == 4) w[i] = __builtin_bit_cast(uint32_t, x[i]);
@@ -208,7 +222,8 @@ template <typename T, int N> __device__ inline void store_n(T* p, const float* x
 }
 
 // Columns in vectors: a group of L lanes a row, each lane two runs of SV columns, which turn together where pairs are
-// halves (columns c .. and pairs + c ..) and by themselves where they are neighbours.
+// halves (columns c .. and pairs + c ..) and by themselves where they are neighbours. SV = 1 takes any number of columns:
+// the last lane's second one may not exist.
 template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEAD_THREADS) void head_vectors(HeadArgs g, int64_t first) {
   constexpr int N = 2 * SV, GROUPS = HEAD_THREADS / L;
   const int j = threadIdx.x % L;
@@ -216,7 +231,7 @@ template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEA
   const HeadPart& p = g.part[blk >= g.part[1].first];
   const int D = g.dim;
   const float inv = 1.0f / (float)D;
-  const bool halves = g.layout == SPZ_PAIRS_HALVES, on = j * N < D;
+  const bool halves = g.layout == SPZ_PAIRS_HALVES, on = j * N < D, both = on && (SV > 1 || j * N + 1 < D);
   int ca = j * N, cb = ca + SV, pair = ca / 2, turning = SV;   // turning: the lane's pairs that turn
   if (halves) {
     if (j * SV < g.pairs) { ca = pair = j * SV; cb = g.pairs + ca; }
@@ -228,8 +243,9 @@ template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEA
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int c = i < SV ? ca + i : cb + i - SV;
-    w[i] = on && p.w ? p.w[c] : 1.0f;
-    b[i] = on && p.b ? p.b[c] : 0.0f;
+    const bool is = i < SV ? on : both;
+    w[i] = is && p.w ? p.w[c] : 1.0f;
+    b[i] = is && p.b ? p.b[c] : 0.0f;
     dw[i] = db[i] = 0.0f;
   }
   const auto turn = [&](float (&x)[N], const float (&co)[SV], const float (&si)[SV]) {
@@ -249,10 +265,32 @@ template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEA
   };
   for (int64_t it = (blk - p.first) * GROUPS + threadIdx.x / L; it < (p.items + GROUPS - 1) / GROUPS * GROUPS; it += p.blocks * GROUPS) {
     const bool item = it < p.items;   // whole waves stay together for the sums
-    const int64_t share = !item || p.items == g.rows ? 0 : it / g.rows, row = item ? it - share * g.rows : 0;
+    const int64_t share = !item ? 0 : share_of(p, g.rows, it), row = item ? it - share * g.rows : 0;
     const int64_t h0 = share * p.share;
     const int count = !item ? 0 : h0 + p.share < p.heads ? p.share : (int)(p.heads - h0);
     const bool live = item && (!g.valid || g.valid[row]);
+    const T* x = static_cast<const T*>(p.x) + row * p.x_row + h0 * p.x_head;
+    const T* dy = BACK ? static_cast<const T*>(p.dy) + row * p.dy_row + h0 * p.dy_head : nullptr;
+    T* out = static_cast<T*>(p.out) + row * p.out_row + h0 * p.out_head;
+    float n[N], d[N];
+    Run<T, SV> next[2], next_d[2];
+    const bool reads = live && on;
+    const auto fetch = [&](int h) {
+      if (reads && h < count) {
+        next[0].load(x + h * p.x_head + ca);
+        if (both) next[1].load(x + h * p.x_head + cb);
+        if (BACK) {
+          next_d[0].load(dy + h * p.dy_head + ca);
+          if (both) next_d[1].load(dy + h * p.dy_head + cb);
+        }
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      next[i].clear();
+      next_d[i].clear();
+    }
+    fetch(0);
     float co[SV], si[SV];
 #pragma unroll
     for (int i = 0; i < SV; ++i) {
@@ -268,28 +306,6 @@ template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEA
           if (BACK) si[i] = -si[i];
         }
     }
-    const T* x = static_cast<const T*>(p.x) + row * p.x_row + h0 * p.x_head;
-    const T* dy = BACK ? static_cast<const T*>(p.dy) + row * p.dy_row + h0 * p.dy_head : nullptr;
-    T* out = static_cast<T*>(p.out) + row * p.out_row + h0 * p.out_head;
-    float n[N], d[N];
-    Run<T, SV> next[2], next_d[2];
-    const bool reads = live && on;
-    const auto fetch = [&](int h) {
-      if (reads && h < count) {
-        next[0].load(x + h * p.x_head + ca);
-        next[1].load(x + h * p.x_head + cb);
-        if (BACK) {
-          next_d[0].load(dy + h * p.dy_head + ca);
-          next_d[1].load(dy + h * p.dy_head + cb);
-        }
-      }
-    };
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      next[i].clear();
-      next_d[i].clear();
-    }
-    fetch(0);
     for (int h = 0; h < p.share; ++h) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -305,7 +321,7 @@ template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEA
           for (int i = 0; i < N; ++i) s1 += n[i];
           const float mean = group_sum<L>(s1) * inv;
 #pragma unroll
-          for (int i = 0; i < N; ++i) n[i] = on ? n[i] - mean : 0.0f;
+          for (int i = 0; i < N; ++i) n[i] = (i < SV ? on : both) ? n[i] - mean : 0.0f;
         }
         float s2 = 0.0f;
 #pragma unroll
@@ -324,7 +340,7 @@ template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEA
             for (int i = 0; i < N; ++i) n[i] = 0.0f;
           }
           store_n<T, SV>(out + h * p.out_head + ca, n);
-          store_n<T, SV>(out + h * p.out_head + cb, n + SV);
+          if (both) store_n<T, SV>(out + h * p.out_head + cb, n + SV);
         }
       } else {
         if (g.pairs) turn(d, co, si);
@@ -352,7 +368,7 @@ template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEA
               for (int i = 0; i < N; ++i) d[i] = 0.0f;
             }
             store_n<T, SV>(out + h * p.out_head + ca, d);
-            store_n<T, SV>(out + h * p.out_head + cb, d + SV);
+            if (both) store_n<T, SV>(out + h * p.out_head + cb, d + SV);
           }
         }
       }
@@ -376,7 +392,7 @@ template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEA
     __syncthreads();
     float* to = g.sums + blk * 2 * D;
     if (threadIdx.x < L && on)
-      for (int i = 0; i < N; ++i)
+      for (int i = 0; i < (both ? N : N - 1); ++i)
         for (int v = 0; v < 2; ++v) {
           float s = 0.0f;
           for (int k = 0; k < HEAD_WAVES; ++k) s += part[k][v][i * L + j];
@@ -409,16 +425,24 @@ __global__ __launch_bounds__(HSUM_COLS* HSUM_GROUPS) void head_sums(const float*
   }
 }
 
-// How columns are held: vectors of sv in groups of `lanes`, or (sv 0) any columns by whole waves.
+// How columns are held: two runs of sv in each of `lanes`, or (sv 0) any columns by whole waves. Forward 16 bytes a run;
+// backward 8, whose registers leave room for twice the waves (65536 x (16 + 4) x 64 bf16: 122 us against 132). Calls that do
+// not fill the card take single columns: a lane then has one angle (16 x (4 + 4) x 64 bf16: 4.0 us against 7.0).
 struct HeadWay { int sv, lanes; };
-HeadWay head_way(const spz_head_norm_args& a) {
-  const int vec = 16 / op_size(a.prec);
-  for (const int sv : {vec, vec / 2})
-    if (a.dim > 0 && a.dim % (2 * sv) == 0 && a.dim / (2 * sv) <= 64 && (a.layout == SPZ_PAIRS_NEIGHBOURS || a.pairs % sv == 0)) {
+HeadWay head_way(const spz_head_norm_args& a, bool back) {
+  const int vec = 16 / op_size(a.prec), wide = back ? vec / 2 : vec;
+  const bool few = a.dim <= 128 && a.rows * (a.heads_q + a.heads_k) * (a.dim / 2) < HEAD_FILL * 64 / 2;
+  for (const int sv : {wide, back ? vec : vec / 2})
+    if (!few && a.dim > 0 && a.dim % (2 * sv) == 0 && a.dim / (2 * sv) <= 64 && (a.layout == SPZ_PAIRS_NEIGHBOURS || a.pairs % sv == 0)) {
       int lanes = 4;
       while (lanes * 2 * sv < a.dim) lanes *= 2;
       return {sv, lanes};
     }
+  if (a.dim > 0 && a.dim <= 128) {
+    int lanes = 4;
+    while (lanes * 2 < a.dim) lanes *= 2;
+    return {1, lanes};
+  }
   return {0, 64};
 }
 
@@ -511,7 +535,8 @@ template <typename T, bool BACK> void head_launch(const HeadArgs& g, const HeadW
     }
   };
   if (way.sv == VEC) lanes(integral_constant<int, VEC>{});
-  else if (way.sv) lanes(integral_constant<int, VEC / 2>{});
+  else if (way.sv == VEC / 2) lanes(integral_constant<int, VEC / 2>{});
+  else if (way.sv) lanes(integral_constant<int, 1>{});
   else if (g.dim <= 64) dispatch(head_any<T, 1, BACK>);
   else if (g.dim <= 128) dispatch(head_any<T, 2, BACK>);
   else if (g.dim <= 256) dispatch(head_any<T, 4, BACK>);
@@ -552,7 +577,7 @@ int head_run(const char* call, const spz_head_norm_args* args, bool back, void* 
         p.heads = 0;
       }
   }
-  const HeadWay way = head_way(a);
+  const HeadWay way = head_way(a, back);
   head_spread(g, way, back);
   const int64_t blocks = g.part[1].first + g.part[1].blocks;
   if (a.dim == 0 || (!back && blocks == 0)) return SPZ_OK;
@@ -584,7 +609,7 @@ int64_t spz_head_norm_workspace(const spz_head_norm_args* args) {
   if (bad) return op_error(SPZ_EINVAL, "spz_head_norm_workspace", bad);
   HeadArgs g{};
   head_parts(*args, true, g);
-  head_spread(g, head_way(*args), true);
+  head_spread(g, head_way(*args, true), true);
   return (g.part[1].first + g.part[1].blocks) * 2 * args->dim * 4;
 }
 

@@ -1,4 +1,4 @@
-// Shared by the operators of the recurrent block (scan.hip, block_norm.hip, quant.hip):
+// Shared by the operators (scan.hip, block_norm.hip, quant.hip, head_norm.hip, attention.hip, adamw.hip):
 // argument checks, vector accesses and the arithmetic they have in common.
 #pragma once
 
@@ -110,6 +110,46 @@ template <typename T> __device__ inline void store_part(T* p, const u32x4& v, in
       const uint32_t bits = sizeof(T) == 4 ? w[i & 3] : (i & 1) ? w[(i / 2) & 3] & 0xFFFF0000u : w[(i / 2) & 3] << 16;
       p[i] = from_f<T>(__builtin_bit_cast(float, bits));   // exact: the value is one of T
     }
+}
+
+// ----------------------------------------------------------------------------- across lanes
+template <int CTRL> __device__ inline float dpp_add(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+}
+// Over 16 lanes (every lane gets it): neighbours, pairs, the halves mirrored, the row mirrored.
+__device__ inline float sum16(float x) {
+  x = dpp_add<0xB1>(x);
+  x = dpp_add<0x4E>(x);
+  x = dpp_add<0x141>(x);
+  return dpp_add<0x140>(x);
+}
+// The sum of the two rows of 16 lanes, and of the two halves of a wave.
+__device__ inline float add16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a = r[0], b = r[1];
+  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+__device__ inline float add32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a = r[0], b = r[1];
+  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+__device__ inline float sum32(float x) { return add16(sum16(x)); }
+__device__ inline float sum64(float x) { return add32(sum32(x)); }
+template <int CTRL> __device__ inline uint32_t dpp_max(uint32_t x) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+  return o > x ? o : x;
+}
+__device__ inline uint32_t max16(uint32_t x) {   // of 16 lanes
+  x = dpp_max<0xB1>(x);    // neighbours, pairs, the halves of 16 lanes mirrored, the 16 mirrored
+  x = dpp_max<0x4E>(x);
+  x = dpp_max<0x141>(x);
+  return dpp_max<0x140>(x);
+}
+__device__ inline uint32_t max32(uint32_t x) {   // of 32 lanes
+  x = max16(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return r[0] > r[1] ? r[0] : r[1];
 }
 
 // ----------------------------------------------------------------------------- arithmetic

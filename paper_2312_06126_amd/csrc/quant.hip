@@ -26,21 +26,6 @@ constexpr int FRAG = 1024;
 
 inline int64_t frag_blocks(int64_t n) { return op_div_up(n, 32); }
 
-template <int CTRL> __device__ inline uint32_t dpp_max(uint32_t x) {
-  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
-  return o > x ? o : x;
-}
-__device__ inline uint32_t max16(uint32_t x) {   // of 16 lanes
-  x = dpp_max<0xB1>(x);    // neighbours, pairs, the halves of 16 lanes mirrored, the 16 mirrored
-  x = dpp_max<0x4E>(x);
-  x = dpp_max<0x141>(x);
-  return dpp_max<0x140>(x);
-}
-__device__ inline uint32_t max32(uint32_t x) {   // of 32 lanes
-  x = max16(x);
-  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  return r[0] > r[1] ? r[0] : r[1];
-}
 __device__ inline uint32_t wave_max(uint32_t x) {
   x = max32(x);
   const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
