@@ -100,6 +100,13 @@ __device__ inline float round_random(float x, uint32_t word) {
   return low ? z - 0x1p-6f : z;
 }
 
+// The hardware's square root and reciprocal (an ulp each; a sixth of the instructions of the correctly rounded ones), outside
+// the range that they take correctly the rounded ones.
+__device__ inline float root(float x) { return x >= 0x1p-100f || x == 0.0f ? __builtin_amdgcn_sqrtf(x) : sqrtf(x); }
+__device__ inline float over(float x, float y) {
+  return y >= 0x1p-100f && y <= 0x1p100f ? x * __builtin_amdgcn_rcpf(y) : x / y;
+}
+
 // The largest of a block's magnitudes (half a wave); a NaN stays one.
 __device__ inline float block_max(const float (&x)[8]) {
   uint32_t m = 0;   // magnitudes order as their bits do, NaN above infinity
@@ -115,8 +122,8 @@ __device__ inline float block_max(const float (&x)[8]) {
 template <typename P, typename G, bool EIGHT>
 __global__ __launch_bounds__(ADAM_THREADS) void adamw_step(AdamArgs g) {
   const int64_t blk = g.from + blockIdx.x;
-  int which = 0;
-  for (int k = 1; k < ADAM_TENSORS; ++k) which += g.first[k] <= blk;
+  // The tensor: a lane looks at each one's first workgroup.
+  const int which = __popcll(__ballot(g.first[threadIdx.x % ADAM_TENSORS] <= blk)) - 1;
   const AdamTensor t = g.t[which];
   const int64_t i0 = (blk - g.first[which]) * ADAM_ELEMS + 8 * (int64_t)threadIdx.x;
   const int64_t left = t.n - i0;
@@ -157,8 +164,8 @@ __global__ __launch_bounds__(ADAM_THREADS) void adamw_step(AdamArgs g) {
     const float x = d[i] * gs;
     m[i] = fmaf(g.b1, m[i], g.c1 * x);
     v[i] = fmaf(g.b2, v[i], g.c2 * x * x);
-    r[i] = sqrtf(v[i]);
-    p[i] = fmaf(-lr, fmaf(t.decay, p[i], m[i] * fix1 / fmaf(r[i], fix2, g.eps)), p[i]);
+    r[i] = root(v[i]);
+    p[i] = fmaf(-lr, fmaf(t.decay, p[i], over(m[i] * fix1, fmaf(r[i], fix2, g.eps))), p[i]);
   }
   store8<P>(pp, cnt, p);
   if (t.copy) store8<bf16_t>(reinterpret_cast<bf16_t*>(t.copy) + i0, cnt, p);
@@ -175,12 +182,15 @@ __global__ __launch_bounds__(ADAM_THREADS) void adamw_step(AdamArgs g) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const uint64_t b = (uint64_t)(e >> 2) + k;
-      const U4 u = philox(U4{(uint32_t)b, step, P_MOMENT + ((uint32_t)(b >> 32) << 8), 0u}, (uint32_t)g.seed, (uint32_t)(g.seed >> 32));
+      const U4 u = philox_words(U4{(uint32_t)b, step, P_MOMENT + ((uint32_t)(b >> 32) << 8), 0u}, g.seed);
       w[4 * k] = u.x; w[4 * k + 1] = u.y; w[4 * k + 2] = u.z; w[4 * k + 3] = u.w;
     }
+    // Both sides of tiny scales are raised: a reciprocal below would not be a number of the type.
+    const float up_m = sm < 0x1p-60f ? 0x1p60f : 1.0f, up_r = sr < 0x1p-60f ? 0x1p60f : 1.0f;
+    const float by_m = 1.0f / (sm * up_m), by_r = 1.0f / (sr * up_r);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float x = sm > 0.0f ? fminf(__builtin_fabsf(m[i]) / sm, E4M3_MAX) : 0.0f, y = sr > 0.0f ? fminf(r[i] / sr, E4M3_MAX) : 0.0f;
+      const float x = sm > 0.0f ? fminf(__builtin_fabsf(m[i]) * up_m * by_m, E4M3_MAX) : 0.0f, y = sr > 0.0f ? fminf(r[i] * up_r * by_r, E4M3_MAX) : 0.0f;
       m[i] = __builtin_copysignf(round_random(x, w[i] & 0xFFFFu), m[i]);
       const float z = round_random(y, w[i] >> 16);
       r[i] = r[i] > 0.0f && sr > 0.0f ? fmaxf(z, 0x1p-9f) : z;

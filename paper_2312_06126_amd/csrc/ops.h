@@ -168,24 +168,26 @@ __device__ inline void sigmoid2(float x, float& a, float& b) {
   b = x < 0.0f ? big : small;
 }
 
-// Dropout's 16-bit words of elements 8 blk .. 8 blk + 7 (two to a word, low half first).
-constexpr uint32_t P_DROP = 5;
 // philox() with each round's two products as one 32 x 32 -> 64 instruction and its two exclusive ors as
 // one three-operand instruction: these rounds are a fifth of what a fused kernel computes.
-__device__ inline U4 drop_words(uint64_t blk, uint64_t seed, uint32_t step, uint32_t tensor) {
-  uint32_t c0 = (uint32_t)blk, c1 = step, c2 = P_DROP + ((uint32_t)(blk >> 32) << 8), c3 = tensor;
+__device__ inline U4 philox_words(U4 c, uint64_t seed) {
   uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
-    const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c1, k0, 0x96);
-    c1 = (uint32_t)p1;
-    c2 = __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), c3, k1, 0x96);
-    c3 = (uint32_t)p0;
+    const uint64_t p0 = (uint64_t)c.x * 0xD2511F53u, p1 = (uint64_t)c.z * 0xCD9E8D57u;
+    c.x = __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c.y, k0, 0x96);
+    c.y = (uint32_t)p1;
+    c.z = __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), c.w, k1, 0x96);
+    c.w = (uint32_t)p0;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
-  return U4{c0, c1, c2, c3};
+  return c;
+}
+// Dropout's 16-bit words of elements 8 blk .. 8 blk + 7 (two to a word, low half first).
+constexpr uint32_t P_DROP = 5;
+__device__ inline U4 drop_words(uint64_t blk, uint64_t seed, uint32_t step, uint32_t tensor) {
+  return philox_words(U4{(uint32_t)blk, step, P_DROP + ((uint32_t)(blk >> 32) << 8), tensor}, seed);
 }
 __device__ inline uint32_t drop_half(const U4& w, int i) {
   const uint32_t v = i < 4 ? (i < 2 ? w.x : w.y) : (i < 6 ? w.z : w.w);

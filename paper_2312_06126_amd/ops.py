@@ -719,13 +719,14 @@ class AdamW:
         spans.sort()
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             _refuse("two of the tensors share elements")
-        self.params, self.copies, self.bits, self.weight_decay = params, copies, bits, decay
+        self.params, self.copies, self.bits, self.weight_decay = tuple(params), tuple(copies), bits, tuple(decay)
         kind = torch.float8_e4m3fn if bits == 8 else _F32
         dev = first.device
         self.m, self.v = (torch.zeros(at, dtype=kind, device=dev) for _ in range(2))
         self.m_scale, self.v_scale = (torch.zeros(at // ADAMW_BLOCK, device=dev) if bits == 8 else None for _ in range(2))
         self._moments = at
-        self._layout = [(p.shape, p.dtype, p.data_ptr(), 0 if c is None else c.data_ptr()) for p, c in zip(params, copies)]
+        self._layout = [(p, c, p.shape, p.data_ptr(), _ptr(c)) for p, c in zip(params, copies)]
+        self._entries = [[p.data_ptr(), 0, _ptr(c), p.numel(), at, d] for p, c, at, d in zip(params, copies, self.places, decay)]
 
     def _tensor(self, p, name):
         if not isinstance(p, torch.Tensor) or p.get_device() != self._gpu or p.dtype not in _PREC or not p.is_contiguous():
@@ -760,19 +761,21 @@ class AdamW:
                 _like(t, name, gpu, t.shape, kind, contiguous=True)
         if grad_scale is not None and not isinstance(grad_scale, torch.Tensor):
             _refuse("grad_scale is no tensor")
-        groups = {}
-        for i, (p, c, g) in enumerate(zip(self.params, self.copies, grads)):
+        entries = self._entries
+        grad_on = _grad_on()
+        kinds = set()
+        for i, (g, (p, c, shape, at, to)) in enumerate(zip(grads, self._layout)):
             if g is None:
+                entries[i][1] = 0
                 continue
-            if not isinstance(g, torch.Tensor) or g.dtype not in _PREC or g.shape != p.shape or g.get_device() != gpu or not g.is_contiguous():
-                _refuse("grads[%d] is no contiguous float32 or bfloat16 tensor %s on cuda:%d" % (i, tuple(p.shape), gpu))
-            if g.requires_grad and _grad_on():
+            if not isinstance(g, torch.Tensor) or g.dtype not in _PREC or g.shape != shape or g.get_device() != gpu or not g.is_contiguous():
+                _refuse("grads[%d] is no contiguous float32 or bfloat16 tensor %s on cuda:%d" % (i, tuple(shape), gpu))
+            if grad_on and g.requires_grad:
                 _refuse_grad("grads[%d]" % i)
-            shape, kind, at, to = self._layout[i]
-            if p.shape != shape or p.dtype is not kind or p.data_ptr() != at or (c is not None and c.data_ptr() != to):
+            if p.data_ptr() != at or p.shape != shape or (c is not None and c.data_ptr() != to):
                 _refuse("params[%d] or its copy is not where it was: make another AdamW of the new tensors" % i)
-            groups.setdefault((_PREC[kind], _PREC[g.dtype]), []).append(
-                pack_adamw_tensor(at, g.data_ptr(), to, p.numel(), self.places[i], self.weight_decay[i]))
+            entries[i][1] = g.data_ptr()
+            kinds.add((p.dtype, g.dtype))
 
         if stream is not None or gpu != _device():
             tensors = [*self.params, *self.copies, *grads, self.m, self.v, self.m_scale, self.v_scale, grad_scale]
@@ -780,17 +783,19 @@ class AdamW:
             return _elsewhere(stream, gpu, tensors, lambda: self.step(grads, step=step, lr=lr, betas=betas, eps=eps, grad_scale=grad_scale))
         s = _stream(gpu)
         on_step, on_lr = isinstance(step, torch.Tensor), isinstance(lr, torch.Tensor)
-        for (p_prec, g_prec), entries in groups.items():
-            block = b"".join(entries)
+        some = [i for i, g in enumerate(grads) if g is not None and g.numel()]
+        for kind in kinds:
+            chosen = some if len(kinds) == 1 else [i for i in some if (self.params[i].dtype, grads[i].dtype) == kind]
+            block = b"".join([pack_adamw_tensor(*entries[i]) for i in chosen])
             host = ctypes.create_string_buffer(block, len(block))
             try:
                 b1, b2 = betas
-                a = pack_adamw(len(entries), self._moments, ctypes.addressof(host), self.m.data_ptr(), self.v.data_ptr(), _ptr(self.m_scale),
+                a = pack_adamw(len(chosen), self._moments, ctypes.addressof(host), self.m.data_ptr(), self.v.data_ptr(), _ptr(self.m_scale),
                                _ptr(self.v_scale), _ptr(grad_scale), step.data_ptr() if on_step else 0, lr.data_ptr() if on_lr else 0,
-                               0 if on_step else step, 0.0 if on_lr else lr, b1, b2, eps, self._seed, self.bits, p_prec, g_prec, 0)
+                               0 if on_step else step, 0.0 if on_lr else lr, b1, b2, eps, self._seed, self.bits, _PREC[kind[0]], _PREC[kind[1]], 0)
             except _NOT_NUMBERS as e:
                 _refuse("step, lr, betas or eps is no number: %s" % e)
             rc = lib.spz_adamw(a, s)
             if rc:
                 _done(rc)
-        torch.autograd.graph.increment_version([p for p, g in zip(self.params, grads) if g is not None])
+        torch.autograd.graph.increment_version([self.params[i] for i in some])
