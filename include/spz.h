@@ -553,7 +553,7 @@ int64_t spz_head_norm_workspace(const spz_head_norm_args* args);
 int spz_head_norm_forward(const spz_head_norm_args* args, void* hip_stream);
 int spz_head_norm_backward(const spz_head_norm_args* args, void* workspace, int64_t workspace_bytes, void* hip_stream);
 
-/* Linear attention over `steps` of each of `batch` sequences, in each of `heads` heads with a
+/* Linear attention over `steps` of each of `batch` sequences, in each of `heads` heads (at most 65536) with a
  * state of key_width x value_width (both at most 256):
  *     S_t = d k_t S_{t-1} + key_t^T value_t,   y_t = scale query_t S_t,   d = exp(-rate[head])
  * with S_{-1} = state and k_t = 0 where reset[t] != 0 (step t starts an episode: nothing of the

@@ -11,6 +11,7 @@ namespace spz {
 namespace {
 
 constexpr int LIN_MAX_WIDTH = 256;
+constexpr int64_t LIN_MAX_HEADS = 65536;
 
 struct LinRole {
   const void *a, *b, *c; void* out;          // [batch, steps, heads, ka], ka, nc, nc
@@ -21,14 +22,22 @@ struct LinRole {
   bool back;
   float in, out_scale;
 };
+// x / d for x < 2^31 by a multiplication: 2^(31 + l) / d rounded up, l = ceil(log2 d).
 struct Divisor { uint32_t mul; int shift; };
+__device__ inline uint32_t divided(uint32_t x, const Divisor& d) { return (uint32_t)(((uint64_t)x * d.mul) >> d.shift); }
+Divisor divisor(uint32_t d) {
+  int l = 0;
+  while (((uint64_t)1 << l) < d) ++l;
+  return {(uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), 31 + l};
+}
+
 struct LinArgs {
   LinRole role[3];
   int roles, units, slices[3];               // units: workgroups of a piece of a head, slices: of it for a role
-  uint32_t groups;                           // pieces of heads of a launch
+  uint32_t groups;                           // of a launch: pieces of heads, or (step by step) sequences
   Divisor by_units, by_pieces, by_heads;
   bool far;                                  // 32 bits do not hold 16 steps of an output
-  int64_t batch, steps, heads, first;        // first: steps' kernel: workgroup; chunks' kernel: sequence
+  int64_t batch, steps, heads, first;        // first: sequence that the launch starts with
   int64_t pieces, len;                       // of time, len steps each
   const float* inits[3];                     // states in front of the pieces [batch, heads, pieces, ..], or NULL
   float *adds[2], *keeps[2];                 // what the pieces add, and keep, of the states of the first two roles
@@ -46,57 +55,93 @@ __device__ inline int64_t lin_length(const LinArgs& g, int64_t b) {
 __device__ inline float lin_decay(float rate, int n) { return n == 0 ? 1.0f : expf(-rate * (float)n); }
 
 // Step by step: a workgroup holds 64 columns of a head's state, thread (column group, row group) rows
-// row, row + 16, .. of four columns.
+// row, row + 16, .. of four columns. vec[role]: a thread's four columns are one access of the state's arrays.
 constexpr int STEP_THREADS = 256, STEP_COLS = 64;
-template <typename T, int KR> __global__ __launch_bounds__(STEP_THREADS) void lin_steps(LinArgs g) {
+struct StepArgs { Divisor by_slices[3], by_heads; bool vec[3]; };
+template <typename T, int KR> __global__ __launch_bounds__(STEP_THREADS) void lin_steps(LinArgs g, StepArgs f) {
   const LinRole& r = g.role[blockIdx.y];
-  const int64_t slices = (r.nc + STEP_COLS - 1) / STEP_COLS;
-  const int64_t at = g.first + blockIdx.x;
-  if (at >= g.batch * g.heads * slices) return;
-  const int64_t sl = at % slices, h = at / slices % g.heads, b = at / slices / g.heads;
-  const int c0 = (int)sl * STEP_COLS + 4 * (threadIdx.x & 15), row0 = threadIdx.x >> 4;
+  const int slices = (r.nc + STEP_COLS - 1) / STEP_COLS;
+  const uint32_t at = blockIdx.x, seq = divided(at, f.by_slices[blockIdx.y]), bq = divided(seq, f.by_heads);
+  if (bq >= g.groups) return;
+  const int sl = (int)(at - seq * (uint32_t)slices);
+  const int64_t h = seq - bq * (uint32_t)g.heads, b = g.first + bq;
+  const int c0 = sl * STEP_COLS + 4 * (threadIdx.x & 15), row0 = threadIdx.x >> 4, left = r.nc - c0;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n = lin_length(g, b);
-  const float d = lin_decay(g.rate ? g.rate[h] : 0.0f, 1);
-  const T* pa = static_cast<const T*>(r.a) + b * r.a_batch + h * r.a_head;
-  const T* pb = static_cast<const T*>(r.b) + b * r.b_batch + h * r.b_head;
-  const T* pc = static_cast<const T*>(r.c) + b * r.c_batch + h * r.c_head;
-  T* po = static_cast<T*>(r.out) + b * r.out_batch + h * r.out_head;
+  const bool vec = f.vec[blockIdx.y];
   __shared__ float part[2][4][STEP_COLS];
-  float S[KR][4];
-  const int64_t st = (b * g.heads + h) * r.ka * r.nc;
-#pragma unroll
-  for (int i = 0; i < KR; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int row = row0 + 16 * i;
-      S[i][j] = r.init && row < r.ka && c0 + j < r.nc ? r.init[st + row * r.row_stride + (c0 + j) * r.col_stride] : 0.0f;
-    }
-  for (int64_t p = 0; p < n; ++p) {
+  f32x4 S[KR];
+  const int rs = (int)r.row_stride, cs = (int)r.col_stride, ka = r.ka;
+  const int64_t st = (b * g.heads + h) * ka * r.nc;
+  const float* init = r.init ? r.init + st : nullptr;
+  const int64_t n = lin_length(g, b);
+  const T* pa = r.a ? static_cast<const T*>(r.a) + b * r.a_batch + h * r.a_head : nullptr;
+  const T* pb = r.b ? static_cast<const T*>(r.b) + b * r.b_batch + h * r.b_head : nullptr;
+  const T* pc = r.c ? static_cast<const T*>(r.c) + b * r.c_batch + h * r.c_head : nullptr;
+  T* po = static_cast<T*>(r.out) + b * r.out_batch + h * r.out_head;
+  // The operands of a step, read before the step in front of it is worked on. Rows and columns that do not exist read the
+  // last one, so that no load waits behind a branch.
+  T xa[KR] = {}, xb[KR] = {}, xc[4] = {};
+  bool cut = false;
+  const auto fetch = [&](int64_t p) {
     const int64_t t = r.back ? n - 1 - p : p;
     const int64_t flag = r.back ? t + 1 : t;   // the step whose start cuts the state off
-    const bool cut = g.reset && flag < n && g.reset[b * g.reset_batch + flag * g.reset_step] != 0;
-    const float keep = r.back && p == 0 ? 1.0f : d;
-    float c[4], o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (pa) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c[j] = c0 + j < r.nc && r.c ? to_f<T>(pc[t * r.c_step + c0 + j]) : 0.0f;
+      for (int i = 0; i < KR; ++i) xa[i] = pa[t * r.a_step + (row0 + 16 * i < ka ? row0 + 16 * i : ka - 1)];
+    }
+    if (pb) {
 #pragma unroll
-    for (int i = 0; i < KR; ++i) {
-      const int row = row0 + 16 * i;
-      const float x = row < r.ka && r.a ? to_f<T>(pa[t * r.a_step + row]) : 0.0f, y = row < r.ka && r.b ? to_f<T>(pb[t * r.b_step + row]) : 0.0f;
+      for (int i = 0; i < KR; ++i) xb[i] = pb[t * r.b_step + (row0 + 16 * i < ka ? row0 + 16 * i : ka - 1)];
+    }
+    if (pc) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        S[i][j] = row < r.ka ? fmaf(r.in * y, c[j], cut ? 0.0f : keep * S[i][j]) : 0.0f;
-        o[j] = fmaf(x, S[i][j], o[j]);
+      for (int j = 0; j < 4; ++j) xc[j] = pc[t * r.c_step + (j < left ? c0 + j : r.nc - 1)];
+    }
+    cut = g.reset && flag < n && g.reset[b * g.reset_batch + flag * g.reset_step] != 0;
+  };
+  if (n > 0 && ka > 0) fetch(0);
+#pragma unroll
+  for (int i = 0; i < KR; ++i) {
+    const int row = row0 + 16 * i;
+    S[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (init && row < ka && left > 0) {
+      if (vec) {
+        S[i] = *reinterpret_cast<const f32x4*>(init + row * rs + c0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j < left) S[i][j] = init[row * rs + (c0 + j) * cs];
       }
     }
+  }
+  const float d = lin_decay(g.rate ? g.rate[h] : 0.0f, 1);
+  for (int64_t p = 0; p < n; ++p) {
+    const int64_t t = r.back ? n - 1 - p : p;
+    const float keep = r.back && p == 0 ? 1.0f : d;
+    const bool cuts = cut;
+    float x[KR], y[KR], c[4], o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      o[j] = add32(add16(o[j]));
-      if (lane < 16) part[p & 1][wave][4 * lane + j] = o[j];
+    for (int i = 0; i < KR; ++i) {
+      x[i] = row0 + 16 * i < ka ? to_f<T>(xa[i]) : 0.0f;
+      y[i] = row0 + 16 * i < ka ? r.in * to_f<T>(xb[i]) : 0.0f;
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = j < left ? to_f<T>(xc[j]) : 0.0f;
+    if (p + 1 < n && ka > 0) fetch(p + 1);
+#pragma unroll
+    for (int i = 0; i < KR; ++i)
+      if (row0 + 16 * i < ka) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          S[i][j] = fmaf(y[i], c[j], cuts ? 0.0f : keep * S[i][j]);
+          o[j] = fmaf(x[i], S[i][j], o[j]);
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = add32(add16(o[j]));
+    if (lane < 16) *reinterpret_cast<f32x4*>(&part[p & 1][wave][4 * lane]) = f32x4{o[0], o[1], o[2], o[3]};
     __syncthreads();
-    const int col = (int)sl * STEP_COLS + threadIdx.x;
+    const int col = sl * STEP_COLS + threadIdx.x;
     if (threadIdx.x < STEP_COLS && col < r.nc) {
       float s = 0.0f;
 #pragma unroll
@@ -105,19 +150,25 @@ template <typename T, int KR> __global__ __launch_bounds__(STEP_THREADS) void li
     }
   }
   for (int64_t t = n; t < g.steps; ++t)
-    if (threadIdx.x < STEP_COLS && (int)sl * STEP_COLS + (int)threadIdx.x < r.nc)
-      po[t * r.out_step + sl * STEP_COLS + threadIdx.x] = from_f<T>(0.0f);
+    if (threadIdx.x < STEP_COLS && sl * STEP_COLS + (int)threadIdx.x < r.nc) po[t * r.out_step + sl * STEP_COLS + threadIdx.x] = from_f<T>(0.0f);
   if (!r.last) return;
-  const bool cut = r.back && n > 0 && g.reset && g.reset[b * g.reset_batch] != 0;
+  const bool gone = r.back && n > 0 && g.reset && g.reset[b * g.reset_batch] != 0;
   const float keep = r.back && n > 0 ? d : 1.0f;
+  float* last = r.last + st;
 #pragma unroll
-  for (int i = 0; i < KR; ++i)
+  for (int i = 0; i < KR; ++i) {
+    const int row = row0 + 16 * i;
+    if (row >= ka || left <= 0) continue;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int row = row0 + 16 * i;
-      if (row < r.ka && c0 + j < r.nc)
-        r.last[st + row * r.row_stride + (c0 + j) * r.col_stride] = cut ? 0.0f : keep * S[i][j];
+    for (int j = 0; j < 4; ++j) S[i][j] = gone ? 0.0f : keep * S[i][j];
+    if (vec) {
+      *reinterpret_cast<f32x4*>(last + row * rs + c0) = S[i];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < left) last[row * rs + (c0 + j) * cs] = S[i][j];
     }
+  }
 }
 
 // ----------------------------------------------------------------------------- chunks of steps
@@ -337,9 +388,6 @@ __device__ inline int opaque(int x) {
   asm("" : "+v"(x));
   return x;
 }
-
-// x / d for x < 2^31 by a multiplication: 2^(31 + l) / d rounded up, l = ceil(log2 d).
-__device__ inline uint32_t divided(uint32_t x, const Divisor& d) { return (uint32_t)(((uint64_t)x * d.mul) >> d.shift); }
 
 // A lane's part of a state at row and column strides rs and cs: rows 16 k + 4 q .. of column c.
 template <int TILES>
@@ -700,7 +748,7 @@ const char* lin_check(const spz_linear_attention_args* p) {
   if (!p) return "NULL arguments";
   const spz_linear_attention_args& a = *p;
   if (!op_prec_ok(a.prec)) return "unknown precision";
-  if (!op_extent_ok(a.batch) || !op_extent_ok(a.steps) || !op_extent_ok(a.heads)) return "extent out of range";
+  if (!op_extent_ok(a.batch) || !op_extent_ok(a.steps) || !op_extent_ok(a.heads) || a.heads > LIN_MAX_HEADS) return "extent out of range";
   if (a.key_width < 0 || a.key_width > LIN_MAX_WIDTH || a.value_width < 0 || a.value_width > LIN_MAX_WIDTH) return "width out of range (256 at most)";
   // No device holds more; keeps every index and count within 62 bits.
   const int64_t state = a.key_width * a.value_width;
@@ -730,23 +778,34 @@ const char* lin_check_arrays(const spz_linear_attention_args& a, bool back) {
   return nullptr;
 }
 
-template <typename T> void lin_steps_launch(const LinArgs& g, hipStream_t s) {
-  int64_t blocks = 0;
+template <typename T> void lin_steps_launch(LinArgs g, hipStream_t s) {
+  StepArgs f{};
+  int64_t slices = 1;
   int ka = 0;
   for (int i = 0; i < g.roles; ++i) {
-    const int64_t n = g.batch * g.heads * op_div_up(g.role[i].nc, STEP_COLS);
-    blocks = n > blocks ? n : blocks;
-    ka = g.role[i].ka > ka ? g.role[i].ka : ka;
+    const LinRole& r = g.role[i];
+    const int64_t n = op_div_up(r.nc, STEP_COLS);
+    slices = n > slices ? n : slices;
+    ka = r.ka > ka ? r.ka : ka;
+    f.by_slices[i] = divisor((uint32_t)n);
+    f.vec[i] = r.col_stride == 1 && r.nc % 4 == 0 && op_aligned(r.init, 16) && op_aligned(r.last, 16);
   }
-  op_dispatch(blocks, STEP_THREADS * 3, [&](int64_t first, dim3 grid) {
-    LinArgs part = g;
-    part.first = first;
-    grid.y = (unsigned)g.roles;
-    if (ka <= 16) lin_steps<T, 1><<<grid, STEP_THREADS, 0, s>>>(part);
-    else if (ka <= 64) lin_steps<T, 4><<<grid, STEP_THREADS, 0, s>>>(part);
-    else if (ka <= 128) lin_steps<T, 8><<<grid, STEP_THREADS, 0, s>>>(part);
-    else lin_steps<T, 16><<<grid, STEP_THREADS, 0, s>>>(part);
-  });
+  f.by_heads = divisor((uint32_t)g.heads);
+  // Sequences whose workgroups one dispatch counts (heads are limited).
+  const int64_t most = OP_DISPATCH / (STEP_THREADS * 3) / (g.heads * slices);
+  const auto go = [&](auto kr) {
+    for (int64_t first = 0; first < g.batch; first += most) {
+      const int64_t count = g.batch - first < most ? g.batch - first : most;
+      g.first = first;
+      g.groups = (uint32_t)count;
+      lin_steps<T, decltype(kr)::value><<<dim3((unsigned)(count * g.heads * slices), (unsigned)g.roles), STEP_THREADS, 0, s>>>(g, f);
+    }
+  };
+  using std::integral_constant;
+  if (ka <= 16) go(integral_constant<int, 1>{});
+  else if (ka <= 64) go(integral_constant<int, 4>{});
+  else if (ka <= 128) go(integral_constant<int, 8>{});
+  else go(integral_constant<int, 16>{});
 }
 
 // How a call is spread: by its sizes alone.
@@ -771,11 +830,6 @@ int64_t lin_states(const spz_linear_attention_args& a, const LinPlan& p) {
 }
 int64_t lin_keeps(const spz_linear_attention_args& a, const LinPlan& p) { return op_div_up(a.batch * a.heads * p.pieces, 4) * 4; }
 
-Divisor divisor(uint32_t d) {
-  int l = 0;
-  while (((uint64_t)1 << l) < d) ++l;
-  return {(uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), 31 + l};
-}
 template <typename T, int KP, int CL, bool STATE> void lin_chunks_go(LinArgs g, hipStream_t s) {
   g.units = 0;
   g.far = false;
