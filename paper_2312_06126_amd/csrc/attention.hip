@@ -432,16 +432,20 @@ __device__ inline void state_store(float* p, const f32x4 (&S)[TILES], bool full,
   }
 }
 
-// A workgroup: slice of a role, head, sequence, piece of time. STATE: only what the piece adds to the state.
-template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(CHUNK_THREADS, KP <= 64 ? 3 : 1) void lin_chunks(LinArgs g) {
+// Workgroups a compute unit is to hold, which bounds their registers.
+template <typename T, int KP, bool STATE, bool ONE> constexpr int chunk_waves = KP > 64 ? 1 : sizeof(T) == 4 ? 2 : ONE ? 4 : 3;
+
+// A workgroup: slice of a role, head, sequence, piece of time. STATE: only what the piece adds to the state. ONE: no
+// sequence is longer than a chunk. The scores take the place of c, of which each wave has its columns in registers by then.
+template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_bounds__(CHUNK_THREADS, (chunk_waves<T, KP, STATE, ONE>)) void lin_chunks(LinArgs g) {
   using M = Mat<T>;
   typedef typename M::frag frag;
   constexpr int TILES = KP / 16, ROWS = CL / 16, PA = KP + M::PAD, PC = CHUNK_COLS + M::PAD, PS = CL + M::PAD, SCORES = CL * PS;
   constexpr int LOWER = ROWS * (ROWS + 1) / 2;         // tiles of scores on and below the diagonal
   __shared__ __align__(16) T lds_a[STATE ? 1 : CL * PA];
   __shared__ __align__(16) T lds_b[CL * PA];
-  __shared__ __align__(16) T lds_c[CL * PC];
-  __shared__ __align__(16) T lds_p[STATE ? 1 : M::SCORE_PARTS * SCORES];
+  __shared__ __align__(16) T lds_c[STATE || M::SCORE_PARTS * SCORES < CL * PC ? CL * PC : M::SCORE_PARTS * SCORES];
+  T* const lds_p = lds_c;
   __shared__ int odd[2];
   __shared__ __align__(16) float fade[CL], enter[CL];    // of a place's c in the state behind the chunk, of the state in front in a place's o
   __shared__ int start[CL];                              // first place of a place's episode within the chunk
@@ -497,9 +501,6 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
       init = g.inits[which] ? g.inits[which] + ((b * g.heads + h) * g.pieces + piece) * size : r.init ? r.init + (b * g.heads + h) * size : nullptr;
     state_load<TILES>(init, S, full, mine, ka, rs, cs, c0 + col, q0);
   }
-  if constexpr (!STATE && M::KB == 32) {   // scores above the diagonal that share an instruction with scores below it
-    for (int e = threadIdx.x; e < M::SCORE_PARTS * SCORES / 8; e += CHUNK_THREADS) reinterpret_cast<u32x4*>(lds_p)[e] = u32x4{0, 0, 0, 0};
-  }
   if (threadIdx.x < 2) odd[threadIdx.x] = 0;
   float keep = 1.0f;   // STATE: what is left of the state in front of the piece
   // Weights of the scores in a tile on the diagonal and in the one below it.
@@ -530,14 +531,24 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
     }
     const int first = cuts ? __builtin_ctzll(cuts) : CL;
     __syncthreads();
-    if (p0 + CL < stop) fetch(p0 + CL);
+    if (!ONE && p0 + CL < stop) fetch(p0 + CL);
     const bool slow = __builtin_amdgcn_readfirstlane(odd[turn]) != 0;
+    frag v[CL / M::KB];
+    if (16 * wave < cols) {
+#pragma unroll
+      for (int kk = 0; kk < CL / M::KB; ++kk) v[kk] = M::col(lds_c, PC, M::KB * kk, 16 * wave, i, q);
+    }
     if constexpr (!STATE) {
+      __syncthreads();
       if (!slow) {   // the scores below the diagonal, tile by tile
 #pragma unroll
-        for (int k = 0; k < (LOWER + 3) / 4; ++k) {
+        for (int k = 0; k < (LOWER + ROWS / 2 + 3) / 4; ++k) {
           const int tile = wave + 4 * k;
           const int ti = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, si = tile - ti * (ti + 1) / 2;
+          if (M::KB == 32 && tile >= LOWER && tile < LOWER + ROWS / 2) {   // above it, but in one instruction with the tile on it
+            const int u = 2 * (tile - LOWER);
+            M::put(lds_p + (16 * u + i) * PS + 16 * (u + 1) + 4 * q, SCORES, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+          }
           if (tile < LOWER && 16 * ti < cnt) {
             f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -564,9 +575,6 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
       __syncthreads();
     }
     if (!slow && 16 * wave < cols) {
-      frag v[CL / M::KB];
-#pragma unroll
-      for (int kk = 0; kk < CL / M::KB; ++kk) v[kk] = M::col(lds_c, PC, M::KB * kk, 16 * wave, i, q);
       if constexpr (!STATE) {
         f32x4 o[ROWS];
 #pragma unroll
@@ -668,6 +676,7 @@ template <typename T, int KP, int CL, bool STATE> __global__ __launch_bounds__(C
         }
       }
     }
+    if (ONE) break;
     __syncthreads();
     if (slow && threadIdx.x == 0) odd[turn] = 0;
   }
@@ -830,7 +839,7 @@ int64_t lin_states(const spz_linear_attention_args& a, const LinPlan& p) {
 }
 int64_t lin_keeps(const spz_linear_attention_args& a, const LinPlan& p) { return op_div_up(a.batch * a.heads * p.pieces, 4) * 4; }
 
-template <typename T, int KP, int CL, bool STATE> void lin_chunks_go(LinArgs g, hipStream_t s) {
+template <typename T, int KP, int CL, bool STATE, bool ONE> void lin_chunks_go(LinArgs g, hipStream_t s) {
   g.units = 0;
   g.far = false;
   for (int i = 0; i < g.roles; ++i) {
@@ -846,16 +855,23 @@ template <typename T, int KP, int CL, bool STATE> void lin_chunks_go(LinArgs g, 
     const int64_t count = g.batch - first < most ? g.batch - first : most;
     g.first = first;
     g.groups = (uint32_t)(count * each);
-    lin_chunks<T, KP, CL, STATE><<<dim3((unsigned)(op_div_up(count * each, 8) * 8 * g.units)), CHUNK_THREADS, 0, s>>>(g);
+    lin_chunks<T, KP, CL, STATE, ONE><<<dim3((unsigned)(op_div_up(count * each, 8) * 8 * g.units)), CHUNK_THREADS, 0, s>>>(g);
   }
 }
 template <typename T, bool STATE> void lin_chunks_launch(const LinArgs& g, hipStream_t s) {
   int ka = 0;
   for (int i = 0; i < g.roles; ++i) ka = g.role[i].ka > ka ? g.role[i].ka : ka;
-  if (ka <= 32) lin_chunks_go<T, 32, 64, STATE>(g, s);
-  else if (ka <= 64) lin_chunks_go<T, 64, 64, STATE>(g, s);
-  else if (ka <= 128) lin_chunks_go<T, 128, 64, STATE>(g, s);
-  else lin_chunks_go<T, 256, sizeof(T) == 4 ? 32 : 64, STATE>(g, s);
+  const auto go = [&](auto one) {
+    constexpr bool ONE = decltype(one)::value;
+    if (ka <= 32) lin_chunks_go<T, 32, 64, STATE, ONE>(g, s);
+    else if (ka <= 64) lin_chunks_go<T, 64, 64, STATE, ONE>(g, s);
+    else if (ka <= 128) lin_chunks_go<T, 128, 64, STATE, ONE && sizeof(T) == 2>(g, s);
+    else lin_chunks_go<T, 256, sizeof(T) == 4 ? 32 : 64, STATE, ONE && sizeof(T) == 2>(g, s);
+  };
+  if constexpr (!STATE) {
+    if (g.steps <= 64) return go(std::true_type{});
+  }
+  go(std::false_type{});
 }
 
 template <typename T> void lin_launch(LinArgs& g, const LinPlan& plan, const spz_linear_attention_args& a, bool back, void* ws, hipStream_t s) {
