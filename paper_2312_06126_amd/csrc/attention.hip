@@ -275,6 +275,17 @@ template <> struct Mat<float> {
   static __device__ inline bool finite(uint32_t m) { return m < 0x7F800000u; }
 };
 
+// The same number, of which the compiler does not know that it stays from chunk to chunk: else it keeps everything that
+// follows from it in registers throughout (the chunks' kernel without: 162 registers instead of 134, at 128 columns 251 instead of 213).
+__device__ inline int opaque(int x) {
+  asm("" : "+v"(x));
+  return x;
+}
+template <typename I> __device__ inline I opaque_scalar(I x) {
+  asm("" : "+s"(x));
+  return x;
+}
+
 // CL steps of W columns (zeros past `width` and past the sequence) on their way from memory to LDS. A thread's vectors
 // are of one column group and RI rows apart, so that one 32-bit offset from scalar addresses serves them all.
 struct Walk { int n; bool back; };   // place p of a walk is step p, or n - 1 - p
@@ -284,46 +295,47 @@ template <typename T, int W, int CL> struct Tile {
   u32x4 v[N];
   const char* at;            // of the next chunk's place that comes first in memory, were the chunk whole
   int64_t step;              // in bytes, forward in the walk
-  uint32_t off;
-  int width, cnt, row, col;
+  int width, cnt;
   bool some, plain;          // plain: rows of a vector and more, and 32 bits hold a chunk's offsets
   __device__ inline void init(const T* p, int64_t stride, int columns, const Walk& w, int begin) {
     some = p != nullptr;
     step = stride * (int)sizeof(T);
     width = columns;
-    row = threadIdx.x / VR;
-    col = threadIdx.x % VR * VW;
     plain = width >= VW && step < (int64_t)1 << 26;
-    off = (uint32_t)((w.back ? CL - 1 - row : row) * (uint32_t)step) + column() * (int)sizeof(T);
     at = reinterpret_cast<const char*>(p) + (w.back ? w.n - begin - CL : begin) * step;
     if (w.back) step = -step;
     cnt = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = u32x4{0, 0, 0, 0};
   }
-  // Where the thread's vector is read: the last one of a row that ends inside it is read whole, from further in front.
-  __device__ inline int column() const { return col + VW <= width ? col : col < width ? width - VW : 0; }
-  // The next chunk, of which `count` > 0 places exist.
-  __device__ inline void load(bool back, int count) {
+  // Where a vector is read: the last one of a row that ends inside it is read whole, from further in front.
+  __device__ inline int column(int col) const { return col + VW <= width ? col : col < width ? width - VW : 0; }
+  // The next chunk, of which `count` > 0 places exist. Rows behind the last one read that one again.
+  __device__ inline void load(int tid, bool back, int count) {
     cnt = count;
     if (!some) return;
-    if (plain && count == CL) {
-      const char* from = at;
+    const int64_t step = opaque_scalar(this->step);
+    if (plain) {
+      const int row = tid / VR;
+      const uint32_t c = column(tid % VR * VW) * (int)sizeof(T), up = (uint32_t)(back ? -step : step);
+      if (count == CL) {
+        const char* from = at;
+        const uint32_t off = (back ? CL - 1 - row : row) * up + c;
 #pragma unroll
-      for (int j = 0; j < N; ++j, from += RI * step) v[j] = load16(reinterpret_cast<const T*>(from + off));
-    } else if (plain) {      // rows behind the last one read that one again
-      const char* from = back ? at - (CL - count) * step : at;
-      const uint32_t c = column() * (int)sizeof(T), up = (uint32_t)(back ? -step : step);
+        for (int j = 0; j < N; ++j, from += RI * step) v[j] = load16(reinterpret_cast<const T*>(from + off));
+      } else {
+        const char* from = back ? at - (CL - count) * step : at;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const int r = row + j * RI < count ? row + j * RI : count - 1;
-        v[j] = load16(reinterpret_cast<const T*>(from + ((uint32_t)(back ? count - 1 - r : r) * up + c)));
+        for (int j = 0; j < N; ++j) {
+          const int r = row + j * RI < count ? row + j * RI : count - 1;
+          v[j] = load16(reinterpret_cast<const T*>(from + ((uint32_t)(back ? count - 1 - r : r) * up + c)));
+        }
       }
     }
     at += CL * step;
   }
   // Zeros where nothing is, and the ragged end of a row in its place.
-  __device__ inline void trim() {
+  __device__ inline void trim(int row, int col) {
     if (!some) return;
     if (width < W) {
       const int part = col < width && col + VW > width ? col - (width - VW) : 0;   // elements to shift down
@@ -349,11 +361,11 @@ template <typename T, int W, int CL> struct Tile {
     }
   }
   // To LDS; returns the largest of the magnitudes and m. Rows that are not `plain` come from memory only here.
-  __device__ inline uint32_t store(T* lds, bool back, uint32_t m) {
+  __device__ inline uint32_t store(int tid, T* lds, bool back, uint32_t m) {
     if (some && !plain) {
       const char* from = at - CL * step + (back ? -(CL - 1) * step : 0);   // of the chunk's first place
 #pragma unroll 1
-      for (int e = threadIdx.x; e < CL * W; e += CHUNK_THREADS) {
+      for (int e = tid; e < CL * W; e += CHUNK_THREADS) {
         const int r = e / W, c = e % W;
         T x = from_f<T>(0.0f);
         if (r < cnt && c < width) x = reinterpret_cast<const T*>(from + r * step)[c];
@@ -362,7 +374,8 @@ template <typename T, int W, int CL> struct Tile {
       }
       return m;
     }
-    trim();
+    const int row = tid / VR, col = tid % VR * VW;
+    trim(row, col);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       *reinterpret_cast<u32x4*>(lds + (row + j * RI) * PITCH + col) = v[j];
@@ -382,13 +395,6 @@ __device__ inline float lin_power(float log2d, int n) { return __builtin_amdgcn_
 
 // The workgroups of a launch: the slices of all roles of a piece of a head follow each other on one XCD, whose L2 holds
 // what they share.
-// The same number, of which the compiler does not know that it stays from chunk to chunk: else it keeps everything that
-// follows from it in registers throughout.
-__device__ inline int opaque(int x) {
-  asm("" : "+v"(x));
-  return x;
-}
-
 // A lane's part of a state at row and column strides rs and cs: rows 16 k + 4 q .. of column c.
 template <int TILES>
 __device__ inline void state_load(const float* p, f32x4 (&S)[TILES], bool full, bool mine, int ka, int rs, int cs, int c, int q) {
@@ -414,6 +420,7 @@ __device__ inline void state_load(const float* p, f32x4 (&S)[TILES], bool full, 
 }
 template <int TILES>
 __device__ inline void state_store(float* p, const f32x4 (&S)[TILES], bool full, bool mine, int ka, int rs, int cs, int c, int q) {
+  rs = opaque_scalar(rs);
   const uint32_t at = 4 * q * rs + c * cs;
   if (full && rs == 1) {
 #pragma unroll
@@ -478,17 +485,17 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
   tc.init(r.c ? static_cast<const T*>(r.c) + b * r.c_batch + h * r.c_head + c0 : nullptr, r.c_step, cols, walk, begin);
   int flag = 0;
   const auto fetch = [&](int p0) {
-    const int count = stop - p0 < CL ? stop - p0 : CL;
-    if constexpr (!STATE) ta.load(back, count);
-    tb.load(back, count);
-    tc.load(back, count);
+    const int count = stop - p0 < CL ? stop - p0 : CL, tid = opaque(threadIdx.x);
+    if constexpr (!STATE) ta.load(tid, back, count);
+    tb.load(tid, back, count);
+    tc.load(tid, back, count);
     flag = lane < CL ? starts(p0 + lane) : 0;
   };
   if (begin < stop) fetch(begin);
   // The next place's row of o, or of 16 places the one that comes first in memory.
-  const int64_t out_step = STATE ? 0 : r.out_step * (int)sizeof(T), out_walk = back ? -out_step : out_step;
+  const int64_t o_step = STATE ? 0 : r.out_step * (int)sizeof(T);
   T* const po = STATE ? nullptr : static_cast<T*>(r.out) + b * r.out_batch + h * r.out_head + c0;
-  char* out = reinterpret_cast<char*>(po) + (back ? (int64_t)n - 16 - begin : (int64_t)begin) * out_step;
+  char* out = reinterpret_cast<char*>(po) + (back ? (int64_t)n - 16 - begin : (int64_t)begin) * o_step;
 
   f32x4 S[TILES];
   const int col = 16 * wave + i0;
@@ -514,12 +521,13 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
   const float two = lin_power(log2d, 16);
   __syncthreads();
   int turn = 0;
-  for (int p0 = begin; p0 < stop; p0 += CL, turn ^= 1, out += CL * out_walk) {
-    const int i = opaque(i0), q = opaque(q0);
+  for (int p0 = begin; p0 < stop; p0 += CL, turn ^= 1, out += CL * (back ? -o_step : o_step)) {
+    const int tid = opaque(threadIdx.x), lane = tid & 63, i = lane & 15, q = lane >> 4;
+    const int64_t out_step = opaque_scalar(o_step), out_walk = back ? -out_step : out_step;
     const int cnt = stop - p0 < CL ? stop - p0 : CL;
     const int lead = back && p0 == 0 ? 0 : 1;   // steps between the state in front and the first place
-    if constexpr (!STATE) ta.store(lds_a, back, 0);
-    if (!M::finite(tc.store(lds_c, back, tb.store(lds_b, back, 0)))) odd[turn] = 1;
+    if constexpr (!STATE) ta.store(tid, lds_a, back, 0);
+    if (!M::finite(tc.store(tid, lds_c, back, tb.store(tid, lds_b, back, 0)))) odd[turn] = 1;
     const uint64_t cuts = __ballot(flag != 0);
     if (wave == 0 && lane < CL) {
       const uint64_t before = cuts & ((2ull << lane) - 1);
