@@ -439,15 +439,17 @@ __device__ inline void state_store(float* p, const f32x4 (&S)[TILES], bool full,
   }
 }
 
+// KP: rows of the state that are worked on, a multiple of the contraction's (48 instead of 64 rows: FP32_48).
 // Workgroups a compute unit is to hold, which bounds their registers.
-template <typename T, int KP, bool STATE, bool ONE> constexpr int chunk_waves = KP > 64 ? 1 : sizeof(T) == 4 ? 2 : ONE ? 4 : 3;
+template <typename T, int KP, bool STATE, bool ONE> constexpr int chunk_waves = KP > 64 ? 1 : sizeof(T) == 4 ? 2 : 4;
 
 // A workgroup: slice of a role, head, sequence, piece of time. STATE: only what the piece adds to the state. ONE: no
 // sequence is longer than a chunk. The scores take the place of c, of which each wave has its columns in registers by then.
 template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_bounds__(CHUNK_THREADS, (chunk_waves<T, KP, STATE, ONE>)) void lin_chunks(LinArgs g) {
   using M = Mat<T>;
   typedef typename M::frag frag;
-  constexpr int TILES = KP / 16, ROWS = CL / 16, PA = KP + M::PAD, PC = CHUNK_COLS + M::PAD, PS = CL + M::PAD, SCORES = CL * PS;
+  constexpr int W = KP <= 32 ? 32 : KP <= 64 ? 64 : KP <= 128 ? 128 : 256;   // columns of a and b in LDS
+  constexpr int TILES = KP / 16, ROWS = CL / 16, PA = W + M::PAD, PC = CHUNK_COLS + M::PAD, PS = CL + M::PAD, SCORES = CL * PS;
   constexpr int LOWER = ROWS * (ROWS + 1) / 2;         // tiles of scores on and below the diagonal
   __shared__ __align__(16) T lds_a[STATE ? 1 : CL * PA];
   __shared__ __align__(16) T lds_b[CL * PA];
@@ -478,7 +480,7 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
     return (int)flags[p * g.reset_step];
   };
 
-  Tile<T, KP, CL> ta, tb;
+  Tile<T, W, CL> ta, tb;
   Tile<T, CHUNK_COLS, CL> tc;
   if constexpr (!STATE) ta.init(r.a ? static_cast<const T*>(r.a) + b * r.a_batch + h * r.a_head : nullptr, r.a_step, ka, walk, begin);
   tb.init(r.b ? static_cast<const T*>(r.b) + b * r.b_batch + h * r.b_head : nullptr, r.b_step, ka, walk, begin);
@@ -825,21 +827,39 @@ template <typename T> void lin_steps_launch(LinArgs g, hipStream_t s) {
   else go(integral_constant<int, 16>{});
 }
 
+// The rows of states that the kernels come in, and workgroups of each that the card holds at once.
+template <typename T> int lin_rows(int ka) {
+  for (const int kp : {32, 48, 64, 96, 128})
+    if (ka <= kp && kp % Mat<T>::KB == 0) return kp;
+  return 256;
+}
+template <typename T> int64_t lin_fill(int ka) {
+  const int kp = lin_rows<T>(ka);
+  return sizeof(T) == 2 ? (kp <= 64 ? 1024 : kp <= 128 ? 512 : 256) : kp <= 64 ? 768 : 256;
+}
 // How a call is spread: by its sizes alone.
 //   steps: a thread keeps its part of the state and walks;
 //   chunks: a workgroup walks in chunks on the matrix cores; pieces > 1: time is cut into pieces whose sums are joined first.
-constexpr int64_t STEPS_MOST = 8, CHUNK_FILL = 1024, PIECE_LEAST = 256;
+constexpr int64_t STEPS_MOST = 8, PIECE_LEAST = 256;
 struct LinPlan { bool chunks; int64_t pieces, len; };
-LinPlan lin_plan(const spz_linear_attention_args& a, bool back) {
+template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bool back) {
   // (Places are counted in 31 bits, a chunk past the last one included.)
   if (a.steps <= STEPS_MOST || a.steps > OP_MAX_EXTENT - 4096 || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
-  const int64_t k = op_div_up(a.key_width, CHUNK_COLS), v = op_div_up(a.value_width, CHUNK_COLS), units = back ? 2 * k + v : v;
-  const int64_t groups = a.batch * a.heads * units;
-  int64_t pieces = groups > 0 ? CHUNK_FILL / groups : 1;
+  const int K = (int)a.key_width, V = (int)a.value_width;
+  const int64_t k = op_div_up(K, CHUNK_COLS), v = op_div_up(V, CHUNK_COLS), heads = a.batch * a.heads;
+  if (heads == 0) return {true, 1, a.steps};
+  // Workgroups of a launch: by key rows (y; dv), by value rows (dq and dk), or all in one.
+  const bool same = lin_rows<T>(K) == lin_rows<T>(V);
+  const int64_t by_k = v + (back && same ? 2 * k : 0), by_v = back && !same ? 2 * k : 0;
+  int64_t pieces = lin_fill<T>(K) / (heads * by_k);
+  if (by_v && lin_fill<T>(V) / (heads * by_v) > pieces) pieces = lin_fill<T>(V) / (heads * by_v);
   if (pieces > a.steps / PIECE_LEAST) pieces = a.steps / PIECE_LEAST;
-  if (pieces < 2) return {true, 1, a.steps};
+  if (pieces < 2 || heads * by_k >= 256) return {true, 1, a.steps};
   const int64_t len = op_div_up(op_div_up(a.steps, pieces), 64) * 64;
   return {true, op_div_up(a.steps, len), len};
+}
+LinPlan lin_plan(const spz_linear_attention_args& a, bool back) {
+  return a.prec == SPZ_PREC_BF16 ? lin_plan_of<bf16_t>(a, back) : lin_plan_of<float>(a, back);
 }
 // Floats of one state of all pieces, and of what they keep, each at 16 bytes.
 int64_t lin_states(const spz_linear_attention_args& a, const LinPlan& p) {
@@ -866,20 +886,34 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> void lin_chunks_go(L
     lin_chunks<T, KP, CL, STATE, ONE><<<dim3((unsigned)(op_div_up(count * each, 8) * 8 * g.units)), CHUNK_THREADS, 0, s>>>(g);
   }
 }
-template <typename T, bool STATE> void lin_chunks_launch(const LinArgs& g, hipStream_t s) {
-  int ka = 0;
-  for (int i = 0; i < g.roles; ++i) ka = g.role[i].ka > ka ? g.role[i].ka : ka;
-  const auto go = [&](auto one) {
-    constexpr bool ONE = decltype(one)::value;
-    if (ka <= 32) lin_chunks_go<T, 32, 64, STATE, ONE>(g, s);
-    else if (ka <= 64) lin_chunks_go<T, 64, 64, STATE, ONE>(g, s);
-    else if (ka <= 128) lin_chunks_go<T, 128, 64, STATE, ONE && sizeof(T) == 2>(g, s);
-    else lin_chunks_go<T, 256, sizeof(T) == 4 ? 32 : 64, STATE, ONE && sizeof(T) == 2>(g, s);
-  };
-  if constexpr (!STATE) {
-    if (g.steps <= 64) return go(std::true_type{});
+// Roles of one number of rows in a launch.
+template <typename T, bool STATE> void lin_chunks_launch(const LinArgs& all, hipStream_t s) {
+  for (const int kp : {32, 48, 64, 96, 128, 256}) {
+    LinArgs g = all;
+    g.roles = 0;
+    for (int i = 0; i < all.roles; ++i)
+      if (lin_rows<T>(all.role[i].ka) == kp) {
+        g.role[g.roles] = all.role[i];
+        g.inits[g.roles++] = all.inits[i];
+      }
+    if (g.roles == 0) continue;
+    const auto go = [&](auto one) {
+      constexpr bool ONE = decltype(one)::value, BF16 = sizeof(T) == 2;
+      if (kp == 32) lin_chunks_go<T, 32, 64, STATE, ONE>(g, s);
+      else if (kp == 48) lin_chunks_go<T, BF16 ? 64 : 48, 64, STATE, ONE>(g, s);
+      else if (kp == 64) lin_chunks_go<T, 64, 64, STATE, ONE>(g, s);
+      else if (kp == 96) lin_chunks_go<T, 96, 64, STATE, ONE && BF16>(g, s);
+      else if (kp == 128) lin_chunks_go<T, 128, 64, STATE, ONE && BF16>(g, s);
+      else lin_chunks_go<T, 256, BF16 ? 64 : 32, STATE, ONE && BF16>(g, s);
+    };
+    if constexpr (!STATE) {
+      if (g.steps <= 64) {
+        go(std::true_type{});
+        continue;
+      }
+    }
+    go(std::false_type{});
   }
-  go(std::false_type{});
 }
 
 template <typename T> void lin_launch(LinArgs& g, const LinPlan& plan, const spz_linear_attention_args& a, bool back, void* ws, hipStream_t s) {
