@@ -375,7 +375,7 @@ template <typename T, int W, int CL> struct Tile {
       return m;
     }
     const int row = tid / VR, col = tid % VR * VW;
-    trim(row, col);
+    if (width < W || cnt < CL) trim(row, col);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       *reinterpret_cast<u32x4*>(lds + (row + j * RI) * PITCH + col) = v[j];
@@ -612,7 +612,11 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
           if (16 * ti >= cnt) continue;
           const float f = enter[t];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[ti][e] = t < first ? o[ti][e] * f : 0.0f;
+          for (int e = 0; e < 4; ++e) o[ti][e] *= f;
+          if (cuts) {   // (a state that is not finite does not pass a start either)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[ti][e] = t < first ? o[ti][e] : 0.0f;
+          }
 #pragma unroll
           for (int kk = 0; kk < CL / M::KB; ++kk)
             if (M::KB * kk <= 16 * ti) {
@@ -642,7 +646,11 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
 #pragma unroll
       for (int k = 0; k < TILES; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[k][e] = cuts ? 0.0f : S[k][e] * whole;
+        for (int e = 0; e < 4; ++e) S[k][e] *= whole;
+      if (cuts) {
+#pragma unroll
+        for (int k = 0; k < TILES; ++k) S[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
       keep = cuts ? 0.0f : keep * whole;
 #pragma unroll
       for (int kk = 0; kk < CL / M::KB; ++kk) {
