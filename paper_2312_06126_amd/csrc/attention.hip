@@ -845,14 +845,19 @@ template <typename T> int64_t lin_fill(int ka) {
   const int kp = lin_rows<T>(ka);
   return sizeof(T) == 2 ? (kp <= 64 ? 1024 : kp <= 128 ? 512 : 256) : kp <= 64 ? 768 : 256;
 }
-// How a call is spread: by its sizes alone.
-//   steps: a thread keeps its part of the state and walks;
-//   chunks: a workgroup walks in chunks on the matrix cores; pieces > 1: time is cut into pieces whose sums are joined first.
-constexpr int64_t STEPS_MOST = 8, PIECE_LEAST = 256;
+// How a call is spread, by its sizes alone (microseconds a call, both sides measured, heads of 64 x 64, bfloat16):
+//   steps: a thread keeps its part of the state and walks: up to 2 steps, in float32 4 (2048 x 4 heads: 2 steps 59 against
+//     68 in chunks, 4 steps 82 against 66; in float32 4 steps 90 against 110, 8 steps 142 against 112);
+//   chunks: a workgroup walks in chunks on the matrix cores, 4.5 a chunk;
+//   pieces: time cut into pieces of PIECE_LEAST steps and more whose sums are joined first, as many as the card holds at
+//     once: two launches and a second reading of keys and values more, where heads leave compute units idle and there are more
+//     than PIECES_FROM steps (1 x 1000 x 4: 23 against 73; 8 x 1000 x 8: 34 against 77; 32 x 256 x 4: 28 against 24;
+//     64 x 1000 x 5 in float32: 167 either way).
+constexpr int64_t PIECE_LEAST = 64, PIECES_FROM = 256;
 struct LinPlan { bool chunks; int64_t pieces, len; };
 template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bool back) {
   // (Places are counted in 31 bits, a chunk past the last one included.)
-  if (a.steps <= STEPS_MOST || a.steps > OP_MAX_EXTENT - 4096 || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
+  if (a.steps <= (sizeof(T) == 2 ? 2 : 4) || a.steps > OP_MAX_EXTENT - 4096 || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
   const int K = (int)a.key_width, V = (int)a.value_width;
   const int64_t k = op_div_up(K, CHUNK_COLS), v = op_div_up(V, CHUNK_COLS), heads = a.batch * a.heads;
   if (heads == 0) return {true, 1, a.steps};
@@ -862,7 +867,7 @@ template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bo
   int64_t pieces = lin_fill<T>(K) / (heads * by_k);
   if (by_v && lin_fill<T>(V) / (heads * by_v) > pieces) pieces = lin_fill<T>(V) / (heads * by_v);
   if (pieces > a.steps / PIECE_LEAST) pieces = a.steps / PIECE_LEAST;
-  if (pieces < 2 || heads * by_k >= 256) return {true, 1, a.steps};
+  if (pieces < 2 || heads * by_k >= 256 || a.steps <= PIECES_FROM) return {true, 1, a.steps};
   const int64_t len = op_div_up(op_div_up(a.steps, pieces), 64) * 64;
   return {true, op_div_up(a.steps, len), len};
 }

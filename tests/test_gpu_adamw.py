@@ -195,6 +195,36 @@ def test_adamw_steps_and_rates_on_the_device(bits):
     check_step(rng, params, grads, opt, bits, "fp32", 9, 1e-2, 0.5, step=torch.tensor(9, device="cuda"), lr_arg=torch.tensor([1e-2], device="cuda"))
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_places_past_32_bits(bits):
+    """Moments behind 2^32 + elements of others: the second tensor, against the same one by itself (32 bits) or its definition."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(8)
+    big = torch.zeros((1 << 32) + 512, dtype=torch.bfloat16, device="cuda")
+    small = gpu(rng.standard_normal(1000))
+    opt = ops.AdamW([big, small], bits=bits, seed=SEED)
+    at = opt.places[1]
+    assert at == (1 << 32) + 512
+    g = gpu(rng.standard_normal(1000) * 0.1)
+    before = host(small)
+    opt.step([None, g], step=3, lr=1e-2)
+    torch.cuda.synchronize()
+    zero = np.zeros(1000)
+    want = ref.adamw(before, host(g), zero, zero, 3, float(np.float32(1e-2)), 0.9, 0.999, 1e-8, 0.0)
+    check("p", host(small), want["p"], "fp32")
+    if bits == 32:
+        check("m", host(opt.m[at:at + 1000]), want["m"], "fp32")
+        check("v", host(opt.v[at:at + 1000]), want["v"], "fp32")
+    else:
+        wm, wv = ref.moment_words(np.arange(at, at + 1000), SEED, 3)
+        for b in range(0, 1000, 256):
+            c, i = slice(b, min(b + 256, 1000)), (at + b) // 256
+            check_rounding("m", codes(opt.m[at:at + 1000])[c], float(opt.m_scale[i]), want["m"][0][c], want["m"][1][c], wm[c], False)
+            check_rounding("v", codes(opt.v[at:at + 1000])[c], float(opt.v_scale[i]), want["r"][0][c], want["r"][1][c], wv[c], True)
+    del opt, big
+
+
 def test_adamw_rounding_is_fair():
     """Moments that change by a hundredth a step in 8 bits: after 400 steps the mean follows the exact moments, which rounding to
     nearest would leave where they are. 4096 elements; the root's standard deviation is below 0.2 of itself (steps

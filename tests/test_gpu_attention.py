@@ -67,6 +67,40 @@ def test_attention(shape, prec):
 
 
 @pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("shape", [(1, 257, 1, 16, 24), (2, 500, 3, 40, 33), (1, 2049, 2, 64, 64), (3, 300, 1, 24, 130), (1, 700, 1, 96, 100), (1, 321, 1, 200, 70)],
+                         ids=str)
+def test_attention_time_in_pieces(shape, prec):
+    """Few heads and many steps: time is cut into pieces whose sums are joined. Sequences that end in the first piece, on a
+    piece's last step and inside one, empty ones; starts on the pieces' ends; states that are not finite in front of a start."""
+    torch = torch_()
+    rng = np.random.default_rng(sum(shape))
+    B, T = shape[:2]
+    t, reset, lengths = inputs(rng, *shape, prec, p_reset=0.01)
+    got = run(t, reset, lengths)
+    check_all(got, t, reset, lengths, prec)
+    for n in (1, 63, 64, 65, 128, 192, 256, T - 1, T):
+        ends = np.full(B, min(n, T), np.int32)
+        check_all(run(t, None, ends), t, None, ends, prec)
+    marks = np.tile((np.arange(T) % 64 == 0).astype(np.uint8), (B, 1))
+    check_all(run(t, marks, lengths), t, marks, lengths, prec)
+    u = dict(t, state=t["state"] * float("nan"), dlast=t["dlast"] * float("inf"))
+    marks = np.zeros((B, T), np.uint8)
+    marks[:, 100] = 1
+    got = run(u, marks)
+    w = ref_of(t, marks, None, prec)
+    for name, part in (("y", slice(100, None)), ("dq", slice(100, None)), ("dk", slice(0, 100)), ("dv", slice(0, 100))):
+        check(name, got[name][:, part], tuple(x[:, part] for x in w[name]), prec)
+    check("last", got["last"], w["last"], "fp32")
+    check("dstate", got["dstate"], w["dstate"], "fp32")
+    state = t["state"].clone()
+    from paper_2312_06126_amd import ops
+    want = run(t, reset, lengths)
+    y, last = ops.linear_attention(t["q"], t["k"], t["v"], t["rate"], state, reset=torch.from_numpy(reset).cuda(), lengths=torch.from_numpy(lengths).cuda(),
+                                   last=state)
+    assert last is state and torch.equal(state, want["last"]) and torch.equal(y, want["y"])
+
+
+@pytest.mark.parametrize("prec", PRECS)
 @pytest.mark.parametrize("T", [3, 90, 200])
 def test_attention_rates_scales_and_absent_states(T, prec):
     """Rates from none to infinite, scales of 0 and below, no state in front, no gradient behind."""
@@ -216,6 +250,45 @@ def test_attention_steps_in_place_are_the_sequence(K, V, prec):
         ys.append(y)
     check("y", torch.cat(ys, 1), want["y"], prec)
     check("last", state, want["last"], "fp32")
+
+
+def test_attention_of_many_heads():
+    """More heads than a launch's workgroups stand side by side; the first and last of them against float64."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(20)
+    for B, T, H in ((3, 1, 20000), (2, 5, 20000), (9000, 1, 3), (1, 3, 65536)):
+        t, _, _ = inputs(rng, B, T, H, 8, 8, "fp32", False, False)
+        y, last = ops.linear_attention(t["q"], t["k"], t["v"], t["rate"], t["state"])
+        dq, dk, dv, ds = ops.linear_attention_backward(t["q"], t["k"], t["v"], t["dy"], t["rate"], t["state"], dlast=t["dlast"])
+        for b, h in ((0, 0), (B - 1, H - 1), (B // 2, H // 2)):
+            x = {n: host(v[b:b + 1, :, h:h + 1] if v.dim() == 4 and n not in ("state", "dlast") else v[b:b + 1, h:h + 1] if v.dim() == 4 else v[h:h + 1]) for n, v in t.items()}
+            want = ref.attention(x["q"], x["k"], x["v"], x["rate"], x["state"], 8 ** -0.5, None, None, x["dy"], x["dlast"])
+            for n, v in (("y", y), ("dq", dq), ("dk", dk), ("dv", dv)):
+                check(n, v[b:b + 1, :, h:h + 1], want[n], "fp32")
+            for n, v in (("last", last), ("dstate", ds)):
+                check(n, v[b:b + 1, h:h + 1], want[n], "fp32")
+
+
+def test_attention_offsets_past_32_bits():
+    """Rows of a chunk further apart than 32 bits of bytes hold, inputs and outputs: the same bits as of arrays without gaps."""
+    torch = torch_()
+    rng = np.random.default_rng(21)
+    B, T, H, K, V = 1, 20, 1, 64, 32
+    t, reset, lengths = inputs(rng, B, T, H, K, V, "bf16", ragged=False)
+    want = run(t, reset, lengths)
+    step = 260_000_000                                   # elements: 20 steps are 9.7 GiB
+    wide = torch.empty(T * step, dtype=torch.bfloat16, device="cuda")
+
+    def far(x, at=0):
+        w = wide[at:].as_strided((B, T, H, x.shape[3]), (T * step, step, x.shape[3], 1))
+        return w.copy_(x)
+
+    u = dict(t, q=far(t["q"], 0), k=far(t["k"], 1000), v=far(t["v"], 2000), dy=far(t["dy"], 3000))
+    outs = tuple(far(torch.zeros_like(x), 4000 + 1000 * i) for i, x in enumerate((t["v"], t["q"], t["k"], t["v"])))
+    got = run(u, reset, lengths, outs=outs)
+    assert all(torch.equal(got[n], want[n]) for n in want)
+    del wide
 
 
 def test_attention_of_nothing():

@@ -154,6 +154,28 @@ def test_head_norm_masked_rows_and_absent_gradients(prec):
     assert not g["dq"].any() and not g["dw_q"].any() and torch.equal(g["dk"], g0["dk"]) and torch.equal(g["dw_k"], g0["dw_k"])
 
 
+def test_head_norm_offsets_past_32_bits():
+    """Rows 2^31 elements and more from the first one."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(7)
+    t = inputs(rng, 5, 2, 2, 64, "bf16")
+    a = dict(w_q=t["w_q"], w_k=t["w_k"], positions=torch.arange(5, dtype=torch.int32, device="cuda"), freqs=ops.rotation_freqs(64))
+    want, grads = ops.head_norm(t["q"], t["k"], **a), ops.head_norm_backward(t["dq"], t["dk"], t["q"], t["k"], **a)
+    step = 900_000_000
+    wide = torch.empty(5 * step, dtype=torch.bfloat16, device="cuda")
+
+    def far(x, at):
+        return wide[at:].as_strided((5, 2, 64), (step, 64, 1)).copy_(x)
+
+    q, k, dq, dk = (far(t[n], 1000 * i) for i, n in enumerate(("q", "k", "dq", "dk")))
+    outs = tuple(far(torch.zeros_like(t["q"]), 5000 + 1000 * i) for i in range(4))
+    got, g = ops.head_norm(q, k, out=outs[:2], **a), ops.head_norm_backward(dq, dk, q, k, out=outs[2:], **a)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert all(grads[n] is None or torch.equal(g[n], grads[n]) for n in grads)
+    del wide
+
+
 def test_head_norm_of_nothing():
     from paper_2312_06126_amd import ops
     torch = torch_()

@@ -89,7 +89,7 @@ def attention_args(**kw):
 
 
 @pytest.mark.parametrize("back,bad,word", [
-    (None, dict(prec=2), "precision"), (None, dict(batch=-1), "extent"), (None, dict(steps=1 << 31), "extent"), (None, dict(heads=-4), "extent"),
+    (None, dict(prec=2), "precision"), (None, dict(batch=-1), "extent"), (None, dict(steps=1 << 31), "extent"), (None, dict(heads=-4), "extent"), (None, dict(heads=65537), "extent"),
     (None, dict(key_width=257), "width"), (None, dict(value_width=300), "width"), (None, dict(value_width=-1), "width"), (None, dict(scale=float("inf")), "scale"),
     (None, dict(scale=float("nan")), "scale"), (None, dict(batch=1 << 30, heads=1 << 20), "range"), (None, dict(batch=1 << 20, steps=1 << 30), "range"),
     (None, dict(q=None), "NULL"), (None, dict(v=None), "NULL"), (None, dict(k=PTR + ODD), "aligned"), (None, dict(rate=PTR + 2), "aligned"),
@@ -105,6 +105,20 @@ def test_attention_refusals(lib, back, bad, word):  # noqa: F811
         if back in (None, direction):
             assert call(ctypes.byref(a), PTR, 1 << 50, None) == spz.SPZ_EINVAL
             assert word in lib.spz_last_error(None).decode()
+
+
+def test_attention_needs_its_workspace(lib):  # noqa: F811
+    from paper_2312_06126_amd import spz
+    a = attention_args(batch=1, steps=4096)
+    for n in ("q", "k", "v", "y", "dy", "dq", "dk", "dv"):
+        setattr(a, n + "_batch", 4096 * getattr(a, n + "_step"))
+    for back, call in ((0, lib.spz_linear_attention_forward), (1, lib.spz_linear_attention_backward)):
+        need = lib.spz_linear_attention_workspace(ctypes.byref(a), back)
+        assert need > 0
+        assert call(ctypes.byref(a), None, need, None) == spz.SPZ_ESIZE
+        assert call(ctypes.byref(a), PTR, need - 1, None) == spz.SPZ_ESIZE
+        assert call(ctypes.byref(a), PTR + 4, need, None) == spz.SPZ_EINVAL
+    assert lib.spz_linear_attention_workspace(None, 0) == spz.SPZ_EINVAL
 
 
 def test_attention_output_orders(lib):  # noqa: F811
