@@ -600,10 +600,11 @@ int spz_linear_attention_backward(const spz_linear_attention_args* args, void* w
 /* An AdamW step over `count` tensors at once, each element by itself:
  *     g = grad_scale grad,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
  *     p = p - lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p)
- * in float32; p is rounded once to its type, and so is the bfloat16 copy for products to read. m
- * and v are two arrays of `moments` elements for all tensors: tensor i has elements at ..
- * at + n - 1 of both, `at` a multiple of SPZ_ADAMW_BLOCK; what lies between is left as it is.
- * Two tensors may share no element.
+ * in float32, the moments with a rounding after each operation in this order (c = 1 - beta in 64
+ * bits, then float32: m = beta1 m + c1 g, v = beta2 v + (c2 g) g); p is rounded once to its type,
+ * and so is the bfloat16 copy for products to read. m and v are two arrays of `moments` elements
+ * for all tensors: tensor i has elements at .. at + n - 1 of both, `at` a multiple of
+ * SPZ_ADAMW_BLOCK; what lies between is left as it is. Two tensors may share no element.
  *
  * bits 32: m and v are float32. bits 8: m holds codes of m and v codes of sqrt(v) in the 8-bit
  * floating point type e4m3 (1 sign, 4 exponent, 3 mantissa bits, largest 448), m_scale and v_scale

@@ -100,11 +100,21 @@ __device__ inline float round_random(float x, uint32_t word) {
   return low ? z - 0x1p-6f : z;
 }
 
-// The hardware's square root and reciprocal (an ulp each; a sixth of the instructions of the correctly rounded ones), outside
-// the range that they take correctly the rounded ones.
-__device__ inline float root(float x) { return x >= 0x1p-100f || x == 0.0f ? __builtin_amdgcn_sqrtf(x) : sqrtf(x); }
+// The square root: the hardware's (an ulp) and a step of Newton's method, whose residual is exact, so that the result is the
+// correctly rounded one but for values next to a border; a third of the library's instructions.
+__device__ inline float root(float x) {
+  if (!(x >= 0x1p-90f && x < 0x1p120f)) return sqrtf(x);
+  const float y = __builtin_amdgcn_rsqf(x), s = x * y;
+  return fmaf(fmaf(-s, s, x), 0.5f * y, s);
+}
+// x / y within two ulp.
 __device__ inline float over(float x, float y) {
   return y >= 0x1p-100f && y <= 0x1p100f ? x * __builtin_amdgcn_rcpf(y) : x / y;
+}
+// x / y correctly rounded from y's correctly rounded reciprocal (Markstein 1990): the residual is exact.
+__device__ inline float divided(float x, float y, float by) {
+  const float q = x * by;
+  return fmaf(fmaf(-q, y, x), by, q);
 }
 
 // The largest of a block's magnitudes (half a wave); a NaN stays one.
@@ -161,9 +171,12 @@ __global__ __launch_bounds__(ADAM_THREADS) void adamw_step(AdamArgs g) {
   float r[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float x = d[i] * gs;
-    m[i] = fmaf(g.b1, m[i], g.c1 * x);
-    v[i] = fmaf(g.b2, v[i], g.c2 * x * x);
+    {   // one rounding an operation, as the definition of the codes has it
+#pragma clang fp contract(off)
+      const float x = d[i] * gs;
+      m[i] = g.b1 * m[i] + g.c1 * x;
+      v[i] = g.b2 * v[i] + g.c2 * x * x;
+    }
     r[i] = root(v[i]);
     p[i] = fmaf(-lr, fmaf(t.decay, p[i], over(m[i] * fix1, fmaf(r[i], fix2, g.eps))), p[i]);
   }
@@ -187,10 +200,11 @@ __global__ __launch_bounds__(ADAM_THREADS) void adamw_step(AdamArgs g) {
     }
     // Both sides of tiny scales are raised: a reciprocal below would not be a number of the type.
     const float up_m = sm < 0x1p-60f ? 0x1p60f : 1.0f, up_r = sr < 0x1p-60f ? 0x1p60f : 1.0f;
-    const float by_m = 1.0f / (sm * up_m), by_r = 1.0f / (sr * up_r);
+    const float high_m = sm * up_m, high_r = sr * up_r, by_m = 1.0f / high_m, by_r = 1.0f / high_r;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float x = sm > 0.0f ? fminf(__builtin_fabsf(m[i]) * up_m * by_m, E4M3_MAX) : 0.0f, y = sr > 0.0f ? fminf(r[i] * up_r * by_r, E4M3_MAX) : 0.0f;
+      const float x = sm > 0.0f ? fminf(divided(__builtin_fabsf(m[i]) * up_m, high_m, by_m), E4M3_MAX) : 0.0f;
+      const float y = sr > 0.0f ? fminf(divided(r[i] * up_r, high_r, by_r), E4M3_MAX) : 0.0f;
       m[i] = __builtin_copysignf(round_random(x, w[i] & 0xFFFFu), m[i]);
       const float z = round_random(y, w[i] >> 16);
       r[i] = r[i] > 0.0f && sr > 0.0f ? fmaxf(z, 0x1p-9f) : z;
