@@ -642,33 +642,37 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
           }
         }
       }
-      const float whole = lin_power(log2d, cnt - 1 + lead);
+      if (!STATE && !r.last && p0 + CL >= stop) {
+        // Nobody asks for the state behind it.
+      } else {
+        const float whole = lin_power(log2d, cnt - 1 + lead);
 #pragma unroll
-      for (int k = 0; k < TILES; ++k)
+        for (int k = 0; k < TILES; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[k][e] *= whole;
-      if (cuts) {
+          for (int e = 0; e < 4; ++e) S[k][e] *= whole;
+        if (cuts) {
 #pragma unroll
-        for (int k = 0; k < TILES; ++k) S[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      }
-      keep = cuts ? 0.0f : keep * whole;
-#pragma unroll
-      for (int kk = 0; kk < CL / M::KB; ++kk) {
-        if (M::KB * kk >= cnt) continue;
-        float x[M::N];
-#pragma unroll
-        for (int e = 0; e < M::N; e += 4) {
-          const f32x4 w = *reinterpret_cast<const f32x4*>(fade + M::KB * kk + M::N * q + e);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[e + j] = M::at(v[kk], e + j) * w[j];
+          for (int k = 0; k < TILES; ++k) S[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        frag f[M::VALUE_PARTS];
-        M::template split<M::VALUE_PARTS>(x, f);
+        keep = cuts ? 0.0f : keep * whole;
 #pragma unroll
-        for (int k = 0; k < TILES; ++k) {
-          const frag a = M::col(lds_b, PA, M::KB * kk, 16 * k, i, q);
+        for (int kk = 0; kk < CL / M::KB; ++kk) {
+          if (M::KB * kk >= cnt) continue;
+          float x[M::N];
 #pragma unroll
-          for (int e = M::VALUE_PARTS - 1; e >= 0; --e) M::mma(S[k], a, f[e]);
+          for (int e = 0; e < M::N; e += 4) {
+            const f32x4 w = *reinterpret_cast<const f32x4*>(fade + M::KB * kk + M::N * q + e);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[e + j] = M::at(v[kk], e + j) * w[j];
+          }
+          frag f[M::VALUE_PARTS];
+          M::template split<M::VALUE_PARTS>(x, f);
+#pragma unroll
+          for (int k = 0; k < TILES; ++k) {
+            const frag a = M::col(lds_b, PA, M::KB * kk, 16 * k, i, q);
+#pragma unroll
+            for (int e = M::VALUE_PARTS - 1; e >= 0; --e) M::mma(S[k], a, f[e]);
+          }
         }
       }
     } else if (slow) {
@@ -721,7 +725,7 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
 }
 
 // The state in front of each piece, in the place of what the piece adds to it: a thread an element.
-constexpr int JOIN_THREADS = 256, JOIN_AHEAD = 8;
+constexpr int JOIN_THREADS = 256, JOIN_AHEAD = 16;
 __global__ __launch_bounds__(JOIN_THREADS) void lin_join(LinArgs g) {
   const int which = blockIdx.y;
   const int64_t size = (int64_t)g.role[which].ka * g.role[which].nc;
