@@ -474,7 +474,7 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
   const float log2d = lin_log2(g.rate ? g.rate[h] : 0.0f);
   const uint8_t* flags = g.reset ? g.reset + b * g.reset_batch : nullptr;
   // Whether place p starts an episode in the order of the walk (backward: whether the step behind it does).
-  const auto starts = [&](int p) {
+  const auto starts = [&](int64_t p) {
     if (!flags || p >= stop) return 0;
     if (back) return p == 0 ? 0 : (int)flags[(n - p) * g.reset_step];
     return (int)flags[p * g.reset_step];
@@ -491,7 +491,7 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
     if constexpr (!STATE) ta.load(tid, back, count);
     tb.load(tid, back, count);
     tc.load(tid, back, count);
-    flag = lane < CL ? starts(p0 + lane) : 0;
+    flag = lane < CL ? starts((int64_t)p0 + lane) : 0;
   };
   if (begin < stop) fetch(begin);
   // The next place's row of o, or of 16 places the one that comes first in memory.
@@ -523,10 +523,10 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
   const float two = lin_power(log2d, 16);
   __syncthreads();
   int turn = 0;
-  for (int p0 = begin; p0 < stop; p0 += CL, turn ^= 1, out += CL * (back ? -o_step : o_step)) {
+  for (int left = stop - begin; left > 0; left -= CL, turn ^= 1, out += CL * (back ? -o_step : o_step)) {   // (31 bits do not hold the place behind the last chunk)
     const int tid = opaque(threadIdx.x), lane = tid & 63, i = lane & 15, q = lane >> 4;
     const int64_t out_step = opaque_scalar(o_step), out_walk = back ? -out_step : out_step;
-    const int cnt = stop - p0 < CL ? stop - p0 : CL;
+    const int p0 = stop - left, cnt = left < CL ? left : CL;
     const int lead = back && p0 == 0 ? 0 : 1;   // steps between the state in front and the first place
     if constexpr (!STATE) ta.store(tid, lds_a, back, 0);
     if (!M::finite(tc.store(tid, lds_c, back, tb.store(tid, lds_b, back, 0)))) odd[turn] = 1;
@@ -541,7 +541,7 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
     }
     const int first = cuts ? __builtin_ctzll(cuts) : CL;
     __syncthreads();
-    if (!ONE && p0 + CL < stop) fetch(p0 + CL);
+    if (!ONE && left > CL) fetch(p0 + CL);
     const bool slow = __builtin_amdgcn_readfirstlane(odd[turn]) != 0;
     frag v[CL / M::KB];
     if (16 * wave < cols) {
@@ -605,7 +605,7 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
             }
           }
         }
-        const int left = cols - 16 * wave - 4 * q;
+        const int wide = cols - 16 * wave - 4 * q;
 #pragma unroll
         for (int ti = 0; ti < ROWS; ++ti) {
           const int t = 16 * ti + i;
@@ -623,11 +623,11 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
 #pragma unroll
               for (int k = M::SCORE_PARTS - 1; k >= 0; --k) M::mma(o[ti], v[kk], M::row(lds_p + k * SCORES, PS, 16 * ti, M::KB * kk, i, q));
             }
-          if (t < cnt && left > 0) {
+          if (t < cnt && wide > 0) {
             const int up = back ? 15 - i : i;
             char* to = out + 16 * ti * out_walk + (g.far ? up * out_step : (int64_t)(uint32_t)(up * (uint32_t)out_step));
             T* y = reinterpret_cast<T*>(to) + 16 * wave + 4 * q;
-            if (left >= 4) {
+            if (wide >= 4) {
               if constexpr (sizeof(T) == 2) {
                 const u32x2 w = {pack_bf16x2(o[ti][0], o[ti][1]), pack_bf16x2(o[ti][2], o[ti][3])};
                 __builtin_memcpy(y, &w, 8);
@@ -637,12 +637,12 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
             } else {
 #pragma unroll
               for (int e = 0; e < 3; ++e)
-                if (e < left) y[e] = from_f<T>(o[ti][e]);
+                if (e < wide) y[e] = from_f<T>(o[ti][e]);
             }
           }
         }
       }
-      if (!STATE && !r.last && p0 + CL >= stop) {
+      if (!STATE && !r.last && left <= CL) {
         // Nobody asks for the state behind it.
       } else {
         const float whole = lin_power(log2d, cnt - 1 + lead);
@@ -860,8 +860,7 @@ template <typename T> int64_t lin_fill(int ka) {
 constexpr int64_t PIECE_LEAST = 64, PIECES_FROM = 256;
 struct LinPlan { bool chunks; int64_t pieces, len; };
 template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bool back) {
-  // (Places are counted in 31 bits, a chunk past the last one included.)
-  if (a.steps <= (sizeof(T) == 2 ? 2 : 4) || a.steps > OP_MAX_EXTENT - 4096 || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
+  if (a.steps <= (sizeof(T) == 2 ? 2 : 4) || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
   const int K = (int)a.key_width, V = (int)a.value_width;
   const int64_t k = op_div_up(K, CHUNK_COLS), v = op_div_up(V, CHUNK_COLS), heads = a.batch * a.heads;
   if (heads == 0) return {true, 1, a.steps};

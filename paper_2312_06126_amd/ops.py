@@ -20,6 +20,7 @@ import math
 import struct
 from typing import NamedTuple, Optional, Sequence
 
+import numpy as np
 import torch
 
 from .spz import (ADAMW_BLOCK, GATES, NORMS, PAIRS, SPZ_EINVAL, SPZ_OK, SpzError, load, pack_adamw, pack_adamw_tensor,
@@ -725,8 +726,11 @@ class AdamW:
         self.m, self.v = (torch.zeros(at, dtype=kind, device=dev) for _ in range(2))
         self.m_scale, self.v_scale = (torch.zeros(at // ADAMW_BLOCK, device=dev) if bits == 8 else None for _ in range(2))
         self._moments = at
-        self._layout = [(p, c, p.shape, p.data_ptr(), _ptr(c)) for p, c in zip(params, copies)]
-        self._entries = [[p.data_ptr(), 0, _ptr(c), p.numel(), at, d] for p, c, at, d in zip(params, copies, self.places, decay)]
+        self._layout = [(p, c, p.shape, p.numel(), p.data_ptr(), _ptr(c)) for p, c in zip(params, copies)]
+        # One row of 64-bit words for each tensor, as the library reads them (spz_adamw_tensor).
+        self._plan = np.frombuffer(b"".join(pack_adamw_tensor(p.data_ptr(), 0, _ptr(c), p.numel(), at, d)
+                                            for p, c, at, d in zip(params, copies, self.places, decay)), np.uint64).reshape(len(params), 6)
+        self._one_type = first.dtype if all(p.dtype is first.dtype for p in params) else None
 
     def _tensor(self, p, name):
         if not isinstance(p, torch.Tensor) or p.get_device() != self._gpu or p.dtype not in _PREC or not p.is_contiguous():
@@ -761,21 +765,24 @@ class AdamW:
                 _like(t, name, gpu, t.shape, kind, contiguous=True)
         if grad_scale is not None and not isinstance(grad_scale, torch.Tensor):
             _refuse("grad_scale is no tensor")
-        entries = self._entries
-        grad_on = _grad_on()
-        kinds = set()
-        for i, (g, (p, c, shape, at, to)) in enumerate(zip(grads, self._layout)):
+        grad_on, first = _grad_on(), None
+        plain, addresses = True, []    # plain: all tensors have a gradient, of one type
+        for i, (g, (p, c, shape, n, at, to)) in enumerate(zip(grads, self._layout)):
             if g is None:
-                entries[i][1] = 0
+                plain = False
+                addresses.append(0)
                 continue
             if not isinstance(g, torch.Tensor) or g.dtype not in _PREC or g.shape != shape or g.get_device() != gpu or not g.is_contiguous():
                 _refuse("grads[%d] is no contiguous float32 or bfloat16 tensor %s on cuda:%d" % (i, tuple(shape), gpu))
             if grad_on and g.requires_grad:
                 _refuse_grad("grads[%d]" % i)
-            if p.data_ptr() != at or p.shape != shape or (c is not None and c.data_ptr() != to):
+            if p.data_ptr() != at or p.numel() != n or (c is not None and c.data_ptr() != to):
                 _refuse("params[%d] or its copy is not where it was: make another AdamW of the new tensors" % i)
-            entries[i][1] = g.data_ptr()
-            kinds.add((p.dtype, g.dtype))
+            addresses.append(g.data_ptr())
+            kind = g.dtype
+            if kind is not first:
+                plain = plain and first is None
+                first = kind
 
         if stream is not None or gpu != _device():
             tensors = [*self.params, *self.copies, *grads, self.m, self.v, self.m_scale, self.v_scale, grad_scale]
@@ -783,19 +790,23 @@ class AdamW:
             return _elsewhere(stream, gpu, tensors, lambda: self.step(grads, step=step, lr=lr, betas=betas, eps=eps, grad_scale=grad_scale))
         s = _stream(gpu)
         on_step, on_lr = isinstance(step, torch.Tensor), isinstance(lr, torch.Tensor)
-        some = [i for i, g in enumerate(grads) if g is not None and g.numel()]
-        for kind in kinds:
-            chosen = some if len(kinds) == 1 else [i for i in some if (self.params[i].dtype, grads[i].dtype) == kind]
-            block = b"".join([pack_adamw_tensor(*entries[i]) for i in chosen])
-            host = ctypes.create_string_buffer(block, len(block))
+        # The entries of a call: a copy of the plan's with the gradients' addresses, one call for each pair of types.
+        entries = self._plan.copy()
+        entries[:, 1] = addresses
+        if plain and self._one_type:
+            calls = ((_PREC[self._one_type], _PREC[first], entries),)
+        else:
+            kinds = [None if g is None else (_PREC[p.dtype], _PREC[g.dtype]) for p, g in zip(self.params, grads)]
+            calls = [(*k, entries[[i for i, x in enumerate(kinds) if x == k]]) for k in sorted(set(kinds) - {None})]
+        for p_prec, g_prec, block in calls:
             try:
                 b1, b2 = betas
-                a = pack_adamw(len(chosen), self._moments, ctypes.addressof(host), self.m.data_ptr(), self.v.data_ptr(), _ptr(self.m_scale),
+                a = pack_adamw(len(block), self._moments, block.ctypes.data, self.m.data_ptr(), self.v.data_ptr(), _ptr(self.m_scale),
                                _ptr(self.v_scale), _ptr(grad_scale), step.data_ptr() if on_step else 0, lr.data_ptr() if on_lr else 0,
-                               0 if on_step else step, 0.0 if on_lr else lr, b1, b2, eps, self._seed, self.bits, _PREC[kind[0]], _PREC[kind[1]], 0)
+                               0 if on_step else step, 0.0 if on_lr else lr, b1, b2, eps, self._seed, self.bits, p_prec, g_prec, 0)
             except _NOT_NUMBERS as e:
                 _refuse("step, lr, betas or eps is no number: %s" % e)
             rc = lib.spz_adamw(a, s)
             if rc:
                 _done(rc)
-        torch.autograd.graph.increment_version([self.params[i] for i in some])
+        torch.autograd.graph.increment_version(self.params if plain else [p for p, g in zip(self.params, grads) if g is not None])
