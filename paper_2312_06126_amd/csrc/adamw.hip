@@ -129,6 +129,9 @@ __device__ inline float block_max(const float (&x)[8]) {
   return __builtin_bit_cast(float, m);
 }
 
+// Bound by HBM: 53 million float32 elements with bfloat16 gradients and copies and 8-bit moments 157 us, 5.4 TB/s; 7.7 million
+// with moments of 32 bits 36 us, 5.9 TB/s of arrays partly in the last-level cache. (Library quotients and roots: 214 us, by
+// their instructions.)
 template <typename P, typename G, bool EIGHT>
 __global__ __launch_bounds__(ADAM_THREADS) void adamw_step(AdamArgs g) {
   const int64_t blk = g.from + blockIdx.x;

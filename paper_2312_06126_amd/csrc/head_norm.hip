@@ -223,7 +223,9 @@ template <typename T, int N> __device__ inline void store_n(T* p, const float* x
 
 // Columns in vectors: a group of L lanes a row, each lane two runs of SV columns, which turn together where pairs are
 // halves (columns c .. and pairs + c ..) and by themselves where they are neighbours. SV = 1 takes any number of columns:
-// the last lane's second one may not exist.
+// the last lane's second one may not exist. The next head's columns are in flight while one is worked on.
+// 65536 x (16 + 4) x 64 bf16: forward 76 us, 4.4 TB/s, backward 118, 4.3 TB/s: HBM. An angle costs some 70 instructions, a
+// head 100: a wave a head each, with the angles taken for each of them, took 500 and 590 us.
 template <typename T, int SV, int L, bool BACK> __global__ __launch_bounds__(HEAD_THREADS) void head_vectors(HeadArgs g, int64_t first) {
   constexpr int N = 2 * SV, GROUPS = HEAD_THREADS / L;
   const int j = threadIdx.x % L;
