@@ -312,7 +312,7 @@ template <typename T, int W, int CL> struct Tile {
   // Where a vector is read: the last one of a row that ends inside it is read whole, from further in front.
   __device__ inline int column(int col) const { return col + VW <= width ? col : col < width ? width - VW : 0; }
   // The next chunk, of which `count` > 0 places exist. Rows behind the last one read that one again.
-  __device__ inline void load(int tid, bool back, int count) {
+  __device__ inline void load(uint32_t tid, bool back, int count) {
     cnt = count;
     if (!some) return;
     const int64_t step = opaque_scalar(this->step);
@@ -362,7 +362,7 @@ template <typename T, int W, int CL> struct Tile {
     }
   }
   // To LDS; returns the largest of the magnitudes and m. Rows that are not `plain` come from memory only here.
-  __device__ inline uint32_t store(int tid, T* lds, bool back, uint32_t m) {
+  __device__ inline uint32_t store(uint32_t tid, T* lds, bool back, uint32_t m) {
     if (some && !plain) {
       const char* from = at - CL * step + (back ? -(CL - 1) * step : 0);   // of the chunk's first place
 #pragma unroll 1

@@ -459,15 +459,19 @@ def _head_check(q, k, vectors, norm, positions, freqs, pairs, valid) -> int:
             _refuse("k is no tensor [rows, heads, dim]")
         _like(k, "k", gpu, (R, k.shape[1], D), q.dtype)
     for i, t in enumerate(vectors):
-        if t is not None:
+        if t is not None and not (isinstance(t, torch.Tensor) and t.dtype is _F32 and t.dim() == 1 and t.numel() == D
+                                  and t.get_device() == gpu and t.is_contiguous() and not t.requires_grad):
             _like(t, ("w_q", "b_q", "w_k", "b_k")[i], gpu, (D,), _F32)
-    if (positions is None) != (freqs is None):
-        _refuse("positions and freqs come together")
-    if freqs is not None:
-        _like(positions, "positions", gpu, (R,), torch.int32, contiguous=True)
-        if not isinstance(freqs, torch.Tensor) or freqs.dim() != 1 or 2 * freqs.shape[0] > D:
+    if freqs is not None and positions is not None:
+        if not (isinstance(positions, torch.Tensor) and positions.dtype is torch.int32 and positions.dim() == 1 and positions.numel() == R
+                and positions.get_device() == gpu and positions.is_contiguous()):
+            _like(positions, "positions", gpu, (R,), torch.int32, contiguous=True)
+        if not isinstance(freqs, torch.Tensor) or freqs.dim() != 1 or 2 * freqs.numel() > D:
             _refuse("freqs is no tensor of at most dim / 2 angles")
-        _like(freqs, "freqs", gpu, freqs.shape, torch.float64, contiguous=True)
+        if freqs.dtype is not torch.float64 or freqs.get_device() != gpu or not freqs.is_contiguous() or freqs.requires_grad:
+            _like(freqs, "freqs", gpu, freqs.shape, torch.float64, contiguous=True)
+    elif positions is not freqs:
+        _refuse("positions and freqs come together")
     if valid is not None:
         _like(valid, "valid", gpu, (R,), torch.bool if getattr(valid, "dtype", None) is torch.bool else torch.uint8, contiguous=True)
     return gpu
@@ -479,9 +483,7 @@ def _two(t):
 
 
 def _pair_out(out, q, k, gpu, names):
-    """The two tensors of an `out` argument, checked (none: two None)."""
-    if out is None:
-        return None, None
+    """The two tensors of an `out` argument, checked."""
     if not isinstance(out, (tuple, list)) or len(out) != 2 or out[0] is None or (out[1] is None) != (k is None):
         _refuse("out holds %s and %s" % names)
     _like(out[0], names[0], gpu, q.shape, q.dtype)
@@ -491,14 +493,23 @@ def _pair_out(out, q, k, gpu, names):
 
 
 def _head_pack(q, k, vectors, positions, freqs, valid, outs, back, grads, eps, norm, pairs) -> bytes:
-    """The argument block; outs: q_out, k_out; back: dq_out, dk_out, dq, dk; grads: dw_q, db_q, dw_k, db_k."""
+    """The argument block; outs (forward): q_out, k_out; back (backward): dq_out, dk_out, dq, dk; grads: dw_q, db_q, dw_k, db_k."""
     R, H, D = q.shape
+    rq, hq, _ = q.stride()
+    if k is None:
+        K = pk = rk = hk = 0
+    else:
+        K, pk, (rk, hk, _) = k.shape[1], k.data_ptr(), k.stride()
+    wq, bq, wk, bk = vectors
     try:
-        return pack_head_norm(
-            R, H, 0 if k is None else k.shape[1], D, 0 if freqs is None else freqs.shape[0], q.data_ptr(), _ptr(k), *_two(q), *_two(k),
-            *map(_ptr, vectors), _ptr(positions), _ptr(freqs), _ptr(valid), _ptr(outs[0]), _ptr(outs[1]), *_two(outs[0]), *_two(outs[1]),
-            _ptr(back[0]), _ptr(back[1]), *_two(back[0]), *_two(back[1]), _ptr(back[2]), _ptr(back[3]), *_two(back[2]), *_two(back[3]),
-            *map(_ptr, grads), eps, NORMS[norm], PAIRS[pairs], _PREC[q.dtype])
+        if outs is not None:
+            a, b = outs
+            rest = (a.data_ptr(), _ptr(b), *_two(a), *_two(b), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+        else:
+            rest = (0, 0, 0, 0, 0, 0, _ptr(back[0]), _ptr(back[1]), *_two(back[0]), *_two(back[1]), _ptr(back[2]), _ptr(back[3]), *_two(back[2]),
+                    *_two(back[3]), *map(_ptr, grads))
+        return pack_head_norm(R, H, K, D, 0 if freqs is None else freqs.numel(), q.data_ptr(), pk, rq, hq, rk, hk, _ptr(wq), _ptr(bq), _ptr(wk), _ptr(bk),
+                              _ptr(positions), _ptr(freqs), _ptr(valid), *rest, eps, NORMS[norm], PAIRS[pairs], _PREC[q.dtype])
     except _NOT_NUMBERS as e:
         _refuse("eps is no number: %s" % e)
 
@@ -514,7 +525,7 @@ def head_norm(q, k=None, w_q=None, w_k=None, b_q=None, b_k=None, *, norm="rms", 
     lib = load()
     vectors = (w_q, b_q, w_k, b_k)
     gpu = _head_check(q, k, vectors, norm, positions, freqs, pairs, valid)
-    q_out, k_out = _pair_out(out, q, k, gpu, ("q'", "k'"))
+    q_out, k_out = (None, None) if out is None else _pair_out(out, q, k, gpu, ("q'", "k'"))
 
     if stream is not None or gpu != _device():
         return _elsewhere(stream, gpu, (q, k, *vectors, positions, freqs, valid, q_out, k_out),
@@ -523,7 +534,7 @@ def head_norm(q, k=None, w_q=None, w_k=None, b_q=None, b_k=None, *, norm="rms", 
     s = _stream(gpu)
     if q_out is None:
         q_out, k_out = q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)
-    rc = lib.spz_head_norm_forward(_head_pack(q, k, vectors, positions, freqs, valid, (q_out, k_out), (None,) * 4, (None,) * 4, eps, norm, pairs), s)
+    rc = lib.spz_head_norm_forward(_head_pack(q, k, vectors, positions, freqs, valid, (q_out, k_out), None, None, eps, norm, pairs), s)
     if rc:
         _done(rc)
     return q_out, k_out
@@ -541,7 +552,7 @@ def head_norm_backward(dq_out, dk_out, q, k=None, w_q=None, w_k=None, b_q=None, 
         _refuse("dk_out without k")
     if k is not None:
         _like(dk_out, "dk_out", gpu, k.shape, q.dtype)
-    dq, dk = _pair_out(out, q, k, gpu, ("dq", "dk"))
+    dq, dk = (None, None) if out is None else _pair_out(out, q, k, gpu, ("dq", "dk"))
 
     if stream is not None or gpu != _device():
         return _elsewhere(stream, gpu, (dq_out, dk_out, q, k, *vectors, positions, freqs, valid, dq, dk),
@@ -554,7 +565,7 @@ def head_norm_backward(dq_out, dk_out, q, k=None, w_q=None, w_k=None, b_q=None, 
     sums = iter(q.new_empty((4, q.shape[2]), dtype=_F32).unbind(0))
     for name, t in zip(("dw_q", "db_q", "dw_k", "db_k"), vectors):
         g[name] = None if t is None else next(sums)
-    a = _head_pack(q, k, vectors, positions, freqs, valid, (None, None), (dq_out, dk_out, dq, dk),
+    a = _head_pack(q, k, vectors, positions, freqs, valid, None, (dq_out, dk_out, dq, dk),
                    (g["dw_q"], g["db_q"], g["dw_k"], g["db_k"]), eps, norm, pairs)
     n = _size(lib.spz_head_norm_workspace(a))
     ws = _workspace(n, q)
@@ -574,16 +585,20 @@ def _attention_sizes(B: int, T: int, H: int, K: int, V: int, prec: int):
 
 def _attention_check(q, k, v, rate, state, reset, lengths) -> int:
     gpu = _operand(q, "q", 4)
-    B, T, H, K = q.shape
+    B, T, H, K = shape = q.shape
     if k is None or v is None:
         _refuse("k or v is missing")
-    _like(k, "k", gpu, q.shape, q.dtype)
+    _like(k, "k", gpu, shape, q.dtype)
     if not isinstance(v, torch.Tensor) or v.dim() != 4:
         _refuse("v is no tensor [batch, steps, heads, width]")
-    _like(v, "v", gpu, (B, T, H, v.shape[3]), q.dtype)
-    _like(rate, "rate", gpu, (H,), _F32, contiguous=True)
-    _like(state, "state", gpu, (B, H, K, v.shape[3]), _F32, contiguous=True)
-    _like(lengths, "lengths", gpu, (B,), torch.int32, contiguous=True)
+    V = v.shape[3]
+    _like(v, "v", gpu, (B, T, H, V), q.dtype)
+    if rate is not None:
+        _like(rate, "rate", gpu, (H,), _F32, contiguous=True)
+    if state is not None:
+        _like(state, "state", gpu, (B, H, K, V), _F32, contiguous=True)
+    if lengths is not None:
+        _like(lengths, "lengths", gpu, (B,), torch.int32, contiguous=True)
     if reset is not None:
         _flags_2d(reset, "reset", gpu, (B, T))
     return gpu
@@ -615,8 +630,10 @@ def linear_attention(q, k, v, rate=None, state=None, *, scale=None, reset=None, 
     gpu = _attention_check(q, k, v, rate, state, reset, lengths)
     B, T, H, K = q.shape
     V = v.shape[3]
-    _like(out, "out", gpu, v.shape, q.dtype)
-    _like(last, "last", gpu, (B, H, K, V), _F32, contiguous=True)
+    if out is not None:
+        _like(out, "out", gpu, v.shape, q.dtype)
+    if last is not None and last is not state:
+        _like(last, "last", gpu, (B, H, K, V), _F32, contiguous=True)
     n = _attention_sizes(B, T, H, K, V, _PREC[q.dtype])[0]
 
     if stream is not None or gpu != _device():
