@@ -442,7 +442,7 @@ __device__ inline void state_store(float* p, const f32x4 (&S)[TILES], bool full,
 
 // KP: rows of the state that are worked on, a multiple of the contraction's (48 instead of 64 for heads of 40 x 39 in float32, 64 x 1000 x 5: 121 us against 140).
 // Workgroups a compute unit is to hold, which bounds their registers.
-template <typename T, int KP, bool STATE, bool ONE> constexpr int chunk_waves = KP > 64 ? 1 : sizeof(T) == 4 ? 2 : 4;
+template <typename T, int KP, bool STATE, bool ONE> constexpr int chunk_waves = KP > 64 ? 1 : sizeof(T) == 4 ? 3 : 4;
 
 // A workgroup: slice of a role, head, sequence, piece of time. STATE: only what the piece adds to the state. ONE: no
 // sequence is longer than a chunk. The scores take the place of c, of which each wave has its columns in registers by then.
@@ -849,34 +849,44 @@ template <typename T> int lin_rows(int ka) {
     if (ka <= kp && kp % Mat<T>::KB == 0) return kp;
   return 256;
 }
-template <typename T> int64_t lin_fill(int ka) {
+// Microseconds of a launch of n workgroups of `chunks` chunks each: a compute unit holds `most` of them at once, whose chunk
+// takes 5 and 1 more for each of them (1 to 4 a unit: 6.0 to 8.7 measured at 64 rows in bfloat16), and a workgroup's start as long
+// as a chunk.
+template <typename T> int64_t lin_time(int ka, int64_t n, int64_t chunks) {
   const int kp = lin_rows<T>(ka);
-  return sizeof(T) == 2 ? (kp <= 64 ? 1024 : kp <= 128 ? 512 : 256) : kp <= 64 ? 768 : 256;
+  const int64_t most = kp > 128 ? 1 : kp > 64 ? (sizeof(T) == 2 ? 2 : 1) : sizeof(T) == 2 ? 4 : 3;
+  const int64_t each = op_div_up(n, 256), rounds = op_div_up(each, most);
+  return (chunks + 1) * (5 * rounds + each);
 }
 // How a call is spread, by its sizes alone (microseconds a call, both sides measured, heads of 64 x 64, bfloat16):
 //   steps: a thread keeps its part of the state and walks: up to 2 steps, in float32 4 (2048 x 4 heads: 2 steps 59 against
 //     68 in chunks, 4 steps 82 against 66; in float32 4 steps 90 against 110, 8 steps 142 against 112);
-//   chunks: a workgroup walks in chunks on the matrix cores, 4.5 a chunk;
-//   pieces: time cut into pieces of PIECE_LEAST steps and more whose sums are joined first, as many as the card holds at
-//     once: two launches and a second reading of keys and values more, where heads leave compute units idle and there are more
-//     than PIECES_FROM steps (1 x 1000 x 4: 23 against 73; 8 x 1000 x 8: 34 against 77; 32 x 256 x 4: 28 against 24;
-//     64 x 1000 x 5 in float32: 167 either way).
-constexpr int64_t PIECE_LEAST = 64, PIECES_FROM = 256;
+//   chunks: a workgroup walks in chunks on the matrix cores, 6 to 9 a chunk;
+//   pieces: time cut into pieces of 64 steps and more whose sums are joined first, two launches and a second reading of keys and
+//     values more, where the model above says that it pays (1 x 1000 x 4: 21 against 73; 8 x 1000 x 8: 37 against 77;
+//     64 x 1000 x 4: 69 against 85, in float32 151 against 133; 32 x 256 x 4: 28 against 24).
 struct LinPlan { bool chunks; int64_t pieces, len; };
 template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bool back) {
   if (a.steps <= (sizeof(T) == 2 ? 2 : 4) || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
   const int K = (int)a.key_width, V = (int)a.value_width;
   const int64_t k = op_div_up(K, CHUNK_COLS), v = op_div_up(V, CHUNK_COLS), heads = a.batch * a.heads;
-  if (heads == 0) return {true, 1, a.steps};
-  // Workgroups of a launch: by key rows (y; dv), by value rows (dq and dk), or all in one.
+  LinPlan best{true, 1, a.steps};
+  if (heads == 0 || a.steps <= 128 || heads > 2048) return best;
+  // Workgroups of a launch: by key rows (y; dv), by value rows (dq and dk), or all in one; and of the pieces' sums.
   const bool same = lin_rows<T>(K) == lin_rows<T>(V);
-  const int64_t by_k = v + (back && same ? 2 * k : 0), by_v = back && !same ? 2 * k : 0;
-  int64_t pieces = lin_fill<T>(K) / (heads * by_k);
-  if (by_v && lin_fill<T>(V) / (heads * by_v) > pieces) pieces = lin_fill<T>(V) / (heads * by_v);
-  if (pieces > a.steps / PIECE_LEAST) pieces = a.steps / PIECE_LEAST;
-  if (pieces < 2 || heads * by_k >= 256 || a.steps <= PIECES_FROM) return {true, 1, a.steps};
-  const int64_t len = op_div_up(op_div_up(a.steps, pieces), 64) * 64;
-  return {true, op_div_up(a.steps, len), len};
+  const int64_t by_k = v + (back && same ? 2 * k : 0), by_v = back && !same ? 2 * k : 0, sums = back ? 2 * v : v;
+  int64_t least = 0;
+  for (const int64_t pieces : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 128}) {
+    const int64_t len = op_div_up(op_div_up(a.steps, pieces), 64) * 64, chunks = len / 64;
+    if (pieces > 1 && op_div_up(a.steps, len) != pieces) continue;
+    int64_t time = lin_time<T>(K, heads * pieces * by_k, chunks) + (by_v ? lin_time<T>(V, heads * pieces * by_v, chunks) : 0);
+    if (pieces > 1) time += lin_time<T>(K, heads * pieces * sums, chunks) / 2 + 20 + pieces / 8;   // joins by 8 pieces
+    if (pieces == 1 || time < least) {
+      least = time;
+      best = {true, pieces, pieces > 1 ? len : a.steps};
+    }
+  }
+  return best;
 }
 LinPlan lin_plan(const spz_linear_attention_args& a, bool back) {
   return a.prec == SPZ_PREC_BF16 ? lin_plan_of<bf16_t>(a, back) : lin_plan_of<float>(a, back);
