@@ -843,28 +843,29 @@ template <typename T> void lin_steps_launch(LinArgs g, hipStream_t s) {
   else go(integral_constant<int, 16>{});
 }
 
-// The rows of states that the kernels come in, and workgroups of each that the card holds at once.
+// The rows of states that the kernels come in.
 template <typename T> int lin_rows(int ka) {
   for (const int kp : {32, 48, 64, 96, 128})
     if (ka <= kp && kp % Mat<T>::KB == 0) return kp;
   return 256;
 }
-// Microseconds of a launch of n workgroups of `chunks` chunks each: a compute unit holds `most` of them at once, whose chunk
-// takes 5 and 1 more for each of them (1 to 4 a unit: 6.0 to 8.7 measured at 64 rows in bfloat16), and a workgroup's start as long
-// as a chunk.
+// Microseconds of a launch of n workgroups of `chunks` chunks each: a compute unit holds `most` of them at once, and a
+// workgroup's start counts as a chunk. A chunk takes 5 and 1 more for each workgroup of the unit (64 x 64 heads, 1 to 4 a unit: 5.8,
+// 6.1, 6.9 and 8.4 measured), in float32 5 and 3 (1 to 3 a unit: 8.3, 10.8 and 14.0).
 template <typename T> int64_t lin_time(int ka, int64_t n, int64_t chunks) {
   const int kp = lin_rows<T>(ka);
   const int64_t most = kp > 128 ? 1 : kp > 64 ? (sizeof(T) == 2 ? 2 : 1) : sizeof(T) == 2 ? 4 : 3;
   const int64_t each = op_div_up(n, 256), rounds = op_div_up(each, most);
-  return (chunks + 1) * (5 * rounds + each);
+  return (chunks + 1) * (5 * rounds + (sizeof(T) == 2 ? 1 : 3) * each);
 }
 // How a call is spread, by its sizes alone (microseconds a call, both sides measured, heads of 64 x 64, bfloat16):
 //   steps: a thread keeps its part of the state and walks: up to 2 steps, in float32 4 (2048 x 4 heads: 2 steps 59 against
 //     68 in chunks, 4 steps 82 against 66; in float32 4 steps 90 against 110, 8 steps 142 against 112);
-//   chunks: a workgroup walks in chunks on the matrix cores, 6 to 9 a chunk;
+//   chunks: a workgroup walks in chunks on the matrix cores;
 //   pieces: time cut into pieces of 64 steps and more whose sums are joined first, two launches and a second reading of keys and
-//     values more, where the model above says that it pays (1 x 1000 x 4: 21 against 73; 8 x 1000 x 8: 37 against 77;
-//     64 x 1000 x 4: 69 against 85, in float32 151 against 133; 32 x 256 x 4: 28 against 24).
+//     values more, where the model above says that it pays (in pieces against whole, forward: 1 x 1000 x 4 20 against 76, in float32
+//     22 against 114; 1 x 300 x 16 20 against 27; 8 x 1000 x 8 37 against 80; 64 x 1000 x 4 69 against 86). The two launches count
+//     as 12: as 8 the model cuts 32 x 256 x 4 (30 against 24), as 16 it leaves 4 x 200 x 4 in float32 whole (31 against 22).
 struct LinPlan { bool chunks; int64_t pieces, len; };
 template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bool back) {
   if (a.steps <= (sizeof(T) == 2 ? 2 : 4) || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
@@ -880,7 +881,7 @@ template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bo
     const int64_t len = op_div_up(op_div_up(a.steps, pieces), 64) * 64, chunks = len / 64;
     if (pieces > 1 && op_div_up(a.steps, len) != pieces) continue;
     int64_t time = lin_time<T>(K, heads * pieces * by_k, chunks) + (by_v ? lin_time<T>(V, heads * pieces * by_v, chunks) : 0);
-    if (pieces > 1) time += lin_time<T>(K, heads * pieces * sums, chunks) / 2 + 20 + pieces / 8;   // joins by 8 pieces
+    if (pieces > 1) time += lin_time<T>(K, heads * pieces * sums, chunks) / 2 + 12 + pieces / 8;   // joins by 8 pieces
     if (pieces == 1 || time < least) {
       least = time;
       best = {true, pieces, pieces > 1 ? len : a.steps};
