@@ -440,8 +440,10 @@ __device__ inline void state_store(float* p, const f32x4 (&S)[TILES], bool full,
   }
 }
 
-// KP: rows of the state that are worked on, a multiple of the contraction's (48 instead of 64 for heads of 40 x 39 in float32, 64 x 1000 x 5: 121 us against 140).
-// Workgroups a compute unit is to hold, which bounds their registers.
+// KP: rows of the state that are worked on, a multiple of the contraction's (48 instead of 64 for heads of 40 x 39 in float32,
+// 64 x 1000 x 5: 157 us against 178, backward 278 against 316).
+// Workgroups a compute unit is to hold, which bounds their registers (three and not two in float32 up to 64 rows: 256 x 500 x 4 x
+// 64 x 64 backward 453 us against 511).
 template <typename T, int KP, bool STATE, bool ONE> constexpr int chunk_waves = KP > 64 ? 1 : sizeof(T) == 4 ? 3 : 4;
 
 // A workgroup: slice of a role, head, sequence, piece of time. STATE: only what the piece adds to the state. ONE: no
@@ -859,17 +861,26 @@ template <typename T> int64_t lin_time(int ka, int64_t n, int64_t chunks) {
   return (chunks + 1) * (5 * rounds + (sizeof(T) == 2 ? 1 : 3) * each);
 }
 // How a call is spread, by its sizes alone (microseconds a call, both sides measured, heads of 64 x 64, bfloat16):
-//   steps: a thread keeps its part of the state and walks: up to 2 steps, in float32 4 (2048 x 4 heads: 2 steps 59 against
-//     68 in chunks, 4 steps 82 against 66; in float32 4 steps 90 against 110, 8 steps 142 against 112);
+//   steps: a thread keeps its part of the state and walks: up to 2 steps, in float32 4 (2048 x 4 heads: 2 steps 60 against
+//     67 in chunks, 4 steps 81 against 66; in float32 4 steps 90 against 110, 8 steps 143 against 111). In bfloat16 not at 97 to 128
+//     rows (2048 x 4 x 128 x 128, 1 step: 320 against 277, backward 611 against 587 and with a gradient to the last state 1045
+//     against 686; 4096 x 8 x 64 x 128, 2 steps backward: 2636 against 1389). Fewer and more rows gain from steps (1 step, 2048 x 4 x
+//     96 x 96 265 against 350; 512 x 4 x 256 x 256 305 against 412; 4096 x 8 x 64 x 64 backward 423 against 513; with that gradient
+//     2048 x 4 x 48 x 48 104 against 166, but 4096 x 8 x 64 x 64 666 against 582);
 //   chunks: a workgroup walks in chunks on the matrix cores;
 //   pieces: time cut into pieces of 64 steps and more whose sums are joined first, two launches and a second reading of keys and
 //     values more, where the model above says that it pays (in pieces against whole, forward: 1 x 1000 x 4 20 against 76, in float32
 //     22 against 114; 1 x 300 x 16 20 against 27; 8 x 1000 x 8 37 against 80; 64 x 1000 x 4 69 against 86). The two launches count
 //     as 12: as 8 the model cuts 32 x 256 x 4 (30 against 24), as 16 it leaves 4 x 200 x 4 in float32 whole (31 against 22).
 struct LinPlan { bool chunks; int64_t pieces, len; };
+template <typename T> int64_t lin_most_steps(int K, int V, bool back) {
+  if (sizeof(T) == 4) return 4;
+  const auto within = [](int rows) { return rows > 96 && rows <= 128; };
+  return within(K) || (back && within(V)) ? 0 : 2;   // forward the state's rows are keys only
+}
 template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bool back) {
-  if (a.steps <= (sizeof(T) == 2 ? 2 : 4) || a.key_width == 0 || a.value_width == 0) return {false, 1, a.steps};
   const int K = (int)a.key_width, V = (int)a.value_width;
+  if (a.steps <= lin_most_steps<T>(K, V, back) || K == 0 || V == 0) return {false, 1, a.steps};
   const int64_t k = op_div_up(K, CHUNK_COLS), v = op_div_up(V, CHUNK_COLS), heads = a.batch * a.heads;
   LinPlan best{true, 1, a.steps};
   if (heads == 0 || a.steps <= 128 || heads > 2048) return best;
