@@ -604,7 +604,8 @@ int spz_linear_attention_backward(const spz_linear_attention_args* args, void* w
  * bits, then float32: m = beta1 m + c1 g, v = beta2 v + (c2 g) g); p is rounded once to its type,
  * and so is the bfloat16 copy for products to read. m and v are two arrays of `moments` elements
  * for all tensors: tensor i has elements at .. at + n - 1 of both, `at` a multiple of
- * SPZ_ADAMW_BLOCK; what lies between is left as it is. Two tensors may share no element.
+ * SPZ_ADAMW_BLOCK; what lies between is left as it is. Two tensors may share no element, and
+ * a gradient none with another tensor's p or copy.
  *
  * bits 32: m and v are float32. bits 8: m holds codes of m and v codes of sqrt(v) in the 8-bit
  * floating point type e4m3 (1 sign, 4 exponent, 3 mantissa bits, largest 448), m_scale and v_scale

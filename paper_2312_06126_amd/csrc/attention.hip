@@ -450,7 +450,7 @@ template <typename T, int KP, bool STATE, bool ONE> constexpr int chunk_waves = 
 // sequence is longer than a chunk. The scores take the place of c, of which each wave has its columns in registers by then.
 // Bound by vector instructions, some 700 a wave and chunk at 64 rows, most of them the splits into bfloat16 parts (issued in
 // 70% of the busy cycles, the matrix instructions run in 23%): 65536 steps x 8 heads of 64 x 128 bf16 in 64 pieces 142 us,
-// 2.8 TB/s. Short sequences by the states' bytes: 2048 x 4 heads of 64 x 64, 50 steps, ragged, 91 us.
+// 2.8 TB/s. Short sequences by the states' bytes: 2048 x 4 heads of 64 x 64, 50 steps, ragged, 94 us.
 template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_bounds__(CHUNK_THREADS, (chunk_waves<T, KP, STATE, ONE>)) void lin_chunks(LinArgs g) {
   using M = Mat<T>;
   typedef typename M::frag frag;

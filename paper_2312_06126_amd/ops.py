@@ -700,7 +700,8 @@ class AdamW:
     each 256 of them, rounded at random by `seed` and the step, so that small changes count on average. `m`, `v` and,
     for 8 bits, `m_scale`, `v_scale` hold the moments of all tensors one after the other, each from places[i] on, and are
     the state to save; they start as zeros and may be copied into. copies: bfloat16 tensors that get each new value as
-    well (a list with None for none). weight_decay: a number, or one for each tensor."""
+    well (a list with None for none). weight_decay: a number, or one for each tensor. No two parameters or copies
+    share elements, and no gradient shares any with another parameter or its copy."""
 
     def __init__(self, params: Sequence[torch.Tensor], *, bits: int = 32, copies=None, weight_decay=0.0, seed: int = 0):
         params = list(params)

@@ -67,6 +67,16 @@ def test_attention(shape, prec):
 
 
 @pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("shape", [(3, T, 2, K, V) for T in (1, 2, 3) for K, V in ((96, 96), (97, 64), (64, 97), (128, 128), (129, 130))]
+                         + [(1, 300, 16, 64, 64), (4, 200, 4, 64, 64), (16, 500, 4, 64, 64)], ids=str)
+def test_attention_ways(shape, prec):
+    """Sizes on both sides of the bounds between steps, chunks and pieces of time."""
+    log("attention ways %s %s" % (shape, prec))
+    t, reset, lengths = inputs(np.random.default_rng(sum(shape)), *shape, prec)
+    check_all(run(t, reset, lengths), t, reset, lengths, prec)
+
+
+@pytest.mark.parametrize("prec", PRECS)
 @pytest.mark.parametrize("shape", [(1, 257, 1, 16, 24), (2, 500, 3, 40, 33), (1, 2049, 2, 64, 64), (3, 300, 1, 24, 130), (1, 700, 1, 96, 100), (1, 321, 1, 200, 70)],
                          ids=str)
 def test_attention_time_in_pieces(shape, prec):
