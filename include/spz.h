@@ -560,7 +560,7 @@ int spz_head_norm_backward(const spz_head_norm_args* args, void* workspace, int6
  * state before it, finite or not, passes), else 1. An infinite rate is d = 0. Sequence b has
  * lengths[b] steps (clamped to [0, steps]): behind them nothing is read, y is 0 and the state
  * stays, so last = S of the last step (`state` of an empty sequence). The states are float32
- * throughout. steps = 1 is the samplers' form; last may be state (updated in place).
+ * throughout, in the products too. steps = 1 is the samplers' form; last may be state (updated in place).
  * Queries, keys or values may be shared by heads (stride 0).
  *
  * Backward, from dy and dlast (the gradient to last): with C = dlast behind the last step,

@@ -180,8 +180,9 @@ template <typename T, int KR> __global__ __launch_bounds__(STEP_THREADS) void li
 // The scores a_t b_s are shared through LDS; everything else is a wave's own. All products are taken so that a lane
 // ends with four consecutive elements of what it stores (o as its transpose), and the accumulators of the state are
 // operands of the next product as they stand: the order of the contraction is the same for both operands.
-// bfloat16 operands: the scores and the state enter a product as two bfloat16 numbers each (2^-17 of each is lost, less
-// than an output's rounding), the weighted c, from which the state is summed, as three (all 24 bits).
+// bfloat16 operands: the scores, the state and the weighted c enter a product as three bfloat16 numbers each, which hold all
+// 24 bits, so that a state is float32 in a product too. (Scores and states as two, with 16 bits: 1 x 65536 x 8 x 64 x 128 training 689 us
+// and not 752, 2048 x 50 x 4 x 64 x 64 284 and not 293; their errors, 2^-17 of a term, show where terms cancel.)
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 #define LDS_PTR(T) __attribute__((address_space(3))) T*
@@ -191,7 +192,7 @@ constexpr int CHUNK_THREADS = 256, CHUNK_COLS = 64;
 template <typename T> struct Mat;
 template <> struct Mat<bf16_t> {
   static constexpr int KB = 32, PAD = 8;               // contraction of one instruction; LDS elements behind a row
-  static constexpr int SCORE_PARTS = 2, STATE_PARTS = 2, VALUE_PARTS = 3;
+  static constexpr int PARTS = 3;                      // numbers that a float32 one enters a product as
   typedef bf16x8 frag;
   static constexpr int N = 8;                          // elements of a lane's fragment
   static __device__ inline void mma(f32x4& acc, const frag& a, const frag& b) { acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0); }
@@ -214,8 +215,8 @@ template <> struct Mat<bf16_t> {
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
   static __device__ inline float at(const frag& f, int j) { return (float)f[j]; }
-  // x as PARTS fragments whose sum it is (to 8 bits more with each).
-  template <int PARTS> static __device__ inline void split(const float (&x)[8], frag (&f)[PARTS]) {
+  // x as fragments whose sum it is (8 bits more with each).
+  static __device__ inline void split(const float (&x)[8], frag (&f)[PARTS]) {
     float r[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) r[j] = x[j];
@@ -231,11 +232,12 @@ template <> struct Mat<bf16_t> {
       f[k] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
     }
   }
-  // Four scores to each of the parts' arrays.
-  static __device__ inline void put(bf16_t* p, int part_size, const f32x4& x) {
+  // Scores of row lane % 16, columns 4 (lane / 16) .. of tile `si`, to each of the parts' arrays of its block.
+  static __device__ inline void put(bf16_t* block, int part_size, int si, int i, int q, const f32x4& x) {
+    bf16_t* p = block + ((2 * (si & 1) + (q >> 1)) * 16 + i) * N + 4 * (q & 1);
     float r[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-    for (int k = 0; k < SCORE_PARTS; ++k) {
+    for (int k = 0; k < PARTS; ++k) {
       const u32x2 w = {pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
       *reinterpret_cast<u32x2*>(p + k * part_size) = w;
 #pragma unroll
@@ -251,7 +253,7 @@ template <> struct Mat<bf16_t> {
 };
 template <> struct Mat<float> {
   static constexpr int KB = 16, PAD = 4;
-  static constexpr int SCORE_PARTS = 1, STATE_PARTS = 1, VALUE_PARTS = 1;
+  static constexpr int PARTS = 1;
   typedef f32x4 frag;
   static constexpr int N = 4;
   static __device__ inline void mma(f32x4& acc, const frag& a, const frag& b) {   // four instructions of four elements
@@ -267,14 +269,23 @@ template <> struct Mat<float> {
     return f32x4{q[0], q[pitch], q[2 * pitch], q[3 * pitch]};
   }
   static __device__ inline float at(const frag& f, int j) { return f[j]; }
-  template <int PARTS> static __device__ inline void split(const float (&x)[4], frag (&f)[PARTS]) { f[0] = f32x4{x[0], x[1], x[2], x[3]}; }
-  static __device__ inline void put(float* p, int, const f32x4& x) { *reinterpret_cast<f32x4*>(p) = x; }
+  static __device__ inline void split(const float (&x)[4], frag (&f)[PARTS]) { f[0] = f32x4{x[0], x[1], x[2], x[3]}; }
+  static __device__ inline void put(float* block, int, int, int i, int q, const f32x4& x) { *reinterpret_cast<f32x4*>(block + (q * 16 + i) * N) = x; }
   static __device__ inline uint32_t most(uint32_t m, uint32_t w) {
     w &= 0x7FFFFFFFu;
     return w > m ? w : m;
   }
   static __device__ inline bool finite(uint32_t m) { return m < 0x7F800000u; }
 };
+
+// The scores in LDS: blocks of 16 rows and one instruction's contraction of columns, those that have an element on or below the
+// diagonal, row by row. Within a block a lane's fragment follows the one of the lane in front, so no bank is asked twice. (In
+// bfloat16 as many bytes with three parts as whole rows, padded, took with two: 18 KB at 64 places.)
+template <typename T> __device__ constexpr int score_block(int ti, int kk) {
+  constexpr int PER = Mat<T>::KB / 16;                 // tiles of a block
+  const int u = ti / PER;
+  return PER * u * (u + 1) / 2 + (ti - PER * u) * (u + 1) + kk;
+}
 
 // The same number, of which the compiler does not know that it stays from chunk to chunk: else it keeps everything that
 // follows from it in registers throughout (the chunks' kernel without: 162 registers instead of 134, at 128 columns 251 instead of 213).
@@ -455,11 +466,11 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
   using M = Mat<T>;
   typedef typename M::frag frag;
   constexpr int W = KP <= 32 ? 32 : KP <= 64 ? 64 : KP <= 128 ? 128 : 256;   // columns of a and b in LDS
-  constexpr int TILES = KP / 16, ROWS = CL / 16, PA = W + M::PAD, PC = CHUNK_COLS + M::PAD, PS = CL + M::PAD, SCORES = CL * PS;
+  constexpr int TILES = KP / 16, ROWS = CL / 16, PA = W + M::PAD, PC = CHUNK_COLS + M::PAD, BLOCK = 16 * M::KB, SCORES = score_block<T>(ROWS, 0) * BLOCK;
   constexpr int LOWER = ROWS * (ROWS + 1) / 2;         // tiles of scores on and below the diagonal
   __shared__ __align__(16) T lds_a[STATE ? 1 : CL * PA];
   __shared__ __align__(16) T lds_b[CL * PA];
-  __shared__ __align__(16) T lds_c[STATE || M::SCORE_PARTS * SCORES < CL * PC ? CL * PC : M::SCORE_PARTS * SCORES];
+  __shared__ __align__(16) T lds_c[STATE || M::PARTS * SCORES < CL * PC ? CL * PC : M::PARTS * SCORES];
   T* const lds_p = lds_c;
   __shared__ int odd[2];
   __shared__ __align__(16) float fade[CL], enter[CL];    // of a place's c in the state behind the chunk, of the state in front in a place's o
@@ -563,7 +574,7 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
           const int ti = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, si = tile - ti * (ti + 1) / 2;
           if (M::KB == 32 && tile >= LOWER && tile < LOWER + ROWS / 2) {   // above it, but in one instruction with the tile on it
             const int u = 2 * (tile - LOWER);
-            M::put(lds_p + (16 * u + i) * PS + 16 * (u + 1) + 4 * q, SCORES, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+            M::put(lds_p + score_block<T>(u, u / 2) * BLOCK, SCORES, u + 1, i, q, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
           }
           if (tile < LOWER && 16 * ti < cnt) {
             f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -584,7 +595,7 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
 #pragma unroll
               for (int e = 0; e < 4; ++e) acc[e] = s + e >= from ? acc[e] : 0.0f;
             }
-            M::put(lds_p + t * PS + s, SCORES, acc);
+            M::put(lds_p + score_block<T>(ti, si / (M::KB / 16)) * BLOCK, SCORES, si, i, q, acc);
           }
         }
       }
@@ -601,13 +612,13 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
             float x[M::N];
 #pragma unroll
             for (int e = 0; e < M::N; ++e) x[e] = S[kk * (M::KB / 16) + e / 4][e % 4];
-            frag f[M::STATE_PARTS];
-            M::template split<M::STATE_PARTS>(x, f);
+            frag f[M::PARTS];
+            M::split(x, f);
 #pragma unroll
             for (int ti = 0; ti < ROWS; ++ti) {
               const frag a = M::row_state(lds_a, PA, 16 * ti, M::KB * kk, i, q);
 #pragma unroll
-              for (int k = M::STATE_PARTS - 1; k >= 0; --k) M::mma(o[ti], f[k], a);
+              for (int k = M::PARTS - 1; k >= 0; --k) M::mma(o[ti], f[k], a);
             }
           }
         }
@@ -627,7 +638,8 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
           for (int kk = 0; kk < CL / M::KB; ++kk)
             if (M::KB * kk <= 16 * ti) {
 #pragma unroll
-              for (int k = M::SCORE_PARTS - 1; k >= 0; --k) M::mma(o[ti], v[kk], M::row(lds_p + k * SCORES, PS, 16 * ti, M::KB * kk, i, q));
+              for (int k = M::PARTS - 1; k >= 0; --k)
+                M::mma(o[ti], v[kk], *reinterpret_cast<const frag*>(lds_p + k * SCORES + score_block<T>(ti, kk) * BLOCK + M::N * lane));
             }
           if (t < cnt && wide > 0) {
             const int up = back ? 15 - i : i;
@@ -671,13 +683,13 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[e + j] = M::at(v[kk], e + j) * w[j];
           }
-          frag f[M::VALUE_PARTS];
-          M::template split<M::VALUE_PARTS>(x, f);
+          frag f[M::PARTS];
+          M::split(x, f);
 #pragma unroll
           for (int k = 0; k < TILES; ++k) {
             const frag a = M::col(lds_b, PA, M::KB * kk, 16 * k, i, q);
 #pragma unroll
-            for (int e = M::VALUE_PARTS - 1; e >= 0; --e) M::mma(S[k], a, f[e]);
+            for (int e = M::PARTS - 1; e >= 0; --e) M::mma(S[k], a, f[e]);
           }
         }
       }

@@ -1,0 +1,96 @@
+"""All 24 bits of linear attention's states and scores count in bfloat16 calls: sums whose terms cancel, which are exact in float32.
+
+Every value is a multiple of 2^-23 and every partial sum below 2 in magnitude, whatever the order, so that float32 holds each
+of them, and a result has at most eight bits, so that bfloat16 does: what comes out is exactly the sum.
+"""
+import numpy as np
+import pytest
+
+from . import more_ops_reference as ref
+from .helpers import log
+from .test_gpu_ops import check, gpu, host, torch_
+
+pytestmark = pytest.mark.gpu
+
+# What an output is made of: the operand it is read with, those that made the state, the state in front, whether that one is transposed and
+# time runs backward.
+ROLES = {"y": ("q", "k", "v", "state", False, False), "dq": ("dy", "v", "k", "state", True, False),
+         "dk": ("v", "dy", "q", "dlast", True, True), "dv": ("k", "q", "dy", "dlast", False, True)}
+
+
+def run(name, parts, init, T):
+    """One output from its role's operands [places, width] and state, the same in two sequences and heads; equal to the sum."""
+    from paper_2312_06126_amd import ops
+    a, b, c, first, swap, back = ROLES[name]
+    B, H = 2, 2
+    x = {n: np.tile((p[::-1] if back else p)[None, :, None], (B, 1, H, 1)) for n, p in zip((a, b, c), parts)}
+    for n, like in (("q", "k"), ("k", "q"), ("v", "dy"), ("dy", "v")):
+        if n not in x:
+            x[n] = np.zeros_like(x[like])
+    s = np.tile((init.T if swap else init)[None, None], (B, H, 1, 1))
+    t = {n: gpu(p, "bf16") for n, p in x.items()}
+    kw = {first: gpu(s)}
+    want = ref.attention(x["q"], x["k"], x["v"], None, s if first == "state" else None, 1.0, None, None, x["dy"], s if first == "dlast" else None)[name][0]
+    assert np.array_equal(host(gpu(want, "bf16")), want)
+    if name == "y":
+        got = ops.linear_attention(t["q"], t["k"], t["v"], scale=1.0, **kw)[0]
+    else:
+        got = ops.linear_attention_backward(t["q"], t["k"], t["v"], t["dy"], scale=1.0, **kw)["dq dk dv".split().index(name)]
+    assert want.any() and np.array_equal(host(got), want), np.abs(host(got) - want).max()
+
+
+@pytest.mark.parametrize("name", ROLES)
+@pytest.mark.parametrize("T,width,cols", [(1, 64, 64), (1, 128, 64), (2, 100, 40), (1, 97, 128), (5, 2, 33), (5, 64, 64), (64, 40, 130), (70, 128, 64), (150, 256, 24), (500, 24, 40)])
+def test_bits_of_the_state(T, width, cols, name):
+    """Two rows of a state that is not written to, of opposite signs and all but equal."""
+    log("bits of the state %s %d %d %d" % (name, T, width, cols))
+    rng = np.random.default_rng(T + width)
+    x = rng.integers(1 << 23, (1 << 24) - (1 << 20), cols).astype(float)        # 1 to 1.875
+    init = np.zeros((width, cols))
+    rows = rng.permutation(width)[:2]
+    init[rows[0]], init[rows[1]] = x * 2.0 ** -23, -(x + rng.integers(1, 256, cols)) * 2.0 ** -23
+    a = np.zeros((T, width))
+    a[:, rows] = 1.0
+    run(name, (a, np.zeros((T, width)), np.ones((T, cols))), init, T)
+
+
+@pytest.mark.parametrize("name", ROLES)
+@pytest.mark.parametrize("T,width,cols", [(5, 3, 33), (5, 64, 64), (33, 40, 64), (64, 128, 64), (64, 100, 130), (70, 256, 24), (200, 64, 64), (500, 24, 40)])
+def test_bits_of_the_scores(T, width, cols, name):
+    """Two places whose scores p = a + 2^-9 b + 2^-17 c (a, b and c below 2, in steps of 2^-6) differ in c alone, with values of 1 and -1,
+    seen from the last place."""
+    log("bits of the scores %s %d %d %d" % (name, T, width, cols))
+    rng = np.random.default_rng(T + width)
+    rows = rng.permutation(width)[:3]
+    for _ in range(8):
+        front = (T - 1) // 64 * 64
+        places = front + rng.permutation(T - 1 - front)[:2]
+        a, b, c = np.zeros((T, width)), np.zeros((T, width)), np.zeros((T, cols))
+        a[T - 1, rows] = 1.0, 2.0 ** -9, 2.0 ** -17
+        high = rng.integers(64, 112, 2) / 64.0                                  # p stays below 1.8
+        low = 64 + rng.permutation(64)[:2]
+        for p, l in zip(places, low):
+            b[p, rows] = high[0], high[1], l / 64.0
+        c[places[0]], c[places[1]] = 1.0, -1.0
+        run(name, (a, b, c), np.zeros((width, cols)), T)
+
+
+@pytest.mark.parametrize("K,V", [(128, 128), (100, 40), (97, 64), (64, 128)])
+def test_single_steps_of_wide_heads_in_place(K, V):
+    """40 single steps that update a state in place, as samplers take them, with the bounds of float32 products and states."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    rng = np.random.default_rng(K + V)
+    B, T, H = 16, 40, 2
+    x = {n: rng.standard_normal((B, T, H, w)) for n, w in (("q", K), ("k", K), ("v", V))}
+    t = {n: gpu(v, "bf16") for n, v in x.items()}
+    start, rate = gpu(rng.standard_normal((B, H, K, V))), gpu(np.array([0.7, 0.01]))
+    reset = (rng.random((B, T)) < 0.08).astype(np.uint8)
+    want = ref.attention(host(t["q"]), host(t["k"]), host(t["v"]), host(rate), host(start), K ** -0.5, reset)
+    flags, state, ys = torch.from_numpy(reset).cuda(), start.clone(), []
+    for i in range(T):
+        y, s = ops.linear_attention(*(t[n][:, i:i + 1] for n in ("q", "k", "v")), rate, state, reset=flags[:, i:i + 1], last=state)
+        assert s is state
+        ys.append(y)
+    check("y", torch.cat(ys, 1), want["y"], "bf16")
+    check("last", state, want["last"], "fp32")
