@@ -872,27 +872,38 @@ template <typename T> int64_t lin_time(int ka, int64_t n, int64_t chunks) {
   const int64_t each = op_div_up(n, 256), rounds = op_div_up(each, most);
   return (chunks + 1) * (5 * rounds + (sizeof(T) == 2 ? 1 : 3) * each);
 }
-// How a call is spread, by its sizes alone (microseconds a call, both sides measured, heads of 64 x 64, bfloat16):
-//   steps: a thread keeps its part of the state and walks: up to 2 steps, in float32 4 (2048 x 4 heads: 2 steps 60 against
-//     67 in chunks, 4 steps 81 against 66; in float32 4 steps 90 against 110, 8 steps 143 against 111). In bfloat16 not at 97 to 128
-//     rows (2048 x 4 x 128 x 128, 1 step: 320 against 277, backward 611 against 587 and with a gradient to the last state 1045
-//     against 686; 4096 x 8 x 64 x 128, 2 steps backward: 2636 against 1389). Fewer and more rows gain from steps (1 step, 2048 x 4 x
-//     96 x 96 265 against 350; 512 x 4 x 256 x 256 305 against 412; 4096 x 8 x 64 x 64 backward 423 against 513; with that gradient
-//     2048 x 4 x 48 x 48 104 against 166, but 4096 x 8 x 64 x 64 666 against 582);
-//   chunks: a workgroup walks in chunks on the matrix cores;
+// How a call is spread, by its sizes and whether it has a gradient to the last state (microseconds a call, both sides measured, bfloat16
+// unless said, steps against chunks):
+//   steps: a thread keeps its part of the state and walks: up to 2 steps, in float32 4 (2048 x 4 heads of 64 x 64: 4 steps 81 against 66; in
+//     float32 4 steps 90 against 110, 8 steps 143 against 111);
+//   chunks: a workgroup walks in chunks on the matrix cores; up to 2 steps of bfloat16 too where they are faster, which takes widths that fill
+//     the tiles (others' states are read element by element: 2048 x 4 x 100 x 100, 1 step 286 against 407, backward 505 against 768):
+//     forward heads of 128 rows, which leave a thread of the step kernel twice the registers, and states past the last-level cache
+//       (1 step, 128 x 128: 16 x 4 7.2 against 9.0, 256 x 4 33 against 42, 1024 x 4 132 against 136, 2 steps 160 against 142; 2048 x 4 314
+//       against 272, 2 steps 350 against 275; 128 x 64: 1024 x 4 58 against 67, 4096 x 8 615 against 527);
+//     backward from 1024 heads on, with a gradient to the last state (4096 x 8 x 64 x 64 670 against 586, 2048 x 4 x 128 x 128 1012 against 677,
+//       256 x 4 108 against 88, 16 x 4 8.7 against 10.8), or without it at 128 rows or columns, but for one step of 128 x 128 (2048 x 4, 1 step: 128 x 64 366
+//       against 294, 64 x 128 334 against 313, 128 x 128 596 against 615, 64 x 64 105 against 137; 2 steps 460 against 296, 411 against 313, 730
+//       against 617, 125 against 140);
 //   pieces: time cut into pieces of 64 steps and more whose sums are joined first, two launches and a second reading of keys and
 //     values more, where the model above says that it pays (in pieces against whole, forward: 1 x 1000 x 4 20 against 76, in float32
 //     22 against 114; 1 x 300 x 16 20 against 27; 8 x 1000 x 8 37 against 80; 64 x 1000 x 4 69 against 86). The two launches count
 //     as 12: as 8 the model cuts 32 x 256 x 4 (30 against 24), as 16 it leaves 4 x 200 x 4 in float32 whole (31 against 22).
 struct LinPlan { bool chunks; int64_t pieces, len; };
-template <typename T> int64_t lin_most_steps(int K, int V, bool back) {
-  if (sizeof(T) == 4) return 4;
-  const auto within = [](int rows) { return rows > 96 && rows <= 128; };
-  return within(K) || (back && within(V)) ? 0 : 2;   // forward the state's rows are keys only
+constexpr int64_t LAST_LEVEL = (int64_t)1 << 28;   // bytes of the last-level cache
+template <typename T> bool lin_in_steps(const spz_linear_attention_args& a, bool back, bool dlast) {
+  const int64_t K = a.key_width, V = a.value_width, heads = a.batch * a.heads;
+  if (a.steps == 0 || K == 0 || V == 0) return true;
+  if (a.steps > (sizeof(T) == 4 ? 4 : 2)) return false;
+  if (sizeof(T) == 4) return true;
+  if (!back) return !(K == 128 && V % CHUNK_COLS == 0 && 4 * heads * K * V >= LAST_LEVEL);
+  const auto fills = [](int64_t w) { return w == 64 || w == 128; };
+  return !(fills(K) && fills(V) && heads >= 1024 && (dlast || (K + V > 128 && (a.steps == 2 || K != V))));
 }
-template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bool back) {
+// dlast: whether a backward call has that gradient. A call of steps needs no workspace, one of so few steps in chunks neither.
+template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bool back, bool dlast) {
   const int K = (int)a.key_width, V = (int)a.value_width;
-  if (a.steps <= lin_most_steps<T>(K, V, back) || K == 0 || V == 0) return {false, 1, a.steps};
+  if (lin_in_steps<T>(a, back, dlast)) return {false, 1, a.steps};
   const int64_t k = op_div_up(K, CHUNK_COLS), v = op_div_up(V, CHUNK_COLS), heads = a.batch * a.heads;
   LinPlan best{true, 1, a.steps};
   if (heads == 0 || a.steps <= 128 || heads > 2048) return best;
@@ -912,8 +923,8 @@ template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bo
   }
   return best;
 }
-LinPlan lin_plan(const spz_linear_attention_args& a, bool back) {
-  return a.prec == SPZ_PREC_BF16 ? lin_plan_of<bf16_t>(a, back) : lin_plan_of<float>(a, back);
+LinPlan lin_plan(const spz_linear_attention_args& a, bool back, bool dlast) {
+  return a.prec == SPZ_PREC_BF16 ? lin_plan_of<bf16_t>(a, back, dlast) : lin_plan_of<float>(a, back, dlast);
 }
 // Floats of one state of all pieces, and of what they keep, each at 16 bytes.
 int64_t lin_states(const spz_linear_attention_args& a, const LinPlan& p) {
@@ -1038,7 +1049,7 @@ int lin_run(const char* call, const spz_linear_attention_args* args, bool back, 
   }
   if (g.roles == 0 || a.batch == 0 || a.heads == 0) return SPZ_OK;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const LinPlan plan = lin_plan(a, back);
+  const LinPlan plan = lin_plan(a, back, back && a.dlast);
   if (a.prec == SPZ_PREC_BF16) lin_launch<bf16_t>(g, plan, a, back, ws, s);
   else lin_launch<float>(g, plan, a, back, ws, s);
   return op_launched(call);
@@ -1054,7 +1065,7 @@ extern "C" {
 int64_t spz_linear_attention_workspace(const spz_linear_attention_args* args, int32_t backward) {
   const char* bad = lin_check(args);
   if (bad) return op_error(SPZ_EINVAL, "spz_linear_attention_workspace", bad);
-  const LinPlan plan = lin_plan(*args, backward != 0);
+  const LinPlan plan = lin_plan(*args, backward != 0, false);
   return plan.pieces > 1 ? 4 * (backward ? 2 : 1) * (lin_states(*args, plan) + lin_keeps(*args, plan)) : 0;
 }
 

@@ -94,3 +94,57 @@ def test_single_steps_of_wide_heads_in_place(K, V):
         ys.append(y)
     check("y", torch.cat(ys, 1), want["y"], "bf16")
     check("last", state, want["last"], "fp32")
+
+
+def parts_of(t, b, h):
+    """One head of one sequence, as float64."""
+    return {n: host(v[b:b + 1, h:h + 1] if n in ("state", "dlast") else v[b:b + 1, :, h:h + 1]) for n, v in t.items()}
+
+
+def test_single_steps_of_many_wide_heads_in_place():
+    """As many states as the last-level cache holds bytes, which single steps take in another way."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    B, T, H, K, V = 1024, 40, 4, 128, 128
+    g = torch.Generator(device="cuda").manual_seed(3)
+    t = {n: torch.randn((B, T, H, w), generator=g, device="cuda").bfloat16() for n, w in (("q", K), ("k", K), ("v", V))}
+    t["state"] = torch.randn((B, H, K, V), generator=g, device="cuda")
+    rate = torch.tensor([0.7, 0.1, 0.01, 0.0], device="cuda")
+    reset = (torch.rand((B, T), generator=g, device="cuda") < 0.08).to(torch.uint8)
+    state, ys = t["state"].clone(), []
+    for i in range(T):
+        ys.append(ops.linear_attention(*(t[n][:, i:i + 1] for n in ("q", "k", "v")), rate, state, reset=reset[:, i:i + 1], last=state)[0])
+    y = torch.cat(ys, 1)
+    for b, h in ((0, 0), (B - 1, H - 1), (500, 1), (501, 2)):
+        x = parts_of(t, b, h)
+        want = ref.attention(x["q"], x["k"], x["v"], host(rate[h:h + 1]), x["state"], K ** -0.5, reset[b:b + 1].cpu().numpy())
+        check("y", y[b:b + 1, :, h:h + 1], want["y"], "bf16")
+        check("last", state[b:b + 1, h:h + 1], want["last"], "fp32")
+
+
+@pytest.mark.parametrize("T", [1, 2])
+@pytest.mark.parametrize("K,V", [(64, 64), (64, 128), (128, 64), (128, 128), (100, 128)])
+def test_few_steps_of_many_heads(T, K, V):
+    """Backward calls with and without a gradient to the last state, in empty sequences and behind episode starts too."""
+    from paper_2312_06126_amd import ops
+    torch = torch_()
+    B, H = 513, 2
+    log("few steps of many heads %d %d %d" % (T, K, V))
+    g = torch.Generator(device="cuda").manual_seed(T + K + V)
+    t = {n: torch.randn((B, T, H, w), generator=g, device="cuda").bfloat16() for n, w in (("q", K), ("k", K), ("v", V), ("dy", V))}
+    for n in ("state", "dlast"):
+        t[n] = torch.randn((B, H, K, V), generator=g, device="cuda")
+    rate = torch.tensor([0.7, 0.01], device="cuda")
+    reset = (torch.rand((B, T), generator=g, device="cuda") < 0.3).to(torch.uint8)
+    lengths = torch.randint(0, T + 1, (B,), generator=g, device="cuda").int()
+    for dlast in (t["dlast"], None):
+        a = dict(rate=rate, state=t["state"], reset=reset, lengths=lengths)
+        y, last = ops.linear_attention(t["q"], t["k"], t["v"], **a)
+        got = dict(zip(("dq", "dk", "dv", "dstate"), ops.linear_attention_backward(t["q"], t["k"], t["v"], t["dy"], dlast=dlast, **a)), y=y, last=last)
+        for b, h in [(int(b), i % 2) for i, b in enumerate(torch.linspace(0, B - 1, 12))]:
+            x = parts_of(t, b, h)
+            want = ref.attention(x["q"], x["k"], x["v"], host(rate[h:h + 1]), x["state"], K ** -0.5, reset[b:b + 1].cpu().numpy(), lengths[b:b + 1].cpu().numpy(),
+                                 x["dy"], None if dlast is None else x["dlast"])
+            for n, v in got.items():
+                state = n in ("last", "dstate")
+                check(n, v[b:b + 1, h:h + 1] if state else v[b:b + 1, :, h:h + 1], want[n], "fp32" if state else "bf16")
