@@ -744,6 +744,7 @@ class AdamW:
         self.m, self.v = (torch.zeros(at, dtype=kind, device=dev) for _ in range(2))
         self.m_scale, self.v_scale = (torch.zeros(at // ADAMW_BLOCK, device=dev) if bits == 8 else None for _ in range(2))
         self._moments = at
+        self._written = (*params, *(c for c in copies if c is not None))
         self._layout = [(p, c, p.shape, p.numel(), p.data_ptr(), _ptr(c)) for p, c in zip(params, copies)]
         # One row of 64-bit words for each tensor, as the library reads them (spz_adamw_tensor).
         self._plan = np.frombuffer(b"".join(pack_adamw_tensor(p.data_ptr(), 0, _ptr(c), p.numel(), at, d)
@@ -827,4 +828,6 @@ class AdamW:
             rc = lib.spz_adamw(a, s)
             if rc:
                 _done(rc)
-        torch.autograd.graph.increment_version(self.params if plain else [p for p, g in zip(self.params, grads) if g is not None])
+        # What autograd has saved of a tensor that is written here is not what it was.
+        torch.autograd.graph.increment_version(self._written if plain else [t for p, c, g in zip(self.params, self.copies, grads) if g is not None
+                                                                            for t in (p, c) if t is not None])
