@@ -522,7 +522,8 @@ int spz_quant_linear(int32_t prec, int64_t rows, int64_t outer, int64_t inner, c
  * (off by 2^-52 of the angle, 1e-6 at 2^31 and a frequency of 1). heads_k may be 0 (no
  * keys: any heads' norms). Rows r with valid[r] == 0 are not read: their outputs are zero
  * and they give no gradient. q_out may be q and k_out may be k (with the same strides), as
- * dq may be dq_out and dk dk_out.
+ * dq may be q or dq_out and dk k or dk_out. Beyond that an output shares no element with another
+ * output or an operand (refused where addresses and strides show it).
  *
  * Backward, from dq_out and dk_out (NULL: zeros): dq, dk (NULL: not wanted) and the sums over
  * rows and heads dw_q, db_q, dw_k, db_k (float32 [dim], written; NULL: not wanted). */
@@ -561,7 +562,9 @@ int spz_head_norm_backward(const spz_head_norm_args* args, void* workspace, int6
  * lengths[b] steps (clamped to [0, steps]): behind them nothing is read, y is 0 and the state
  * stays, so last = S of the last step (`state` of an empty sequence). The states are float32
  * throughout, in the products too. steps = 1 is the samplers' form; last may be state (updated in place).
- * Queries, keys or values may be shared by heads (stride 0).
+ * Queries, keys or values may be shared by heads (stride 0). y may be v (with the same strides).
+ * Beyond that an output shares no element with another output or an operand, dstate none with dlast
+ * or state (refused where addresses and strides show it).
  *
  * Backward, from dy and dlast (the gradient to last): with C = dlast behind the last step,
  *     G_t = C + scale query_t^T dy_t,  dquery_t = scale dy_t S_t^T,

@@ -113,6 +113,13 @@ int spzt_row_range(int32_t td3, int32_t bf16, int32_t sequential, int32_t n_stre
  * Runs on the host alone.
  */
 int spzt_scan_way(const spz_scan_args* args, int32_t backward);
+/*
+ * Whether the operators hold two arrays to share an element: addresses, widths, [3] extents and strides
+ * of each, in elements of `size` bytes. At least one is an output, whose elements do not overlap. 1: they do; 0: they do not, or
+ * their strides do not tell. Runs on the host alone.
+ */
+int spzt_shares(int32_t size, const void* x, int64_t x_width, const int64_t* x_n, const int64_t* x_s, const void* y, int64_t y_width,
+                const int64_t* y_n, const int64_t* y_s);
 
 #ifdef __cplusplus
 }

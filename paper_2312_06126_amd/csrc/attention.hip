@@ -827,6 +827,31 @@ const char* lin_check_arrays(const spz_linear_attention_args& a, bool back) {
   return nullptr;
 }
 
+// Arrays that workgroups of one launch read and write in any order. (y in the place of v is sound: a workgroup has read the columns of a
+// step before it writes them, and no other one reads them.)
+const char* lin_check_shares(const spz_linear_attention_args& a, bool back) {
+  const int64_t K = a.key_width, V = a.value_width;
+  const int e = op_size(a.prec);
+  const auto rows = [&](const void* p, int64_t w, int64_t s0, int64_t s1, int64_t s2) { return OpArray{p, w, {a.batch, a.steps, a.heads}, {s0, s1, s2}}; };
+  const auto states = [&](const float* x, const float* y) {
+    return op_shares(4, OpArray{x, K * V, {a.batch, a.heads, 1}, {a.heads * K * V, K * V, 0}}, OpArray{y, K * V, {a.batch, a.heads, 1}, {a.heads * K * V, K * V, 0}});
+  };
+  const OpArray q = rows(a.q, K, a.q_batch, a.q_step, a.q_head), k = rows(a.k, K, a.k_batch, a.k_step, a.k_head), v = rows(a.v, V, a.v_batch, a.v_step, a.v_head);
+  if (!back) {
+    const OpArray y = rows(a.y, V, a.y_batch, a.y_step, a.y_head);
+    if (op_shares(e, y, q) || op_shares(e, y, k) || (!op_same(y, v) && op_shares(e, y, v))) return "y shares elements with q, k or other places of v";
+    return a.last != a.state && states(a.last, a.state) ? "last shares elements with other places of state" : nullptr;
+  }
+  const OpArray dy = rows(a.dy, V, a.dy_batch, a.dy_step, a.dy_head);
+  const OpArray outs[3] = {rows(a.dq, K, a.dq_batch, a.dq_step, a.dq_head), rows(a.dk, K, a.dk_batch, a.dk_step, a.dk_head), rows(a.dv, V, a.dv_batch, a.dv_step, a.dv_head)};
+  for (int i = 0; i < 3; ++i) {
+    if (op_shares(e, outs[i], outs[(i + 1) % 3])) return "dq, dk and dv share elements";
+    for (const OpArray* x : {&q, &k, &v, &dy})
+      if (op_shares(e, outs[i], *x)) return "dq, dk or dv shares elements with q, k, v or dy";
+  }
+  return states(a.dstate, a.dlast) || states(a.dstate, a.state) ? "dstate shares elements with dlast or state" : nullptr;
+}
+
 template <typename T> void lin_steps_launch(LinArgs g, hipStream_t s) {
   StepArgs f{};
   int64_t slices = 1;
@@ -1020,6 +1045,8 @@ int lin_run(const char* call, const spz_linear_attention_args* args, bool back, 
   const int64_t need = spz_linear_attention_workspace(args, back);
   if (need > 0 && (!ws || ws_bytes < need)) return op_error(SPZ_ESIZE, call, "workspace too small");
   if (need > 0 && !op_aligned(ws, 16)) return op_error(SPZ_EINVAL, call, "workspace not aligned to 16 bytes");
+  bad = lin_check_shares(a, back);
+  if (bad) return op_error(SPZ_EINVAL, call, bad);
   LinArgs g{};
   g.batch = a.batch;
   g.steps = a.steps;

@@ -504,6 +504,23 @@ const char* head_check_arrays(const spz_head_norm_args& a, bool back) {
   return nullptr;
 }
 
+// Arrays that workgroups of one launch read and write in any order. A head is read before it is written, so an output may take the
+// place of its own part's input.
+const char* head_check_shares(const spz_head_norm_args& a, bool back) {
+  const int e = op_size(a.prec);
+  const auto part = [&](const void* p, int64_t heads, int64_t row, int64_t head) { return OpArray{p, a.dim, {a.rows, heads, 1}, {row, head, 0}}; };
+  const OpArray q = part(a.q, a.heads_q, a.q_row, a.q_head), k = part(a.k, a.heads_k, a.k_row, a.k_head);
+  const OpArray dy = part(back ? a.dq_out : nullptr, a.heads_q, a.dq_out_row, a.dq_out_head), dz = part(back ? a.dk_out : nullptr, a.heads_k, a.dk_out_row, a.dk_out_head);
+  const OpArray to_q = back ? part(a.dq, a.heads_q, a.dq_row, a.dq_head) : part(a.q_out, a.heads_q, a.q_out_row, a.q_out_head);
+  const OpArray to_k = back ? part(a.dk, a.heads_k, a.dk_row, a.dk_head) : part(a.k_out, a.heads_k, a.k_out_row, a.k_out_head);
+  if (op_shares(e, to_q, to_k)) return back ? "dq and dk share elements" : "q_out and k_out share elements";
+  for (const OpArray* x : {&q, &dy})
+    if ((!op_same(to_q, *x) && op_shares(e, to_q, *x)) || op_shares(e, to_k, *x)) return "an output shares elements with other places of q or dq_out";
+  for (const OpArray* x : {&k, &dz})
+    if ((!op_same(to_k, *x) && op_shares(e, to_k, *x)) || op_shares(e, to_q, *x)) return "an output shares elements with other places of k or dk_out";
+  return nullptr;
+}
+
 void head_parts(const spz_head_norm_args& a, bool back, HeadArgs& g) {
   g.rows = a.rows;
   g.part[0] = {a.q, a.q_row, a.q_head, a.w_q, a.b_q, a.dq_out, a.dq_out_row, a.dq_out_head,
@@ -551,6 +568,11 @@ int head_run(const char* call, const spz_head_norm_args* args, bool back, void* 
   if (!bad) bad = head_check_arrays(*args, back);
   if (bad) return op_error(SPZ_EINVAL, call, bad);
   const spz_head_norm_args& a = *args;
+  const int64_t need = back ? spz_head_norm_workspace(args) : 0;
+  if (need > 0 && (!ws || ws_bytes < need)) return op_error(SPZ_ESIZE, call, "workspace too small");
+  if (need > 0 && !op_aligned(ws, 16)) return op_error(SPZ_EINVAL, call, "workspace not aligned to 16 bytes");
+  bad = head_check_shares(a, back);
+  if (bad) return op_error(SPZ_EINVAL, call, bad);
   HeadArgs g{};
   head_parts(a, back, g);
   g.positions = a.positions;
@@ -564,9 +586,6 @@ int head_run(const char* call, const spz_head_norm_args* args, bool back, void* 
   g.eps = a.eps;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (back) {
-    const int64_t need = spz_head_norm_workspace(args);
-    if (need > 0 && (!ws || ws_bytes < need)) return op_error(SPZ_ESIZE, call, "workspace too small");
-    if (need > 0 && !op_aligned(ws, 16)) return op_error(SPZ_EINVAL, call, "workspace not aligned to 16 bytes");
     g.sums = static_cast<float*>(ws);
     for (HeadPart& p : g.part)
       if (!p.dy && p.heads > 0 && a.rows > 0) {   // no gradient comes in: zeros, and nothing for the kernel to do

@@ -32,6 +32,68 @@ inline bool op_out_strides_ok(int64_t n0, int64_t n1, int64_t width, int64_t s0,
   return s0 >= s1 ? (s0 - width) / s1 >= n1 - 1 : (s1 - width) / s0 >= n0 - 1;
 }
 
+// An array [n0, n1, n2, width] of elements of `size` bytes at strides s.
+struct OpArray { const void* p; int64_t width, n[3], s[3]; };
+inline bool op_dense(const OpArray& a) {   // every element of its span is its own
+  __int128 span = a.width;
+  bool done[3] = {a.n[0] == 1, a.n[1] == 1, a.n[2] == 1};
+  for (int k = 0; k < 3; ++k)
+    for (int i = 0; i < 3; ++i)
+      if (!done[i] && a.s[i] == span) {
+        span *= a.n[i];
+        done[i] = true;
+      }
+  return done[0] && done[1] && done[2];
+}
+// Whether two such arrays certainly share an element, one of them an output, whose elements do not overlap: they start at the same one,
+// or they are dense and their spans meet, or their strides are the same, so that places differ by a multiple of each stride and,
+// within the smallest one, by less than a row. (Arrays of other strides may share elements all the same.)
+inline bool op_shares(int size, const OpArray& x, const OpArray& y) {
+  if (!x.p || !y.p || x.width <= 0 || y.width <= 0) return false;
+  __int128 x_end = x.width, y_end = y.width;
+  for (int i = 0; i < 3; ++i) {
+    if (x.n[i] <= 0 || y.n[i] <= 0) return false;
+    if (x.n[i] > 1) x_end += (__int128)(x.n[i] - 1) * x.s[i];
+    if (y.n[i] > 1) y_end += (__int128)(y.n[i] - 1) * y.s[i];
+  }
+  if (x.p == y.p) return true;
+  const __int128 ahead = ((__int128)reinterpret_cast<uintptr_t>(y.p) - (__int128)reinterpret_cast<uintptr_t>(x.p)) / size;
+  if (ahead >= x_end || -ahead >= y_end) return false;
+  int dims = 0, d[3];                      // dimensions of more than one element, in falling order of their strides
+  __int128 step[3];
+  for (int i = 0; i < 3; ++i) {
+    if (x.n[i] == 1 && y.n[i] == 1) continue;
+    if (x.n[i] > 1 && y.n[i] > 1 && x.s[i] != y.s[i]) return op_dense(x) && op_dense(y);
+    const int64_t s = x.n[i] > 1 ? x.s[i] : y.s[i];
+    if (s == 0) return false;              // neither is an output
+    int j = dims++;
+    for (; j > 0 && step[j - 1] < s; --j) {
+      step[j] = step[j - 1];
+      d[j] = d[j - 1];
+    }
+    step[j] = s;
+    d[j] = i;
+  }
+  // How far y is ahead, less a multiple of each stride in turn: the one below it or the one above.
+  for (int pick = 0; pick < 1 << dims; ++pick) {
+    __int128 rest = ahead;
+    bool in = true;
+    for (int i = 0; i < dims && in; ++i) {
+      const __int128 m = rest / step[i] - (rest % step[i] < 0) + (pick >> i & 1);
+      in = m < x.n[d[i]] && -m < y.n[d[i]];
+      rest -= m * step[i];
+    }
+    if (in && rest < x.width && -rest < y.width) return true;
+  }
+  return false;
+}
+// Whether two arrays of one shape are the same one.
+inline bool op_same(const OpArray& x, const OpArray& y) {
+  bool same = x.p == y.p;
+  for (int i = 0; i < 3; ++i) same = same && (x.n[i] <= 1 || x.s[i] == y.s[i]);
+  return same;
+}
+
 inline int64_t op_div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // launch(first, grid) over `blocks` workgroups of `threads`, as many dispatches as it takes. A dispatch counts its

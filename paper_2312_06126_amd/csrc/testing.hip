@@ -1,5 +1,6 @@
 // Test hooks (include/spz_testing.h): the GEMM kernels on caller-owned device memory.
 #include "../../include/spz_testing.h"
+#include "ops.h"
 #include "rows.h"
 
 using namespace spz;
@@ -202,4 +203,10 @@ extern "C" int spzt_row_wgrad(int32_t bf16, int32_t split, int32_t rows, int32_t
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e == hipErrorInvalidValue) return SPZ_EINVAL;
   return e == hipSuccess ? SPZ_OK : SPZ_EHIP;
+}
+
+extern "C" int spzt_shares(int32_t size, const void* x, int64_t x_width, const int64_t* x_n, const int64_t* x_s, const void* y, int64_t y_width,
+                           const int64_t* y_n, const int64_t* y_s) {
+  return op_shares(size, OpArray{x, x_width, {x_n[0], x_n[1], x_n[2]}, {x_s[0], x_s[1], x_s[2]}},
+                   OpArray{y, y_width, {y_n[0], y_n[1], y_n[2]}, {y_s[0], y_s[1], y_s[2]}});
 }

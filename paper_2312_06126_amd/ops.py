@@ -521,7 +521,7 @@ def head_norm(q, k=None, w_q=None, w_k=None, b_q=None, b_k=None, *, norm="rms", 
 
     norm "none", "rms", "layer"; pairs "halves" (columns i and len(freqs) + i) or "neighbours" (2 i and 2 i + 1).
     positions int32 [rows] and freqs float64 (rotation_freqs makes some) come together. Rows with valid == 0 are
-    not read, their outputs are zero. `out`: (q', k'); they may be q and k."""
+    not read, their outputs are zero. `out`: (q', k'); they may be q and k and otherwise share no elements with them or each other."""
     lib = load()
     vectors = (w_q, b_q, w_k, b_k)
     gpu = _head_check(q, k, vectors, norm, positions, freqs, pairs, valid)
@@ -543,7 +543,8 @@ def head_norm(q, k=None, w_q=None, w_k=None, b_q=None, b_k=None, *, norm="rms", 
 def head_norm_backward(dq_out, dk_out, q, k=None, w_q=None, w_k=None, b_q=None, b_k=None, *, norm="rms", eps=1e-6, positions=None,
                        freqs=None, pairs="halves", valid=None, out=None, stream=None):
     """Gradients of head_norm from those of q' and k' (None: zeros): a dict of dq, dk and, for the vectors that were
-    given, dw_q, db_q, dw_k, db_k (float32, summed over rows and heads). `out`: (dq, dk), e.g. two parts of one."""
+    given, dw_q, db_q, dw_k, db_k (float32, summed over rows and heads). `out`: (dq, dk), e.g. two parts of one; dq may be dq_out or q and dk dk_out or k, and
+    otherwise they share no elements with these or each other."""
     lib = load()
     vectors = (w_q, b_q, w_k, b_k)
     gpu = _head_check(q, k, vectors, norm, positions, freqs, pairs, valid)
@@ -625,7 +626,8 @@ def linear_attention(q, k, v, rate=None, state=None, *, scale=None, reset=None, 
     rate: float32 [heads] (default zeros). state, last: float32 [batch, heads, width, other width], S in front
     (default zeros) and behind; pass last=state to update a state in place. scale: default 1 / sqrt(width). reset
     [batch, steps] (uint8 or bool): steps that start an episode, cut off from the state before. lengths [batch]
-    (int32): steps of each sequence; y is 0 behind it. Heads may share q, k or v (stride 0). `out`: y."""
+    (int32): steps of each sequence; y is 0 behind it. Heads may share q, k or v (stride 0). `out`: y; it may be v and
+    otherwise shares no elements with the operands."""
     lib = load()
     gpu = _attention_check(q, k, v, rate, state, reset, lengths)
     B, T, H, K = q.shape
@@ -659,7 +661,7 @@ def linear_attention(q, k, v, rate=None, state=None, *, scale=None, reset=None, 
 def linear_attention_backward(q, k, v, dy, rate=None, state=None, *, scale=None, dlast=None, reset=None, lengths=None, out=None, stream=None):
     """Gradients (dq, dk, dv, dstate) of linear_attention's (y, last) from dy and dlast (None: zeros), with the forward
     call's other arguments (`state` as it was before the call). Those of shared heads are one for each
-    head. `out`: the tensors (dq, dk, dv) to write, e.g. three parts of one."""
+    head. `out`: the tensors (dq, dk, dv) to write, e.g. three parts of one; they share no elements with each other or the operands."""
     lib = load()
     gpu = _attention_check(q, k, v, rate, state, reset, lengths)
     B, T, H, K = q.shape
