@@ -40,7 +40,8 @@ struct LinArgs {
   int64_t batch, steps, heads, first;        // first: sequence that the launch starts with
   int64_t pieces, len;                       // of time, len steps each
   const float* inits[3];                     // states in front of the pieces [batch, heads, pieces, ..], or NULL
-  float *adds[2], *keeps[2];                 // what the pieces add, and keep, of the states of the first two roles
+  float *adds[2], *keeps[2];                 // what the pieces add to the states of the first two roles, and the factor that
+                                             // they keep of them (-1: an episode starts in the piece)
   const float* rate;
   const uint8_t* reset; int64_t reset_batch, reset_step;
   const int32_t* lengths;
@@ -528,7 +529,8 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
     state_load<TILES>(init, S, full, mine, ka, rs, cs, c0 + col, q0);
   }
   if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-  float keep = 1.0f;   // STATE: what is left of the state in front of the piece
+  float keep = 1.0f;   // STATE: what is left of the state in front of the piece, but for
+  bool opens = false;  // an episode's start, behind which nothing is
   // Weights of the scores in a tile on the diagonal and in the one below it.
   float on[4], below[4];
   const float score = r.in * r.out_scale;
@@ -672,7 +674,8 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
 #pragma unroll
           for (int k = 0; k < TILES; ++k) S[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        keep = cuts ? 0.0f : keep * whole;
+        keep *= whole;
+        opens = opens || cuts;
 #pragma unroll
         for (int kk = 0; kk < CL / M::KB; ++kk) {
           if (M::KB * kk >= cnt) continue;
@@ -709,7 +712,8 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
               if constexpr (!STATE) o = fmaf(to_f<T>(lds_a[p * PA + row]), S[k][e], o);
             }
           }
-        keep = cut ? 0.0f : keep * d;
+        keep *= d;
+        opens = opens || cut;
         if constexpr (!STATE) {
           o = add32(add16(o));
           if (q == 0 && mine) reinterpret_cast<T*>(out + (back ? 15 * out_step : 0) + p * out_walk)[col] = from_f<T>(r.out_scale * o);
@@ -723,7 +727,7 @@ template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_
   if constexpr (STATE) {
     const int64_t at = (b * g.heads + h) * g.pieces + piece;
     state_store<TILES>(g.adds[which] + at * size, S, full, mine, ka, r.nc, 1, c0 + col, q0);
-    if (unit == 0 && threadIdx.x == 0) g.keeps[which][at] = keep;
+    if (unit == 0 && threadIdx.x == 0) g.keeps[which][at] = opens ? -1.0f : keep;
   } else {
     // Steps behind the sequence.
     const int64_t end = begin + g.len < g.steps ? begin + g.len : g.steps;
@@ -765,7 +769,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void lin_join(LinArgs g) {
     for (int j = 0; j < JOIN_AHEAD; ++j)
       if (p + j < g.pieces) {
         u[(p + j) * size] = s;
-        s = k[j] == 0.0f ? x[j] : fmaf(k[j], s, x[j]);   // nothing passes an episode's start, finite or not
+        s = k[j] < 0.0f ? x[j] : fmaf(k[j], s, x[j]);   // nothing passes an episode's start, finite or not (a factor of 0 does not stop a NaN)
       }
   }
 }
