@@ -10,7 +10,8 @@ captured into a HIP graph. Errors: SpzError.
 
 torch's autograd does not record the calls: gradients come from scan_backward, block_norm_backward, head_norm_backward,
 linear_attention_backward and, for dropout, the same call on the gradient (quant_linear has none). Tensors that require a gradient are refused, so that none is
-lost; within torch.no_grad() they are taken. The calls work on data pointers: they are not for tracing or vmap.
+lost; within torch.no_grad() they are taken. A tensor that a caller gives to be written counts as changed in place, so that autograd
+refuses what it has saved of it. The calls work on data pointers: they are not for tracing or vmap.
 """
 from __future__ import annotations
 
@@ -126,6 +127,13 @@ def _empty(x: torch.Tensor) -> torch.Tensor:
     return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
 
 
+def _wrote(*given: Optional[torch.Tensor]):
+    """Marks a caller's own tensors as written: what autograd has saved of one is not what it was."""
+    given = [t for t in given if t is not None]
+    if given:
+        torch.autograd.graph.increment_version(given)
+
+
 def _workspace(n: int, ref: torch.Tensor) -> Optional[torch.Tensor]:
     return ref.new_empty((n,), dtype=torch.uint8) if n else None
 
@@ -195,6 +203,7 @@ def scan(f, v, h0=None, *, reset=None, lengths=None, save: bool = False, out=Non
     rc = lib.spz_scan_forward(a, _ptr(ws), n, s)
     if rc:
         _done(rc)
+    _wrote(out, hT)
     return (y, last, saved) if save else (y, last)
 
 
@@ -228,6 +237,7 @@ def scan_backward(f, v, dy, saved, *, dhT=None, reset=None, lengths=None, out=No
                   0, 0, 0, 0, 0, saved.data_ptr(), _ptr(dy), *_outer(dy), _ptr(dhT), df.data_ptr(), dv.data_ptr(),
                   *_outer(df), *_outer(dv), dh0.data_ptr(), prec)
     _done(lib.spz_scan_backward(a, _ptr(ws), n, s))
+    _wrote(*out or ())
     return df, dv, dh0
 
 
@@ -352,6 +362,7 @@ def dropout(x, p: float, seed: int, step: int, tensor: int = 0, *, out=None, str
         _refuse("p, seed, step or tensor is no number: %s" % e)
     if rc:
         _done(rc)
+    _wrote(out)
     return y
 
 
@@ -437,6 +448,7 @@ def quant_linear(x, weights: QuantWeights, *, bias=None, out=None, stream=None):
                               y.data_ptr(), y.stride(0), _ptr(ws), n, s)
     if rc:
         _done(rc)
+    _wrote(out)
     return y
 
 
@@ -537,6 +549,7 @@ def head_norm(q, k=None, w_q=None, w_k=None, b_q=None, b_k=None, *, norm="rms", 
     rc = lib.spz_head_norm_forward(_head_pack(q, k, vectors, positions, freqs, valid, (q_out, k_out), None, None, eps, norm, pairs), s)
     if rc:
         _done(rc)
+    _wrote(*out or ())
     return q_out, k_out
 
 
@@ -571,6 +584,7 @@ def head_norm_backward(dq_out, dk_out, q, k=None, w_q=None, w_k=None, b_q=None, 
     n = _size(lib.spz_head_norm_workspace(a))
     ws = _workspace(n, q)
     _done(lib.spz_head_norm_backward(a, _ptr(ws), n, s))
+    _wrote(*out or ())
     return g
 
 
@@ -655,6 +669,7 @@ def linear_attention(q, k, v, rate=None, state=None, *, scale=None, reset=None, 
     rc = lib.spz_linear_attention_forward(a, _ptr(ws), n, s)
     if rc:
         _done(rc)
+    _wrote(out, last)
     return y, end
 
 
@@ -690,6 +705,7 @@ def linear_attention_backward(q, k, v, dy, rate=None, state=None, *, scale=None,
     except _NOT_NUMBERS as e:
         _refuse("scale is no number: %s" % e)
     _done(lib.spz_linear_attention_backward(a, _ptr(ws), n, s))
+    _wrote(*out or ())
     return dq, dk, dv, dstate
 
 
@@ -830,6 +846,4 @@ class AdamW:
             rc = lib.spz_adamw(a, s)
             if rc:
                 _done(rc)
-        # What autograd has saved of a tensor that is written here is not what it was.
-        torch.autograd.graph.increment_version(self._written if plain else [t for p, c, g in zip(self.params, self.copies, grads) if g is not None
-                                                                            for t in (p, c) if t is not None])
+        _wrote(*self._written if plain else (t for p, c, g in zip(self.params, self.copies, grads) if g is not None for t in (p, c)))
