@@ -566,6 +566,11 @@ int spz_head_norm_backward(const spz_head_norm_args* args, void* workspace, int6
  * Beyond that an output shares no element with another output or an operand, dstate none with dlast
  * or state (refused where addresses and strides show it).
  *
+ * Sequences are worked on in chunks of up to 64 steps: products of queries and keys, and of queries and the
+ * state in front, are taken in float32 before the decay and the values meet them. Where such a product (of
+ * finite numbers) or exp(-64 rate) passes float32's range, results may be infinite or NaN though S itself
+ * is finite, and below the range they are 0; with rates >= 0 and operands and |scale| below 1e6 none passes it.
+ *
  * Backward, from dy and dlast (the gradient to last): with C = dlast behind the last step,
  *     G_t = C + scale query_t^T dy_t,  dquery_t = scale dy_t S_t^T,
  *     dkey_t = value_t G_t^T,  dvalue_t = key_t G_t,  C = d k_t G_t;   dstate = C in front of the first step
@@ -636,7 +641,7 @@ typedef struct spz_adamw_args {
   void *m, *v;                             /* [moments]: float32, or 8-bit codes                 */
   float *m_scale, *v_scale;                /* bits 8: [moments / SPZ_ADAMW_BLOCK]                */
   const float* grad_scale;                 /* device [1], or NULL (1)                            */
-  const int64_t* step_at;                  /* device [1]: t, read when the kernel runs, or NULL  */
+  const int64_t* step_at;                  /* device [1]: t >= 1, read when the kernel runs, or NULL */
   const float* lr_at;                      /* device [1], as step_at, or NULL                    */
   int64_t step;                            /* t >= 1 where step_at is NULL                       */
   double lr, beta1, beta2, eps;            /* lr where lr_at is NULL; betas in [0, 1), eps >= 0  */

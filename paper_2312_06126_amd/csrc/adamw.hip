@@ -100,8 +100,9 @@ __device__ inline float round_random(float x, uint32_t word) {
   return low ? z - 0x1p-6f : z;
 }
 
-// The square root: the hardware's (an ulp) and a step of Newton's method, whose residual is exact, so that the result is the
-// correctly rounded one but for values next to a border; a third of the library's instructions.
+// The square root: the hardware's (an ulp) and a step of Newton's method, whose residual is exact to some 2^-46 of x. It is the correctly
+// rounded one for each of float32's mantissas at an even and at an odd exponent (all 2^24 compared; others differ by powers of
+// 4, which change nothing); a third of the library's instructions.
 __device__ inline float root(float x) {
   if (!(x >= 0x1p-90f && x < 0x1p120f)) return sqrtf(x);
   const float y = __builtin_amdgcn_rsqf(x), s = x * y;
@@ -131,7 +132,8 @@ __device__ inline float block_max(const float (&x)[8]) {
 
 // Bound by HBM: 53 million float32 elements with bfloat16 gradients and copies and 8-bit moments 157 us, 5.4 TB/s; 7.7 million
 // with moments of 32 bits 36 us, 5.9 TB/s of arrays partly in the last-level cache. (Library quotients and roots: 214 us, by
-// their instructions.)
+// their instructions.) With the step on the device each thread takes the corrections itself, in 64 bits: in a replayed graph 176 us and not
+// 162 of the 53 million, 35.8 and not 35.3 of the 7.7 million, 5.7 and not 5.3 of 0.2 million.
 template <typename P, typename G, bool EIGHT>
 __global__ __launch_bounds__(ADAM_THREADS) void adamw_step(AdamArgs g) {
   const int64_t blk = g.from + blockIdx.x;

@@ -289,7 +289,7 @@ template <typename T> __device__ constexpr int score_block(int ti, int kk) {
 }
 
 // The same number, of which the compiler does not know that it stays from chunk to chunk: else it keeps everything that
-// follows from it in registers throughout (the chunks' kernel without: 162 registers instead of 134, at 128 columns 251 instead of 213).
+// follows from it in registers throughout (1 x 65536 x 8 x 64 x 128 bfloat16 without: forward 281 us and not 205, backward 729 and not 514).
 __device__ inline int opaque(int x) {
   asm("" : "+v"(x));
   return x;
@@ -406,8 +406,6 @@ __device__ inline float lin_log2(float rate) {
 }
 __device__ inline float lin_power(float log2d, int n) { return __builtin_amdgcn_exp2f(log2d * (float)n); }
 
-// The workgroups of a launch: the slices of all roles of a piece of a head follow each other on one XCD, whose L2 holds
-// what they share.
 // A lane's part of a state at row and column strides rs and cs: rows 16 k + 4 q .. of column c.
 template <int TILES>
 __device__ inline void state_load(const float* p, f32x4 (&S)[TILES], bool full, bool mine, int ka, int rs, int cs, int c, int q) {
@@ -456,14 +454,17 @@ __device__ inline void state_store(float* p, const f32x4 (&S)[TILES], bool full,
 // 64 x 1000 x 5: 157 us against 178, backward 278 against 316).
 // Workgroups a compute unit is to hold, which bounds their registers (three and not two in float32 up to 64 rows: 256 x 500 x 4 x
 // 64 x 64 backward 453 us against 511).
-template <typename T, int KP, bool STATE, bool ONE> constexpr int chunk_waves = KP > 64 ? 1 : sizeof(T) == 4 ? 3 : 4;
+template <typename T, int KP> constexpr int chunk_waves = KP > 64 ? 1 : sizeof(T) == 4 ? 3 : 4;
 
 // A workgroup: slice of a role, head, sequence, piece of time. STATE: only what the piece adds to the state. ONE: no
 // sequence is longer than a chunk. The scores take the place of c, of which each wave has its columns in registers by then.
-// Bound by vector instructions, some 700 a wave and chunk at 64 rows, most of them the splits into bfloat16 parts (issued in
-// 70% of the busy cycles, the matrix instructions run in 23%): 65536 steps x 8 heads of 64 x 128 bf16 in 64 pieces 142 us,
-// 2.8 TB/s. Short sequences by the states' bytes: 2048 x 4 heads of 64 x 64, 50 steps, ragged, 94 us.
-template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_bounds__(CHUNK_THREADS, (chunk_waves<T, KP, STATE, ONE>)) void lin_chunks(LinArgs g) {
+// The slices of all roles of a piece of a head follow each other on one XCD, whose L2 holds what they share.
+// 65536 steps x 8 heads of 64 x 128 bf16 in 64 pieces take 157 us, 2.6 TB/s: 732 vector instructions a wave and chunk at 64 rows, issued in 59%
+// of the cycles that a compute unit is busy, and 71 matrix instructions, which run in 23%. Of the vector instructions some 270 split
+// scores, states and weighted values into bfloat16 parts; the others are addresses, predicates, trimming, the test for values that
+// are not finite, and scalars (117 do not fit) read back from lanes. The rest of the time waits: three barriers and products that
+// follow from each other a chunk. Short sequences are bound by the states' bytes: 2048 x 4 heads of 64 x 64, 50 steps, ragged, 92 us.
+template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_bounds__(CHUNK_THREADS, (chunk_waves<T, KP>)) void lin_chunks(LinArgs g) {
   using M = Mat<T>;
   typedef typename M::frag frag;
   constexpr int W = KP <= 32 ? 32 : KP <= 64 ? 64 : KP <= 128 ? 128 : 256;   // columns of a and b in LDS
@@ -893,8 +894,8 @@ template <typename T> int lin_rows(int ka) {
   return 256;
 }
 // Microseconds of a launch of n workgroups of `chunks` chunks each: a compute unit holds `most` of them at once, and a
-// workgroup's start counts as a chunk. A chunk takes 5 and 1 more for each workgroup of the unit (64 x 64 heads, 1 to 4 a unit: 5.8,
-// 6.1, 6.9 and 8.4 measured), in float32 5 and 3 (1 to 3 a unit: 8.3, 10.8 and 14.0).
+// workgroup's start counts as a chunk. A chunk takes 5 and 1 more for each workgroup of the unit (64 x 64 heads, 1 to 4 a unit: 5.3,
+// 6.3, 7.5 and 9.2 measured), in float32 5 and 3 (1 to 3 a unit: 7.7, 10.7 and 14.0). Other heads count as these, by their workgroups.
 template <typename T> int64_t lin_time(int ka, int64_t n, int64_t chunks) {
   const int kp = lin_rows<T>(ka);
   const int64_t most = kp > 128 ? 1 : kp > 64 ? (sizeof(T) == 2 ? 2 : 1) : sizeof(T) == 2 ? 4 : 3;
@@ -915,9 +916,9 @@ template <typename T> int64_t lin_time(int ka, int64_t n, int64_t chunks) {
 //       against 294, 64 x 128 334 against 313, 128 x 128 596 against 615, 64 x 64 105 against 137; 2 steps 460 against 296, 411 against 313, 730
 //       against 617, 125 against 140);
 //   pieces: time cut into pieces of 64 steps and more whose sums are joined first, two launches and a second reading of keys and
-//     values more, where the model above says that it pays (in pieces against whole, forward: 1 x 1000 x 4 20 against 76, in float32
-//     22 against 114; 1 x 300 x 16 20 against 27; 8 x 1000 x 8 37 against 80; 64 x 1000 x 4 69 against 86). The two launches count
-//     as 12: as 8 the model cuts 32 x 256 x 4 (30 against 24), as 16 it leaves 4 x 200 x 4 in float32 whole (31 against 22).
+//     values more, where the model above says that it pays (in pieces against whole, forward: 1 x 1000 x 4 18 against 80, in float32
+//     20 against 112; 1 x 300 x 16 18 against 29; 8 x 1000 x 8 39 against 84; 64 x 1000 x 4 70 against 89). The two launches count
+//     as 12: as 8 the model cuts 32 x 256 x 4 (31 against 24), as 16 it leaves 4 x 200 x 4 in float32 whole (30 against 20).
 struct LinPlan { bool chunks; int64_t pieces, len; };
 constexpr int64_t LAST_LEVEL = (int64_t)1 << 28;   // bytes of the last-level cache
 template <typename T> bool lin_in_steps(const spz_linear_attention_args& a, bool back, bool dlast) {
@@ -944,7 +945,7 @@ template <typename T> LinPlan lin_plan_of(const spz_linear_attention_args& a, bo
     const int64_t len = op_div_up(op_div_up(a.steps, pieces), 64) * 64, chunks = len / 64;
     if (pieces > 1 && op_div_up(a.steps, len) != pieces) continue;
     int64_t time = lin_time<T>(K, heads * pieces * by_k, chunks) + (by_v ? lin_time<T>(V, heads * pieces * by_v, chunks) : 0);
-    if (pieces > 1) time += lin_time<T>(K, heads * pieces * sums, chunks) / 2 + 12 + pieces / 8;   // joins by 8 pieces
+    if (pieces > 1) time += lin_time<T>(K, heads * pieces * sums, chunks) / 2 + 12 + pieces / 8;   // the launches and the join, 3, 10 and 15 us for 16, 64 and 128 pieces of 8 heads
     if (pieces == 1 || time < least) {
       least = time;
       best = {true, pieces, pieces > 1 ? len : a.steps};

@@ -641,7 +641,8 @@ def linear_attention(q, k, v, rate=None, state=None, *, scale=None, reset=None, 
     (default zeros) and behind; pass last=state to update a state in place. scale: default 1 / sqrt(width). reset
     [batch, steps] (uint8 or bool): steps that start an episode, cut off from the state before. lengths [batch]
     (int32): steps of each sequence; y is 0 behind it. Heads may share q, k or v (stride 0). `out`: y; it may be v and
-    otherwise shares no elements with the operands."""
+    otherwise shares no elements with the operands. Products of queries with keys and states are taken in float32 before decays
+    and values meet them: include/spz.h says which magnitudes that takes."""
     lib = load()
     gpu = _attention_check(q, k, v, rate, state, reset, lengths)
     B, T, H, K = q.shape
