@@ -183,7 +183,7 @@ template <typename T, int KR> __global__ __launch_bounds__(STEP_THREADS) void li
 // operands of the next product as they stand: the order of the contraction is the same for both operands.
 // bfloat16 operands: the scores, the state and the weighted c enter a product as three bfloat16 numbers each, which hold all
 // 24 bits, so that a state is float32 in a product too. (Scores and states as two, with 16 bits: 1 x 65536 x 8 x 64 x 128 training 689 us
-// and not 752, 2048 x 50 x 4 x 64 x 64 284 and not 293; their errors, 2^-17 of a term, show where terms cancel.)
+// and not 729, 2048 x 50 x 4 x 64 x 64 284 and not 291; their errors, 2^-17 of a term, show where terms cancel.)
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 #define LDS_PTR(T) __attribute__((address_space(3))) T*
@@ -459,11 +459,11 @@ template <typename T, int KP> constexpr int chunk_waves = KP > 64 ? 1 : sizeof(T
 // A workgroup: slice of a role, head, sequence, piece of time. STATE: only what the piece adds to the state. ONE: no
 // sequence is longer than a chunk. The scores take the place of c, of which each wave has its columns in registers by then.
 // The slices of all roles of a piece of a head follow each other on one XCD, whose L2 holds what they share.
-// 65536 steps x 8 heads of 64 x 128 bf16 in 64 pieces take 157 us, 2.6 TB/s: 732 vector instructions a wave and chunk at 64 rows, issued in 59%
+// 65536 steps x 8 heads of 64 x 128 bf16 in 64 pieces take 158 us, 2.6 TB/s: 732 vector instructions a wave and chunk at 64 rows, issued in 59%
 // of the cycles that a compute unit is busy, and 71 matrix instructions, which run in 23%. Of the vector instructions some 270 split
 // scores, states and weighted values into bfloat16 parts; the others are addresses, predicates, trimming, the test for values that
 // are not finite, and scalars (117 do not fit) read back from lanes. The rest of the time waits: three barriers and products that
-// follow from each other a chunk. Short sequences are bound by the states' bytes: 2048 x 4 heads of 64 x 64, 50 steps, ragged, 92 us.
+// follow from each other a chunk. Short sequences are bound by the states' bytes: 2048 x 4 heads of 64 x 64, 50 steps, ragged, 96 us.
 template <typename T, int KP, int CL, bool STATE, bool ONE> __global__ __launch_bounds__(CHUNK_THREADS, (chunk_waves<T, KP>)) void lin_chunks(LinArgs g) {
   using M = Mat<T>;
   typedef typename M::frag frag;
